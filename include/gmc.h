@@ -425,6 +425,114 @@ int gmc_test_refuse_cooperative(int64_t launches);
 int gmc_topk_noalloc(const float* x_dev, int64_t n, int64_t k, uint32_t* idx_dev, float* val_dev,
                      void* stream);
 
+/*
+ * Operators of a language model's post-training step. The paper has no
+ * counterpart: they produce the stochastic gradients g_{t,k} that Alg. 1 takes
+ * when a simulated worker trains a language model on preferences or rewards --
+ * the loss and its gradient in the logits, and the worker's dropout masks.
+ *
+ * Logits are n rows of `vocab` values of type `dtype`, row r at logits_dev + r*ld
+ * elements (ld >= vocab; any alignment of at least an element). For a row x with
+ * target y, and `scale` > 0 (1 / temperature):
+ *   logp = scale*x_y - log sum_v exp(scale*x_v),
+ *   d logp / d x_v = scale*([v = y] - p_v),  p_v = exp(scale*x_v) / sum_u exp(scale*x_u).
+ * targets_dev holds n int64. A row with a negative target is not scored: it is not
+ * read, its logp is 0, and it adds nothing to a loss or a gradient (its gradient
+ * row is written as zeros). A target >= vocab marks its row: logp, loss and the
+ * row's gradient are NaN. Logits may be -inf (p_v = 0); a row of -inf alone has
+ * no distribution: its logp is -inf, and it adds nothing to a loss or a gradient.
+ * +inf and NaN among the logits of a row that counts make its outputs NaN.
+ * Sums and exponentials are formed in 32 bits whatever the type, and a gradient
+ * is rounded once, to the logits' type; a sum over rows is held in 64 bits and
+ * taken in a fixed order: the same call gives the same bits.
+ * dlogits_dev has rows of stride dld >= vocab and may be logits_dev itself (with
+ * dld = ld): the gradient then replaces the logits. Other overlaps of an output
+ * with an input are the caller's mistake. Requires vocab < 2^31, n <= 2^27.
+ */
+#define GMC_F32  0 /* float */
+#define GMC_BF16 1 /* bfloat16 */
+#define GMC_F16  2 /* IEEE half */
+
+/* gmc_token_logp -- logp of each row into logp_dev (n floats). stats_dev: NULL, or
+ * 2n floats (8-byte aligned) for gmc_token_logp_backward. Takes no handle, runs on
+ * the current device, stream-ordered. GMC_EINVAL for a bad argument, GMC_ECUDA if a
+ * launch fails. */
+int gmc_token_logp(const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, float scale,
+                   const int64_t* targets_dev, float* logp_dev, float* stats_dev, void* stream);
+
+/* gmc_token_logp_backward -- the gradient of sum_r dlogp[r]*logp[r] in the logits,
+ * from the logits, scale, targets and stats of a gmc_token_logp call. A row with
+ * dlogp = 0 is written as zeros and not read. */
+int gmc_token_logp_backward(const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, float scale,
+                            const int64_t* targets_dev, const float* stats_dev, const float* dlogp_dev,
+                            void* dlogits_dev, int64_t dld, void* stream);
+
+/* Workspace of the two losses below, for calls of at most max_rows rows and
+ * max_pairs pairs: allocated once on the current device (about 20 bytes a row). Calls
+ * with one handle are ordered by the caller (one stream, or events between
+ * streams); distinct handles are independent. gmc_loss_destroy synchronises the
+ * device; NULL is ignored. GMC_EINVAL, GMC_ENOMEM or GMC_ECUDA, with *out set to
+ * NULL. Requires 1 <= max_rows <= 2^27, 0 <= max_pairs <= 2^26. */
+typedef struct gmc_loss_ctx* gmc_loss_t;
+int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs);
+void gmc_loss_destroy(gmc_loss_t h);
+
+/* gmc_policy_loss -- the clipped policy loss with a KL term, and its gradient:
+ *   ratio = exp(logp - old_logp),
+ *   l = -min(ratio*A, clip(ratio, 1 - clip_low, 1 + clip_high)*A)
+ *       + kl*(exp(ref_logp - logp) - (ref_logp - logp) - 1),
+ *   loss = sum_r weights[r]*l_r.
+ * The slope in logp is -ratio*A where the unclipped term is the smaller (ties
+ * count as unclipped) and 0 elsewhere, plus kl*(1 - exp(ref_logp - logp)).
+ * old_logp_dev, advantages_dev: n floats; ref_logp_dev: n floats, read only when
+ * kl > 0 (else it may be NULL); weights_dev: n floats, or NULL for 1/n each. A row with
+ * weight 0 is not scored, as one with a negative target. loss_dev receives one
+ * float; token_loss_dev (l_r, 0 for rows not scored), logp_dev and dlogits_dev may
+ * be NULL. 0 <= clip_low <= 1, clip_high >= 0, kl >= 0, all finite.
+ * GMC_EINVAL also for n > max_rows. */
+int gmc_policy_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld,
+                    float scale, const int64_t* targets_dev, const float* old_logp_dev, const float* ref_logp_dev,
+                    const float* advantages_dev, const float* weights_dev, float clip_low, float clip_high, float kl,
+                    float* loss_dev, float* token_loss_dev, float* logp_dev, void* dlogits_dev, int64_t dld,
+                    void* stream);
+
+/* gmc_preference_loss -- the preference loss on paired log ratios, and its gradient.
+ * The rows are 2*pairs sequences one after the other, sequence s being rows
+ * offsets[s] .. offsets[s+1] (2*pairs + 1 int64, ascending, from 0 to n; sequences may
+ * be empty); pair p prefers sequence 2p over 2p + 1:
+ *   S_s = sum of logp - ref_logp over the sequence's rows with a target >= 0,
+ *   margin = beta*(S_{2p} - S_{2p+1}),
+ *   l = -(1 - smoothing)*log sigmoid(margin) - smoothing*log sigmoid(-margin),
+ *   loss = sum_p weights[p]*l_p.
+ * ref_logp_dev: n floats, or NULL for zeros; weights_dev: `pairs` floats, or NULL
+ * for 1/pairs each (a pair with weight 0 has zero gradients; its l is still given).
+ * loss_dev receives one float; pair_loss_dev (pairs), seq_ratio_dev (S, 2*pairs),
+ * logp_dev (n) and dlogits_dev may be NULL. A row outside all sequences has a zero
+ * gradient. beta > 0, 0 <= smoothing <= 1. GMC_EINVAL also for n > max_rows or
+ * pairs > max_pairs. */
+int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld,
+                        float scale, const int64_t* targets_dev, const int64_t* offsets_dev, int64_t pairs,
+                        const float* ref_logp_dev, const float* weights_dev, float beta, float smoothing,
+                        float* loss_dev, float* pair_loss_dev, float* seq_ratio_dev, float* logp_dev,
+                        void* dlogits_dev, int64_t dld, void* stream);
+
+/* gmc_dropout -- out = residual + x*65536/(65536 - q) where kept, residual + 0
+ * elsewhere, for K workers' rows of n elements (row strides ldx, ldr, ldo elements,
+ * ignored when K = 1), q = p*65536 rounded to nearest even, 0 <= p <= 1; residual_dev may
+ * be NULL (zeros) and out_dev may be x_dev or residual_dev (same stride). Dropped
+ * elements are not computed with: a NaN or Inf there leaves the residual.
+ * Element i of row k is kept iff b >= q, b being bits 16*(i mod 4) .. +15 of
+ * draw i/4 of the SplitMix64 stream (the library's counter stream, as for RBGS)
+ * keyed by (seed, t, worker0 + k, site): the same mask wherever the row lies and
+ * whatever rows it is called with, so it is never stored. The gradient in x is the same
+ * call on the output's gradient, without the residual; the residual's gradient is the
+ * output's. The element is computed in 32 bits and rounded once. Takes no handle,
+ * runs on the current device, stream-ordered. Requires K <= 2^20, n <= 2^40,
+ * K*ceil(n/1024) < 2^31, worker0, t, site >= 0 (GMC_EINVAL otherwise). */
+int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_t ldr, void* out_dev, int64_t ldo,
+                int32_t dtype, int64_t worker0, int64_t K, int64_t n, double p, uint64_t seed, int64_t t,
+                int64_t site, void* stream);
+
 /* gmc_strerror -- a static message for a status code. */
 const char* gmc_strerror(int status);
 

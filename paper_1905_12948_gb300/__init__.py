@@ -5,3 +5,5 @@ The method runs in the CUDA kernels of ``libgmc.so`` behind the C ABI of
 ``include/gmc.h``; ``gmc`` is its Python binding.
 """
 from .gmc import GMC, GMCError, load  # noqa: F401
+from .tokens import (TokenLoss, dropout, dropout_backward, token_logp,  # noqa: F401
+                     token_logp_backward)

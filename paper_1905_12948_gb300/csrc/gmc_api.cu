@@ -125,21 +125,6 @@ struct gmc_ctx {
 
 namespace {
 
-class DeviceGuard {
- public:
-  explicit DeviceGuard(int dev) {
-    cudaGetDevice(&prev_);
-    if (prev_ != dev) cudaSetDevice(dev);
-    dev_ = dev;
-  }
-  ~DeviceGuard() {
-    if (prev_ != dev_) cudaSetDevice(prev_);
-  }
-
- private:
-  int prev_ = 0, dev_ = 0;
-};
-
 // Test hook (gmc_test_fail_alloc): the device allocation that finds the
 // countdown at 0 fails as cudaMalloc does when memory runs out; -1 = off.
 std::atomic<int64_t> g_fail_countdown{-1};
@@ -159,11 +144,9 @@ cudaError_t dalloc(gmc_ctx* h, T** p, size_t count) {
   void* q = nullptr;
   *p = nullptr;
   const size_t bytes = std::max<size_t>(count, 1) * sizeof(T);
-  if (injected_alloc_failure()) return cudaErrorMemoryAllocation;
-  cudaError_t err = cudaMalloc(&q, bytes);
+  cudaError_t err = lib_malloc(&q, bytes);
   if (err != cudaSuccess) return err;
   h->allocations.push_back(q);
-  g_live_allocations.fetch_add(1);
   *p = static_cast<T*>(q);
   return cudaMemset(q, 0, bytes);
 }
@@ -723,6 +706,23 @@ int read_state(gmc_ctx* h, cudaStream_t s, F&& read) {
 bool finite_f(float x) { return std::isfinite(x); }
 
 }  // namespace
+
+namespace gmc {
+
+cudaError_t lib_malloc(void** p, size_t bytes) {
+  *p = nullptr;
+  if (injected_alloc_failure()) return cudaErrorMemoryAllocation;
+  const cudaError_t err = cudaMalloc(p, bytes);
+  if (err == cudaSuccess) g_live_allocations.fetch_add(1);
+  return err;
+}
+void lib_free(void* p) {
+  if (!p) return;
+  cudaFree(p);
+  g_live_allocations.fetch_sub(1);
+}
+
+}  // namespace gmc
 
 extern "C" {
 

@@ -175,6 +175,26 @@ struct DetachArgs {
   int k0, k1;                // workers [k0, k1)
 };
 
+// The current device for the length of a scope.
+class DeviceGuard {
+ public:
+  explicit DeviceGuard(int dev) {
+    cudaGetDevice(&prev_);
+    if (prev_ != dev) cudaSetDevice(dev);
+    dev_ = dev;
+  }
+  ~DeviceGuard() {
+    if (prev_ != dev_) cudaSetDevice(prev_);
+  }
+
+ private:
+  int prev_ = 0, dev_ = 0;
+};
+
+// Device memory of the library's handles, with gmc_test_fail_alloc's count and failure.
+cudaError_t lib_malloc(void** p, size_t bytes);
+void lib_free(void* p);
+
 // Launch with programmatic stream serialization (the kernel begins with
 // griddep_wait): its scheduling overlaps the end of the kernel before it.
 template <typename... P, typename... Args>

@@ -66,6 +66,18 @@ _SIGNATURES = {
     "gmc_kernel_name": (ctypes.c_char_p, [_i32]),
     "gmc_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "gmc_topk_noalloc": (ctypes.c_int, [_c_p, _i64, _i64, _c_p, _c_p, _c_p]),
+    "gmc_token_logp": (ctypes.c_int, [_c_p, _i32, _i64, _i64, _i64, _f32, _c_p, _c_p, _c_p, _c_p]),
+    "gmc_token_logp_backward": (ctypes.c_int, [_c_p, _i32, _i64, _i64, _i64, _f32, _c_p, _c_p, _c_p,
+                                               _c_p, _i64, _c_p]),
+    "gmc_loss_create": (ctypes.c_int, [ctypes.POINTER(_c_p), _i64, _i64]),
+    "gmc_loss_destroy": (None, [_c_p]),
+    "gmc_policy_loss": (ctypes.c_int, [_c_p, _c_p, _i32, _i64, _i64, _i64, _f32, _c_p, _c_p, _c_p, _c_p,
+                                       _c_p, _f32, _f32, _f32, _c_p, _c_p, _c_p, _c_p, _i64, _c_p]),
+    "gmc_preference_loss": (ctypes.c_int, [_c_p, _c_p, _i32, _i64, _i64, _i64, _f32, _c_p, _c_p, _i64,
+                                           _c_p, _c_p, _f32, _f32, _c_p, _c_p, _c_p, _c_p, _c_p, _i64,
+                                           _c_p]),
+    "gmc_dropout": (ctypes.c_int, [_c_p, _i64, _c_p, _i64, _c_p, _i64, _i32, _i64, _i64, _i64, _f64, _u64,
+                                   _i64, _i64, _c_p]),
     "gmc_test_fail_alloc": (_i64, [_i64]),
     "gmc_test_withhold_copy": (ctypes.c_int, [_c_p, _i64, _i32, _u64]),
     "gmc_test_pass": (ctypes.c_int, [_c_p]),
