@@ -528,7 +528,7 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
  * call on the output's gradient, without the residual; the residual's gradient is the
  * output's. The element is computed in 32 bits and rounded once. Takes no handle,
  * runs on the current device, stream-ordered. Requires K <= 2^20, n <= 2^40,
- * K*ceil(n/1024) < 2^31, worker0, t, site >= 0 (GMC_EINVAL otherwise). */
+ * K*(n/4096 + 1) < 2^31, worker0, t, site >= 0 (GMC_EINVAL otherwise). */
 int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_t ldr, void* out_dev, int64_t ldo,
                 int32_t dtype, int64_t worker0, int64_t K, int64_t n, double p, uint64_t seed, int64_t t,
                 int64_t site, void* stream);

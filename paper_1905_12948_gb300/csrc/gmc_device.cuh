@@ -187,7 +187,7 @@ __device__ __forceinline__ void store_row(float* row, int l, int lim, float4 x, 
 // step t's stream (stream 0 = shared by all workers, k+1 = worker k), the
 // stream's i-th draw, and [0, n) from a draw's top 32 bits by multiply-shift.
 constexpr uint64_t kGamma = 0x9E3779B97F4A7C15ull;
-__device__ __forceinline__ uint64_t sm64_mix(uint64_t z) {
+__host__ __device__ __forceinline__ uint64_t sm64_mix(uint64_t z) {
   z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
   z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
   return z ^ (z >> 31);

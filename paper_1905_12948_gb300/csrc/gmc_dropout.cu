@@ -15,6 +15,7 @@ using namespace gmc;
 namespace {
 
 constexpr int kDropThreads = 256;
+constexpr int kDropVecs = 4;  // 16-byte vectors of a tensor that a thread loads together
 // Sets the dropout streams apart from those of the block choice and the sample
 // of the same (seed, t).
 constexpr uint64_t kDropTag = 0x44524F504F555421ull;
@@ -25,42 +26,117 @@ struct DropArgs {
   T* out;
   int64_t ldx, ldr, ldo;
   int64_t n;
-  int64_t k0;
+  uint64_t key;       // of (seed, t)
+  uint64_t worker0, site;
   uint32_t q;
   float gain;
-  uint64_t seed;
-  int64_t t, site;
 };
 
-__device__ __forceinline__ uint64_t drop_key(uint64_t seed, int64_t t, int64_t worker, int64_t site) {
-  return sm64_mix(stream_key(seed ^ kDropTag, t, (uint64_t)(worker + 1)) + kGamma * (uint64_t)(site + 1));
+// N consecutive elements at p, in one piece where p lies on a 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ uint4 load_vec(const T* p, bool aligned) {
+  if (aligned) return __ldcs(reinterpret_cast<const uint4*>(p));
+  T v[Vec<T>::N];
+#pragma unroll
+  for (int e = 0; e < Vec<T>::N; ++e) v[e] = p[e];
+  return *reinterpret_cast<const uint4*>(v);
+}
+__device__ __forceinline__ bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// The stream's 16-bit numbers of N elements from element i on, two to a word. r =
+// i mod 4 is the same for the whole row: 0 where its vectors begin with a draw.
+template <int N>
+__device__ __forceinline__ void bits_of(uint64_t key, int64_t i, int r, uint32_t* w) {
+  uint64_t z[N / 4];
+  uint64_t at = key + kGamma * (uint64_t)(i / 4 + 1);
+#pragma unroll
+  for (int d = 0; d < N / 4; ++d, at += kGamma) z[d] = sm64_mix(at);
+  if (r) {  // each word pair spans two draws
+    const uint64_t last = sm64_mix(at);
+#pragma unroll
+    for (int d = 0; d < N / 4; ++d) z[d] = (z[d] >> (16 * r)) | ((d + 1 < N / 4 ? z[d + 1] : last) << (64 - 16 * r));
+  }
+#pragma unroll
+  for (int d = 0; d < N / 4; ++d) w[2 * d] = (uint32_t)z[d], w[2 * d + 1] = (uint32_t)(z[d] >> 32);
 }
 
-// A thread a group of 4 elements (one draw).
-template <typename T>
+// A block takes kDropThreads * kDropVecs vectors of a worker's row: the 16-byte vectors
+// of x, of which the row's first elements (before its first boundary) and last are left
+// to a few threads of the row's first block.
+//
+// Bound by memory: a draw (two 64-bit products) gives four elements their 16 bits, so
+// about 6 of a dozen instructions an element are the generator's, under half of what an
+// SM issues while its share of the memory's rate moves.
+template <typename T, bool RES>
 __global__ void __launch_bounds__(kDropThreads) k_dropout(DropArgs<T> A, int64_t blocks_per_row) {
+  constexpr int N = Vec<T>::N, U = kDropVecs;
   const int64_t k = blockIdx.x / blocks_per_row;
-  const int64_t g = (blockIdx.x - k * blocks_per_row) * kDropThreads + threadIdx.x;
-  const int64_t i0 = g * 4;
-  if (i0 >= A.n) return;
-  const uint64_t z = draw(drop_key(A.seed, A.t, A.k0 + k, A.site), (uint64_t)g);
+  const int64_t b = blockIdx.x - k * blocks_per_row;
   const T* x = A.x + k * A.ldx;
-  const T* res = A.res ? A.res + k * A.ldr : nullptr;
+  const T* res = RES ? A.res + k * A.ldr : nullptr;
   T* out = A.out + k * A.ldo;
-  for (int e = 0; e < 4; ++e) {
-    const int64_t i = i0 + e;
-    if (i >= A.n) break;
-    const bool keep = ((uint32_t)(z >> (16 * e)) & 0xffffu) >= A.q;
-    float v = keep ? Vec<T>::one(x[i]) * A.gain : 0.f;
-    if (res) v += Vec<T>::one(res[i]);
-    out[i] = Vec<T>::round(v);
+  const uint64_t key = sm64_mix(sm64_mix(A.key + kGamma * (A.worker0 + (uint64_t)k + 2)) + kGamma * (A.site + 1));
+  const int head = head_of(x, A.n);
+  const int64_t nv = (A.n - head) / N;
+  const int r = head & 3;
+  const bool res_on = RES && on16(res + head), out_on = on16(out + head);
+  const uint32_t q = A.q << 16;
+  const bool none = A.q > 0xffffu;  // p = 1
+  const int64_t v0 = b * (kDropThreads * U) + threadIdx.x;
+  uint4 xv[U], rv[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t v = v0 + u * kDropThreads;
+    if (v >= nv) continue;
+    const int64_t i = head + v * N;
+    xv[u] = __ldcs(reinterpret_cast<const uint4*>(x + i));
+    if (RES) rv[u] = load_vec(res + i, res_on);
   }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t v = v0 + u * kDropThreads;
+    if (v >= nv) continue;
+    const int64_t i = head + v * N;
+    uint32_t w[N / 2];
+    bits_of<N>(key, i, r, w);
+    float f[N], g[N];
+    Vec<T>::get(xv[u], f);
+    if (RES) Vec<T>::get(rv[u], g);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const uint32_t bits = e & 1 ? w[e / 2] : w[e / 2] << 16;  // the number in the upper half
+      f[e] = bits >= q && !none ? f[e] * A.gain : 0.f;
+      if (RES) f[e] += g[e];
+    }
+    if (out_on) {
+      __stcs(reinterpret_cast<uint4*>(out + i), Vec<T>::put(f));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) out[i + e] = Vec<T>::round(f[e]);
+    }
+  }
+  const int tail = (int)(A.n - head - nv * N);
+  if (b == 0 && (int)threadIdx.x < head + tail) {
+    const int t = (int)threadIdx.x;
+    const int64_t i = t < head ? (int64_t)t : A.n - tail + (t - head);
+    const uint32_t bits = (uint32_t)(draw(key, (uint64_t)(i / 4)) >> (16 * (i & 3))) & 0xffffu;
+    float f = bits >= A.q ? Vec<T>::one(x[i]) * A.gain : 0.f;
+    if (RES) f += Vec<T>::one(res[i]);
+    out[i] = Vec<T>::round(f);
+  }
+}
+
+// Blocks of a row: its vectors, and at least one for its edges.
+int64_t blocks_of(int64_t n, int64_t per_vec) {
+  const int64_t per = kDropThreads * kDropVecs * per_vec;
+  return n / per + 1;
 }
 
 template <typename T>
 cudaError_t run(const DropArgs<T>& A, int64_t K, cudaStream_t s) {
-  const int64_t per = (A.n + 4 * kDropThreads - 1) / (4 * kDropThreads);
-  k_dropout<T><<<(unsigned)(per * K), kDropThreads, 0, s>>>(A, per);
+  const int64_t per = blocks_of(A.n, Vec<T>::N);
+  if (A.res) k_dropout<T, true><<<(unsigned)(per * K), kDropThreads, 0, s>>>(A, per);
+  else k_dropout<T, false><<<(unsigned)(per * K), kDropThreads, 0, s>>>(A, per);
   return cudaGetLastError();
 }
 
@@ -76,8 +152,7 @@ extern "C" int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_
   if (K > (int64_t(1) << 20) || n > kMost || worker0 > (int64_t(1) << 40)) return GMC_EINVAL;
   if (K > 1 && (ldx < n || ldo < n || ldx > kMost || ldo > kMost)) return GMC_EINVAL;
   if (K > 1 && residual_dev && (ldr < n || ldr > kMost)) return GMC_EINVAL;
-  const int64_t per = (n + 4 * kDropThreads - 1) / (4 * kDropThreads);
-  if (K * per >= (int64_t(1) << 31)) return GMC_EINVAL;
+  if (K * blocks_of(n, 16 / (int64_t)size) >= (int64_t(1) << 31)) return GMC_EINVAL;
   if (K == 0 || n == 0) return GMC_OK;
   if (!x_dev || !out_dev) return GMC_EINVAL;
   for (const void* q : {x_dev, residual_dev, (const void*)out_dev})
@@ -87,7 +162,8 @@ extern "C" int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_
   const cudaError_t err = by_type(dtype, [&](auto z) {
     using T = decltype(z);
     const DropArgs<T> A{static_cast<const T*>(x_dev), static_cast<const T*>(residual_dev), static_cast<T*>(out_dev),
-                        ldx, ldr, ldo, n, worker0, q, gain, seed, t, site};
+                        ldx, ldr, ldo, n, sm64_mix((seed ^ kDropTag) + kGamma * (uint64_t)(t + 1)),
+                        (uint64_t)worker0, (uint64_t)site, q, gain};
     return run(A, K, static_cast<cudaStream_t>(stream));
   });
   return err == cudaSuccess ? GMC_OK : GMC_ECUDA;

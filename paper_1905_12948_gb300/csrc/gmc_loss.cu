@@ -34,13 +34,6 @@ struct Rows {
   const int64_t* y;
 };
 
-// The elements of a row that lie before its first 16-byte boundary.
-template <typename T>
-__device__ __forceinline__ int head_of(const T* p, int64_t V) {
-  const int h = (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T);
-  return V < h ? (int)V : h;
-}
-
 // A maximum and the sum of exp(s (x - m)) below it. m = -inf: nothing yet.
 struct MaxSum {
   float m = -INFINITY, s = 0.f;

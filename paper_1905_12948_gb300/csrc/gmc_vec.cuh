@@ -77,6 +77,13 @@ struct Vec<__half> {
   __device__ static __half round(float v) { return __float2half_rn(v); }
 };
 
+// The elements of a row that lie before its first 16-byte boundary.
+template <typename T>
+__device__ __forceinline__ int head_of(const T* p, int64_t V) {
+  const int h = (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T);
+  return V < h ? (int)V : h;
+}
+
 template <typename F>
 inline cudaError_t by_type(int32_t dtype, F&& f) {
   if (dtype == GMC_F32) return f(float());

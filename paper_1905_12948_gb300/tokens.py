@@ -13,70 +13,76 @@ where a token is not scored. Outputs are allocated on the stream of the call.
 from __future__ import annotations
 
 import ctypes
-from typing import NamedTuple, Optional
+from typing import NamedTuple
 
-from .gmc import _check, _i64, _import_torch, _stream_ptr, load
 from . import gmc as _gmc
+from .gmc import _check, _import_torch, load
 
-_DTYPES = None   # torch dtype -> GMC_F32 / GMC_BF16 / GMC_F16
+_torch = None    # set with the library, on the first call
+_lib = None
+_f32 = _i64 = None
+_DTYPES = {}     # torch dtype -> GMC_F32 / GMC_BF16 / GMC_F16
+_current = None  # () -> the current device's index
 
 
-def _dtype(t, name: str) -> int:
-    global _DTYPES
-    if _DTYPES is None:
-        torch = _import_torch()
-        _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+def _setup() -> None:
+    global _torch, _lib, _f32, _i64, _current
+    torch = _import_torch()
+    _f32, _i64 = torch.float32, torch.int64
+    _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _lib = load()
+    _torch = torch
+
+
+def _device(t, name: str) -> int:
+    """The index of a CUDA tensor's device."""
+    if _torch is None:
+        _setup()
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    return t.get_device()
+
+
+def _elsewhere(dev: int, stream):
+    """None where the call can be made at once: on the current device and stream. Else
+    the context to make it under, so that its outputs are allocated there too."""
+    if stream is not None:
+        if stream.device_index != dev:
+            raise TypeError(f"stream must be one of cuda:{dev}")
+        return _torch.cuda.stream(stream)
+    return None if _current() == dev else _torch.cuda.device(dev)
+
+
+def _rows(t, name: str):
+    """Row stride of a 2-D CUDA tensor with contiguous rows."""
+    if t.dim() != 2:
+        raise TypeError(f"{name} must be 2-D")
+    n, v = t.shape
+    if t.is_contiguous():
+        return n, v, v
+    ld, step = t.stride()
+    if step != 1 and v > 1:
+        raise TypeError(f"{name}'s rows must be contiguous")
+    if n <= 1:
+        return n, v, v
+    if ld < v:
+        raise TypeError(f"{name}'s rows must not overlap")
+    return n, v, ld
+
+
+def _kind(t, name: str) -> int:
     code = _DTYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16")
     return code
 
 
-class _On:
-    """The device and the stream of a call: outputs are allocated and the library is
-    called under them."""
-
-    def __init__(self, device, stream):
-        torch = _import_torch()
-        self.stream = stream
-        self.swap = None
-        if stream is not None:
-            self.swap = torch.cuda.stream(stream)
-        elif torch.cuda.current_device() != device.index:
-            self.swap = torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.swap is not None:
-            self.swap.__enter__()
-        return _stream_ptr(self.stream)
-
-    def __exit__(self, *exc):
-        if self.swap is not None:
-            self.swap.__exit__(*exc)
-
-
-def _rows(t, name: str, like=None):
-    """(pointer, row stride) of a 2-D CUDA tensor with contiguous rows."""
-    torch = _import_torch()
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise TypeError(f"{name} must be 2-D with contiguous rows")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
-        raise TypeError(f"{name} must have the shape, dtype and device of {like.shape}, {like.dtype}, {like.device}")
-    n, v = t.shape
-    ld = t.stride(0) if n > 1 else v
-    if ld < v:
-        raise TypeError(f"{name}'s rows must not overlap")
-    return t.data_ptr(), ld
-
-
-def _vector(t, n: int, dtype, device, name: str) -> Optional[int]:
+def _vector(t, n: int, dtype, dev: int, name: str):
     if t is None:
         return None
-    torch = _import_torch()
-    if not isinstance(t, torch.Tensor) or t.device != device:
-        raise TypeError(f"{name} must be a CUDA tensor on {device}")
+    if not isinstance(t, _torch.Tensor) or not t.is_cuda or t.get_device() != dev:
+        raise TypeError(f"{name} must be a CUDA tensor on cuda:{dev}")
     if t.dtype != dtype or not t.is_contiguous():
         raise TypeError(f"{name} must be a contiguous {dtype} tensor")
     if t.numel() != n:
@@ -84,39 +90,55 @@ def _vector(t, n: int, dtype, device, name: str) -> Optional[int]:
     return t.data_ptr()
 
 
+def _gradient(logits, out, grad: bool, vocab: int):
+    """(tensor, pointer, row stride) of the gradient's destination."""
+    if not grad:
+        return None, None, vocab
+    if out is None:
+        out = _torch.empty_like(logits, memory_format=_torch.contiguous_format)
+        return out, out.data_ptr(), vocab
+    if out is not logits and (not isinstance(out, _torch.Tensor) or out.shape != logits.shape
+                              or out.dtype != logits.dtype or out.device != logits.device):
+        raise TypeError("out must have the logits' shape, dtype and device")
+    return out, out.data_ptr(), _rows(out, "out")[2]
+
+
 def token_logp(logits, targets, *, scale: float = 1.0, return_stats: bool = False, stream=None):
     """Log-probability of each row's target under softmax(scale * logits): n float32
     (gmc_token_logp). With ``return_stats`` also the (n, 2) float32 that
     ``token_logp_backward`` takes."""
-    torch = _import_torch()
-    ptr, ld = _rows(logits, "logits")
-    n, vocab = logits.shape
-    dev = logits.device
-    tgt = _vector(targets, n, torch.int64, dev, "targets")
-    with _On(dev, stream) as s:
-        logp = torch.empty(n, dtype=torch.float32, device=dev)
-        stats = torch.empty((n, 2), dtype=torch.float32, device=dev) if return_stats else None
-        _check(load().gmc_token_logp(ptr, _dtype(logits, "logits"), n, vocab, ld, scale, tgt, logp.data_ptr(),
-                                     stats.data_ptr() if return_stats else None, s), "gmc_token_logp")
+    dev = _device(logits, "logits")
+    under = _elsewhere(dev, stream)
+    if under is not None:
+        with under:
+            return token_logp(logits, targets, scale=scale, return_stats=return_stats)
+    n, vocab, ld = _rows(logits, "logits")
+    code = _kind(logits, "logits")
+    tgt = _vector(targets, n, _i64, dev, "targets")
+    where = logits.device
+    logp = _torch.empty(n, dtype=_f32, device=where)
+    stats = _torch.empty((n, 2), dtype=_f32, device=where) if return_stats else None
+    _check(_lib.gmc_token_logp(logits.data_ptr(), code, n, vocab, ld, scale, tgt, logp.data_ptr(),
+                               stats.data_ptr() if return_stats else None, _gmc._raw_stream(dev)), "gmc_token_logp")
     return (logp, stats) if return_stats else logp
 
 
 def token_logp_backward(logits, targets, stats, dlogp, *, scale: float = 1.0, out=None, stream=None):
     """Gradient of sum(dlogp * logp) in the logits (gmc_token_logp_backward), of the
     logits' dtype; ``out`` may be the logits themselves."""
-    torch = _import_torch()
-    ptr, ld = _rows(logits, "logits")
-    n, vocab = logits.shape
-    dev = logits.device
-    tgt = _vector(targets, n, torch.int64, dev, "targets")
-    st = _vector(stats, 2 * n, torch.float32, dev, "stats")
-    g = _vector(dlogp, n, torch.float32, dev, "dlogp")
-    with _On(dev, stream) as s:
-        if out is None:
-            out = torch.empty((n, vocab), dtype=logits.dtype, device=dev)
-        optr, old = _rows(out, "out", logits)
-        _check(load().gmc_token_logp_backward(ptr, _dtype(logits, "logits"), n, vocab, ld, scale, tgt, st, g, optr,
-                                              old, s), "gmc_token_logp_backward")
+    dev = _device(logits, "logits")
+    under = _elsewhere(dev, stream)
+    if under is not None:
+        with under:
+            return token_logp_backward(logits, targets, stats, dlogp, scale=scale, out=out)
+    n, vocab, ld = _rows(logits, "logits")
+    code = _kind(logits, "logits")
+    tgt = _vector(targets, n, _i64, dev, "targets")
+    st = _vector(stats, 2 * n, _f32, dev, "stats")
+    g = _vector(dlogp, n, _f32, dev, "dlogp")
+    out, optr, old = _gradient(logits, out, True, vocab)
+    _check(_lib.gmc_token_logp_backward(logits.data_ptr(), code, n, vocab, ld, scale, tgt, st, g, optr, old,
+                                        _gmc._raw_stream(dev)), "gmc_token_logp_backward")
     return out
 
 
@@ -140,14 +162,16 @@ class TokenLoss:
     ``max_pairs`` pairs a call. Calls with one instance are ordered by the caller."""
 
     def __init__(self, max_rows: int, max_pairs: int = 0, device=None):
-        torch = _import_torch()
-        self.lib = load()
-        self.device = torch.device(device if device is not None else "cuda")
+        if _torch is None:
+            _setup()
+        self.lib = _lib
+        self.device = _torch.device(device if device is not None else "cuda")
         if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
+            self.device = _torch.device("cuda", _torch.cuda.current_device())
+        self.index = self.device.index
         h = _gmc._c_p()
-        with torch.cuda.device(self.device):
-            _check(self.lib.gmc_loss_create(ctypes.byref(h), int(max_rows), int(max_pairs)), "gmc_loss_create")
+        with _torch.cuda.device(self.device):
+            _check(_lib.gmc_loss_create(ctypes.byref(h), int(max_rows), int(max_pairs)), "gmc_loss_create")
         self.h = h
 
     def close(self) -> None:
@@ -161,43 +185,37 @@ class TokenLoss:
         except Exception:
             pass
 
-    def _logits(self, logits, targets):
-        torch = _import_torch()
-        ptr, ld = _rows(logits, "logits")
-        if logits.device != self.device:
+    def _elsewhere(self, logits, stream):
+        if _device(logits, "logits") != self.index:
             raise TypeError(f"logits must be on {self.device}")
-        return ptr, ld, _vector(targets, logits.shape[0], torch.int64, self.device, "targets")
-
-    def _gradient(self, logits, out, grad: bool):
-        torch = _import_torch()
-        if not grad:
-            return None, None, logits.shape[1]
-        if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
-        return (out, *_rows(out, "out", logits))
+        return _elsewhere(self.index, stream)
 
     def policy(self, logits, targets, old_logp, advantages, *, weights=None, ref_logp=None,
                clip_low: float = 0.2, clip_high: float = 0.2, kl: float = 0.0, scale: float = 1.0,
                grad: bool = True, out=None, stream=None) -> PolicyLoss:
         """Clipped policy loss with a KL term, and its gradient in the logits
         (gmc_policy_loss). ``out`` may be the logits themselves."""
-        torch = _import_torch()
-        ptr, ld, tgt = self._logits(logits, targets)
-        n, vocab = logits.shape
-        f32, dev = torch.float32, self.device
-        old = _vector(old_logp, n, f32, dev, "old_logp")
-        adv = _vector(advantages, n, f32, dev, "advantages")
-        ref = _vector(ref_logp, n, f32, dev, "ref_logp")
-        w = _vector(weights, n, f32, dev, "weights")
-        with _On(dev, stream) as s:
-            # one allocation for the loss and the rows' outputs
-            buf = torch.empty(2 * n + 1, dtype=f32, device=dev)
-            base = buf.data_ptr()
-            out, optr, old_ = self._gradient(logits, out, grad)
-            _check(self.lib.gmc_policy_loss(self.h, ptr, _dtype(logits, "logits"), n, vocab, ld, scale, tgt, old,
-                                            ref, adv, w, clip_low, clip_high, kl, base + 8 * n, base, base + 4 * n,
-                                            optr, old_, s), "gmc_policy_loss")
-        return PolicyLoss(buf[2 * n], buf[:n], buf[n: 2 * n], out)
+        under = self._elsewhere(logits, stream)
+        if under is not None:
+            with under:
+                return self.policy(logits, targets, old_logp, advantages, weights=weights, ref_logp=ref_logp,
+                                   clip_low=clip_low, clip_high=clip_high, kl=kl, scale=scale, grad=grad, out=out)
+        dev, where = self.index, self.device
+        n, vocab, ld = _rows(logits, "logits")
+        code = _kind(logits, "logits")
+        tgt = _vector(targets, n, _i64, dev, "targets")
+        old = _vector(old_logp, n, _f32, dev, "old_logp")
+        adv = _vector(advantages, n, _f32, dev, "advantages")
+        ref = _vector(ref_logp, n, _f32, dev, "ref_logp")
+        w = _vector(weights, n, _f32, dev, "weights")
+        out, optr, dld = _gradient(logits, out, grad, vocab)
+        loss = _torch.empty((), dtype=_f32, device=where)
+        token_loss = _torch.empty(n, dtype=_f32, device=where)
+        logp = _torch.empty(n, dtype=_f32, device=where)
+        _check(_lib.gmc_policy_loss(self.h, logits.data_ptr(), code, n, vocab, ld, scale, tgt, old, ref, adv, w,
+                                    clip_low, clip_high, kl, loss.data_ptr(), token_loss.data_ptr(), logp.data_ptr(),
+                                    optr, dld, _gmc._raw_stream(dev)), "gmc_policy_loss")
+        return PolicyLoss(loss, token_loss, logp, out)
 
     def preference(self, logits, targets, offsets, *, beta: float, smoothing: float = 0.0, ref_logp=None,
                    weights=None, scale: float = 1.0, grad: bool = True, out=None, stream=None) -> PreferenceLoss:
@@ -205,25 +223,42 @@ class TokenLoss:
         (gmc_preference_loss). ``offsets``: int64, 2 * pairs + 1 row numbers on the
         device, the preferred sequence of a pair first. ``out`` may be the logits
         themselves."""
-        torch = _import_torch()
-        ptr, ld, tgt = self._logits(logits, targets)
-        n, vocab = logits.shape
-        f32, dev = torch.float32, self.device
-        if not isinstance(offsets, torch.Tensor) or offsets.numel() % 2 != 1:
+        under = self._elsewhere(logits, stream)
+        if under is not None:
+            with under:
+                return self.preference(logits, targets, offsets, beta=beta, smoothing=smoothing, ref_logp=ref_logp,
+                                       weights=weights, scale=scale, grad=grad, out=out)
+        dev, where = self.index, self.device
+        n, vocab, ld = _rows(logits, "logits")
+        code = _kind(logits, "logits")
+        tgt = _vector(targets, n, _i64, dev, "targets")
+        if not isinstance(offsets, _torch.Tensor) or offsets.numel() % 2 != 1:
             raise ValueError("offsets must have 2 * pairs + 1 elements")
         pairs = offsets.numel() // 2
-        off = _vector(offsets, 2 * pairs + 1, torch.int64, dev, "offsets")
-        ref = _vector(ref_logp, n, f32, dev, "ref_logp")
-        w = _vector(weights, pairs, f32, dev, "weights")
-        with _On(dev, stream) as s:
-            buf = torch.empty(n + 3 * pairs + 1, dtype=f32, device=dev)
-            logp, seq, each, loss = buf.split([n, 2 * pairs, pairs, 1])
-            out, optr, old_ = self._gradient(logits, out, grad)
-            _check(self.lib.gmc_preference_loss(self.h, ptr, _dtype(logits, "logits"), n, vocab, ld, scale, tgt, off,
-                                                pairs, ref, w, beta, smoothing, loss.data_ptr(), each.data_ptr(),
-                                                seq.data_ptr(), logp.data_ptr(), optr, old_, s),
-                   "gmc_preference_loss")
-        return PreferenceLoss(loss[0], each, seq, logp, out)
+        off = _vector(offsets, 2 * pairs + 1, _i64, dev, "offsets")
+        ref = _vector(ref_logp, n, _f32, dev, "ref_logp")
+        w = _vector(weights, pairs, _f32, dev, "weights")
+        out, optr, dld = _gradient(logits, out, grad, vocab)
+        loss = _torch.empty((), dtype=_f32, device=where)
+        each = _torch.empty(pairs, dtype=_f32, device=where)
+        ratio = _torch.empty(2 * pairs, dtype=_f32, device=where)
+        logp = _torch.empty(n, dtype=_f32, device=where)
+        _check(_lib.gmc_preference_loss(self.h, logits.data_ptr(), code, n, vocab, ld, scale, tgt, off, pairs, ref, w,
+                                        beta, smoothing, loss.data_ptr(), each.data_ptr(), ratio.data_ptr(),
+                                        logp.data_ptr(), optr, dld, _gmc._raw_stream(dev)), "gmc_preference_loss")
+        return PreferenceLoss(loss, each, ratio, logp, out)
+
+
+def _workers(u, x, K: int, n: int, name: str):
+    """(pointer, worker stride) of one of dropout's tensors."""
+    if u is not x and (not isinstance(u, _torch.Tensor) or u.shape != x.shape or u.dtype != x.dtype
+                       or u.device != x.device):
+        raise TypeError(f"{name} must be a tensor of x's shape, dtype and device")
+    if u.is_contiguous():
+        return u.data_ptr(), n
+    if K == 0 or not u[0].is_contiguous() or (K > 1 and u.stride(0) < n):
+        raise TypeError(f"each worker's part of {name} must be contiguous, and none overlap")
+    return u.data_ptr(), u.stride(0)
 
 
 def dropout(x, p: float, *, seed: int, t: int = 0, worker: int = 0, site: int = 0, residual=None, out=None,
@@ -233,30 +268,25 @@ def dropout(x, p: float, *, seed: int, t: int = 0, worker: int = 0, site: int = 
     whose elements are contiguous, is drawn as worker ``worker`` + k. p is rounded to a
     multiple of 2**-16 and the kept elements are divided by the share kept. ``out`` may
     be x or the residual."""
-    torch = _import_torch()
-    if not isinstance(x, torch.Tensor) or not x.is_cuda:
-        raise TypeError("x must be a CUDA tensor")
+    dev = _device(x, "x")
+    under = _elsewhere(dev, stream)
+    if under is not None:
+        with under:
+            return dropout(x, p, seed=seed, t=t, worker=worker, site=site, residual=residual, out=out)
     if x.dim() < 2:
         raise TypeError("x must have the workers as its first dimension")
-    dev, K = x.device, x.shape[0]
+    code = _kind(x, "x")
+    K = x.shape[0]
     n = x.numel() // K if K else 0
-    code = _dtype(x, "x")
-    with _On(dev, stream) as s:
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=dev)
-        ptrs = []
-        for u, name in ((x, "x"), (residual, "residual"), (out, "out")):
-            if u is None:
-                ptrs += [None, 0]
-                continue
-            if u is not x and (not isinstance(u, torch.Tensor) or u.shape != x.shape or u.dtype != x.dtype
-                               or u.device != dev):
-                raise TypeError(f"{name} must be a tensor of x's shape, dtype and device")
-            if not u.is_contiguous() and (K == 0 or not u[0].is_contiguous() or (K > 1 and u.stride(0) < n)):
-                raise TypeError(f"each worker's part of {name} must be contiguous, and none overlap")
-            ptrs += [u.data_ptr(), n if u.is_contiguous() else u.stride(0)]
-        _check(load().gmc_dropout(*ptrs, code, int(worker), K, n, float(p), int(seed) & ((1 << 64) - 1),
-                                  int(t), int(site), s), "gmc_dropout")
+    px, ldx = _workers(x, x, K, n, "x")
+    pr, ldr = _workers(residual, x, K, n, "residual") if residual is not None else (None, 0)
+    if out is None:
+        out = _torch.empty_like(x, memory_format=_torch.contiguous_format)
+        po, ldo = out.data_ptr(), n
+    else:
+        po, ldo = _workers(out, x, K, n, "out")
+    _check(_lib.gmc_dropout(px, ldx, pr, ldr, po, ldo, code, worker, K, n, p, seed & ((1 << 64) - 1), t, site,
+                            _gmc._raw_stream(dev)), "gmc_dropout")
     return out
 
 
