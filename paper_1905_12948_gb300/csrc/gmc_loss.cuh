@@ -1,0 +1,375 @@
+// Device-side definitions shared by the loss kernels: rows of logits, exponents,
+// the running maximum and sum of a row, its log-probability, and its gradient.
+//
+// For a row x of V logits, a scale s (1 / temperature) and a target y:
+//   m = max x,  S = sum_v exp(s (x_v - m)),  logp = s (x_y - m) - log S,
+//   d logp / d x_v = s ([v = y] - p_v),  p_v = exp(s (x_v - m) - log S).
+// A row whose logits are all -inf has no distribution: S = 0, logp = -inf, and
+// it adds nothing to a loss or a gradient.
+#pragma once
+
+#include <cmath>
+
+#include "gmc_internal.h"
+#include "gmc_vec.cuh"
+
+namespace gmc {
+
+constexpr int kLossThreads = 256;
+constexpr int kSweepVecs = 4;  // vectors that a thread of a sweep loads together
+constexpr double kLog2e = 1.4426950408889634;
+constexpr double kLn2 = 0.6931471805599453;
+constexpr int kMaxParts = 8;  // blocks of a cluster that share a row (the portable limit)
+
+// Exponents are formed to base 2, by s log2 e in two words c + lo (c its lower
+// neighbour, so that lo > 0 and -inf stays -inf): a log sum is then off by roundings of
+// either sign alone, and a sum over a sequence's rows stays as good as its rows.
+struct Base {
+  float scale, c, lo;
+};
+inline Base base_of(float scale) {
+  const double b = (double)scale * kLog2e;
+  float c = (float)b;
+  if ((double)c >= b) c = std::nextafter(c, 0.f);
+  return Base{scale, c, (float)(b - (double)c)};
+}
+
+// n rows of V logits, row r at x + r * ld, with the target of each.
+template <typename T>
+struct Rows {
+  const T* x;
+  int64_t n, V, ld;
+  Base b;
+  const int64_t* y;
+};
+
+// What is subtracted from a row's exponents: those of its maximum m. x c - m c is one
+// fused operation, whose rounded m c every element shares, as long as m c is not so
+// large that its rounding matters (masks of the type's lowest value in a whole row);
+// then the difference x - m is taken first.
+struct Shift {
+  float h, hc;  // m (0 where nothing but -inf was seen), and m c
+  bool far;
+};
+__device__ __forceinline__ Shift shift_of(float m, const Base& b) {
+  Shift s;
+  s.h = m == -INFINITY ? 0.f : m;
+  s.hc = s.h * b.c;
+  s.far = !(fabsf(s.hc) < 1048576.f);
+  return s;
+}
+// Exponent of x (of x - h, with 0 for hc, where the shift is far).
+__device__ __forceinline__ float exponent(float x, float hc, const Base& b) {
+  return __fmaf_rn(x, b.lo, __fmaf_rn(x, b.c, -hc));
+}
+// Of a maximum m's own shift below s.
+__device__ __forceinline__ float between(float m, const Shift& s, const Base& b) {
+  return s.far ? (m - s.h) * b.c : m * b.c - s.hc;
+}
+
+// A maximum and the sum of the exponentials below its shift. m = -inf: nothing yet.
+struct MaxSum {
+  float m = -INFINITY, s = 0.f;
+};
+__device__ __forceinline__ MaxSum merge(const MaxSum& a, const MaxSum& o, const Base& b) {
+  MaxSum r;
+  r.m = fmaxf(a.m, o.m);
+  const Shift h = shift_of(r.m, b);
+  r.s = a.s * exp2_fast(between(a.m, h, b)) + o.s * exp2_fast(between(o.m, h, b));
+  return r;
+}
+// One value into a, and U vectors. Sums are kept four to a thread, and no NaN hides in a
+// maximum's shadow: its exponential is NaN.
+__device__ __forceinline__ void add_one(MaxSum* a, float x, const Base& b) {
+  const float m = fmaxf(a->m, x);
+  const Shift h = shift_of(m, b);
+  const float e = h.far ? exponent(x - h.h, 0.f, b) : exponent(x, h.hc, b);
+  a->s = a->s * exp2_fast(between(a->m, h, b)) + exp2_fast(e);
+  a->m = m;
+}
+template <typename T, int U>
+__device__ __forceinline__ void add(MaxSum* a, const uint4 (&v)[U], const Base& b) {
+  constexpr int P = Vec<T>::N / 2;
+  uint32_t top = Vec<T>::top(Vec<T>::top(v[0].x, v[0].y), Vec<T>::top(v[0].z, v[0].w));
+#pragma unroll
+  for (int u = 1; u < U; ++u)
+    top = Vec<T>::top(top, Vec<T>::top(Vec<T>::top(v[u].x, v[u].y), Vec<T>::top(v[u].z, v[u].w)));
+  const float m = fmaxf(a->m, Vec<T>::top_of(top));
+  const Shift h = shift_of(m, b);
+  const Pair c = pair_of(b.c, b.c), lo = pair_of(b.lo, b.lo), hc = pair_of(-h.hc, -h.hc);
+  Pair s0 = pair_of(a->s * exp2_fast(between(a->m, h, b)), 0.f), s1 = pair_of(0.f, 0.f);
+  if (!h.far) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      Pair x[P];
+      Vec<T>::pairs(v[u], x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const Pair e = exp2_pair(fma_pair(x[i], lo, fma_pair(x[i], c, hc)));
+        if (i & 1) s1 = add_pair(s1, e);
+        else s0 = add_pair(s0, e);
+      }
+    }
+  } else {
+    const Pair sh = pair_of(-h.h, -h.h), none = pair_of(0.f, 0.f);
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) {
+      Pair x[P];
+      uint4 w = v[0];
+#pragma unroll
+      for (int i = 1; i < U; ++i)
+        if (u == i) w = v[i];
+      Vec<T>::pairs(w, x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        x[i] = add_pair(x[i], sh);
+        s0 = add_pair(s0, exp2_pair(fma_pair(x[i], lo, fma_pair(x[i], c, none))));
+      }
+    }
+  }
+  float s[4];
+  split(s0, s, s + 1);
+  split(s1, s + 2, s + 3);
+  a->s = (s[0] + s[1]) + (s[2] + s[3]);
+  a->m = m;
+}
+// Over a warp; every lane returns the result.
+__device__ __forceinline__ MaxSum warp_merge(MaxSum a, const Base& b) {
+  MaxSum r;
+  r.m = a.m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
+  r.s = warp_sum(a.s * exp2_fast(between(a.m, shift_of(r.m, b), b)));
+  return r;
+}
+// Over the block; every thread returns the result. ws: 32 entries of shared memory.
+__device__ __forceinline__ MaxSum block_merge(MaxSum a, const Base& b, MaxSum* ws) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  a = warp_merge(a, b);
+  if (lane == 0) ws[warp] = a;
+  __syncthreads();
+  return warp_merge(lane < warps ? ws[lane] : MaxSum(), b);
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Over the blocks of a cluster, in rank order: a is the block's, the same in all its
+// threads. The caller has passed the cluster's barrier once before, so that none
+// writes into a block that has not begun.
+__device__ __forceinline__ MaxSum cluster_merge(MaxSum a, int parts, const Base& b, MaxSum* ws) {
+  if (parts == 1) return a;
+  if (threadIdx.x < (unsigned)parts) {  // into slot `rank` of every block
+    const uint32_t here = (uint32_t)__cvta_generic_to_shared(ws + cluster_rank());
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(threadIdx.x));
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(there), "f"(a.m), "f"(a.s) : "memory");
+  }
+  cluster_arrive();
+  cluster_wait();
+  MaxSum r = ws[0];
+  for (int i = 1; i < parts; ++i) r = merge(r, ws[i], b);
+  return r;
+}
+
+// One block's share (`part` of `parts`) of a row's maximum and sum: the row's 16-byte
+// vectors, U at a time a thread, and its edges by a few threads of part 0.
+template <typename T>
+__device__ __forceinline__ MaxSum sweep(const T* x, int64_t V, const Base& b, int part, int parts) {
+  constexpr int N = Vec<T>::N, U = kSweepVecs;
+  MaxSum a;
+  const int head = head_of(x, V);
+  const int64_t nv = (V - head) / N;
+  const int tail = (int)(V - head - nv * N);
+  const uint4* q = reinterpret_cast<const uint4*>(x + head);
+  const int64_t per = (nv + parts - 1) / parts;
+  const int64_t lo = per * part, hi = lo + per < nv ? lo + per : nv;
+  for (int64_t i = lo + threadIdx.x; i < hi; i += U * (int64_t)blockDim.x) {
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[u] = i + u * (int64_t)blockDim.x < hi ? q[i + u * (int64_t)blockDim.x]
+                                              : make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+    add<T>(&a, v, b);
+  }
+  if (part == 0) {
+    const int t = (int)threadIdx.x;
+    if (t < head + tail) {
+      add_one(&a, Vec<T>::one(x[t < head ? (int64_t)t : V - tail + (t - head)]), b);
+    }
+  }
+  return a;
+}
+
+// What follows from a row's maximum and sum.
+struct RowStats {
+  Shift h;
+  float ls, logp;  // log of the sum (0 for an empty row), log-probability of the target
+  bool empty;
+};
+// s x_y - (m c log 2 + log S): the shift's rounded product counts, not the maximum.
+__device__ __forceinline__ float logp_of(float xy, const Shift& h, float ls, const Base& b) {
+  return h.far ? (xy - h.h) * b.scale - ls
+               : (float)((double)xy * (double)b.scale - ((double)h.hc * kLn2 + (double)ls));
+}
+__device__ __forceinline__ RowStats finish(const MaxSum& a, float xy, const Base& b) {
+  RowStats r;
+  r.h = shift_of(a.m, b);
+  r.empty = a.m == -INFINITY && a.s == 0.f;
+  r.ls = r.empty ? 0.f : logf(a.s);
+  r.logp = logp_of(xy, r.h, r.ls, b);
+  return r;
+}
+constexpr uint32_t kNan = 0x7fffffffu;
+// The target's logit; NaN for one outside the vocabulary.
+template <typename T>
+__device__ __forceinline__ float target_logit(const T* x, int64_t V, int64_t y) {
+  return y < V ? Vec<T>::one(x[y]) : __uint_as_float(kNan);
+}
+
+// A row's gradient k ([v = y] - p_v), k = coef s, from its shift and log S.
+struct RowGrad {
+  Shift h;
+  float k, f, ls;  // f = -k / S
+  int64_t y;
+};
+__device__ __forceinline__ RowGrad grad_of(const Shift& h, float ls, float coef, int64_t y, const Base& b) {
+  const float k = coef * b.scale;
+  return RowGrad{h, k, -k * expf(-ls), ls, y};
+}
+// 1 - p_y without cancellation.
+__device__ __forceinline__ float grad_at_target(float x, const RowGrad& g, const Base& b) {
+  return g.k * -expm1f(logp_of(x, g.h, g.ls, b));
+}
+// f: logits j .. j + N - 1 of the row, replaced by their gradients.
+template <int N>
+__device__ __forceinline__ void grad_vec(float* f, int64_t j, const RowGrad& g, const Base& b) {
+  const uint64_t at = (uint64_t)(g.y - j);
+  float fy = 0.f;
+  if (at < N) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (at == e) fy = grad_at_target(f[e], g, b);
+  }
+  const float h = g.h.far ? g.h.h : 0.f, hc = g.h.far ? 0.f : g.h.hc;
+#pragma unroll
+  for (int e = 0; e < N; ++e) f[e] = g.f * exp2_fast(exponent(f[e] - h, hc, b));
+  if (at < N) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (at == e) f[e] = fy;
+  }
+}
+
+// One block's share of a row's gradient, or of zeros (skip: x is not read, it may
+// hold anything): 16-byte loads and, where the output row lies at the same offset from
+// a 16-byte boundary, stores.
+template <typename T>
+__device__ __forceinline__ void write_gradient(const T* x, T* dx, int64_t V, const RowGrad& g, const Base& b, bool skip,
+                                               int64_t part, int64_t parts) {
+  constexpr int N = Vec<T>::N;
+  const int head = head_of(x, V);
+  const int64_t nv = (V - head) / N;
+  const int tail = (int)(V - head - nv * N);
+  const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15) == 0;
+  const int64_t per = (nv + parts - 1) / parts;
+  const int64_t lo = per * part, hi = lo + per < nv ? lo + per : nv;
+  for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x) {
+    const int64_t j = head + i * N;
+    float f[N];
+    if (skip) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[e] = 0.f;
+    } else {
+      Vec<T>::get(*reinterpret_cast<const uint4*>(x + j), f);
+      grad_vec<N>(f, j, g, b);
+    }
+    if (same) {
+      __stcs(reinterpret_cast<uint4*>(dx + j), Vec<T>::put(f));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) dx[j + e] = Vec<T>::round(f[e]);
+    }
+  }
+  if (part == 0 && (int)threadIdx.x < head + tail) {
+    const int t = (int)threadIdx.x;
+    const int64_t j = t < head ? (int64_t)t : V - tail + (t - head);
+    float f = skip ? 0.f : Vec<T>::one(x[j]);
+    if (!skip) grad_vec<1>(&f, j, g, b);
+    dx[j] = Vec<T>::round(f);
+  }
+}
+
+struct PolicyArgs {
+  const float *old_logp, *ref_logp, *adv, *weights;  // ref_logp NULL: no KL term
+  float clip_low, clip_high, kl, weight;  // weight: of every row, where weights is NULL
+  float *token_loss, *logp;               // either may be NULL
+  float* loss;
+  double* partial;                        // the clusters' sums of weighted losses
+  uint32_t* ticket;                       // counts the clusters that are done; 0 between calls
+  uint64_t wait_ns;
+};
+
+// The token's loss and its slope in logp.
+__device__ __forceinline__ void policy_terms(const PolicyArgs& P, float adv, float old_logp, float ref_logp, float logp,
+                                             float* loss, float* slope) {
+  const float ratio = expf(logp - old_logp);
+  const float plain = ratio * adv;
+  const float lo = 1.f - P.clip_low, hi = 1.f + P.clip_high;
+  const float clipped = (ratio < lo ? lo : ratio > hi ? hi : ratio) * adv;  // NaN stays NaN
+  float l = plain <= clipped ? -plain : -clipped;
+  float d = plain <= clipped ? -plain : 0.f;
+  if (P.ref_logp) {
+    const float far = ref_logp - logp, ef = expf(far);
+    l += P.kl * (ef - far - 1.f);
+    d += P.kl * (1.f - ef);
+  }
+  if (l != l) d = l;
+  *loss = l;
+  *slope = d;
+}
+
+// Launch a kernel of `blocks` blocks in clusters of `parts`.
+struct LaunchConfig {
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[1];
+  LaunchConfig(int64_t blocks, int threads, int parts, size_t smem, cudaStream_t s) {
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)parts;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
+  }
+};
+template <typename... A, typename... B>
+inline cudaError_t launch(void (*f)(A...), int64_t blocks, int threads, int parts, cudaStream_t s, B... args) {
+  LaunchConfig l(blocks, threads, parts, 0, s);
+  return cudaLaunchKernelEx(&l.cfg, f, args...);
+}
+
+// Blocks that share a row: enough of them for two a SM, down to 16 KB of it each.
+inline int parts_for(int64_t n, int64_t row_bytes) {
+  int parts = 1;
+  while (parts < kMaxParts && n * parts < 304 && row_bytes / parts > 16384) parts *= 2;
+  return parts;
+}
+
+// Facts of the current device: its SMs, and the clusters of a launch configuration that
+// can be resident; looked up once a host thread.
+struct Residency {
+  static cudaError_t sms(int* out);
+  static cudaError_t clusters(const void* f, const LaunchConfig& l, int parts, int64_t* out);
+};
+
+// The policy loss over n > 0 rows (gmc_policy.cu). A.partial has kMostClusters slots.
+constexpr int kMostClusters = 8192;
+template <typename T>
+cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, cudaStream_t s);
+}  // namespace gmc

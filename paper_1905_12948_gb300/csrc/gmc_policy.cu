@@ -1,0 +1,592 @@
+// Row passes over logits: log-probabilities, and the clipped policy loss with its
+// gradient in one pass. A row's policy slope depends on its own log-probability
+// alone, so a row is read from HBM once, kept on the chip until its sum is known,
+// and its gradient written.
+//
+// k_policy_rows: persistent clusters of 1 to 8 blocks, a block per SM taking its share of each
+// of its cluster's rows. The block's warps have one task each and meet at mbarriers only:
+//   load    one warp copies the share into a ring of 32 KB chunks in shared memory by
+//           bulk copies (the vectors at the row's two ends element by element, with
+//           -inf beside the row)
+//   stats   eight warps read the chunks as they land, keeping a maximum and a sum a thread,
+//           and merge them at the row's end
+//   finish  four warps, a row each in turn, merge the block's sums, exchange them with the
+//           cluster's other blocks by messages, and form the token's loss and slope
+//   grad    eight warps read the chunks again, write k ([v = y] - p_v) and free them
+// so that nothing in a row's long chain of small steps (3 to 4 us) holds up another row's
+// traffic: 224 KB of ring cover about 40 KB in flight from HBM, the chain, and a row's
+// share of up to 64 KB (128 KB for the longest rows).
+// k_policy: the policy loss of rows over 1 MB, swept twice from global memory.
+#include <new>
+
+#include "gmc.h"
+#include "gmc_loss.cuh"
+
+namespace gmc {
+namespace {
+
+constexpr int kChunkVecs = 2048;       // 16-byte vectors of a chunk
+constexpr int kMostChunks = 6;         // of the ring
+constexpr int kRowSlots = 8;           // rows between the load of their first chunk and their end
+constexpr int kFinishers = 4;
+constexpr int kStatsWarps = 8, kGradWarps = 8;
+constexpr int kStatsBatch = 8;         // vectors of a chunk that a thread takes at once
+constexpr int kGradBatch = 4;
+constexpr int kWorkWarps = kStatsWarps + kGradWarps;
+constexpr int kRowsThreads = (kWorkWarps + kFinishers + 1) * 32;
+constexpr int64_t kMostShare = 4 * kChunkVecs;  // vectors of a row that a block takes at most
+static_assert(kChunkVecs % (kStatsWarps * 32 * kStatsBatch) == 0, "whole batches");
+static_assert(kChunkVecs % (kGradWarps * 32 * kGradBatch) == 0, "whole batches");
+static_assert(kRowSlots % kFinishers == 0, "a slot's rows have one finisher");
+
+// The weighted losses' sum in cluster order, by the last of `clusters` to be done (lane
+// 0 of a warp of each calls with its sum; the lanes of the last warp add).
+__device__ __forceinline__ void reduce_loss(const PolicyArgs& P, double mine, uint32_t cluster, uint32_t clusters) {
+  const int lane = threadIdx.x & 31;
+  uint32_t last = 0;
+  if (lane == 0) {
+    P.partial[cluster] = mine;
+    __threadfence();
+    last = atomicInc(P.ticket, clusters - 1) == clusters - 1;  // back to 0 with the last
+    __threadfence();
+  }
+  if (!__shfl_sync(0xffffffffu, last, 0)) return;
+  double s = 0.;
+  for (uint32_t i = lane; i < clusters; i += 32) s += __ldcg(P.partial + i);
+  s = warp_sum(s);
+  if (lane == 0) *P.loss = (float)s;
+}
+
+// What the gradient of a row needs.
+struct RowResult {
+  float h, hc;   // subtracted from a logit, and from its exponent
+  float f, at_y; // -k / S, and k (1 - p_y)
+  int64_t y;
+  int go, far;   // go: a gradient (else zeros); far: h is subtracted
+};
+struct alignas(128) RowsShared {
+  uint64_t full[kMostChunks], empty[kMostChunks];
+  uint64_t summed[kRowSlots];            // the stats warps' sums are there
+  uint64_t heard[kFinishers][2];         // the cluster's sums have come, for a finisher's rows in turn
+  uint64_t ready[kRowSlots];             // the result is there
+  uint64_t free[kRowSlots];              // the row is done
+  uint64_t from[kFinishers][2][kMaxParts];  // (m, S) of each block of the cluster
+  MaxSum ws[kRowSlots][kWorkWarps];
+  RowResult res[kRowSlots];
+  double total[kFinishers];
+  int dead;                              // a wait gave up
+};
+
+__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                   smem_addr(dst)),
+               "l"(src), "r"(bytes), "r"(smem_addr(bar))
+               : "memory");
+}
+// Eight bytes into block `rank`'s copy of dst, counted by its barrier.
+__device__ __forceinline__ void send(uint64_t* dst, uint64_t* bar, uint32_t rank, uint64_t v) {
+  uint32_t d, b;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(smem_addr(dst)), "r"(rank));
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(smem_addr(bar)), "r"(rank));
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(d), "l"(v), "r"(b)
+               : "memory");
+}
+__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_addr(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// A warp's waits: bounded, with one answer for all its lanes.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
+  return __all_sync(0xffffffffu, wait_bounded(bar, parity, limit_ns));
+}
+__device__ __forceinline__ bool warp_wait_cluster(uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
+  bool ok = try_wait_cluster(bar, parity);
+  const uint64_t t0 = global_ns();
+  while (!ok && global_ns() - t0 <= limit_ns) ok = try_wait_cluster(bar, parity);
+  return __all_sync(0xffffffffu, ok);
+}
+
+// A row cut into the 16-byte vectors that cover it: vector i begins `ph` elements
+// before element i N.
+template <typename T>
+struct Cover {
+  int ph;
+  int64_t nv;        // vectors, the first and last perhaps in part
+  bool first, last;  // whether those are in part
+  __device__ Cover(const T* x, int64_t V) {
+    constexpr int N = Vec<T>::N;
+    ph = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
+    nv = (ph + V + N - 1) / N;
+    first = ph != 0;
+    last = (ph + V) % N != 0;
+  }
+};
+
+// A place in the ring, and how often it was used before.
+struct RingAt {
+  int i = 0;
+  uint32_t turn = 0;
+  __device__ __forceinline__ void next(int size) {
+    if (++i == size) i = 0, ++turn;
+  }
+};
+
+// The loss and its gradient (dx may be NULL). per: vectors of a block's share of a row;
+// chunks: of the ring.
+template <typename T>
+__global__ void __launch_bounds__(kRowsThreads, 1)
+    k_policy_rows(Rows<T> R, PolicyArgs P, T* dx, int64_t dld, int parts, int per, int chunks) {
+  constexpr int N = Vec<T>::N;
+  extern __shared__ __align__(128) unsigned char smem[];
+  RowsShared& S = *reinterpret_cast<RowsShared*>(smem);
+  uint4* ring = reinterpret_cast<uint4*>(smem + sizeof(RowsShared));
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int rank = parts > 1 ? (int)cluster_rank() : 0;
+  const int64_t cluster = blockIdx.x / parts, clusters = gridDim.x / parts;
+  const int64_t lo = (int64_t)per * rank;  // this block's first vector of a row
+  const uint64_t limit = P.wait_ns;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < chunks; ++i) {
+      mbar_init(&S.full[i], 1);
+      mbar_init(&S.empty[i], kGradWarps);
+    }
+    for (int i = 0; i < kRowSlots; ++i) {
+      mbar_init(&S.summed[i], kStatsWarps);
+      mbar_init(&S.ready[i], 1);
+      mbar_init(&S.free[i], kGradWarps);
+    }
+    for (int i = 0; i < 2 * kFinishers; ++i) mbar_init(&S.heard[i / 2][i & 1], 1);
+    S.dead = 0;
+    fence_mbar_init();
+  }
+  __syncthreads();
+  if (parts > 1) {  // no message before every block's barriers are there
+    cluster_arrive();
+    cluster_wait();
+  }
+
+  // whether a row counts, asked a row ahead of its use
+  auto weight_of = [&](int64_t row) { return P.weights ? P.weights[row] : P.weight; };
+  auto counts_at = [&](int64_t row) { return row < R.n && R.y[row] >= 0 && weight_of(row) != 0.f; };
+  // this block's vectors of a row
+  auto share_of = [&](const Cover<T>& c) { return (int)max((int64_t)0, (lo + per < c.nv ? lo + per : c.nv) - lo); };
+
+  if (warp < kStatsWarps) {
+    const int tid = (int)threadIdx.x;
+    RingAt at;
+    uint32_t r = 0;  // rows taken before this one
+    bool counts = counts_at(cluster);
+    for (int64_t row = cluster; row < R.n; row += clusters, ++r) {
+      const bool now = counts;
+      counts = counts_at(row + clusters);
+      const int slot = r % kRowSlots;
+      const uint32_t turn = r / kRowSlots;
+      // every row passes every barrier of its slot, also one that does not count: a
+      // parity told in advance is then never two phases old
+      bool ok = !turn || warp_wait(&S.free[slot], (turn - 1) & 1, limit);
+      const Cover<T> c(R.x + row * R.ld, R.V);
+      const int cnt = now ? share_of(c) : 0;
+      MaxSum a;
+      for (int q = 0; q < cnt; q += kChunkVecs, at.next(chunks)) {
+        if (!(ok = ok && warp_wait(&S.full[at.i], at.turn & 1, limit))) break;
+        const uint4* chunk = ring + at.i * kChunkVecs;
+        const int here = min(kChunkVecs, cnt - q);
+#pragma unroll 1
+        for (int v0 = tid; v0 < here; v0 += kStatsWarps * 32 * kStatsBatch) {
+          uint4 v[kStatsBatch];
+#pragma unroll
+          for (int u = 0; u < kStatsBatch; ++u) {
+            const int i = v0 + u * kStatsWarps * 32;
+            v[u] = i < here ? chunk[i] : make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+          }
+          add<T>(&a, v, R.b);
+        }
+      }
+      if (!ok) {
+        S.dead = 1;
+        break;
+      }
+      if (now) a = warp_merge(a, R.b);
+      if (lane == 0) {
+        S.ws[slot][warp] = a;
+        mbar_arrive(&S.summed[slot]);
+      }
+    }
+  } else if (warp < kWorkWarps) {
+    constexpr int kGradThreads = kGradWarps * 32;
+    const int tid = (int)threadIdx.x - kStatsWarps * 32;
+    RingAt at;
+    uint32_t r = 0;
+    bool counts = counts_at(cluster);
+    for (int64_t row = cluster; row < R.n; row += clusters, ++r) {
+      const bool now = counts;
+      counts = counts_at(row + clusters);
+      const int slot = r % kRowSlots;
+      // the result comes after the sums, and these after the row's chunks
+      if (!warp_wait(&S.ready[slot], (r / kRowSlots) & 1, limit)) {
+        S.dead = 1;
+        break;
+      }
+      const T* x = R.x + row * R.ld;
+      const Cover<T> c(x, R.V);
+      const int cnt = share_of(c);
+      const RowResult g = S.res[slot];
+      T* out = dx + row * dld;
+      // whether vectors can be written whole; the few far rows are left to the slow path too
+      const bool same = !g.far && (reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T) == (unsigned)c.ph;
+      const int64_t vy = g.y < R.V ? (g.y + c.ph) / N - lo : -1;  // the target's vector
+      for (int q = 0; q < cnt; q += kChunkVecs) {
+        const int place = at.i;
+        if (now) at.next(chunks);  // a row that does not count holds no chunks
+        const uint4* chunk = ring + place * kChunkVecs;
+        const int here = min(kChunkVecs, cnt - q);
+        const Pair cc = pair_of(R.b.c, R.b.c), cl = pair_of(R.b.lo, R.b.lo), hc = pair_of(-g.hc, -g.hc),
+                   by = pair_of(g.f, g.f);
+        auto slope = [&](Pair v) { return mul_pair(by, exp2_pair(fma_pair(v, cl, fma_pair(v, cc, hc)))); };
+        const int64_t j0 = (lo + q) * N - c.ph;  // the chunk's first element
+        // the whole vectors among them
+        const int vb = !same ? here : j0 < 0 ? 1 : 0;
+        const int ve = !same ? here : j0 + (int64_t)here * N > R.V ? here - 1 : here;
+        uint4* dst = reinterpret_cast<uint4*>(out + j0);
+        if (!dx) {
+        } else if (g.go) {
+#pragma unroll 1
+          for (int v0 = tid; v0 < ve; v0 += kGradThreads * kGradBatch) {
+            uint4 w[kGradBatch];  // (past the end: what the chunk last held, not stored)
+#pragma unroll
+            for (int u = 0; u < kGradBatch; ++u) w[u] = chunk[v0 + u * kGradThreads];
+#pragma unroll
+            for (int u = 0; u < kGradBatch; ++u) {
+              const int v = v0 + u * kGradThreads;
+              Pair f[N / 2];
+              Vec<T>::pairs(w[u], f);
+#pragma unroll
+              for (int e = 0; e < N / 2; ++e) f[e] = slope(f[e]);
+              w[u] = Vec<T>::put_pairs(f);
+              if (v >= vb && v < ve) __stcs(dst + v, w[u]);
+            }
+          }
+        } else {
+          for (int v = tid; v < ve; v += kGradThreads)
+            if (v >= vb) __stcs(dst + v, make_uint4(0, 0, 0, 0));
+        }
+        // the rest element by element: the row's ends, or all of a row that lies otherwise
+        if (dx && (vb > 0 || ve < here)) {
+          auto single = [&](int i) {
+            const int64_t j = j0 + i;
+            if (j < 0 || j >= R.V) return;
+            float one = 0.f, none = 0.f;
+            if (g.go)
+              split(slope(pair_of(Vec<T>::one(reinterpret_cast<const T*>(chunk)[i]) - (g.far ? g.h : 0.f), 0.f)), &one,
+                    &none);
+            out[j] = Vec<T>::round(one);
+          };
+          for (int i = tid; i < vb * N; i += kGradThreads) single(i);
+          for (int i = max(ve, vb) * N + tid; i < here * N; i += kGradThreads) single(i);
+        }
+        // the target's own, by the thread that wrote its place
+        const int64_t v = vy - q;
+        if (dx && g.go && v >= 0 && v < here) {
+          const int i = (int)(g.y - j0);
+          const int by_tid = (v >= vb && v < ve ? (int)v : v < vb ? i : i - max(ve, vb) * N) & (kGradThreads - 1);
+          if (tid == by_tid) out[g.y] = Vec<T>::round(g.at_y);
+        }
+        if (now) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&S.empty[place]);
+        }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.free[slot]);
+    }
+  } else if (warp < kWorkWarps + kFinishers) {
+    const int me = warp - kWorkWarps;
+    double total = 0.;
+    uint32_t r = (uint32_t)me;
+    uint32_t trades = 0;  // rows whose sums this finisher exchanged
+    bool alive = true;
+    for (int64_t row = cluster + me * clusters; row < R.n; row += kFinishers * clusters, r += kFinishers) {
+      const int slot = r % kRowSlots;
+      const uint32_t turn = r / kRowSlots;
+      const int64_t y = R.y[row];
+      const float w = weight_of(row);
+      const bool counts = y >= 0 && w != 0.f;
+      float xy = 0.f, adv = 0.f, old_logp = 0.f, ref_logp = 0.f;
+      if (counts) {
+        xy = target_logit(R.x + row * R.ld, R.V, y);
+        adv = P.adv[row];
+        old_logp = P.old_logp[row];
+        ref_logp = P.ref_logp ? P.ref_logp[row] : 0.f;
+      }
+      RowResult g = {};
+      RowStats st = {};
+      float loss = 0.f;
+      alive = (!turn || warp_wait(&S.free[slot], (turn - 1) & 1, limit)) && warp_wait(&S.summed[slot], turn & 1, limit);
+      if (alive && counts) {
+        MaxSum a = warp_merge(lane < kStatsWarps ? S.ws[slot][lane] : MaxSum(), R.b);
+        if (parts > 1) {
+          // two sets of slots in turn: a block sends its next but one row's sums only after
+          // it has heard this one's next, which this one sends after it has read these
+          const int set = trades & 1;
+          uint64_t* bar = &S.heard[me][set];
+          if (lane == 0) mbar_arrive_expect_tx(bar, 8u * (uint32_t)parts);
+          __syncwarp();
+          if (lane < parts)
+            send(&S.from[me][set][rank], bar, (uint32_t)lane,
+                 ((uint64_t)__float_as_uint(a.s) << 32) | __float_as_uint(a.m));
+          alive = warp_wait_cluster(bar, (trades >> 1) & 1, limit);
+          ++trades;
+          a = MaxSum();
+          if (lane < parts) {
+            const uint64_t v = *reinterpret_cast<volatile uint64_t*>(&S.from[me][set][lane]);
+            a.m = __uint_as_float((uint32_t)v);
+            a.s = __uint_as_float((uint32_t)(v >> 32));
+          }
+          a = warp_merge(a, R.b);
+        }
+        st = finish(a, xy, R.b);
+        float slope = 0.f;
+        if (!st.empty) policy_terms(P, adv, old_logp, ref_logp, st.logp, &loss, &slope);
+        const float k = w * slope * R.b.scale;
+        g.h = st.h.h;
+        g.far = st.h.far;
+        g.hc = st.h.far ? 0.f : st.h.hc;
+        g.f = -k / a.s;
+        g.at_y = k * -expm1f(st.logp);
+        g.y = y;
+        g.go = slope != 0.f && !st.empty;
+        total += (double)w * (double)loss;
+      }
+      if (!alive) {
+        S.dead = 1;
+        break;
+      }
+      if (lane == 0) {
+        S.res[slot] = g;
+        mbar_arrive(&S.ready[slot]);
+        if (rank == 0) {
+          if (P.token_loss) P.token_loss[row] = loss;
+          if (P.logp) P.logp[row] = st.logp;
+        }
+      }
+    }
+    if (lane == 0) S.total[me] = total;
+  } else {
+    RingAt at;
+    bool counts = counts_at(cluster), alive = true;
+    for (int64_t row = cluster; row < R.n && alive; row += clusters) {
+      const bool now = counts;
+      counts = counts_at(row + clusters);
+      if (!now) continue;
+      const T* x = R.x + row * R.ld;
+      const Cover<T> c(x, R.V);
+      const int cnt = share_of(c);
+      for (int q = 0; q < cnt; q += kChunkVecs) {
+        if (at.turn && !warp_wait(&S.empty[at.i], (at.turn - 1) & 1, limit)) {
+          S.dead = 1;
+          alive = false;
+          break;
+        }
+        uint4* chunk = ring + at.i * kChunkVecs;
+        const int64_t v0 = lo + q, v1 = v0 + min(kChunkVecs, cnt - q);
+        const int64_t a = c.first && v0 == 0 ? 1 : v0, b = c.last && v1 == c.nv ? v1 - 1 : v1;
+        if (lane == 0 && b > a) {
+          const uint32_t bytes = (uint32_t)(b - a) * 16u;
+          mbar_expect_tx(&S.full[at.i], bytes);
+          bulk_load(chunk + (a - v0), x - c.ph + a * N, bytes, &S.full[at.i]);
+        }
+        // the vectors that the row covers in part
+        if (a > v0 && lane < N) {
+          const int64_t j = (int64_t)lane - c.ph;
+          reinterpret_cast<T*>(chunk)[lane] = j >= 0 && j < R.V ? x[j] : Vec<T>::round(-INFINITY);
+        }
+        if (b < v1 && b >= a && lane < N) {
+          const int64_t j = b * N - c.ph + lane;
+          reinterpret_cast<T*>(chunk + (b - v0))[lane] = j < R.V ? x[j] : Vec<T>::round(-INFINITY);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S.full[at.i]);
+        at.next(chunks);
+      }
+    }
+    // no copy is under way when the block ends, whatever became of its readers
+    for (int i = 0; i < chunks; ++i) {
+      const uint32_t uses = i < at.i ? at.turn + 1 : at.turn;
+      if (uses) wait_bounded(&S.full[i], (uses - 1) & 1, limit);
+    }
+  }
+  __syncthreads();
+  if (parts > 1) {  // no block ends while another may still send to it
+    cluster_arrive();
+    cluster_wait();
+  }
+  if (warp == 0 && rank == 0) {
+    double total = 0.;
+    for (int i = 0; i < kFinishers; ++i) total += S.total[i];
+    if (S.dead) total = (double)__uint_as_float(kNan);
+    reduce_loss(P, total, (uint32_t)cluster, (uint32_t)clusters);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rows swept twice
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads) k_policy(Rows<T> R, PolicyArgs P, T* dx, int64_t dld, int parts) {
+  __shared__ MaxSum ws[32], cs[kMaxParts];
+  const int64_t cluster = blockIdx.x / parts, clusters = gridDim.x / parts;
+  const int part = (int)(blockIdx.x - cluster * parts);
+  double total = 0.;
+  if (parts > 1) {  // no message before every block has begun
+    cluster_arrive();
+    cluster_wait();
+  }
+  for (int64_t row = cluster; row < R.n; row += clusters) {
+    const int64_t y = R.y[row];
+    const float w = P.weights ? P.weights[row] : P.weight;
+    const T* x = R.x + row * R.ld;
+    RowStats r = {};
+    float loss = 0.f, slope = 0.f;
+    const bool counts = y >= 0 && w != 0.f;
+    if (counts) {
+      const float xy = target_logit(x, R.V, y);
+      MaxSum a = block_merge(sweep(x, R.V, R.b, part, parts), R.b, ws);
+      a = cluster_merge(a, parts, R.b, cs);
+      r = finish(a, xy, R.b);
+      if (!r.empty)
+        policy_terms(P, P.adv[row], P.old_logp[row], P.ref_logp ? P.ref_logp[row] : 0.f, r.logp, &loss, &slope);
+    }
+    if (part == 0 && threadIdx.x == 0) {
+      total += (double)w * (double)loss;
+      if (P.token_loss) P.token_loss[row] = loss;
+      if (P.logp) P.logp[row] = r.logp;
+    }
+    // every block has read its x[y] and the shared maxima before dx (perhaps x itself) is
+    // written and the next row begins
+    if (counts && parts > 1) {
+      cluster_arrive();
+      cluster_wait();
+    } else {
+      __syncthreads();
+    }
+    if (dx)
+      write_gradient(x, dx + row * dld, R.V, grad_of(r.h, r.ls, w * slope, y, R.b), R.b,
+                     !counts || slope == 0.f || r.empty, part, parts);
+  }
+  if (part == 0 && threadIdx.x < 32) reduce_loss(P, total, (uint32_t)cluster, (uint32_t)clusters);
+}
+
+// The vectors that cover a row at most, whatever its alignment (all rows alike: at theirs).
+template <typename T>
+int64_t most_vecs(const Rows<T>& R) {
+  const int64_t bytes = R.V * (int64_t)sizeof(T);
+  const bool alike = (reinterpret_cast<uintptr_t>(R.x) & 15) == 0 && (R.ld * (int64_t)sizeof(T) & 15) == 0;
+  return alike ? (bytes + 15) / 16 : (bytes + 15) / 16 + 1;
+}
+
+template <typename T>
+cudaError_t launch_rows(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, int64_t nv, cudaStream_t s) {
+  int sms = 1;
+  cudaError_t err = Residency::sms(&sms);
+  if (err != cudaSuccess) return err;
+  // shares of 64 KB at most where 8 blocks a row allow it, and smaller ones while there
+  // are blocks without a row
+  int parts = 1;
+  while (parts < kMaxParts && (nv > (int64_t)parts * 2 * kChunkVecs || (R.n * parts * 2 <= sms && nv > parts * 512)))
+    parts *= 2;
+  const int per = (int)((nv + parts - 1) / parts);
+  const int64_t mine = (R.n * parts + sms - 1) / sms * ((per + kChunkVecs - 1) / kChunkVecs);  // chunks of a block's rows
+  int chunks = kMostChunks;
+  if (mine < chunks) chunks = (int)mine;
+  const int least = (per + kChunkVecs - 1) / kChunkVecs;
+  if (chunks < least) chunks = least;
+  LaunchConfig l(parts, kRowsThreads, parts, sizeof(RowsShared) + (size_t)chunks * kChunkVecs * 16, s);
+  int64_t clusters = 1;
+  err = Residency::clusters((const void*)k_policy_rows<T>, l, parts, &clusters);
+  if (err != cudaSuccess) return err;
+  if (clusters > R.n) clusters = R.n;
+  if (clusters > kMostClusters) clusters = kMostClusters;
+  l.cfg.gridDim.x = (unsigned)(clusters * parts);
+  return cudaLaunchKernelEx(&l.cfg, k_policy_rows<T>, R, A, dx, dld, parts, per, chunks);
+}
+
+}  // namespace
+
+namespace {
+struct Known {
+  const void* f = nullptr;
+  int device = 0, threads = 0, parts = 0, clusters = 0;
+  size_t smem = 0;
+};
+thread_local Known t_known[32];
+thread_local int t_next = 0;
+thread_local int t_device = -1, t_sms = 0;
+}  // namespace
+
+cudaError_t Residency::sms(int* out) {
+  int device = 0;
+  cudaError_t err = cudaGetDevice(&device);
+  if (err == cudaSuccess && device != t_device) {
+    err = cudaDeviceGetAttribute(&t_sms, cudaDevAttrMultiProcessorCount, device);
+    if (err == cudaSuccess) t_device = device;
+  }
+  *out = t_sms;
+  return err;
+}
+cudaError_t Residency::clusters(const void* f, const LaunchConfig& l, int parts, int64_t* out) {
+  int sms = 1;
+  cudaError_t err = Residency::sms(&sms);
+  if (err != cudaSuccess) return err;
+  const int threads = (int)l.cfg.blockDim.x;
+  const size_t smem = l.cfg.dynamicSmemBytes;
+  for (const Known& k : t_known)
+    if (k.f == f && k.device == t_device && k.threads == threads && k.parts == parts && k.smem == smem) {
+      *out = k.clusters;
+      return cudaSuccess;
+    }
+  err = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  int n = 0;
+  if (err == cudaSuccess)
+    err = parts > 1 ? cudaOccupancyMaxActiveClusters(&n, f, &l.cfg)
+                    : cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, f, threads, smem);
+  if (err != cudaSuccess) {
+    cudaGetLastError();  // this call's
+    return err;
+  }
+  if (parts == 1) n *= sms;
+  if (n < 1) return cudaErrorLaunchOutOfResources;
+  t_known[t_next] = {f, t_device, threads, parts, n, smem};
+  t_next = (t_next + 1) % 32;
+  *out = n;
+  return cudaSuccess;
+}
+
+template <typename T>
+cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, cudaStream_t s) {
+  const int64_t nv = most_vecs(R);
+  if (nv <= kMaxParts * kMostShare) return launch_rows<T>(R, A, dx, dld, nv, s);
+  const int parts = kMaxParts;
+  int sms = 1;
+  const cudaError_t err = Residency::sms(&sms);
+  if (err != cudaSuccess) return err;
+  int64_t clusters = 2 * sms / parts;
+  if (clusters > R.n) clusters = R.n;
+  return launch(k_policy<T>, clusters * parts, kLossThreads, parts, s, R, A, dx, dld, parts);
+}
+template cudaError_t launch_policy<float>(const Rows<float>&, const PolicyArgs&, float*, int64_t, cudaStream_t);
+template cudaError_t launch_policy<__nv_bfloat16>(const Rows<__nv_bfloat16>&, const PolicyArgs&, __nv_bfloat16*, int64_t,
+                                                  cudaStream_t);
+template cudaError_t launch_policy<__half>(const Rows<__half>&, const PolicyArgs&, __half*, int64_t, cudaStream_t);
+
+}  // namespace gmc

@@ -17,12 +17,59 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
-// 16 bytes of a row, as floats and back (one rounding, to nearest even).
+// Two floats in a register pair: one instruction for both (each rounded as alone).
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair pair_of(float a, float b) {
+  Pair p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+  return p;
+}
+__device__ __forceinline__ void split(Pair p, float* a, float* b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(p));
+}
+__device__ __forceinline__ Pair fma_pair(Pair a, Pair b, Pair c) {
+  Pair d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ Pair add_pair(Pair a, Pair b) {
+  Pair d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair mul_pair(Pair a, Pair b) {
+  Pair d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ Pair exp2_pair(Pair x) {
+  float a, b;
+  split(x, &a, &b);
+  return pair_of(exp2_fast(a), exp2_fast(b));
+}
+
+// 16 bytes of a row, as floats and back (one rounding, to nearest even). top: the larger
+// of two words' values, place by place; kLow: a word of -inf.
 template <typename T>
 struct Vec;
 template <>
 struct Vec<float> {
   static constexpr int N = 4;
+  static constexpr uint32_t kLow = 0xff800000u;
+  __device__ static uint32_t top(uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }
+  __device__ static float top_of(uint32_t w) { return __uint_as_float(w); }
+  __device__ static void pairs(const uint4& q, Pair* p) {
+    p[0] = pair_of(__uint_as_float(q.x), __uint_as_float(q.y));
+    p[1] = pair_of(__uint_as_float(q.z), __uint_as_float(q.w));
+  }
+  __device__ static uint4 put_pairs(const Pair* p) {
+    float f[4];
+    split(p[0], f, f + 1);
+    split(p[1], f + 2, f + 3);
+    return put(f);
+  }
   __device__ static void get(const uint4& q, float* f) {
     f[0] = __uint_as_float(q.x), f[1] = __uint_as_float(q.y);
     f[2] = __uint_as_float(q.z), f[3] = __uint_as_float(q.w);
@@ -36,6 +83,25 @@ struct Vec<float> {
 template <>
 struct Vec<__nv_bfloat16> {
   static constexpr int N = 8;
+  static constexpr uint32_t kLow = 0xff80ff80u;
+  __device__ static uint32_t top(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 h = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  __device__ static float top_of(uint32_t w) {
+    return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+  }
+  __device__ static void pairs(const uint4& q, Pair* p) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = pair_of(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+  __device__ static uint4 put_pairs(const Pair* p) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split(p[i], f + 2 * i, f + 2 * i + 1);
+    return put(f);
+  }
   __device__ static void get(const uint4& q, float* f) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -56,6 +122,29 @@ struct Vec<__nv_bfloat16> {
 template <>
 struct Vec<__half> {
   static constexpr int N = 8;
+  static constexpr uint32_t kLow = 0xfc00fc00u;
+  __device__ static uint32_t top(uint32_t a, uint32_t b) {
+    const __half2 h = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  __device__ static float top_of(uint32_t w) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return fmaxf(f.x, f.y);
+  }
+  __device__ static void pairs(const uint4& q, Pair* p) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      p[i] = pair_of(f.x, f.y);
+    }
+  }
+  __device__ static uint4 put_pairs(const Pair* p) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split(p[i], f + 2 * i, f + 2 * i + 1);
+    return put(f);
+  }
   __device__ static void get(const uint4& q, float* f) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
