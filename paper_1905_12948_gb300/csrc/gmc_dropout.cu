@@ -36,7 +36,7 @@ struct DropArgs {
 template <typename T>
 __device__ __forceinline__ uint4 load_vec(const T* p, bool aligned) {
   if (aligned) return __ldcs(reinterpret_cast<const uint4*>(p));
-  T v[Vec<T>::N];
+  alignas(16) T v[Vec<T>::N];
 #pragma unroll
   for (int e = 0; e < Vec<T>::N; ++e) v[e] = p[e];
   return *reinterpret_cast<const uint4*>(v);

