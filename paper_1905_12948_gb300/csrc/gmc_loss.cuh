@@ -244,61 +244,73 @@ __device__ __forceinline__ RowGrad grad_of(const Shift& h, float ls, float coef,
 __device__ __forceinline__ float grad_at_target(float x, const RowGrad& g, const Base& b) {
   return g.k * -expm1f(logp_of(x, g.h, g.ls, b));
 }
-// f: logits j .. j + N - 1 of the row, replaced by their gradients.
-template <int N>
-__device__ __forceinline__ void grad_vec(float* f, int64_t j, const RowGrad& g, const Base& b) {
-  const uint64_t at = (uint64_t)(g.y - j);
-  float fy = 0.f;
-  if (at < N) {
+// A vector's logits to their gradients (the target's as any other's).
+template <typename T>
+__device__ __forceinline__ uint4 grad_vec(const uint4& v, const RowGrad& g, const Base& b) {
+  constexpr int P = Vec<T>::N / 2;
+  const float h = g.h.far ? -g.h.h : 0.f, hc = g.h.far ? 0.f : -g.h.hc;
+  const Pair sh = pair_of(h, h), by = pair_of(g.f, g.f), c = pair_of(b.c, b.c), lo = pair_of(b.lo, b.lo),
+             off = pair_of(hc, hc);
+  Pair x[P];
+  Vec<T>::pairs(v, x);
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (at == e) fy = grad_at_target(f[e], g, b);
+  for (int i = 0; i < P; ++i) {
+    x[i] = add_pair(x[i], sh);
+    x[i] = mul_pair(by, exp2_pair(fma_pair(x[i], lo, fma_pair(x[i], c, off))));
   }
-  const float h = g.h.far ? g.h.h : 0.f, hc = g.h.far ? 0.f : g.h.hc;
-#pragma unroll
-  for (int e = 0; e < N; ++e) f[e] = g.f * exp2_fast(exponent(f[e] - h, hc, b));
-  if (at < N) {
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (at == e) f[e] = fy;
-  }
+  return Vec<T>::put_pairs(x);
 }
 
-// One block's share of a row's gradient, or of zeros (skip: x is not read, it may
-// hold anything): 16-byte loads and, where the output row lies at the same offset from
-// a 16-byte boundary, stores.
+// A share (`part` of `parts`) of a row's gradient, or of zeros (skip: x is not read, it may
+// hold anything), by a block: 16-byte loads, kSweepVecs at a time a thread, and, where
+// the output row lies at the same offset from a 16-byte boundary, stores.
 template <typename T>
 __device__ __forceinline__ void write_gradient(const T* x, T* dx, int64_t V, const RowGrad& g, const Base& b, bool skip,
                                                int64_t part, int64_t parts) {
-  constexpr int N = Vec<T>::N;
+  constexpr int N = Vec<T>::N, U = kSweepVecs;
   const int head = head_of(x, V);
   const int64_t nv = (V - head) / N;
   const int tail = (int)(V - head - nv * N);
   const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15) == 0;
   const int64_t per = (nv + parts - 1) / parts;
   const int64_t lo = per * part, hi = lo + per < nv ? lo + per : nv;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x) {
-    const int64_t j = head + i * N;
-    float f[N];
-    if (skip) {
+  const uint4* q = reinterpret_cast<const uint4*>(x + head);
+  const int64_t vy = g.y >= head ? (g.y - head) / N : -1;  // the target's vector (none of [lo, hi) where it is at an edge)
+  for (int64_t i0 = lo + threadIdx.x; i0 < hi; i0 += U * (int64_t)blockDim.x) {
+    uint4 v[U];
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = 0.f;
-    } else {
-      Vec<T>::get(*reinterpret_cast<const uint4*>(x + j), f);
-      grad_vec<N>(f, j, g, b);
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * (int64_t)blockDim.x;
+      v[u] = make_uint4(0, 0, 0, 0);
+      if (!skip && i < hi) v[u] = q[i];
     }
-    if (same) {
-      __stcs(reinterpret_cast<uint4*>(dx + j), Vec<T>::put(f));
-    } else {
 #pragma unroll
-      for (int e = 0; e < N; ++e) dx[j + e] = Vec<T>::round(f[e]);
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * (int64_t)blockDim.x;
+      if (i >= hi) continue;
+      T* to = dx + head + i * N;
+      // (x may be dx: the target's logit is taken before its place is written)
+      const float fy = !skip && i == vy ? grad_at_target(Vec<T>::one(x[g.y]), g, b) : 0.f;
+      const uint4 w = skip ? v[u] : grad_vec<T>(v[u], g, b);
+      if (same) {
+        __stcs(reinterpret_cast<uint4*>(to), w);
+      } else {
+        const T* one = reinterpret_cast<const T*>(&w);
+#pragma unroll
+        for (int e = 0; e < N; ++e) to[e] = one[e];
+      }
+      if (!skip && i == vy) dx[g.y] = Vec<T>::round(fy);
     }
   }
   if (part == 0 && (int)threadIdx.x < head + tail) {
     const int t = (int)threadIdx.x;
     const int64_t j = t < head ? (int64_t)t : V - tail + (t - head);
-    float f = skip ? 0.f : Vec<T>::one(x[j]);
-    if (!skip) grad_vec<1>(&f, j, g, b);
+    float f = 0.f;
+    if (!skip) {
+      const float v = Vec<T>::one(x[j]);
+      f = j == g.y ? grad_at_target(v, g, b)
+                   : g.f * exp2_fast(g.h.far ? exponent(v - g.h.h, 0.f, b) : exponent(v, g.h.hc, b));
+    }
     dx[j] = Vec<T>::round(f);
   }
 }
