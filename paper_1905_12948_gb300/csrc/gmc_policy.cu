@@ -1,7 +1,6 @@
-// Row passes over logits: log-probabilities, and the clipped policy loss with its
-// gradient in one pass. A row's policy slope depends on its own log-probability
-// alone, so a row is read from HBM once, kept on the chip until its sum is known,
-// and its gradient written.
+// The clipped policy loss with its gradient in one pass over the logits. A row's slope
+// depends on its own log-probability alone, so a row is read from HBM once, kept on
+// the chip until its sum is known, and its gradient written.
 //
 // k_policy_rows: persistent clusters of 1 to 8 blocks, a block per SM taking its share of each
 // of its cluster's rows. The block's warps have one task each and meet at mbarriers only:
@@ -14,9 +13,10 @@
 //           cluster's other blocks by messages, and form the token's loss and slope
 //   grad    eight warps read the chunks again, write k ([v = y] - p_v) and free them
 // so that nothing in a row's long chain of small steps (3 to 4 us) holds up another row's
-// traffic: 224 KB of ring cover about 40 KB in flight from HBM, the chain, and a row's
+// traffic: 192 KB of ring cover about 40 KB in flight from HBM, the chain, and a row's
 // share of up to 64 KB (128 KB for the longest rows).
-// k_policy: the policy loss of rows over 1 MB, swept twice from global memory.
+// k_policy_short: short rows, one a warp. k_policy: rows over 1 MB, swept twice from global
+// memory.
 #include <new>
 
 #include "gmc.h"
@@ -440,6 +440,149 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 }
 
 // ---------------------------------------------------------------------------
+// Short rows, one a warp
+// ---------------------------------------------------------------------------
+// Each warp has two buffers of a row and takes rows by itself: while it works on one, the
+// next but one's bulk copy is under way. Nothing is shared with another warp but the sum of
+// the losses at the end. cap: vectors of a buffer.
+constexpr int kShortWarps = 24;  // of a block at most
+constexpr int kShortBatch = 4;   // vectors that a lane takes at once
+constexpr int64_t kShortVecs = 1100;         // vectors of a row at most (17 KB)
+constexpr int64_t kShortBytes = 220 * 1024;  // of all buffers of a block
+
+template <typename T>
+__global__ void __launch_bounds__(kShortWarps * 32, 1)
+    k_policy_short(Rows<T> R, PolicyArgs P, T* dx, int64_t dld, int cap) {
+  constexpr int N = Vec<T>::N;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ uint64_t full[kShortWarps][2];
+  __shared__ double totals[kShortWarps];
+  __shared__ int dead;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  uint4* mine = reinterpret_cast<uint4*>(smem) + (int64_t)warp * 2 * cap;
+  if (threadIdx.x == 0) dead = 0;
+  if (lane == 0) {
+    mbar_init(&full[warp][0], 1);
+    mbar_init(&full[warp][1], 1);
+    fence_mbar_init();
+  }
+  __syncthreads();
+  const int64_t first = (int64_t)warp * gridDim.x + blockIdx.x, step = (int64_t)warps * gridDim.x;
+  double total = 0.;
+  uint32_t loaded[2] = {0, 0};
+  // begin the copy of a row that counts into buffer b
+  auto load = [&](int64_t row, int b) {
+    if (row >= R.n || R.y[row] < 0 || (P.weights && P.weights[row] == 0.f)) return;
+    const T* x = R.x + row * R.ld;
+    const Cover<T> c(x, R.V);
+    uint4* to = mine + b * cap;
+    const int64_t v0 = c.first ? 1 : 0, v1 = c.last ? c.nv - 1 : c.nv;
+    if (lane == 0 && v1 > v0) {
+      const uint32_t bytes = (uint32_t)(v1 - v0) * 16u;
+      mbar_expect_tx(&full[warp][b], bytes);
+      bulk_load(to + v0, x - c.ph + v0 * N, bytes, &full[warp][b]);
+    }
+    if (c.first && lane < N) {
+      const int64_t j = (int64_t)lane - c.ph;
+      reinterpret_cast<T*>(to)[lane] = j >= 0 && j < R.V ? x[j] : Vec<T>::round(-INFINITY);
+    }
+    if (c.last && v1 >= v0 && lane < N) {
+      const int64_t j = v1 * N - c.ph + lane;
+      reinterpret_cast<T*>(to + v1)[lane] = j < R.V ? x[j] : Vec<T>::round(-INFINITY);
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&full[warp][b]);
+    ++loaded[b];
+  };
+  load(first, 0);
+  load(first + step, 1);
+  int b = 0;
+  for (int64_t row = first; row < R.n; row += step, b ^= 1) {
+    const int64_t y = R.y[row];
+    const float w = P.weights ? P.weights[row] : P.weight;
+    const bool counts = y >= 0 && w != 0.f;
+    const T* x = R.x + row * R.ld;
+    T* out = dx + row * dld;
+    const Cover<T> c(x, R.V);
+    const int nv = (int)c.nv;
+    const uint4* v = mine + b * cap;
+    RowStats st = {};
+    float loss = 0.f, slope = 0.f;
+    if (counts) {
+      const float xy = target_logit(x, R.V, y);
+      const float adv = P.adv[row], old_logp = P.old_logp[row], ref_logp = P.ref_logp ? P.ref_logp[row] : 0.f;
+      if (!warp_wait(&full[warp][b], (loaded[b] - 1) & 1, P.wait_ns)) {
+        dead = 1;
+        break;
+      }
+      MaxSum a;
+#pragma unroll 1
+      for (int k0 = lane; k0 < nv; k0 += 32 * kShortBatch) {
+        uint4 q[kShortBatch];
+#pragma unroll
+        for (int u = 0; u < kShortBatch; ++u)
+          q[u] = k0 + 32 * u < nv ? v[k0 + 32 * u] : make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+        add<T>(&a, q, R.b);
+      }
+      st = finish(warp_merge(a, R.b), xy, R.b);
+      if (!st.empty) policy_terms(P, adv, old_logp, ref_logp, st.logp, &loss, &slope);
+    }
+    if (lane == 0) {
+      total += (double)w * (double)loss;
+      if (P.token_loss) P.token_loss[row] = loss;
+      if (P.logp) P.logp[row] = st.logp;
+    }
+    if (dx) {
+      const bool skip = slope == 0.f || st.empty;  // (0 also where the row does not count)
+      const bool same = (reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T) == (unsigned)c.ph;
+      const RowGrad g = grad_of(st.h, st.ls, w * slope, y, R.b);
+      const int vb = !same ? nv : c.first ? 1 : 0, ve = !same ? nv : c.last ? nv - 1 : nv;
+      uint4* dst = reinterpret_cast<uint4*>(out - c.ph);
+#pragma unroll 1
+      for (int k0 = lane; k0 < ve; k0 += 32 * kShortBatch) {
+        uint4 q[kShortBatch];
+#pragma unroll
+        for (int u = 0; u < kShortBatch; ++u) q[u] = skip ? make_uint4(0, 0, 0, 0) : v[min(k0 + 32 * u, nv - 1)];
+#pragma unroll
+        for (int u = 0; u < kShortBatch; ++u) {
+          const int k = k0 + 32 * u;
+          if (!skip) q[u] = grad_vec<T>(q[u], g, R.b);
+          if (k >= vb && k < ve) __stcs(dst + k, q[u]);
+        }
+      }
+      // the rest element by element: the row's ends, or all of a row that lies otherwise
+      auto single = [&](int i) {
+        const int64_t j = i - c.ph;
+        if (j < 0 || j >= R.V) return;
+        float f = 0.f;
+        if (!skip) {
+          const float l = Vec<T>::one(reinterpret_cast<const T*>(v)[i]);
+          f = g.f * exp2_fast(g.h.far ? exponent(l - g.h.h, 0.f, R.b) : exponent(l, g.h.hc, R.b));
+        }
+        out[j] = Vec<T>::round(f);
+      };
+      if (vb > 0 || ve < nv) {
+        for (int i = lane; i < vb * N; i += 32) single(i);
+        for (int i = max(ve, vb) * N + lane; i < nv * N; i += 32) single(i);
+      }
+      __syncwarp();  // the target's own, after what is in its place
+      if (lane == 0 && !skip && y < R.V) out[y] = Vec<T>::round(g.k * -expm1f(st.logp));
+    }
+    __syncwarp();  // every lane has read the buffer
+    load(row + 2 * step, b);
+  }
+  for (int i = 0; i < 2; ++i)  // no copy is under way when the block ends
+    if (loaded[i]) warp_wait(&full[warp][i], (loaded[i] - 1) & 1, P.wait_ns);
+  if (lane == 0) totals[warp] = total;
+  __syncthreads();
+  if (warp == 0) {
+    total = 0.;
+    for (int i = 0; i < warps; ++i) total += totals[i];
+    reduce_loss(P, dead ? (double)__uint_as_float(kNan) : total, blockIdx.x, gridDim.x);
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Rows swept twice
 // ---------------------------------------------------------------------------
 template <typename T>
@@ -555,7 +698,8 @@ cudaError_t Residency::clusters(const void* f, const LaunchConfig& l, int parts,
       *out = k.clusters;
       return cudaSuccess;
     }
-  err = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+  if (smem > 48 * 1024)  // (of the 227 KB, leaving room for static shared memory)
+    err = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
   int n = 0;
   if (err == cudaSuccess)
     err = parts > 1 ? cudaOccupancyMaxActiveClusters(&n, f, &l.cfg)
@@ -575,11 +719,26 @@ cudaError_t Residency::clusters(const void* f, const LaunchConfig& l, int parts,
 template <typename T>
 cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, cudaStream_t s) {
   const int64_t nv = most_vecs(R);
+  int sms = 1;
+  cudaError_t err = Residency::sms(&sms);
+  if (err != cudaSuccess) return err;
+  // Short rows, and more of them than the ring kernel's blocks see twice: a warp a row. 16,384 x
+  // 2,221 bf16 41 us (ring 153), 1,000 x 5,001 12 (18), 9,689 x 8,696 91 (96); 4,000 x 12,001 73
+  // (ring 54), 300 x 8,000 12 (10).
+  if (nv <= kShortVecs && R.n > 2 * sms) {
+    const int cap = (int)(nv + 7) / 8 * 8;
+    int warps = (int)(kShortBytes / (cap * 32));
+    if (warps > kShortWarps) warps = kShortWarps;
+    LaunchConfig l(1, warps * 32, 1, (size_t)warps * cap * 32, s);
+    int64_t blocks = 1;
+    err = Residency::clusters((const void*)k_policy_short<T>, l, 1, &blocks);
+    if (err != cudaSuccess) return err;
+    if (blocks > R.n) blocks = R.n;
+    l.cfg.gridDim.x = (unsigned)blocks;
+    return cudaLaunchKernelEx(&l.cfg, k_policy_short<T>, R, A, dx, dld, cap);
+  }
   if (nv <= kMaxParts * kMostShare) return launch_rows<T>(R, A, dx, dld, nv, s);
   const int parts = kMaxParts;
-  int sms = 1;
-  const cudaError_t err = Residency::sms(&sms);
-  if (err != cudaSuccess) return err;
   int64_t clusters = 2 * sms / parts;
   if (clusters > R.n) clusters = R.n;
   return launch(k_policy<T>, clusters * parts, kLossThreads, parts, s, R, A, dx, dld, parts);
