@@ -73,3 +73,36 @@ def test_failure_hooks_without_gpu(lib):
     assert lib.gmc_test_refuse_cooperative(-1) == 1
     assert lib.gmc_test_refuse_cooperative(0) == 0
     assert lib.gmc_check(None) == 1
+
+
+def test_operators_module_loads_and_refuses_without_gpu(lib):
+    """The compiled Python module of the operators: loads, wants init() once, and refuses
+    what is not a CUDA tensor with an exception of Python's."""
+    torch = pytest.importorskip("torch")
+    from paper_1905_12948_gb300 import dropout, token_logp, tokens
+    with pytest.raises(TypeError, match="logits must be a CUDA tensor"):
+        token_logp(torch.zeros(2, 3), torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(TypeError, match="x must be a CUDA tensor"):
+        dropout(3.0, 0.1, seed=1)
+    module = tokens._load()
+    with pytest.raises(TypeError, match="expected"):
+        module.policy(1, 2)
+    with pytest.raises(ValueError):
+        module.init(RuntimeError, 0, 0, 0, 0, 0)
+
+
+def test_operators_refuse_bad_arguments_without_gpu(lib):
+    import ctypes
+    buf = ctypes.create_string_buffer(4096)
+    p = ctypes.addressof(buf) + 16 - ctypes.addressof(buf) % 16
+    # type, stride, alignment, vocabulary, scale: refused before anything is launched
+    for args in [(p, 3, 4, 10, 10, 1.0), (p, 0, 4, 10, 9, 1.0), (p + 2, 0, 4, 10, 10, 1.0), (p, 0, 4, 0, 10, 1.0),
+                 (p, 0, 4, 10, 10, 0.0), (p, 0, 4, 10, 10, float("inf")), (None, 0, 4, 10, 10, 1.0),
+                 (p, 0, -1, 10, 10, 1.0), (p, 0, 4, 1 << 31, 1 << 31, 1.0)]:
+        assert lib.gmc_token_logp(*args, p, p, None, None) == 1, args
+    assert lib.gmc_token_logp(None, 0, 0, 10, 10, 1.0, None, None, None, None) == 0     # no rows: nothing to do
+    assert lib.gmc_dropout(p, 8, None, 0, p, 8, 0, 0, 2, 8, 1.5, 0, 0, 0, None) == 1
+    assert lib.gmc_dropout(None, 0, None, 0, None, 0, 0, 0, 0, 8, 0.5, 0, 0, 0, None) == 0
+    assert lib.gmc_policy_loss(None, p, 0, 4, 10, 10, 1.0, p, p, None, p, None, 0.2, 0.2, 0.0, p, None, None, None, 10,
+                               None) == 1
+    lib.gmc_loss_destroy(None)

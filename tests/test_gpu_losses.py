@@ -472,3 +472,46 @@ def test_workspace_allocation_failure():
     assert lib.gmc_test_fail_alloc(-1) == held + 1
     h.close()
     assert lib.gmc_test_fail_alloc(-1) == held
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("pad,shift", [(0, 3), (7, 0), (5, 2), (16, 8), (1, 0)])
+def test_gradients_of_views(pad, shift, kind):
+    """A gradient allocated for a view (padded rows, an odd start) has the view's shape,
+    and its rows lie at the same offsets from a 16-byte boundary."""
+    import torch
+    from paper_1905_12948_gb300 import token_logp, token_logp_backward
+    n, V = 5, 1_003
+    rng, t, x, y = _logits(n, V, 11, kind, pad, shift)
+    _, st = token_logp(t, _dev(y), return_stats=True)
+    d = token_logp_backward(t, _dev(y), st, torch.ones(n, device="cuda"))
+    assert d.shape == t.shape and d.dtype == t.dtype
+    for i in range(n):
+        assert (d[i].data_ptr() - t[i].data_ptr()) % 16 == 0
+    _check_gradient(d, x, y, np.ones(n), np.zeros(n), 1.0, kind)
+
+
+def test_one_row_views_and_requires_grad():
+    """A row of a larger tensor, and logits that autograd follows: logits.backward takes
+    the gradient."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    n, V = 8, 77
+    w = torch.randn((16, V), device="cuda", requires_grad=True)
+    h = torch.randn((n, 16), device="cuda")
+    logits = h @ w
+    y = torch.arange(n, device="cuda")
+    old, adv = torch.full((n,), -3.0, device="cuda"), torch.ones(n, device="cuda")
+    loss = TokenLoss(n)
+    r = loss.policy(logits, y, old, adv, clip_high=1e6)
+    assert not r.loss.requires_grad
+    logits.backward(r.dlogits)
+    ratio = torch.exp(torch.log_softmax((h @ w.detach()).double(), -1)[y, y] - old.double())
+    z = w.detach().double().requires_grad_()
+    lp = torch.log_softmax(h.double() @ z, -1)[y, y]
+    (-torch.exp(lp - old.double()).mean()).backward()
+    # products of fp32 matrices: 16 terms of about 1, and a gradient good to P of itself
+    np.testing.assert_allclose(w.grad.double().cpu().numpy(), z.grad.cpu().numpy(), rtol=1e-3, atol=1e-5 * float(ratio.max()))
+    one = loss.policy(logits.detach()[3:4], y[3:4], old[3:4], adv[3:4], clip_high=1e6)
+    assert torch.equal(one.logp, r.logp[3:4])
+    loss.close()
