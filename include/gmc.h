@@ -443,8 +443,9 @@ int gmc_topk_noalloc(const float* x_dev, int64_t n, int64_t k, uint32_t* idx_dev
  * no distribution: its logp is -inf, and it adds nothing to a loss or a gradient.
  * +inf and NaN among the logits of a row that counts make its outputs NaN.
  * Sums and exponentials are formed in 32 bits whatever the type, and a gradient
- * is rounded once, to the logits' type; a sum over rows is held in 64 bits and
- * taken in a fixed order: the same call gives the same bits.
+ * is rounded once, to the logits' type; a sum over rows is held in 64 bits (a
+ * sequence's, of its rows' logp before they are rounded) and taken in a fixed order: the
+ * same call gives the same bits.
  * dlogits_dev has rows of stride dld >= vocab and may be logits_dev itself (with
  * dld = ld): the gradient then replaces the logits. Other overlaps of an output
  * with an input are the caller's mistake. Requires vocab < 2^31, n <= 2^27.

@@ -16,7 +16,8 @@ namespace {
 // logp and (m, log S) of a row, by a cluster of blocks (thread 0 of part 0 writes). S is
 // written as +inf for an empty row, which no sum reaches.
 template <typename T>
-__device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int part, int parts, float* logp, float2* stats) {
+__device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int part, int parts, float* logp, float2* stats,
+                                          float* low) {
   __shared__ MaxSum ws[32], cs[kMaxParts];
   const int64_t y = R.y[row];
   if (y < 0) {  // not scored
@@ -36,6 +37,7 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
     const RowStats r = finish(a, xy, R.b);
     logp[row] = r.logp;
     if (stats) stats[row] = make_float2(r.h.h, r.empty ? INFINITY : r.ls);
+    if (low) low[row] = r.low;
   }
 }
 
@@ -44,7 +46,7 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
 template <typename T>
 __global__ void __launch_bounds__(kLossThreads) k_stats(Rows<T> R, float* logp, float2* stats, int parts) {
   const int64_t row = blockIdx.x / parts;
-  row_stats(R, row, (int)(blockIdx.x - row * parts), parts, logp, stats);
+  row_stats(R, row, (int)(blockIdx.x - row * parts), parts, logp, stats, (float*)nullptr);
 }
 
 struct PairArgs {
@@ -53,6 +55,7 @@ struct PairArgs {
   const int64_t* y;
   const float* logp;
   const float2* stats;
+  float* low;                             // of each row: what logp's rounding took away
   const float *ref_logp, *weights;
   float weight, beta, smoothing;          // weight: of every pair, where weights is NULL
   float *loss, *pair_loss, *seq_ratio;    // the last two may be NULL
@@ -105,7 +108,7 @@ __device__ __forceinline__ void pair_of_rows(const PairArgs& P, int64_t p) {
     double s = 0.;
     for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x)
       if (P.y[i] >= 0 && __ldcg(&P.stats[i].y) != INFINITY)
-        s += (double)__ldcg(P.logp + i) - (P.ref_logp ? (double)P.ref_logp[i] : 0.);
+        s += (double)__ldcg(P.logp + i) + (double)__ldcg(P.low + i) - (P.ref_logp ? (double)P.ref_logp[i] : 0.);
     sums[side] = block_sum(s);
   }
   if (threadIdx.x == 0) finish_pair(P, p, sums[0], sums[1]);
@@ -162,7 +165,7 @@ __global__ void __launch_bounds__(kLossThreads) k_pair_stats(Rows<T> R, PairArgs
       rows = P.offsets[2 * p + 2] - P.offsets[2 * p];
     }
   }
-  row_stats(R, row, part, parts, logp, stats);
+  row_stats(R, row, part, parts, logp, stats, P.low);
   if (p < 0 || !last_of(P.count + p, 1, rows)) return;
   pair_of_rows(P, p);
   if (threadIdx.x == 0) P.count[p] = 0;
@@ -207,6 +210,7 @@ struct gmc_loss_ctx {
   double* partial = nullptr; // kMostClusters
   uint32_t* ticket = nullptr;
   float* logp = nullptr;     // max_rows
+  float* low = nullptr;      // max_rows
   float* slope = nullptr;    // max_pairs
   uint32_t* count = nullptr; // max_pairs + 1, zero between calls
 };
@@ -292,7 +296,7 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   h->max_rows = max_rows;
   h->max_pairs = max_pairs;
   const size_t bytes =
-      8 * (size_t)(kMostClusters + 1 + max_pairs + max_rows) + 4 * (size_t)(max_rows + 2 * max_pairs + 1);
+      8 * (size_t)(kMostClusters + 1 + max_pairs + max_rows) + 4 * (size_t)(2 * max_rows + 2 * max_pairs + 1);
   cudaError_t err = cudaGetDevice(&h->device);
   if (err == cudaSuccess) err = lib_malloc(&h->mem, bytes);
   // the memset runs on the default stream, with which a caller's need not be ordered
@@ -308,7 +312,8 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   h->wloss = h->partial + kMostClusters + 1;
   h->stats = reinterpret_cast<float2*>(h->wloss + max_pairs);
   h->logp = reinterpret_cast<float*>(h->stats + max_rows);
-  h->slope = h->logp + max_rows;
+  h->low = h->logp + max_rows;
+  h->slope = h->low + max_rows;
   h->count = reinterpret_cast<uint32_t*>(h->slope + max_pairs);
   *out = h;
   return GMC_OK;
@@ -369,7 +374,7 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   float* logp = logp_dev ? logp_dev : h->logp;
   const float weight = pairs ? (float)(1.0 / (double)pairs) : 0.f;
-  const PairArgs P{offsets_dev, n, pairs, targets_dev, logp, h->stats, ref_logp_dev, weights_dev, weight, beta,
+  const PairArgs P{offsets_dev, n, pairs, targets_dev, logp, h->stats, h->low, ref_logp_dev, weights_dev, weight, beta,
                    smoothing, loss_dev, pair_loss_dev, seq_ratio_dev, h->slope, h->wloss, h->count};
   const bool grad = n > 0 && dlogits_dev;
   cudaError_t err = by_type(dtype, [&](auto t) {
