@@ -13,23 +13,26 @@ using namespace gmc;
 
 namespace {
 
-// logp and (m, log S) of a row, by a cluster of blocks (thread 0 of part 0 writes). S is
-// written as +inf for an empty row, which no sum reaches.
+// logp and (m, log S) of a row, by a cluster of blocks (thread 0 of part 0 writes), and
+// in ratio (NULL: not wanted) logp before its rounding, less ref's; 0 for a row that adds
+// nothing. S is written as +inf for an empty row, which no sum reaches.
 template <typename T>
 __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int part, int parts, float* logp, float2* stats,
-                                          float* low) {
+                                          const float* ref, double* ratio) {
   __shared__ MaxSum ws[32], cs[kMaxParts];
   const int64_t y = R.y[row];
   if (y < 0) {  // not scored
     if (part == 0 && threadIdx.x == 0) {
       logp[row] = 0.f;
       if (stats) stats[row] = make_float2(0.f, 0.f);
+      if (ratio) ratio[row] = 0.;
     }
     return;
   }
   if (parts > 1) cluster_arrive();
   const T* x = R.x + row * R.ld;
   const float xy = target_logit(x, R.V, y);
+  const double less = ref ? (double)ref[row] : 0.;
   MaxSum a = block_merge(sweep(x, R.V, R.b, part, parts), R.b, ws);
   if (parts > 1) cluster_wait();  // every block has begun
   a = cluster_merge(a, parts, R.b, cs);
@@ -37,7 +40,7 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
     const RowStats r = finish(a, xy, R.b);
     logp[row] = r.logp;
     if (stats) stats[row] = make_float2(r.h.h, r.empty ? INFINITY : r.ls);
-    if (low) low[row] = r.low;
+    if (ratio) ratio[row] = r.empty ? 0. : (double)r.logp + (double)r.low - less;
   }
 }
 
@@ -46,17 +49,14 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
 template <typename T>
 __global__ void __launch_bounds__(kLossThreads) k_stats(Rows<T> R, float* logp, float2* stats, int parts) {
   const int64_t row = blockIdx.x / parts;
-  row_stats(R, row, (int)(blockIdx.x - row * parts), parts, logp, stats, (float*)nullptr);
+  row_stats(R, row, (int)(blockIdx.x - row * parts), parts, logp, stats, (const float*)nullptr, (double*)nullptr);
 }
 
 struct PairArgs {
   const int64_t* offsets;
   int64_t n, pairs;
-  const int64_t* y;
-  const float* logp;
-  const float2* stats;
-  float* low;                             // of each row: what logp's rounding took away
   const float *ref_logp, *weights;
+  double* ratio;                          // log ratio of each row
   float weight, beta, smoothing;          // weight: of every pair, where weights is NULL
   float *loss, *pair_loss, *seq_ratio;    // the last two may be NULL
   float* slope;                           // beta w dl/dmargin of each pair
@@ -75,21 +75,23 @@ __device__ __forceinline__ int64_t sequence_of(const PairArgs& P, int64_t row) {
 }
 
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.f) + log1pf(expf(-fabsf(x))); }
-// Sum over the block in a fixed order; every thread returns it.
-__device__ __forceinline__ double block_sum(double s) {
+// Sums over the first and the second half of the block, in a fixed order, for every thread.
+struct Halves {
+  double a, b;
+};
+__device__ __forceinline__ Halves block_sums(double s) {
   __shared__ double ws[kLossThreads / 32];
   s = warp_sum(s);
   __syncthreads();
   if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = s;
   __syncthreads();
-  s = 0.;
-  for (int i = 0; i < kLossThreads / 32; ++i) s += ws[i];
-  return s;
+  Halves h{0., 0.};
+  for (int i = 0; i < kLossThreads / 64; ++i) h.a += ws[i], h.b += ws[kLossThreads / 64 + i];
+  return h;
 }
 // A pair's loss and slope from its sequences' log ratios.
-__device__ __forceinline__ void finish_pair(const PairArgs& P, int64_t p, double chosen, double other) {
+__device__ __forceinline__ void finish_pair(const PairArgs& P, int64_t p, float w, double chosen, double other) {
   const float margin = (float)((double)P.beta * (chosen - other));
-  const float w = P.weights ? P.weights[p] : P.weight;
   const float up = softplus(-margin), down = softplus(margin);  // -log sigmoid(margin), -log sigmoid(-margin)
   const float loss = (1.f - P.smoothing) * up + P.smoothing * down;
   const float sig_up = 1.f / (1.f + expf(-margin)), sig_down = 1.f / (1.f + expf(margin));
@@ -98,20 +100,19 @@ __device__ __forceinline__ void finish_pair(const PairArgs& P, int64_t p, double
   if (P.pair_loss) P.pair_loss[p] = loss;
   if (P.seq_ratio) P.seq_ratio[2 * p] = (float)chosen, P.seq_ratio[2 * p + 1] = (float)other;
 }
-// By one block: the log ratios of a pair whose rows are all done.
+__device__ __forceinline__ float weight_of(const PairArgs& P, int64_t p) { return P.weights ? P.weights[p] : P.weight; }
+// By one block, half of it a sequence: the log ratios of a pair whose rows are all done.
 __device__ __forceinline__ void pair_of_rows(const PairArgs& P, int64_t p) {
-  double sums[2];
-  for (int side = 0; side < 2; ++side) {
-    int64_t lo = P.offsets[2 * p + side], hi = P.offsets[2 * p + side + 1];
-    lo = lo < 0 ? 0 : lo;
-    hi = hi > P.n ? P.n : hi;
-    double s = 0.;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += blockDim.x)
-      if (P.y[i] >= 0 && __ldcg(&P.stats[i].y) != INFINITY)
-        s += (double)__ldcg(P.logp + i) + (double)__ldcg(P.low + i) - (P.ref_logp ? (double)P.ref_logp[i] : 0.);
-    sums[side] = block_sum(s);
-  }
-  if (threadIdx.x == 0) finish_pair(P, p, sums[0], sums[1]);
+  constexpr int half = kLossThreads / 2;
+  const int side = (int)threadIdx.x / half;
+  const float w = weight_of(P, p);
+  int64_t lo = P.offsets[2 * p + side], hi = P.offsets[2 * p + side + 1];
+  lo = lo < 0 ? 0 : lo;
+  hi = hi > P.n ? P.n : hi;
+  double s = 0.;
+  for (int64_t i = lo + threadIdx.x % half; i < hi; i += half) s += __ldcg(P.ratio + i);
+  const Halves h = block_sums(s);
+  if (threadIdx.x == 0) finish_pair(P, p, w, h.a, h.b);
 }
 // Thread 0 adds to a count that other blocks add to; every thread returns whether it
 // has reached `all`. What the blocks wrote before is then visible to this one.
@@ -126,50 +127,53 @@ __device__ __forceinline__ bool last_of(uint32_t* count, uint32_t mine, int64_t 
   __syncthreads();
   return last != 0;
 }
-// The loss, by the block that did the last pairs.
-__device__ __forceinline__ void sum_pairs(const PairArgs& P, uint32_t mine) {
-  if (!last_of(P.count + P.pairs, mine, P.pairs)) return;
+// The pairs' weighted losses added up, by one block.
+__device__ __forceinline__ void sum_pairs(const PairArgs& P) {
   double s = 0.;
   for (int64_t p = threadIdx.x; p < P.pairs; p += blockDim.x) s += __ldcg(P.wloss + p);
-  s = block_sum(s);
-  if (threadIdx.x == 0) {
-    *P.loss = (float)s;
-    P.count[P.pairs] = 0;
-  }
+  const Halves h = block_sums(s);
+  if (threadIdx.x == 0) *P.loss = (float)(h.a + h.b);
 }
 
 // k_stats, and the pairs' losses and slopes: the block that does a pair's last row does the
-// pair, the one that does the last pair the sum. The cluster past the last row does the
-// pairs that have no rows.
+// pair. The cluster past the last row does the pairs that have no rows. total: the block
+// that does the last pair adds up the loss (k_grad does so where it follows).
+// Six blocks an SM (40 registers): the pairs' part would take 58, and the sums' loads four
+// blocks at once (16 pairs of 50,257: 391 us instead of 363).
 template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_pair_stats(Rows<T> R, PairArgs P, float* logp, float2* stats, int parts) {
+__global__ void __launch_bounds__(kLossThreads, 6) k_pair_stats(Rows<T> R, PairArgs P, float* logp, float2* stats, int parts,
+                                                                bool total) {
   const int64_t row = blockIdx.x / parts;
   const int part = (int)(blockIdx.x - row * parts);
+  uint32_t done = 1;
   if (row == R.n) {
     if (part != 0) return;
     uint32_t empty = 0;
     for (int64_t p = threadIdx.x; p < P.pairs; p += blockDim.x)
       if (P.offsets[2 * p] >= P.offsets[2 * p + 2]) {
-        finish_pair(P, p, 0., 0.);
+        finish_pair(P, p, weight_of(P, p), 0., 0.);
         ++empty;
       }
     __threadfence();
-    sum_pairs(P, (uint32_t)block_sum((double)empty));
-    return;
-  }
-  int64_t p = -1, rows = 0;
-  if (part == 0) {
-    p = sequence_of(P, row);
-    if (p >= 0) {
-      p >>= 1;
-      rows = P.offsets[2 * p + 2] - P.offsets[2 * p];
+    const Halves h = block_sums((double)empty);
+    done = (uint32_t)(h.a + h.b);
+  } else {
+    int64_t p = -1, rows = 0;
+    if (part == 0) {
+      p = sequence_of(P, row);
+      if (p >= 0) {
+        p >>= 1;
+        rows = P.offsets[2 * p + 2] - P.offsets[2 * p];
+      }
     }
+    row_stats(R, row, part, parts, logp, stats, P.ref_logp, P.ratio);
+    if (p < 0 || !last_of(P.count + p, 1, rows)) return;
+    pair_of_rows(P, p);
+    if (threadIdx.x == 0) P.count[p] = 0;
   }
-  row_stats(R, row, part, parts, logp, stats, P.low);
-  if (p < 0 || !last_of(P.count + p, 1, rows)) return;
-  pair_of_rows(P, p);
-  if (threadIdx.x == 0) P.count[p] = 0;
-  sum_pairs(P, 1);
+  if (!total || !last_of(P.count + P.pairs, done, P.pairs)) return;
+  sum_pairs(P);
+  if (threadIdx.x == 0) P.count[P.pairs] = 0;
 }
 
 // dx = g s ([v = y] - p) of each row from its saved (m, log S). Without g, a row's is the
@@ -192,11 +196,13 @@ __global__ void __launch_bounds__(kLossThreads) k_grad(Rows<T> R, const float2* 
     }
     if (y >= R.V) coef = __uint_as_float(kNan);
   }
-  if (!g && blockIdx.x == 0)  // whatever the offsets were, the next call finds the counts at 0
-    for (int64_t i = threadIdx.x; i <= P.pairs; i += blockDim.x) P.count[i] = 0;
   const float2 st = coef != 0.f ? stats[row] : make_float2(0.f, 0.f);
   write_gradient(R.x + row * R.ld, dx + row * dld, R.V, grad_of(shift_of(st.x, R.b), st.y, coef, y, R.b), R.b,
                  coef == 0.f || st.y == INFINITY, part, parts);
+  if (g || blockIdx.x != 0) return;
+  sum_pairs(P);
+  // whatever the offsets were, the next call finds the counts at 0
+  for (int64_t i = threadIdx.x; i <= P.pairs; i += blockDim.x) P.count[i] = 0;
 }
 
 }  // namespace
@@ -210,7 +216,7 @@ struct gmc_loss_ctx {
   double* partial = nullptr; // kMostClusters
   uint32_t* ticket = nullptr;
   float* logp = nullptr;     // max_rows
-  float* low = nullptr;      // max_rows
+  double* ratio = nullptr;   // max_rows
   float* slope = nullptr;    // max_pairs
   uint32_t* count = nullptr; // max_pairs + 1, zero between calls
 };
@@ -296,7 +302,7 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   h->max_rows = max_rows;
   h->max_pairs = max_pairs;
   const size_t bytes =
-      8 * (size_t)(kMostClusters + 1 + max_pairs + max_rows) + 4 * (size_t)(2 * max_rows + 2 * max_pairs + 1);
+      8 * (size_t)(kMostClusters + 1 + max_pairs + 2 * max_rows) + 4 * (size_t)(max_rows + 2 * max_pairs + 1);
   cudaError_t err = cudaGetDevice(&h->device);
   if (err == cudaSuccess) err = lib_malloc(&h->mem, bytes);
   // the memset runs on the default stream, with which a caller's need not be ordered
@@ -311,9 +317,9 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   h->ticket = reinterpret_cast<uint32_t*>(h->partial + kMostClusters);
   h->wloss = h->partial + kMostClusters + 1;
   h->stats = reinterpret_cast<float2*>(h->wloss + max_pairs);
-  h->logp = reinterpret_cast<float*>(h->stats + max_rows);
-  h->low = h->logp + max_rows;
-  h->slope = h->low + max_rows;
+  h->ratio = reinterpret_cast<double*>(h->stats + max_rows);
+  h->logp = reinterpret_cast<float*>(h->ratio + max_rows);
+  h->slope = h->logp + max_rows;
   h->count = reinterpret_cast<uint32_t*>(h->slope + max_pairs);
   *out = h;
   return GMC_OK;
@@ -374,14 +380,14 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   float* logp = logp_dev ? logp_dev : h->logp;
   const float weight = pairs ? (float)(1.0 / (double)pairs) : 0.f;
-  const PairArgs P{offsets_dev, n, pairs, targets_dev, logp, h->stats, h->low, ref_logp_dev, weights_dev, weight, beta,
-                   smoothing, loss_dev, pair_loss_dev, seq_ratio_dev, h->slope, h->wloss, h->count};
+  const PairArgs P{offsets_dev, n, pairs, ref_logp_dev, weights_dev, h->ratio, weight, beta, smoothing,
+                   loss_dev, pair_loss_dev, seq_ratio_dev, h->slope, h->wloss, h->count};
   const bool grad = n > 0 && dlogits_dev;
   cudaError_t err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
     const Rows<T> R = rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev);
     const int parts = parts_for(n, vocab * (int64_t)sizeof(T));
-    const cudaError_t e = launch(k_pair_stats<T>, (n + 1) * parts, kLossThreads, parts, s, R, P, logp, h->stats, parts);
+    const cudaError_t e = launch(k_pair_stats<T>, (n + 1) * parts, kLossThreads, parts, s, R, P, logp, h->stats, parts, !grad);
     if (e != cudaSuccess || !grad) return e;
     return launch_pdl(k_grad<T>, dim3((unsigned)(n * parts)), dim3(kLossThreads), 0, s, R, (const float2*)h->stats,
                       (const float*)nullptr, P, static_cast<T*>(dlogits_dev), dld, parts);
