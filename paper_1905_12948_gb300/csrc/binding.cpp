@@ -115,11 +115,11 @@ const int64_t* targets(PyObject* o, int64_t n, const Tensor& like) {
 }
 
 // A new tensor of t's shape whose parts t[0], t[1], ... (n elements each, ld apart in t) lie
-// at the offsets from a 16-byte boundary that t's do: contiguous but where t is a view with
+// at the offsets from a `whole`-byte boundary that t's do: contiguous but where t is a view with
 // padded parts or an odd start. The kernels then store whole vectors.
-Tensor empty_beside(const Tensor& t, int64_t parts, int64_t n, int64_t ld) {
-  const int64_t per = 16 / t.element_size();
-  const int64_t shift = (int64_t)(reinterpret_cast<uintptr_t>(t.data_ptr()) & 15) / t.element_size();
+Tensor empty_beside(const Tensor& t, int64_t parts, int64_t n, int64_t ld, int64_t whole) {
+  const int64_t per = whole / t.element_size();
+  const int64_t shift = (int64_t)(reinterpret_cast<uintptr_t>(t.data_ptr()) & (whole - 1)) / t.element_size();
   const int64_t pad = parts > 1 ? (ld - n) % per : 0;
   if (shift == 0 && pad == 0) return at::empty(t.sizes(), t.options());
   std::vector<int64_t> strides(t.dim());
@@ -135,7 +135,7 @@ Tensor empty_beside(const Tensor& t, int64_t parts, int64_t n, int64_t ld) {
 // The gradient's destination: `o`, or a new tensor for None; its row stride in *ld.
 Tensor gradient(PyObject* o, const Tensor& logits, const Rows& r, int64_t* ld) {
   if (o == Py_None) {
-    Tensor t = empty_beside(logits, r.n, r.v, r.ld);
+    Tensor t = empty_beside(logits, r.n, r.v, r.ld, 16);
     *ld = r.n > 1 ? t.stride(0) : r.v;
     return t;
   }
@@ -314,7 +314,7 @@ PyObject* dropout(Args a, Py_ssize_t na) {
     res = r.data_ptr();
   }
   const c10::cuda::OptionalCUDAGuard guard(x.device());
-  const Tensor out = a[7] == Py_None ? empty_beside(x, K, n, ldx) : tensor(a[7], "out");
+  const Tensor out = a[7] == Py_None ? empty_beside(x, K, n, ldx, 32) : tensor(a[7], "out");
   const int64_t ldo = worker_stride(out, x, K, n, "out");
   check(g_abi.dropout(x.data_ptr(), ldx, res, ldr, out.data_ptr(), ldo, k, worker, K, n, p, seed, t, site, stream_of(x)),
         "gmc_dropout");

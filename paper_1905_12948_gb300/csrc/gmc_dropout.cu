@@ -15,7 +15,7 @@ using namespace gmc;
 namespace {
 
 constexpr int kDropThreads = 256;
-constexpr int kDropVecs = 4;  // 16-byte vectors of a tensor that a thread loads together
+constexpr int kDropVecs = 2;  // 32-byte vectors of a tensor that a thread loads together
 // Sets the dropout streams apart from those of the block choice and the sample
 // of the same (seed, t).
 constexpr uint64_t kDropTag = 0x44524F504F555421ull;
@@ -32,16 +32,40 @@ struct DropArgs {
   float gain;
 };
 
-// N consecutive elements at p, in one piece where p lies on a 16-byte boundary.
+// 32 bytes of a row: the widest load and store there is. N elements.
 template <typename T>
-__device__ __forceinline__ uint4 load_vec(const T* p, bool aligned) {
-  if (aligned) return __ldcs(reinterpret_cast<const uint4*>(p));
-  alignas(16) T v[Vec<T>::N];
+struct Wide {
+  static constexpr int N = 2 * Vec<T>::N;
+  uint4 a, b;
+};
+__device__ __forceinline__ bool on32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
+template <typename T>
+__device__ __forceinline__ Wide<T> load_wide(const T* p, bool aligned) {
+  Wide<T> v;
+  if (aligned) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v.a.x), "=r"(v.a.y), "=r"(v.a.z), "=r"(v.a.w), "=r"(v.b.x), "=r"(v.b.y), "=r"(v.b.z), "=r"(v.b.w)
+                 : "l"(p));
+    return v;
+  }
+  alignas(16) T e[Wide<T>::N];
 #pragma unroll
-  for (int e = 0; e < Vec<T>::N; ++e) v[e] = p[e];
-  return *reinterpret_cast<const uint4*>(v);
+  for (int i = 0; i < Wide<T>::N; ++i) e[i] = p[i];
+  v.a = *reinterpret_cast<const uint4*>(e);
+  v.b = *reinterpret_cast<const uint4*>(e + Vec<T>::N);
+  return v;
 }
-__device__ __forceinline__ bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+__device__ __forceinline__ void store_wide(void* p, const uint4& a, const uint4& b) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w),
+               "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+               : "memory");
+}
+// The elements of a row that lie before its first 32-byte boundary.
+template <typename T>
+__device__ __forceinline__ int wide_head(const T* p, int64_t n) {
+  const int h = (int)((32 - (reinterpret_cast<uintptr_t>(p) & 31)) & 31) / (int)sizeof(T);
+  return n < h ? (int)n : h;
+}
 
 // The stream's 16-bit numbers of N elements from element i on, two to a word. r =
 // i mod 4 is the same for the whole row: 0 where its vectors begin with a draw.
@@ -60,37 +84,53 @@ __device__ __forceinline__ void bits_of(uint64_t key, int64_t i, int r, uint32_t
   for (int d = 0; d < N / 4; ++d) w[2 * d] = (uint32_t)z[d], w[2 * d + 1] = (uint32_t)(z[d] >> 32);
 }
 
-// A block takes kDropThreads * kDropVecs vectors of a worker's row: the 16-byte vectors
-// of x, of which the row's first elements (before its first boundary) and last are left
-// to a few threads of the row's first block.
+// One vector's elements: x kept and divided, or 0, plus res.
+template <typename T, bool RES>
+__device__ __forceinline__ uint4 drop_vec(const uint4& x, const uint4& res, const uint32_t* w, uint32_t q, bool none,
+                                          float gain) {
+  constexpr int N = Vec<T>::N;
+  float f[N], g[N];
+  Vec<T>::get(x, f);
+  if (RES) Vec<T>::get(res, g);
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const uint32_t bits = e & 1 ? w[e / 2] : w[e / 2] << 16;  // the number in the upper half
+    f[e] = bits >= q && !none ? f[e] * gain : 0.f;
+    if (RES) f[e] += g[e];
+  }
+  return Vec<T>::put(f);
+}
+
+// A block takes kDropThreads * kDropVecs vectors of 32 bytes of a worker's row: those
+// between x's 32-byte boundaries; the row's first elements (before its first boundary) and
+// its last are left to a few threads of the row's first block.
 //
-// Bound by memory: a draw (two 64-bit products) gives four elements their 16 bits, so
-// about 6 of a dozen instructions an element are the generator's, under half of what an
-// SM issues while its share of the memory's rate moves.
+// Bound by memory, nearly: a draw (two 64-bit products) gives four elements their 16 bits, so
+// about 6 of a dozen instructions an element are the generator's.
 template <typename T, bool RES>
 __global__ void __launch_bounds__(kDropThreads) k_dropout(DropArgs<T> A, int64_t blocks_per_row) {
-  constexpr int N = Vec<T>::N, U = kDropVecs;
+  constexpr int N = Wide<T>::N, H = Vec<T>::N, U = kDropVecs;
   const int64_t k = blockIdx.x / blocks_per_row;
   const int64_t b = blockIdx.x - k * blocks_per_row;
   const T* x = A.x + k * A.ldx;
   const T* res = RES ? A.res + k * A.ldr : nullptr;
   T* out = A.out + k * A.ldo;
   const uint64_t key = sm64_mix(sm64_mix(A.key + kGamma * (A.worker0 + (uint64_t)k + 2)) + kGamma * (A.site + 1));
-  const int head = head_of(x, A.n);
+  const int head = wide_head(x, A.n);
   const int64_t nv = (A.n - head) / N;
   const int r = head & 3;
-  const bool res_on = RES && on16(res + head), out_on = on16(out + head);
+  const bool res_on = RES && on32(res + head), out_on = on32(out + head);
   const uint32_t q = A.q << 16;
   const bool none = A.q > 0xffffu;  // p = 1
   const int64_t v0 = b * (kDropThreads * U) + threadIdx.x;
-  uint4 xv[U], rv[U];
+  Wide<T> xv[U], rv[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t v = v0 + u * kDropThreads;
     if (v >= nv) continue;
     const int64_t i = head + v * N;
-    xv[u] = __ldcs(reinterpret_cast<const uint4*>(x + i));
-    if (RES) rv[u] = load_vec(res + i, res_on);
+    xv[u] = load_wide(x + i, true);
+    if (RES) rv[u] = load_wide(res + i, res_on);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
@@ -99,20 +139,16 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout(DropArgs<T> A, int64_t
     const int64_t i = head + v * N;
     uint32_t w[N / 2];
     bits_of<N>(key, i, r, w);
-    float f[N], g[N];
-    Vec<T>::get(xv[u], f);
-    if (RES) Vec<T>::get(rv[u], g);
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const uint32_t bits = e & 1 ? w[e / 2] : w[e / 2] << 16;  // the number in the upper half
-      f[e] = bits >= q && !none ? f[e] * A.gain : 0.f;
-      if (RES) f[e] += g[e];
-    }
+    alignas(16) T one[N];
+    const uint4 lo = drop_vec<T, RES>(xv[u].a, rv[u].a, w, q, none, A.gain);
+    const uint4 hi = drop_vec<T, RES>(xv[u].b, rv[u].b, w + H / 2, q, none, A.gain);
     if (out_on) {
-      __stcs(reinterpret_cast<uint4*>(out + i), Vec<T>::put(f));
+      store_wide(out + i, lo, hi);
     } else {
+      *reinterpret_cast<uint4*>(one) = lo;
+      *reinterpret_cast<uint4*>(one + H) = hi;
 #pragma unroll
-      for (int e = 0; e < N; ++e) out[i + e] = Vec<T>::round(f[e]);
+      for (int e = 0; e < N; ++e) out[i + e] = one[e];
     }
   }
   const int tail = (int)(A.n - head - nv * N);
@@ -134,7 +170,7 @@ int64_t blocks_of(int64_t n, int64_t per_vec) {
 
 template <typename T>
 cudaError_t run(const DropArgs<T>& A, int64_t K, cudaStream_t s) {
-  const int64_t per = blocks_of(A.n, Vec<T>::N);
+  const int64_t per = blocks_of(A.n, Wide<T>::N);
   if (A.res) k_dropout<T, true><<<(unsigned)(per * K), kDropThreads, 0, s>>>(A, per);
   else k_dropout<T, false><<<(unsigned)(per * K), kDropThreads, 0, s>>>(A, per);
   return cudaGetLastError();
@@ -152,7 +188,7 @@ extern "C" int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_
   if (K > (int64_t(1) << 20) || n > kMost || worker0 > (int64_t(1) << 40)) return GMC_EINVAL;
   if (K > 1 && (ldx < n || ldo < n || ldx > kMost || ldo > kMost)) return GMC_EINVAL;
   if (K > 1 && residual_dev && (ldr < n || ldr > kMost)) return GMC_EINVAL;
-  if (K * blocks_of(n, 16 / (int64_t)size) >= (int64_t(1) << 31)) return GMC_EINVAL;
+  if (K * blocks_of(n, 32 / (int64_t)size) >= (int64_t(1) << 31)) return GMC_EINVAL;
   if (K == 0 || n == 0) return GMC_OK;
   if (!x_dev || !out_dev) return GMC_EINVAL;
   for (const void* q : {x_dev, residual_dev, (const void*)out_dev})

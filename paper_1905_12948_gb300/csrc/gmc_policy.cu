@@ -9,7 +9,7 @@
 //           -inf beside the row)
 //   stats   eight warps read the chunks as they land, keeping a maximum and a sum a thread,
 //           and merge them at the row's end
-//   finish  four warps, a row each in turn, merge the block's sums, exchange them with the
+//   finish  two warps, a row each in turn, merge the block's sums, exchange them with the
 //           cluster's other blocks by messages, and form the token's loss and slope
 //   grad    eight warps read the chunks again, write k ([v = y] - p_v) and free them
 // so that nothing in a row's long chain of small steps (3 to 4 us) holds up another row's
@@ -28,7 +28,7 @@ namespace {
 constexpr int kChunkVecs = 2048;       // 16-byte vectors of a chunk
 constexpr int kMostChunks = 6;         // of the ring
 constexpr int kRowSlots = 8;           // rows between the load of their first chunk and their end
-constexpr int kFinishers = 4;
+constexpr int kFinishers = 2;
 constexpr int kStatsWarps = 8, kGradWarps = 8;
 constexpr int kStatsBatch = 8;         // vectors of a chunk that a thread takes at once
 constexpr int kGradBatch = 4;
