@@ -389,8 +389,8 @@ int gmc_test_leave_barrier(gmc_t h, uint64_t wait_limit_ns);
 /*
  * gmc_test_refuse_cooperative -- process-wide: the next `launches` launches whose
  * blocks wait for one another (the one-launch step of small top-k problems,
- * gmc_topk_noalloc) are answered as CUDA answers one that is too large for its
- * context; 0 disarms the hook. GMC_EINVAL for a negative count.
+ * gmc_topk_noalloc, the clusters of the losses below) are answered as CUDA answers one
+ * that is too large for its context; 0 disarms the hook. GMC_EINVAL for a negative count.
  */
 int gmc_test_refuse_cooperative(int64_t launches);
 
@@ -433,7 +433,7 @@ int gmc_topk_noalloc(const float* x_dev, int64_t n, int64_t k, uint32_t* idx_dev
  *
  * Logits are n rows of `vocab` values of type `dtype`, row r at logits_dev + r*ld
  * elements (ld >= vocab; any alignment of at least an element). For a row x with
- * target y, and `scale` > 0 (1 / temperature):
+ * target y, and `scale` (1 / temperature, 2^-64 to 2^64):
  *   logp = scale*x_y - log sum_v exp(scale*x_v),
  *   d logp / d x_v = scale*([v = y] - p_v),  p_v = exp(scale*x_v) / sum_u exp(scale*x_u).
  * targets_dev holds n int64. A row with a negative target is not scored: it is not
@@ -489,13 +489,21 @@ void gmc_loss_destroy(gmc_loss_t h);
  * kl > 0 (else it may be NULL); weights_dev: n floats, or NULL for 1/n each. A row with
  * weight 0 is not scored, as one with a negative target. loss_dev receives one
  * float; token_loss_dev (l_r, 0 for rows not scored), logp_dev and dlogits_dev may
- * be NULL. 0 <= clip_low <= 1, clip_high >= 0, kl >= 0, all finite.
+ * be NULL. 0 <= clip_low <= 1, clip_high >= 0, kl >= 0, all finite. The blocks that share a
+ * row wait for one another (they run together, as one cluster); should such a wait give up
+ * (about two seconds without progress), loss is NaN and dlogits incomplete.
  * GMC_EINVAL also for n > max_rows. */
 int gmc_policy_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld,
                     float scale, const int64_t* targets_dev, const float* old_logp_dev, const float* ref_logp_dev,
                     const float* advantages_dev, const float* weights_dev, float clip_low, float clip_high, float kl,
                     float* loss_dev, float* token_loss_dev, float* logp_dev, void* dlogits_dev, int64_t dld,
                     void* stream);
+
+/* gmc_test_withhold_row -- for tests, as gmc_test_withhold_copy: the next
+ * gmc_policy_loss of h (only that one) makes no copy of row `row`, and every wait in
+ * it is bounded by wait_limit_ns (1 .. 2e9). The waits on that row give up, and the loss is
+ * NaN if the row counts and is of up to 1 MB (longer rows are not copied). */
+int gmc_test_withhold_row(gmc_loss_t h, int64_t row, uint64_t wait_limit_ns);
 
 /* gmc_preference_loss -- the preference loss on paired log ratios, and its gradient.
  * The rows are 2*pairs sequences one after the other, sequence s being rows

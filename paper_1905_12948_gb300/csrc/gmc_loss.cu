@@ -209,6 +209,9 @@ __global__ void __launch_bounds__(kLossThreads) k_grad(Rows<T> R, const float2* 
 
 struct gmc_loss_ctx {
   int device = 0;
+  Residency resident;
+  int64_t hold_row = -1;     // test hook (gmc_test_withhold_row): of the next policy call,
+  uint64_t hold_ns = 0;      // with this wait limit; 0: off
   int64_t max_rows = 0, max_pairs = 0;
   void* mem = nullptr;
   float2* stats = nullptr;   // max_rows
@@ -229,7 +232,7 @@ bool rows_ok(const void* x, int32_t dtype, int64_t n, int64_t V, int64_t ld, flo
   const uintptr_t size = dtype == GMC_F32 ? 4 : 2;
   if (n < 0 || V < 1 || V >= (int64_t(1) << 31) || n > (int64_t(1) << 27)) return false;
   if (ld < V || ld > (int64_t(1) << 40)) return false;
-  if (!std::isfinite(scale) || !(scale > 0.f)) return false;
+  if (!(scale >= 0x1p-64f && scale <= 0x1p64f)) return false;
   if (n == 0) return true;
   return x && y && reinterpret_cast<uintptr_t>(x) % size == 0 && reinterpret_cast<uintptr_t>(y) % 8 == 0;
 }
@@ -267,10 +270,11 @@ int gmc_token_logp(const void* logits_dev, int32_t dtype, int64_t n, int64_t voc
   if (!logp_dev) return GMC_EINVAL;
   return done(by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    const int parts = parts_for(n, vocab * (int64_t)sizeof(T));
-    return launch(k_stats<T>, n * parts, kLossThreads, parts, static_cast<cudaStream_t>(stream),
-                  rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev), logp_dev,
-                  reinterpret_cast<float2*>(stats_dev), parts);
+    return with_parts(parts_for(n, vocab * (int64_t)sizeof(T)), [&](int parts) {
+      return launch(k_stats<T>, n * parts, kLossThreads, parts, static_cast<cudaStream_t>(stream),
+                    rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev), logp_dev,
+                    reinterpret_cast<float2*>(stats_dev), parts);
+    });
   }));
 }
 
@@ -304,6 +308,7 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   const size_t bytes =
       8 * (size_t)(kMostClusters + 1 + max_pairs + 2 * max_rows) + 4 * (size_t)(max_rows + 2 * max_pairs + 1);
   cudaError_t err = cudaGetDevice(&h->device);
+  if (err == cudaSuccess) err = cudaDeviceGetAttribute(&h->resident.sms, cudaDevAttrMultiProcessorCount, h->device);
   if (err == cudaSuccess) err = lib_malloc(&h->mem, bytes);
   // the memset runs on the default stream, with which a caller's need not be ordered
   if (err == cudaSuccess) err = cudaMemset(h->mem, 0, bytes);
@@ -333,6 +338,13 @@ void gmc_loss_destroy(gmc_loss_t h) {
   delete h;
 }
 
+int gmc_test_withhold_row(gmc_loss_t h, int64_t row, uint64_t wait_limit_ns) {
+  if (!h || row < 0 || row >= h->max_rows || wait_limit_ns < 1 || wait_limit_ns > 2000000000ull) return GMC_EINVAL;
+  h->hold_row = row;
+  h->hold_ns = wait_limit_ns;
+  return GMC_OK;
+}
+
 int gmc_policy_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld,
                     float scale, const int64_t* targets_dev, const float* old_logp_dev, const float* ref_logp_dev,
                     const float* advantages_dev, const float* weights_dev, float clip_low, float clip_high, float kl,
@@ -352,11 +364,12 @@ int gmc_policy_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int64_t
   if (n > 0) {
     const PolicyArgs P{old_logp_dev, kl > 0.f ? ref_logp_dev : nullptr, advantages_dev, weights_dev, clip_low,
                        clip_high, kl, (float)(1.0 / (double)n), token_loss_dev, logp_dev, loss_dev, h->partial,
-                       h->ticket, kWaitLimitNs};
+                       h->ticket, h->hold_ns ? h->hold_ns : kWaitLimitNs, h->hold_ns ? h->hold_row : -1};
+    h->hold_ns = 0;
     err = by_type(dtype, [&](auto t) {
       using T = decltype(t);
       return launch_policy<T>(rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev), P, static_cast<T*>(dlogits_dev),
-                              dld, s);
+                              dld, &h->resident, s);
     });
   } else {
     err = cudaMemsetAsync(loss_dev, 0, sizeof(float), s);
@@ -386,11 +399,13 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
   cudaError_t err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
     const Rows<T> R = rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev);
-    const int parts = parts_for(n, vocab * (int64_t)sizeof(T));
-    const cudaError_t e = launch(k_pair_stats<T>, (n + 1) * parts, kLossThreads, parts, s, R, P, logp, h->stats, parts, !grad);
+    const int most = parts_for(n, vocab * (int64_t)sizeof(T));
+    const cudaError_t e = with_parts(most, [&](int parts) {
+      return launch(k_pair_stats<T>, (n + 1) * parts, kLossThreads, parts, s, R, P, logp, h->stats, parts, !grad);
+    });
     if (e != cudaSuccess || !grad) return e;
-    return launch_pdl(k_grad<T>, dim3((unsigned)(n * parts)), dim3(kLossThreads), 0, s, R, (const float2*)h->stats,
-                      (const float*)nullptr, P, static_cast<T*>(dlogits_dev), dld, parts);
+    return launch_pdl(k_grad<T>, dim3((unsigned)(n * most)), dim3(kLossThreads), 0, s, R, (const float2*)h->stats,
+                      (const float*)nullptr, P, static_cast<T*>(dlogits_dev), dld, most);
   });
   if (err == cudaSuccess && !grad) err = cudaMemsetAsync(h->count, 0, sizeof(uint32_t) * (size_t)(pairs + 1), s);
   return done(err);

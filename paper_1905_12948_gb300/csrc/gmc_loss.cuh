@@ -341,7 +341,8 @@ struct PolicyArgs {
   float* loss;
   double* partial;                        // the clusters' sums of weighted losses
   uint32_t* ticket;                       // counts the clusters that are done; 0 between calls
-  uint64_t wait_ns;
+  uint64_t wait_ns;                       // bound of the waits on mbarriers
+  int64_t hold_row;                       // test hook: no copy of this row is made; -1: none
 };
 
 // The token's loss and its slope in logp.
@@ -381,8 +382,20 @@ struct LaunchConfig {
 };
 template <typename... A, typename... B>
 inline cudaError_t launch(void (*f)(A...), int64_t blocks, int threads, int parts, cudaStream_t s, B... args) {
+  if (parts > 1 && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
   LaunchConfig l(blocks, threads, parts, 0, s);
   return cudaLaunchKernelEx(&l.cfg, f, args...);
+}
+// f(parts), or f(1) where the context (an MPS share, a partitioned GPU) cannot hold clusters of
+// that many blocks.
+template <typename F>
+inline cudaError_t with_parts(int parts, F&& f) {
+  cudaError_t err = f(parts);
+  if (parts > 1 && too_large_here(err)) {
+    cudaGetLastError();  // this launch's
+    err = f(1);
+  }
+  return err;
 }
 
 // Blocks that share a row: enough of them for two a SM, down to 16 KB of it each.
@@ -392,15 +405,21 @@ inline int parts_for(int64_t n, int64_t row_bytes) {
   return parts;
 }
 
-// Facts of the current device: its SMs, and the clusters of a launch configuration that
-// can be resident; looked up once a host thread.
+// Facts of a handle's device: its SMs, and the clusters of a launch configuration that can
+// be resident, looked up once (with what the kernel needs set).
 struct Residency {
-  static cudaError_t sms(int* out);
-  static cudaError_t clusters(const void* f, const LaunchConfig& l, int parts, int64_t* out);
+  int sms = 1;
+  struct {
+    const void* f = nullptr;
+    int threads = 0, parts = 0, clusters = 0;
+    size_t smem = 0;
+  } known[32];
+  int next = 0;
+  cudaError_t clusters(const void* f, const LaunchConfig& l, int parts, int64_t* out);
 };
 
 // The policy loss over n > 0 rows (gmc_policy.cu). A.partial has kMostClusters slots.
 constexpr int kMostClusters = 8192;
 template <typename T>
-cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, cudaStream_t s);
+cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, Residency* device, cudaStream_t s);
 }  // namespace gmc

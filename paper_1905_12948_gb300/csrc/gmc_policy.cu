@@ -401,6 +401,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         uint4* chunk = ring + at.i * kChunkVecs;
         const int64_t v0 = lo + q, v1 = v0 + min(kChunkVecs, cnt - q);
         const int64_t a = c.first && v0 == 0 ? 1 : v0, b = c.last && v1 == c.nv ? v1 - 1 : v1;
+        if (row == P.hold_row) {
+          at.next(chunks);
+          continue;
+        }
         if (lane == 0 && b > a) {
           const uint32_t bytes = (uint32_t)(b - a) * 16u;
           mbar_expect_tx(&S.full[at.i], bytes);
@@ -473,6 +477,8 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
   // begin the copy of a row that counts into buffer b
   auto load = [&](int64_t row, int b) {
     if (row >= R.n || R.y[row] < 0 || (P.weights && P.weights[row] == 0.f)) return;
+    ++loaded[b];
+    if (row == P.hold_row) return;
     const T* x = R.x + row * R.ld;
     const Cover<T> c(x, R.V);
     uint4* to = mine + b * cap;
@@ -492,7 +498,6 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&full[warp][b]);
-    ++loaded[b];
   };
   load(first, 0);
   load(first + step, 1);
@@ -639,10 +644,9 @@ int64_t most_vecs(const Rows<T>& R) {
 }
 
 template <typename T>
-cudaError_t launch_rows(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, int64_t nv, cudaStream_t s) {
-  int sms = 1;
-  cudaError_t err = Residency::sms(&sms);
-  if (err != cudaSuccess) return err;
+cudaError_t launch_rows(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, int64_t nv, Residency* device,
+                        cudaStream_t s) {
+  const int sms = device->sms;
   // shares of 64 KB at most where 8 blocks a row allow it, and smaller ones while there
   // are blocks without a row
   int parts = 1;
@@ -655,8 +659,9 @@ cudaError_t launch_rows(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dl
   const int least = (per + kChunkVecs - 1) / kChunkVecs;
   if (chunks < least) chunks = least;
   LaunchConfig l(parts, kRowsThreads, parts, sizeof(RowsShared) + (size_t)chunks * kChunkVecs * 16, s);
+  if (parts > 1 && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
   int64_t clusters = 1;
-  err = Residency::clusters((const void*)k_policy_rows<T>, l, parts, &clusters);
+  const cudaError_t err = device->clusters((const void*)k_policy_rows<T>, l, parts, &clusters);
   if (err != cudaSuccess) return err;
   if (clusters > R.n) clusters = R.n;
   if (clusters > kMostClusters) clusters = kMostClusters;
@@ -666,38 +671,15 @@ cudaError_t launch_rows(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dl
 
 }  // namespace
 
-namespace {
-struct Known {
-  const void* f = nullptr;
-  int device = 0, threads = 0, parts = 0, clusters = 0;
-  size_t smem = 0;
-};
-thread_local Known t_known[32];
-thread_local int t_next = 0;
-thread_local int t_device = -1, t_sms = 0;
-}  // namespace
-
-cudaError_t Residency::sms(int* out) {
-  int device = 0;
-  cudaError_t err = cudaGetDevice(&device);
-  if (err == cudaSuccess && device != t_device) {
-    err = cudaDeviceGetAttribute(&t_sms, cudaDevAttrMultiProcessorCount, device);
-    if (err == cudaSuccess) t_device = device;
-  }
-  *out = t_sms;
-  return err;
-}
 cudaError_t Residency::clusters(const void* f, const LaunchConfig& l, int parts, int64_t* out) {
-  int sms = 1;
-  cudaError_t err = Residency::sms(&sms);
-  if (err != cudaSuccess) return err;
   const int threads = (int)l.cfg.blockDim.x;
   const size_t smem = l.cfg.dynamicSmemBytes;
-  for (const Known& k : t_known)
-    if (k.f == f && k.device == t_device && k.threads == threads && k.parts == parts && k.smem == smem) {
+  for (const auto& k : known)
+    if (k.f == f && k.threads == threads && k.parts == parts && k.smem == smem) {
       *out = k.clusters;
       return cudaSuccess;
     }
+  cudaError_t err = cudaSuccess;
   if (smem > 48 * 1024)  // (of the 227 KB, leaving room for static shared memory)
     err = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
   int n = 0;
@@ -710,18 +692,16 @@ cudaError_t Residency::clusters(const void* f, const LaunchConfig& l, int parts,
   }
   if (parts == 1) n *= sms;
   if (n < 1) return cudaErrorLaunchOutOfResources;
-  t_known[t_next] = {f, t_device, threads, parts, n, smem};
-  t_next = (t_next + 1) % 32;
+  known[next] = {f, threads, parts, n, smem};
+  next = (next + 1) % 32;
   *out = n;
   return cudaSuccess;
 }
 
 template <typename T>
-cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, cudaStream_t s) {
+cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, Residency* device, cudaStream_t s) {
   const int64_t nv = most_vecs(R);
-  int sms = 1;
-  cudaError_t err = Residency::sms(&sms);
-  if (err != cudaSuccess) return err;
+  const int sms = device->sms;
   // Short rows, and more of them than the ring kernel's blocks see twice: a warp a row. 16,384 x
   // 2,221 bf16 41 us (ring 153), 1,000 x 5,001 12 (18), 9,689 x 8,696 91 (96); 4,000 x 12,001 73
   // (ring 54), 300 x 8,000 12 (10).
@@ -731,21 +711,28 @@ cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t 
     if (warps > kShortWarps) warps = kShortWarps;
     LaunchConfig l(1, warps * 32, 1, (size_t)warps * cap * 32, s);
     int64_t blocks = 1;
-    err = Residency::clusters((const void*)k_policy_short<T>, l, 1, &blocks);
+    const cudaError_t err = device->clusters((const void*)k_policy_short<T>, l, 1, &blocks);
     if (err != cudaSuccess) return err;
     if (blocks > R.n) blocks = R.n;
     l.cfg.gridDim.x = (unsigned)blocks;
     return cudaLaunchKernelEx(&l.cfg, k_policy_short<T>, R, A, dx, dld, cap);
   }
-  if (nv <= kMaxParts * kMostShare) return launch_rows<T>(R, A, dx, dld, nv, s);
-  const int parts = kMaxParts;
-  int64_t clusters = 2 * sms / parts;
-  if (clusters > R.n) clusters = R.n;
-  return launch(k_policy<T>, clusters * parts, kLossThreads, parts, s, R, A, dx, dld, parts);
+  if (nv <= kMaxParts * kMostShare) {
+    const cudaError_t err = launch_rows<T>(R, A, dx, dld, nv, device, s);
+    if (!too_large_here(err)) return err;
+    cudaGetLastError();  // this launch's: no room for its clusters in this context
+  }
+  return with_parts(nv > kMaxParts * kMostShare ? kMaxParts : 1, [&](int parts) {
+    int64_t clusters = 2 * sms / parts;
+    if (clusters > R.n) clusters = R.n;
+    return launch(k_policy<T>, clusters * parts, kLossThreads, parts, s, R, A, dx, dld, parts);
+  });
 }
-template cudaError_t launch_policy<float>(const Rows<float>&, const PolicyArgs&, float*, int64_t, cudaStream_t);
-template cudaError_t launch_policy<__nv_bfloat16>(const Rows<__nv_bfloat16>&, const PolicyArgs&, __nv_bfloat16*, int64_t,
-                                                  cudaStream_t);
-template cudaError_t launch_policy<__half>(const Rows<__half>&, const PolicyArgs&, __half*, int64_t, cudaStream_t);
+template cudaError_t launch_policy<float>(const Rows<float>&, const PolicyArgs&, float*, int64_t, Residency*,
+                                                 cudaStream_t);
+template cudaError_t launch_policy<__nv_bfloat16>(const Rows<__nv_bfloat16>&, const PolicyArgs&, __nv_bfloat16*, int64_t, Residency*,
+                                                 cudaStream_t);
+template cudaError_t launch_policy<__half>(const Rows<__half>&, const PolicyArgs&, __half*, int64_t, Residency*,
+                                                 cudaStream_t);
 
 }  // namespace gmc

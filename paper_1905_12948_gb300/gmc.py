@@ -73,6 +73,7 @@ _SIGNATURES = {
     "gmc_loss_destroy": (None, [_c_p]),
     "gmc_policy_loss": (ctypes.c_int, [_c_p, _c_p, _i32, _i64, _i64, _i64, _f32, _c_p, _c_p, _c_p, _c_p,
                                        _c_p, _f32, _f32, _f32, _c_p, _c_p, _c_p, _c_p, _i64, _c_p]),
+    "gmc_test_withhold_row": (ctypes.c_int, [_c_p, _i64, _u64]),
     "gmc_preference_loss": (ctypes.c_int, [_c_p, _c_p, _i32, _i64, _i64, _i64, _f32, _c_p, _c_p, _i64,
                                            _c_p, _c_p, _f32, _f32, _c_p, _c_p, _c_p, _c_p, _c_p, _i64,
                                            _c_p]),

@@ -515,3 +515,68 @@ def test_one_row_views_and_requires_grad():
     one = loss.policy(logits.detach()[3:4], y[3:4], old[3:4], adv[3:4], clip_high=1e6)
     assert torch.equal(one.logp, r.logp[3:4])
     loss.close()
+
+
+@pytest.mark.parametrize("n,V", [(3, 50_257), (2, 300_001), (40, 8_192)])
+def test_contexts_without_room_for_clusters(n, V):
+    """Launches of clusters answered as in a context with too few SMs: the same results by
+    one block a row."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss, gmc, token_logp
+    rng, t, x, y = _logits(n, V, 12, "f32")
+    lp = ref.token_logp(x, y, 1.0)
+    old, adv = _f32(lp - 0.1), _f32(rng.uniform(0.5, 1.5, n))
+    f, lib = torch.float32, gmc.load()
+    h = TokenLoss(n, 1)
+    want = np.full(n, 1 / n)
+    loss, each, coef = ref.policy(lp, y, old, adv, want, lp, 0.2, 0.2, 0.0)
+    off = np.array([0, n // 2, n])
+    none = np.zeros(n, bool)
+    _, _, ratio, pcoef = ref.preference(lp, y, off, np.zeros(n), np.ones(1), 0.1, 0.0, none)
+    try:
+        for refuse in (1, 2):      # the ring, and the clusters of the two-sweep kernel
+            assert lib.gmc_test_refuse_cooperative(refuse) == 0
+            r = h.policy(t, _dev(y), _dev(old, f), _dev(adv, f))
+            _check_logp(r.logp.double().cpu().numpy(), lp)
+            _check_gradient(r.dlogits, x, y, coef, want * ref.policy_bound(lp, old, adv, lp, 0.0), 1.0, "f32")
+        assert lib.gmc_test_refuse_cooperative(1) == 0
+        _check_logp(token_logp(t, _dev(y)).double().cpu().numpy(), lp)
+        assert lib.gmc_test_refuse_cooperative(1) == 0
+        r = h.preference(t, _dev(y), _dev(off), beta=0.1)
+        _check_logp(r.logp.double().cpu().numpy(), lp)
+        _check_gradient(r.dlogits, x, y, pcoef, np.full(n, 0.1 * 0.1 * (n * 2e-5) + 1e-7), 1.0, "f32")
+    finally:
+        lib.gmc_test_refuse_cooperative(0)
+    h.close()
+
+
+@pytest.mark.parametrize("n,V,kind", [(40, 50_257, "f32"), (200, 9_000, "bf16"), (3, 131_072, "bf16"), (700, 900, "f16"),
+                                      (1, 40, "f32")])
+def test_a_wait_that_runs_out(n, V, kind):
+    """A row whose copy is withheld: every wait gives up, the loss is NaN, and the next call
+    (and a new handle) is right again. By the ring with and without clusters, and a warp a row."""
+    import time
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    rng, t, x, y = _logits(n, V, 13, kind)
+    lp = ref.token_logp(x, y, 1.0)
+    old, adv = _dev(_f32(lp - 0.1), torch.float32), _dev(_f32(rng.uniform(0.5, 1.5, n)), torch.float32)
+    h = TokenLoss(n)
+    want = h.policy(t, _dev(y), old, adv)
+    assert h.lib.gmc_test_withhold_row(h.h, n // 2, 20_000_000) == 0
+    t0 = time.time()
+    assert np.isnan(float(h.policy(t, _dev(y), old, adv).loss))
+    assert time.time() - t0 < 5
+    for handle in (h, TokenLoss(n)):
+        r = handle.policy(t, _dev(y), old, adv)
+        assert torch.equal(r.loss, want.loss) and torch.equal(r.dlogits, want.dlogits)
+        handle.close()
+
+
+def test_withhold_refusals():
+    from paper_1905_12948_gb300 import TokenLoss, gmc
+    lib, h = gmc.load(), TokenLoss(10)
+    assert lib.gmc_test_withhold_row(None, 0, 1000) == GMC_EINVAL
+    for row, ns in ((-1, 1000), (10, 1000), (0, 0), (0, 2_000_000_001)):
+        assert lib.gmc_test_withhold_row(h.h, row, ns) == GMC_EINVAL
+    h.close()
