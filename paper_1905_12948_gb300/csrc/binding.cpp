@@ -135,7 +135,7 @@ Tensor empty_beside(const Tensor& t, int64_t parts, int64_t n, int64_t ld, int64
 // The gradient's destination: `o`, or a new tensor for None; its row stride in *ld.
 Tensor gradient(PyObject* o, const Tensor& logits, const Rows& r, int64_t* ld) {
   if (o == Py_None) {
-    Tensor t = empty_beside(logits, r.n, r.v, r.ld, 16);
+    Tensor t = empty_beside(logits, r.n, r.v, r.ld, 32);
     *ld = r.n > 1 ? t.stride(0) : r.v;
     return t;
   }

@@ -32,41 +32,6 @@ struct DropArgs {
   float gain;
 };
 
-// 32 bytes of a row: the widest load and store there is. N elements.
-template <typename T>
-struct Wide {
-  static constexpr int N = 2 * Vec<T>::N;
-  uint4 a, b;
-};
-__device__ __forceinline__ bool on32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
-template <typename T>
-__device__ __forceinline__ Wide<T> load_wide(const T* p, bool aligned) {
-  Wide<T> v;
-  if (aligned) {
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(v.a.x), "=r"(v.a.y), "=r"(v.a.z), "=r"(v.a.w), "=r"(v.b.x), "=r"(v.b.y), "=r"(v.b.z), "=r"(v.b.w)
-                 : "l"(p));
-    return v;
-  }
-  alignas(16) T e[Wide<T>::N];
-#pragma unroll
-  for (int i = 0; i < Wide<T>::N; ++i) e[i] = p[i];
-  v.a = *reinterpret_cast<const uint4*>(e);
-  v.b = *reinterpret_cast<const uint4*>(e + Vec<T>::N);
-  return v;
-}
-__device__ __forceinline__ void store_wide(void* p, const uint4& a, const uint4& b) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w),
-               "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
-               : "memory");
-}
-// The elements of a row that lie before its first 32-byte boundary.
-template <typename T>
-__device__ __forceinline__ int wide_head(const T* p, int64_t n) {
-  const int h = (int)((32 - (reinterpret_cast<uintptr_t>(p) & 31)) & 31) / (int)sizeof(T);
-  return n < h ? (int)n : h;
-}
-
 // The stream's 16-bit numbers of N elements from element i on, two to a word. r =
 // i mod 4 is the same for the whole row: 0 where its vectors begin with a draw.
 template <int N>
@@ -139,17 +104,10 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout(DropArgs<T> A, int64_t
     const int64_t i = head + v * N;
     uint32_t w[N / 2];
     bits_of<N>(key, i, r, w);
-    alignas(16) T one[N];
-    const uint4 lo = drop_vec<T, RES>(xv[u].a, rv[u].a, w, q, none, A.gain);
-    const uint4 hi = drop_vec<T, RES>(xv[u].b, rv[u].b, w + H / 2, q, none, A.gain);
-    if (out_on) {
-      store_wide(out + i, lo, hi);
-    } else {
-      *reinterpret_cast<uint4*>(one) = lo;
-      *reinterpret_cast<uint4*>(one + H) = hi;
-#pragma unroll
-      for (int e = 0; e < N; ++e) out[i + e] = one[e];
-    }
+    Wide<T> y;
+    y.a = drop_vec<T, RES>(xv[u].a, rv[u].a, w, q, none, A.gain);
+    y.b = drop_vec<T, RES>(xv[u].b, rv[u].b, w + H / 2, q, none, A.gain);
+    store_wide(out + i, y, out_on);
   }
   const int tail = (int)(A.n - head - nv * N);
   if (b == 0 && (int)threadIdx.x < head + tail) {

@@ -16,7 +16,7 @@
 namespace gmc {
 
 constexpr int kLossThreads = 256;
-constexpr int kSweepVecs = 4;  // vectors that a thread of a sweep loads together
+constexpr int kSweepVecs = 2;  // 32-byte vectors that a thread of a sweep loads together
 constexpr double kLog2e = 1.4426950408889634;
 constexpr double kLn2 = 0.6931471805599453;
 // By how much of itself ex2.approx is too small on the mean (measured: 4.9e-8 to 5.1e-8 over each
@@ -180,31 +180,35 @@ __device__ __forceinline__ MaxSum cluster_merge(MaxSum a, int parts, const Base&
   return r;
 }
 
-// One block's share (`part` of `parts`) of a row's maximum and sum: the row's 16-byte
+// One block's share (`part` of `parts`) of a row's maximum and sum: the row's 32-byte
 // vectors, U at a time a thread, and its edges by a few threads of part 0.
 template <typename T>
 __device__ __forceinline__ MaxSum sweep(const T* x, int64_t V, const Base& b, int part, int parts) {
-  constexpr int N = Vec<T>::N, U = kSweepVecs;
+  constexpr int N = Wide<T>::N, U = kSweepVecs;
   MaxSum a;
-  const int head = head_of(x, V);
+  const int head = wide_head(x, V);
   const int64_t nv = (V - head) / N;
   const int tail = (int)(V - head - nv * N);
-  const uint4* q = reinterpret_cast<const uint4*>(x + head);
+  const T* q = x + head;
   const int64_t per = (nv + parts - 1) / parts;
   const int64_t lo = per * part, hi = lo + per < nv ? lo + per : nv;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += U * (int64_t)blockDim.x) {
-    uint4 v[U];
+  for (int64_t i0 = lo + threadIdx.x; i0 < hi; i0 += U * (int64_t)blockDim.x) {
+    uint4 v[2 * U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      v[u] = i + u * (int64_t)blockDim.x < hi ? q[i + u * (int64_t)blockDim.x]
-                                              : make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * (int64_t)blockDim.x;
+      v[2 * u] = v[2 * u + 1] = make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+      if (i < hi) {
+        const Wide<T> w = load_wide(q + i * N, true);
+        v[2 * u] = w.a;
+        v[2 * u + 1] = w.b;
+      }
+    }
     add<T>(&a, v, b);
   }
   if (part == 0) {
     const int t = (int)threadIdx.x;
-    if (t < head + tail) {
-      add_one(&a, Vec<T>::one(x[t < head ? (int64_t)t : V - tail + (t - head)]), b);
-    }
+    if (t < head + tail) add_one(&a, Vec<T>::one(x[t < head ? (int64_t)t : V - tail + (t - head)]), b);
   }
   return a;
 }
@@ -281,27 +285,26 @@ __device__ __forceinline__ uint4 grad_vec(const uint4& v, const RowGrad& g, cons
 }
 
 // A share (`part` of `parts`) of a row's gradient, or of zeros (skip: x is not read, it may
-// hold anything), by a block: 16-byte loads, kSweepVecs at a time a thread, and, where
-// the output row lies at the same offset from a 16-byte boundary, stores.
+// hold anything), by a block: 32-byte loads, kSweepVecs at a time a thread, and, where
+// the output row lies at the same offset from a 32-byte boundary, stores.
 template <typename T>
 __device__ __forceinline__ void write_gradient(const T* x, T* dx, int64_t V, const RowGrad& g, const Base& b, bool skip,
                                                int64_t part, int64_t parts) {
-  constexpr int N = Vec<T>::N, U = kSweepVecs;
-  const int head = head_of(x, V);
+  constexpr int N = Wide<T>::N, U = kSweepVecs;
+  const int head = wide_head(x, V);
   const int64_t nv = (V - head) / N;
   const int tail = (int)(V - head - nv * N);
-  const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15) == 0;
+  const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 31) == 0;
   const int64_t per = (nv + parts - 1) / parts;
   const int64_t lo = per * part, hi = lo + per < nv ? lo + per : nv;
-  const uint4* q = reinterpret_cast<const uint4*>(x + head);
   const int64_t vy = g.y >= head ? (g.y - head) / N : -1;  // the target's vector (none of [lo, hi) where it is at an edge)
   for (int64_t i0 = lo + threadIdx.x; i0 < hi; i0 += U * (int64_t)blockDim.x) {
-    uint4 v[U];
+    Wide<T> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t i = i0 + u * (int64_t)blockDim.x;
-      v[u] = make_uint4(0, 0, 0, 0);
-      if (!skip && i < hi) v[u] = q[i];
+      v[u].a = v[u].b = make_uint4(0, 0, 0, 0);
+      if (!skip && i < hi) v[u] = load_wide(x + head + i * N, true);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -310,14 +313,11 @@ __device__ __forceinline__ void write_gradient(const T* x, T* dx, int64_t V, con
       T* to = dx + head + i * N;
       // (x may be dx: the target's logit is taken before its place is written)
       const float fy = !skip && i == vy ? grad_at_target(Vec<T>::one(x[g.y]), g, b) : 0.f;
-      const uint4 w = skip ? v[u] : grad_vec<T>(v[u], g, b);
-      if (same) {
-        __stcs(reinterpret_cast<uint4*>(to), w);
-      } else {
-        const T* one = reinterpret_cast<const T*>(&w);
-#pragma unroll
-        for (int e = 0; e < N; ++e) to[e] = one[e];
+      if (!skip) {
+        v[u].a = grad_vec<T>(v[u].a, g, b);
+        v[u].b = grad_vec<T>(v[u].b, g, b);
       }
+      store_wide(to, v[u], same);
       if (!skip && i == vy) dx[g.y] = Vec<T>::round(fy);
     }
   }

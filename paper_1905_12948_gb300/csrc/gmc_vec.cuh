@@ -173,6 +173,50 @@ __device__ __forceinline__ int head_of(const T* p, int64_t V) {
   return V < h ? (int)V : h;
 }
 
+// 32 bytes of a row: the widest load and store there is. N elements.
+template <typename T>
+struct Wide {
+  static constexpr int N = 2 * Vec<T>::N;
+  uint4 a, b;
+};
+__device__ __forceinline__ bool on32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
+template <typename T>
+__device__ __forceinline__ Wide<T> load_wide(const T* p, bool aligned) {
+  Wide<T> v;
+  if (aligned) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v.a.x), "=r"(v.a.y), "=r"(v.a.z), "=r"(v.a.w), "=r"(v.b.x), "=r"(v.b.y), "=r"(v.b.z), "=r"(v.b.w)
+                 : "l"(p));
+    return v;
+  }
+  alignas(16) T e[Wide<T>::N];
+#pragma unroll
+  for (int i = 0; i < Wide<T>::N; ++i) e[i] = p[i];
+  v.a = *reinterpret_cast<const uint4*>(e);
+  v.b = *reinterpret_cast<const uint4*>(e + Vec<T>::N);
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_wide(T* p, const Wide<T>& v, bool aligned) {
+  if (aligned) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v.a.x), "r"(v.a.y), "r"(v.a.z),
+                 "r"(v.a.w), "r"(v.b.x), "r"(v.b.y), "r"(v.b.z), "r"(v.b.w)
+                 : "memory");
+    return;
+  }
+  alignas(16) T e[Wide<T>::N];
+  *reinterpret_cast<uint4*>(e) = v.a;
+  *reinterpret_cast<uint4*>(e + Vec<T>::N) = v.b;
+#pragma unroll
+  for (int i = 0; i < Wide<T>::N; ++i) p[i] = e[i];
+}
+// The elements of a row that lie before its first 32-byte boundary.
+template <typename T>
+__device__ __forceinline__ int wide_head(const T* p, int64_t n) {
+  const int h = (int)((32 - (reinterpret_cast<uintptr_t>(p) & 31)) & 31) / (int)sizeof(T);
+  return n < h ? (int)n : h;
+}
+
 template <typename F>
 inline cudaError_t by_type(int32_t dtype, F&& f) {
   if (dtype == GMC_F32) return f(float());
