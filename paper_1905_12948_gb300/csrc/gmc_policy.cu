@@ -71,7 +71,7 @@ struct alignas(128) RowsShared {
   uint64_t ready[kRowSlots];             // the result is there
   uint64_t free[kRowSlots];              // the row is done
   uint64_t from[kFinishers][2][kMaxParts];  // (m, S) of each block of the cluster
-  MaxSum ws[kRowSlots][kWorkWarps];
+  MaxSum ws[kRowSlots][kStatsWarps * 32];  // of each stats thread
   RowResult res[kRowSlots];
   double total[kFinishers];
   int dead;                              // a wait gave up
@@ -132,6 +132,34 @@ struct Cover {
   }
 };
 
+constexpr int kStatsThreads = kStatsWarps * 32;
+// U of a chunk's vectors into a: those at q, q + kStatsThreads, ... that lie before `left`.
+template <typename T, int U>
+__device__ __forceinline__ void add_some(MaxSum* a, const uint4* q, int left, const Base& b) {
+  uint4 v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    v[u] = u * kStatsThreads < left ? q[u * kStatsThreads]
+                                    : make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+  add<T>(a, v, b);
+}
+// A warp's merge of all stats threads' maxima and sums.
+__device__ __forceinline__ MaxSum block_of(const MaxSum* ws, int lane, const Base& b) {
+  MaxSum t[kStatsWarps], r;
+#pragma unroll
+  for (int i = 0; i < kStatsWarps; ++i) {
+    t[i] = ws[i * 32 + lane];
+    r.m = fmaxf(r.m, t[i].m);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
+  const Shift h = shift_of(r.m, b);
+#pragma unroll
+  for (int i = 0; i < kStatsWarps; ++i) r.s += t[i].s * exp2_fast(between(t[i].m, h, b));
+  r.s = warp_sum(r.s);
+  return r;
+}
+
 // A place in the ring, and how often it was used before.
 struct RingAt {
   int i = 0;
@@ -176,9 +204,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     cluster_wait();
   }
 
-  // whether a row counts, asked a row ahead of its use
-  auto weight_of = [&](int64_t row) { return P.weights ? P.weights[row] : P.weight; };
-  auto counts_at = [&](int64_t row) { return row < R.n && R.y[row] >= 0 && weight_of(row) != 0.f; };
+  // what tells whether a row counts: loaded a row ahead of its use, and looked at only then
+  struct Facts {
+    int64_t y;
+    float w;
+    __device__ bool count() const { return y >= 0 && w != 0.f; }
+  };
+  auto facts_at = [&](int64_t row) {
+    if (row >= R.n) row = R.n - 1;
+    return Facts{R.y[row], P.weights ? P.weights[row] : P.weight};
+  };
   // this block's vectors of a row
   auto share_of = [&](const Cover<T>& c) { return (int)max((int64_t)0, (lo + per < c.nv ? lo + per : c.nv) - lo); };
 
@@ -186,10 +221,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     const int tid = (int)threadIdx.x;
     RingAt at;
     uint32_t r = 0;  // rows taken before this one
-    bool counts = counts_at(cluster);
+    Facts next = facts_at(cluster);
     for (int64_t row = cluster; row < R.n; row += clusters, ++r) {
-      const bool now = counts;
-      counts = counts_at(row + clusters);
+      const bool now = next.count();
+      next = facts_at(row + clusters);
       const int slot = r % kRowSlots;
       const uint32_t turn = r / kRowSlots;
       // every row passes every barrier of its slot, also one that does not count: a
@@ -202,36 +237,35 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         if (!(ok = ok && warp_wait(&S.full[at.i], at.turn & 1, limit))) break;
         const uint4* chunk = ring + at.i * kChunkVecs;
         const int here = min(kChunkVecs, cnt - q);
+        const int here_warp = here - (int)threadIdx.x + lane;  // from this warp's first vector on
 #pragma unroll 1
-        for (int v0 = tid; v0 < here; v0 += kStatsWarps * 32 * kStatsBatch) {
-          uint4 v[kStatsBatch];
-#pragma unroll
-          for (int u = 0; u < kStatsBatch; ++u) {
-            const int i = v0 + u * kStatsWarps * 32;
-            v[u] = i < here ? chunk[i] : make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
-          }
-          add<T>(&a, v, R.b);
+        for (int v0 = 0; v0 < here_warp; v0 += kStatsThreads * kStatsBatch) {
+          // as many vectors at once as the warp has, or the next power of two
+          const int left = here_warp - v0;
+          const uint4* from = chunk + tid + v0;
+          if (left > 4 * kStatsThreads) add_some<T, 8>(&a, from, left - lane, R.b);
+          else if (left > 2 * kStatsThreads) add_some<T, 4>(&a, from, left - lane, R.b);
+          else if (left > kStatsThreads) add_some<T, 2>(&a, from, left - lane, R.b);
+          else add_some<T, 1>(&a, from, left - lane, R.b);
         }
       }
       if (!ok) {
         S.dead = 1;
         break;
       }
-      if (now) a = warp_merge(a, R.b);
-      if (lane == 0) {
-        S.ws[slot][warp] = a;
-        mbar_arrive(&S.summed[slot]);
-      }
+      S.ws[slot][tid] = a;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.summed[slot]);
     }
   } else if (warp < kWorkWarps) {
     constexpr int kGradThreads = kGradWarps * 32;
     const int tid = (int)threadIdx.x - kStatsWarps * 32;
     RingAt at;
     uint32_t r = 0;
-    bool counts = counts_at(cluster);
+    Facts next = facts_at(cluster);
     for (int64_t row = cluster; row < R.n; row += clusters, ++r) {
-      const bool now = counts;
-      counts = counts_at(row + clusters);
+      const bool now = next.count();
+      next = facts_at(row + clusters);
       const int slot = r % kRowSlots;
       // the result comes after the sums, and these after the row's chunks
       if (!warp_wait(&S.ready[slot], (r / kRowSlots) & 1, limit)) {
@@ -315,13 +349,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     double total = 0.;
     uint32_t r = (uint32_t)me;
     uint32_t trades = 0;  // rows whose sums this finisher exchanged
+    Facts next = facts_at(cluster + me * clusters);
     bool alive = true;
     for (int64_t row = cluster + me * clusters; row < R.n; row += kFinishers * clusters, r += kFinishers) {
       const int slot = r % kRowSlots;
       const uint32_t turn = r / kRowSlots;
-      const int64_t y = R.y[row];
-      const float w = weight_of(row);
-      const bool counts = y >= 0 && w != 0.f;
+      const Facts facts = next;
+      const int64_t y = facts.y;
+      const float w = facts.w;
+      const bool counts = facts.count();
+      next = facts_at(row + kFinishers * clusters);
       float xy = 0.f, adv = 0.f, old_logp = 0.f, ref_logp = 0.f;
       if (counts) {
         xy = target_logit(R.x + row * R.ld, R.V, y);
@@ -334,7 +371,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       float loss = 0.f;
       alive = (!turn || warp_wait(&S.free[slot], (turn - 1) & 1, limit)) && warp_wait(&S.summed[slot], turn & 1, limit);
       if (alive && counts) {
-        MaxSum a = warp_merge(lane < kStatsWarps ? S.ws[slot][lane] : MaxSum(), R.b);
+        MaxSum a = block_of(S.ws[slot], lane, R.b);
         if (parts > 1) {
           // two sets of slots in turn: a block sends its next but one row's sums only after
           // it has heard this one's next, which this one sends after it has read these
@@ -384,10 +421,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     if (lane == 0) S.total[me] = total;
   } else {
     RingAt at;
-    bool counts = counts_at(cluster), alive = true;
+    bool alive = true;
+    Facts next = facts_at(cluster);
     for (int64_t row = cluster; row < R.n && alive; row += clusters) {
-      const bool now = counts;
-      counts = counts_at(row + clusters);
+      const bool now = next.count();
+      next = facts_at(row + clusters);
       if (!now) continue;
       const T* x = R.x + row * R.ld;
       const Cover<T> c(x, R.V);
