@@ -7,14 +7,16 @@
 //   load    one warp copies the share into a ring of 32 KB chunks in shared memory by
 //           bulk copies (the vectors at the row's two ends element by element, with
 //           -inf beside the row)
-//   stats   eight warps read the chunks as they land, keeping a maximum and a sum a thread,
-//           and merge them at the row's end
-//   finish  two warps, a row each in turn, merge the block's sums, exchange them with the
+//   stats   eight warps read the chunks as they land, keeping a maximum and a sum a thread
+//   finish  two warps, a row each in turn, merge the threads' sums, exchange them with the
 //           cluster's other blocks by messages, and form the token's loss and slope
 //   grad    eight warps read the chunks again, write k ([v = y] - p_v) and free them
 // so that nothing in a row's long chain of small steps (3 to 4 us) holds up another row's
 // traffic: 192 KB of ring cover about 40 KB in flight from HBM, the chain, and a row's
-// share of up to 64 KB (128 KB for the longest rows).
+// share of up to 64 KB (128 KB for the longest rows). Bound by HBM at shares of 64 KB (8,192 x
+// 131,072 bf16: 610 us, 6.7 TB/s read and written), by what the SMs issue where a share is an
+// odd number of batches (12,160 x 50,257: 400 us, 6.1 TB/s), and by the first and last row's
+// chains where there are few rows (64 x 32,000: 9 us).
 // k_policy_short: short rows, one a warp. k_policy: rows over 1 MB, swept twice from global
 // memory.
 #include <new>
@@ -160,6 +162,19 @@ __device__ __forceinline__ MaxSum block_of(const MaxSum* ws, int lane, const Bas
   return r;
 }
 
+// What tells whether a row counts: loaded a row ahead of its use, and looked at only then,
+// so that nothing waits for it.
+struct Facts {
+  int64_t y;
+  float w;
+  __device__ __forceinline__ bool count() const { return y >= 0 && w != 0.f; }
+};
+template <typename T>
+__device__ __forceinline__ Facts facts_of(const Rows<T>& R, const PolicyArgs& P, int64_t row) {
+  if (row >= R.n) row = R.n - 1;
+  return Facts{R.y[row], P.weights ? P.weights[row] : P.weight};
+}
+
 // A place in the ring, and how often it was used before.
 struct RingAt {
   int i = 0;
@@ -204,16 +219,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     cluster_wait();
   }
 
-  // what tells whether a row counts: loaded a row ahead of its use, and looked at only then
-  struct Facts {
-    int64_t y;
-    float w;
-    __device__ bool count() const { return y >= 0 && w != 0.f; }
-  };
-  auto facts_at = [&](int64_t row) {
-    if (row >= R.n) row = R.n - 1;
-    return Facts{R.y[row], P.weights ? P.weights[row] : P.weight};
-  };
+  auto facts_at = [&](int64_t row) { return facts_of(R, P, row); };
   // this block's vectors of a row
   auto share_of = [&](const Cover<T>& c) { return (int)max((int64_t)0, (lo + per < c.nv ? lo + per : c.nv) - lo); };
 
@@ -308,12 +314,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 #pragma unroll
               for (int e = 0; e < N / 2; ++e) f[e] = slope(f[e]);
               w[u] = Vec<T>::put_pairs(f);
-              if (v >= vb && v < ve) __stcs(dst + v, w[u]);
+              if (v >= vb && v < ve) dst[v] = w[u];
             }
           }
         } else {
           for (int v = tid; v < ve; v += kGradThreads)
-            if (v >= vb) __stcs(dst + v, make_uint4(0, 0, 0, 0));
+            if (v >= vb) dst[v] = make_uint4(0, 0, 0, 0);
         }
         // the rest element by element: the row's ends, or all of a row that lies otherwise
         if (dx && (vb > 0 || ve < here)) {
@@ -489,7 +495,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 // the losses at the end. cap: vectors of a buffer.
 constexpr int kShortWarps = 24;  // of a block at most
 constexpr int kShortBatch = 4;   // vectors that a lane takes at once
-constexpr int64_t kShortVecs = 1100;         // vectors of a row at most (17 KB)
+constexpr int64_t kShortVecs = 960;          // vectors of a row at most (15 KB)
 constexpr int64_t kShortBytes = 220 * 1024;  // of all buffers of a block
 
 template <typename T>
@@ -513,8 +519,8 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
   double total = 0.;
   uint32_t loaded[2] = {0, 0};
   // begin the copy of a row that counts into buffer b
-  auto load = [&](int64_t row, int b) {
-    if (row >= R.n || R.y[row] < 0 || (P.weights && P.weights[row] == 0.f)) return;
+  auto load = [&](int64_t row, const Facts& f, int b) {
+    if (row >= R.n || !f.count()) return;
     ++loaded[b];
     if (row == P.hold_row) return;
     const T* x = R.x + row * R.ld;
@@ -537,13 +543,15 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
     __syncwarp();
     if (lane == 0) mbar_arrive(&full[warp][b]);
   };
-  load(first, 0);
-  load(first + step, 1);
+  Facts now = facts_of(R, P, first), next = facts_of(R, P, first + step);
+  load(first, now, 0);
+  load(first + step, next, 1);
   int b = 0;
   for (int64_t row = first; row < R.n; row += step, b ^= 1) {
-    const int64_t y = R.y[row];
-    const float w = P.weights ? P.weights[row] : P.weight;
-    const bool counts = y >= 0 && w != 0.f;
+    const Facts after = facts_of(R, P, row + 2 * step);
+    const int64_t y = now.y;
+    const float w = now.w;
+    const bool counts = now.count();
     const T* x = R.x + row * R.ld;
     T* out = dx + row * dld;
     const Cover<T> c(x, R.V);
@@ -590,7 +598,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
         for (int u = 0; u < kShortBatch; ++u) {
           const int k = k0 + 32 * u;
           if (!skip) q[u] = grad_vec<T>(q[u], g, R.b);
-          if (k >= vb && k < ve) __stcs(dst + k, q[u]);
+          if (k >= vb && k < ve) dst[k] = q[u];
         }
       }
       // the rest element by element: the row's ends, or all of a row that lies otherwise
@@ -612,7 +620,9 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
       if (lane == 0 && !skip && y < R.V) out[y] = Vec<T>::round(g.k * -expm1f(st.logp));
     }
     __syncwarp();  // every lane has read the buffer
-    load(row + 2 * step, b);
+    load(row + 2 * step, after, b);
+    now = next;
+    next = after;
   }
   for (int i = 0; i < 2; ++i)  // no copy is under way when the block ends
     if (loaded[i]) warp_wait(&full[warp][i], (loaded[i] - 1) & 1, P.wait_ns);
@@ -740,9 +750,9 @@ template <typename T>
 cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, Residency* device, cudaStream_t s) {
   const int64_t nv = most_vecs(R);
   const int sms = device->sms;
-  // Short rows, and more of them than the ring kernel's blocks see twice: a warp a row. 16,384 x
-  // 2,221 bf16 41 us (ring 153), 1,000 x 5,001 12 (18), 9,689 x 8,696 91 (96); 4,000 x 12,001 73
-  // (ring 54), 300 x 8,000 12 (10).
+  // Short rows, and more of them than the ring kernel's blocks see twice: a warp a row. bf16
+  // 16,384 x 2,221 43 us (by the ring 128), 4,000 x 6,001 28 (40), 1,000 x 2,500 10 (14); the ring is
+  // the faster from 16 KB a row: 4,000 x 4,096 fp32 32 us (36), 9,689 x 8,696 88 (91), 4,000 x 12,001 49 (72).
   if (nv <= kShortVecs && R.n > 2 * sms) {
     const int cap = (int)(nv + 7) / 8 * 8;
     int warps = (int)(kShortBytes / (cap * 32));
