@@ -75,6 +75,7 @@ __device__ __forceinline__ uint4 drop_vec(const uint4& x, const uint4& res, cons
 template <typename T, bool RES>
 __global__ void __launch_bounds__(kDropThreads) k_dropout(DropArgs<T> A, int64_t blocks_per_row) {
   constexpr int N = Wide<T>::N, H = Vec<T>::N, U = kDropVecs;
+  griddep_wait();
   const int64_t k = blockIdx.x / blocks_per_row;
   const int64_t b = blockIdx.x - k * blocks_per_row;
   const T* x = A.x + k * A.ldx;
@@ -129,9 +130,9 @@ int64_t blocks_of(int64_t n, int64_t per_vec) {
 template <typename T>
 cudaError_t run(const DropArgs<T>& A, int64_t K, cudaStream_t s) {
   const int64_t per = blocks_of(A.n, Wide<T>::N);
-  if (A.res) k_dropout<T, true><<<(unsigned)(per * K), kDropThreads, 0, s>>>(A, per);
-  else k_dropout<T, false><<<(unsigned)(per * K), kDropThreads, 0, s>>>(A, per);
-  return cudaGetLastError();
+  const dim3 grid((unsigned)(per * K)), block(kDropThreads);
+  return A.res ? launch_pdl(k_dropout<T, true>, grid, block, 0, s, A, per)
+               : launch_pdl(k_dropout<T, false>, grid, block, 0, s, A, per);
 }
 
 }  // namespace

@@ -364,20 +364,23 @@ __device__ __forceinline__ void policy_terms(const PolicyArgs& P, float adv, flo
   *slope = d;
 }
 
-// Launch a kernel of `blocks` blocks in clusters of `parts`.
+// Launch a kernel of `blocks` blocks in clusters of `parts`, with programmatic stream
+// serialization (it begins with griddep_wait).
 struct LaunchConfig {
   cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   LaunchConfig(int64_t blocks, int threads, int parts, size_t smem, cudaStream_t s) {
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = (unsigned)parts;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)parts;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = parts > 1 ? 1 : 0;
+    cfg.numAttrs = parts > 1 ? 2 : 1;
   }
 };
 template <typename... A, typename... B>

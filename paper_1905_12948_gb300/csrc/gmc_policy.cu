@@ -218,6 +218,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     cluster_arrive();
     cluster_wait();
   }
+  griddep_wait();
 
   auto facts_at = [&](int64_t row) { return facts_of(R, P, row); };
   // this block's vectors of a row
@@ -515,6 +516,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
     fence_mbar_init();
   }
   __syncthreads();
+  griddep_wait();
   const int64_t first = (int64_t)warp * gridDim.x + blockIdx.x, step = (int64_t)warps * gridDim.x;
   double total = 0.;
   uint32_t loaded[2] = {0, 0};
@@ -644,6 +646,7 @@ __global__ void __launch_bounds__(kLossThreads) k_policy(Rows<T> R, PolicyArgs P
   const int64_t cluster = blockIdx.x / parts, clusters = gridDim.x / parts;
   const int part = (int)(blockIdx.x - cluster * parts);
   double total = 0.;
+  griddep_wait();
   if (parts > 1) {  // no message before every block has begun
     cluster_arrive();
     cluster_wait();
