@@ -146,6 +146,14 @@ Tensor gradient(PyObject* o, const Tensor& logits, const Rows& r, int64_t* ld) {
   return t;
 }
 
+// `sizes` elements of a 1-D tensor from `at` on, as a tensor of its own.
+Tensor part(const Tensor& whole, at::IntArrayRef sizes, int64_t at) {
+  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+  t.unsafeGetTensorImpl()->set_storage_offset(at);
+  t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
+  return t;
+}
+
 void* stream_of(const Tensor& t) { return c10::cuda::getCurrentCUDAStream(t.device().index()).stream(); }
 
 void arguments(Py_ssize_t got, Py_ssize_t want) {
@@ -242,7 +250,8 @@ PyObject* policy(Args a, Py_ssize_t na) {
   Tensor out;
   if (grad) out = gradient(a[13], x, r, &dld);
   const auto f32 = x.options().dtype(at::kFloat);
-  Tensor loss = at::empty({}, f32), each = at::empty({r.n}, f32), logp = at::empty({r.n}, f32);
+  const Tensor all = at::empty({2 * r.n + 1}, f32);  // one allocation: each one costs a microsecond
+  const Tensor each = part(all, {r.n}, 0), logp = part(all, {r.n}, r.n), loss = part(all, {}, 2 * r.n);
   check(g_abi.policy_loss(h, x.data_ptr(), k, r.n, r.v, r.ld, scale, y, old_logp, ref, adv, w, lo, hi, kl,
                           loss.data_ptr<float>(), each.data_ptr<float>(), logp.data_ptr<float>(),
                           grad ? out.data_ptr() : nullptr, dld, stream_of(x)),
@@ -273,8 +282,9 @@ PyObject* preference(Args a, Py_ssize_t na) {
   Tensor out;
   if (grad) out = gradient(a[11], x, r, &dld);
   const auto f32 = x.options().dtype(at::kFloat);
-  Tensor loss = at::empty({}, f32), each = at::empty({pairs}, f32), ratio = at::empty({2 * pairs}, f32),
-         logp = at::empty({r.n}, f32);
+  const Tensor all = at::empty({r.n + 3 * pairs + 1}, f32);  // one allocation, as above
+  const Tensor logp = part(all, {r.n}, 0), ratio = part(all, {2 * pairs}, r.n),
+               each = part(all, {pairs}, r.n + 2 * pairs), loss = part(all, {}, r.n + 3 * pairs);
   check(g_abi.preference_loss(h, x.data_ptr(), k, r.n, r.v, r.ld, scale, y, offsets, pairs, ref, w, beta, smoothing,
                               loss.data_ptr<float>(), each.data_ptr<float>(), ratio.data_ptr<float>(),
                               logp.data_ptr<float>(), grad ? out.data_ptr() : nullptr, dld, stream_of(x)),
