@@ -121,9 +121,7 @@ __device__ __forceinline__ bool last_of(uint32_t* count, uint32_t mine, int64_t 
   __shared__ int last;
   __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
-    last = (int64_t)atomicAdd(count, mine) + mine == all;
-    __threadfence();
+    last = (int64_t)count_add(count, mine) + mine == all;
   }
   __syncthreads();
   return last != 0;
@@ -156,7 +154,6 @@ __global__ void __launch_bounds__(kLossThreads, 6) k_pair_stats(Rows<T> R, PairA
         finish_pair(P, p, weight_of(P, p), 0., 0.);
         ++empty;
       }
-    __threadfence();
     const Halves h = block_sums((double)empty);
     done = (uint32_t)(h.a + h.b);
   } else {

@@ -48,9 +48,7 @@ __device__ __forceinline__ void reduce_loss(const PolicyArgs& P, double mine, ui
   uint32_t last = 0;
   if (lane == 0) {
     P.partial[cluster] = mine;
-    __threadfence();
-    last = atomicInc(P.ticket, clusters - 1) == clusters - 1;  // back to 0 with the last
-    __threadfence();
+    last = count_inc(P.ticket, clusters - 1) == clusters - 1;
   }
   if (!__shfl_sync(0xffffffffu, last, 0)) return;
   double s = 0.;
@@ -425,7 +423,17 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         }
       }
     }
+    // The loss, before the last gradients are out. A wait that gave up anywhere in the block
+    // ends, or has ended, a finisher's too.
     if (lane == 0) S.total[me] = total;
+    __syncwarp();
+    asm volatile("bar.sync 1, %0;" ::"n"(kFinishers * 32) : "memory");
+    if (me == 0 && rank == 0) {
+      total = 0.;
+      for (int i = 0; i < kFinishers; ++i) total += S.total[i];
+      if (*(volatile int*)&S.dead) total = (double)__uint_as_float(kNan);
+      reduce_loss(P, total, (uint32_t)cluster, (uint32_t)clusters);
+    }
   } else {
     RingAt at;
     bool alive = true;
@@ -475,16 +483,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       if (uses) wait_bounded(&S.full[i], (uses - 1) & 1, limit);
     }
   }
-  __syncthreads();
   if (parts > 1) {  // no block ends while another may still send to it
+    __syncthreads();
     cluster_arrive();
     cluster_wait();
-  }
-  if (warp == 0 && rank == 0) {
-    double total = 0.;
-    for (int i = 0; i < kFinishers; ++i) total += S.total[i];
-    if (S.dead) total = (double)__uint_as_float(kNan);
-    reduce_loss(P, total, (uint32_t)cluster, (uint32_t)clusters);
   }
 }
 
