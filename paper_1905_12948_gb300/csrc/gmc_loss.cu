@@ -13,16 +13,75 @@ using namespace gmc;
 
 namespace {
 
-// logp and (m, log S) of a row, by a cluster of blocks (thread 0 of part 0 writes), and
-// in ratio (NULL: not wanted) logp before its rounding, less ref's; 0 for a row that adds
-// nothing. S is written as +inf for an empty row, which no sum reaches.
-template <typename T>
+// The threads that work on a row: a block (G = kLossThreads), of which up to 8 share a row as
+// a cluster, or a warp (G = 32).
+struct Halves {
+  double a, b;
+};
+template <int G>
+struct Group {
+  static_assert(G == 32 || G == kLossThreads, "a warp or a block");
+  static constexpr int kRows = kLossThreads / G;  // rows of a block
+  __device__ static int tid() { return G == 32 ? (int)threadIdx.x % 32 : (int)threadIdx.x; }
+  __device__ static int of_block() { return G == 32 ? (int)threadIdx.x / 32 : 0; }  // of the block's rows
+  // Over the group; every thread returns the result.
+  __device__ static MaxSum merge(const MaxSum& a, const Base& b) {
+    if constexpr (G == 32) {
+      return warp_merge(a, b);
+    } else {
+      __shared__ MaxSum ws[32];
+      return block_merge(a, b, ws);
+    }
+  }
+  // Sums over the first and the second half of the group, in a fixed order.
+  __device__ static Halves sums(double s) {
+    Halves h{0., 0.};
+    if constexpr (G == 32) {
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      h.a = __shfl_sync(0xffffffffu, s, 0);
+      h.b = __shfl_sync(0xffffffffu, s, 16);
+    } else {
+      __shared__ double ws[kLossThreads / 32];
+      s = warp_sum(s);
+      __syncthreads();
+      if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = s;
+      __syncthreads();
+      for (int i = 0; i < kLossThreads / 64; ++i) h.a += ws[i], h.b += ws[kLossThreads / 64 + i];
+    }
+    return h;
+  }
+  // Thread 0 adds to a count that other groups add to; every thread returns whether it has
+  // reached `all`. What the groups wrote before is then visible to this one.
+  __device__ static bool last_of(uint32_t* count, uint32_t mine, int64_t all) {
+    if constexpr (G == 32) {
+      __syncwarp();
+      int last = 0;
+      if (tid() == 0) last = (int64_t)count_add(count, mine) + mine == all;
+      last = __shfl_sync(0xffffffffu, last, 0);
+      __syncwarp();  // what thread 0 acquired holds for all
+      return last != 0;
+    } else {
+      __shared__ int last;
+      __syncthreads();
+      if (threadIdx.x == 0) last = (int64_t)count_add(count, mine) + mine == all;
+      __syncthreads();
+      return last != 0;
+    }
+  }
+};
+
+// logp and (m, log S) of a row, by a group or a cluster of blocks (thread 0 of part 0
+// writes), and in ratio (NULL: not wanted) logp before its rounding, less ref's; 0 for a row
+// that adds nothing. S is written as +inf for an empty row, which no sum reaches.
+template <int G, typename T>
 __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int part, int parts, float* logp, float2* stats,
                                           const float* ref, double* ratio) {
-  __shared__ MaxSum ws[32], cs[kMaxParts];
+  __shared__ MaxSum cs[kMaxParts];
+  const bool writes = part == 0 && Group<G>::tid() == 0;
   const int64_t y = R.y[row];
   if (y < 0) {  // not scored
-    if (part == 0 && threadIdx.x == 0) {
+    if (writes) {
       logp[row] = 0.f;
       if (stats) stats[row] = make_float2(0.f, 0.f);
       if (ratio) ratio[row] = 0.;
@@ -33,10 +92,12 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
   const T* x = R.x + row * R.ld;
   const float xy = target_logit(x, R.V, y);
   const double less = ref ? (double)ref[row] : 0.;
-  MaxSum a = block_merge(sweep(x, R.V, R.b, part, parts), R.b, ws);
-  if (parts > 1) cluster_wait();  // every block has begun
-  a = cluster_merge(a, parts, R.b, cs);
-  if (part == 0 && threadIdx.x == 0) {
+  MaxSum a = Group<G>::merge(sweep(x, R.V, R.b, part, parts, Group<G>::tid(), G), R.b);
+  if (G != 32 && parts > 1) {
+    cluster_wait();  // every block has begun
+    a = cluster_merge(a, parts, R.b, cs);
+  }
+  if (writes) {
     const RowStats r = finish(a, xy, R.b);
     logp[row] = r.logp;
     if (stats) stats[row] = make_float2(r.h.h, r.empty ? INFINITY : r.ls);
@@ -44,13 +105,16 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
   }
 }
 
-// Bound by memory: a block of 256 threads loads 16 KB at once, and four or more of them
-// share an SM. 8,192 rows of 32,000 bf16 logits: 84 us, 6.2 TB/s.
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_stats(Rows<T> R, float* logp, float2* stats, int parts) {
+// Bound by memory: a block of 256 threads loads 16 KB at once, and six of them share an SM.
+// 8,192 rows of 32,000 bf16 logits: 84 us, 6.2 TB/s; by warps, 8,000 rows of 4,096: 11.3 us,
+// 5.8 TB/s, and 40,000 of 2,048: 39.6 us with 48 registers (five blocks an SM), 46 with 54.
+template <typename T, int G>
+__global__ void __launch_bounds__(kLossThreads, G == 32 ? 5 : 6) k_stats(Rows<T> R, float* logp, float2* stats,
+                                                                         int parts) {
   griddep_wait();
-  const int64_t row = blockIdx.x / parts;
-  row_stats(R, row, (int)(blockIdx.x - row * parts), parts, logp, stats, (const float*)nullptr, (double*)nullptr);
+  const int64_t at = blockIdx.x / parts, row = at * Group<G>::kRows + Group<G>::of_block();
+  if (row < R.n)
+    row_stats<G>(R, row, (int)(blockIdx.x - at * parts), parts, logp, stats, (const float*)nullptr, (double*)nullptr);
 }
 
 struct PairArgs {
@@ -76,20 +140,6 @@ __device__ __forceinline__ int64_t sequence_of(const PairArgs& P, int64_t row) {
 }
 
 __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.f) + log1pf(expf(-fabsf(x))); }
-// Sums over the first and the second half of the block, in a fixed order, for every thread.
-struct Halves {
-  double a, b;
-};
-__device__ __forceinline__ Halves block_sums(double s) {
-  __shared__ double ws[kLossThreads / 32];
-  s = warp_sum(s);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = s;
-  __syncthreads();
-  Halves h{0., 0.};
-  for (int i = 0; i < kLossThreads / 64; ++i) h.a += ws[i], h.b += ws[kLossThreads / 64 + i];
-  return h;
-}
 // A pair's loss and slope from its sequences' log ratios.
 __device__ __forceinline__ void finish_pair(const PairArgs& P, int64_t p, float w, double chosen, double other) {
   const float margin = (float)((double)P.beta * (chosen - other));
@@ -102,61 +152,53 @@ __device__ __forceinline__ void finish_pair(const PairArgs& P, int64_t p, float 
   if (P.seq_ratio) P.seq_ratio[2 * p] = (float)chosen, P.seq_ratio[2 * p + 1] = (float)other;
 }
 __device__ __forceinline__ float weight_of(const PairArgs& P, int64_t p) { return P.weights ? P.weights[p] : P.weight; }
-// By one block, half of it a sequence: the log ratios of a pair whose rows are all done.
+// By one group, half of it a sequence: the log ratios of a pair whose rows are all done.
+template <int G>
 __device__ __forceinline__ void pair_of_rows(const PairArgs& P, int64_t p) {
-  constexpr int half = kLossThreads / 2;
-  const int side = (int)threadIdx.x / half;
+  constexpr int half = G / 2;
+  const int tid = Group<G>::tid(), side = tid / half;
   const float w = weight_of(P, p);
   int64_t lo = P.offsets[2 * p + side], hi = P.offsets[2 * p + side + 1];
   lo = lo < 0 ? 0 : lo;
   hi = hi > P.n ? P.n : hi;
   double s = 0.;
-  for (int64_t i = lo + threadIdx.x % half; i < hi; i += half) s += __ldcg(P.ratio + i);
-  const Halves h = block_sums(s);
-  if (threadIdx.x == 0) finish_pair(P, p, w, h.a, h.b);
+  for (int64_t i = lo + tid % half; i < hi; i += half) s += __ldcg(P.ratio + i);
+  const Halves h = Group<G>::sums(s);
+  if (tid == 0) finish_pair(P, p, w, h.a, h.b);
 }
-// Thread 0 adds to a count that other blocks add to; every thread returns whether it
-// has reached `all`. What the blocks wrote before is then visible to this one.
-__device__ __forceinline__ bool last_of(uint32_t* count, uint32_t mine, int64_t all) {
-  __shared__ int last;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    last = (int64_t)count_add(count, mine) + mine == all;
-  }
-  __syncthreads();
-  return last != 0;
-}
-// The pairs' weighted losses added up, by one block.
+// The pairs' weighted losses added up, by one group.
+template <int G>
 __device__ __forceinline__ void sum_pairs(const PairArgs& P) {
   double s = 0.;
-  for (int64_t p = threadIdx.x; p < P.pairs; p += blockDim.x) s += __ldcg(P.wloss + p);
-  const Halves h = block_sums(s);
-  if (threadIdx.x == 0) *P.loss = (float)(h.a + h.b);
+  for (int64_t p = Group<G>::tid(); p < P.pairs; p += G) s += __ldcg(P.wloss + p);
+  const Halves h = Group<G>::sums(s);
+  if (Group<G>::tid() == 0) *P.loss = (float)(h.a + h.b);
 }
 
-// k_stats, and the pairs' losses and slopes: the block that does a pair's last row does the
-// pair. The cluster past the last row does the pairs that have no rows. total: the block
-// that does the last pair adds up the loss (k_grad does so where it follows).
+// k_stats, and the pairs' losses and slopes: the group that does a pair's last row does the
+// pair. The block (or cluster) past the last row does the pairs that have no rows. total:
+// the group that does the last pair adds up the loss (k_grad does so where it follows).
 // Six blocks an SM (40 registers): the pairs' part would take 58, and the sums' loads four
 // blocks at once (16 pairs of 50,257: 391 us instead of 363).
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads, 6) k_pair_stats(Rows<T> R, PairArgs P, float* logp, float2* stats, int parts,
-                                                                bool total) {
+template <typename T, int G>
+__global__ void __launch_bounds__(kLossThreads, 6) k_pair_stats(Rows<T> R, PairArgs P, float* logp, float2* stats,
+                                                                int parts, bool total) {
   griddep_wait();
-  const int64_t row = blockIdx.x / parts;
-  const int part = (int)(blockIdx.x - row * parts);
+  const int64_t at = blockIdx.x / parts, row = at * Group<G>::kRows + Group<G>::of_block();
+  const int part = (int)(blockIdx.x - at * parts);
   uint32_t done = 1;
-  if (row == R.n) {
-    if (part != 0) return;
+  if ((at + 1) * parts == gridDim.x) {
+    if (part != 0 || Group<G>::of_block() != 0) return;
     uint32_t empty = 0;
-    for (int64_t p = threadIdx.x; p < P.pairs; p += blockDim.x)
+    for (int64_t p = Group<G>::tid(); p < P.pairs; p += G)
       if (P.offsets[2 * p] >= P.offsets[2 * p + 2]) {
         finish_pair(P, p, weight_of(P, p), 0., 0.);
         ++empty;
       }
-    const Halves h = block_sums((double)empty);
+    const Halves h = Group<G>::sums((double)empty);
     done = (uint32_t)(h.a + h.b);
   } else {
+    if (row >= R.n) return;
     int64_t p = -1, rows = 0;
     if (part == 0) {
       p = sequence_of(P, row);
@@ -165,43 +207,45 @@ __global__ void __launch_bounds__(kLossThreads, 6) k_pair_stats(Rows<T> R, PairA
         rows = P.offsets[2 * p + 2] - P.offsets[2 * p];
       }
     }
-    row_stats(R, row, part, parts, logp, stats, P.ref_logp, P.ratio);
-    if (p < 0 || !last_of(P.count + p, 1, rows)) return;
-    pair_of_rows(P, p);
-    if (threadIdx.x == 0) P.count[p] = 0;
+    row_stats<G>(R, row, part, parts, logp, stats, P.ref_logp, P.ratio);
+    if (p < 0 || !Group<G>::last_of(P.count + p, 1, rows)) return;
+    pair_of_rows<G>(P, p);
+    if (Group<G>::tid() == 0) P.count[p] = 0;
   }
-  if (!total || !last_of(P.count + P.pairs, done, P.pairs)) return;
-  sum_pairs(P);
-  if (threadIdx.x == 0) P.count[P.pairs] = 0;
+  if (!total || !Group<G>::last_of(P.count + P.pairs, done, P.pairs)) return;
+  sum_pairs<G>(P);
+  if (Group<G>::tid() == 0) P.count[P.pairs] = 0;
 }
 
 // dx = g s ([v = y] - p) of each row from its saved (m, log S). Without g, a row's is the
 // slope of its pair (negated in the sequence not preferred).
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_grad(Rows<T> R, const float2* stats, const float* g,
-                                                       PairArgs P, T* dx, int64_t dld, int parts) {
+template <typename T, int G>
+__global__ void __launch_bounds__(kLossThreads, G == 32 ? 4 : 6) k_grad(Rows<T> R, const float2* stats, const float* g,
+                                                                        PairArgs P, T* dx, int64_t dld, int parts) {
   griddep_wait();
   // from the last row to the first: the logits read last are still in the L2 cache
-  const int64_t row = gridDim.x / parts - 1 - blockIdx.x / parts;
+  const int64_t row = R.n - 1 - (blockIdx.x / parts * Group<G>::kRows + Group<G>::of_block());
   const int part = (int)(blockIdx.x % parts);
-  const int64_t y = R.y[row];
-  float coef = 0.f;
-  if (y >= 0) {
-    if (!g) {
-      const int64_t q = sequence_of(P, row);
-      if (q >= 0) coef = q & 1 ? -P.slope[q >> 1] : P.slope[q >> 1];
-    } else {
-      coef = g[row];
+  if (row >= 0) {
+    const int64_t y = R.y[row];
+    float coef = 0.f;
+    if (y >= 0) {
+      if (!g) {
+        const int64_t q = sequence_of(P, row);
+        if (q >= 0) coef = q & 1 ? -P.slope[q >> 1] : P.slope[q >> 1];
+      } else {
+        coef = g[row];
+      }
+      if (y >= R.V) coef = __uint_as_float(kNan);
     }
-    if (y >= R.V) coef = __uint_as_float(kNan);
+    const float2 st = coef != 0.f ? stats[row] : make_float2(0.f, 0.f);
+    write_gradient(R.x + row * R.ld, dx + row * dld, R.V, grad_of(shift_of(st.x, R.b), st.y, coef, y, R.b), R.b,
+                   coef == 0.f || st.y == INFINITY, part, parts, Group<G>::tid(), G);
   }
-  const float2 st = coef != 0.f ? stats[row] : make_float2(0.f, 0.f);
-  write_gradient(R.x + row * R.ld, dx + row * dld, R.V, grad_of(shift_of(st.x, R.b), st.y, coef, y, R.b), R.b,
-                 coef == 0.f || st.y == INFINITY, part, parts);
-  if (g || blockIdx.x != 0) return;
-  sum_pairs(P);
+  if (g || blockIdx.x != 0 || Group<G>::of_block() != 0) return;
+  sum_pairs<G>(P);
   // whatever the offsets were, the next call finds the counts at 0
-  for (int64_t i = threadIdx.x; i <= P.pairs; i += blockDim.x) P.count[i] = 0;
+  for (int64_t i = Group<G>::tid(); i <= P.pairs; i += G) P.count[i] = 0;
 }
 
 }  // namespace
@@ -255,6 +299,32 @@ Rows<T> rows_of(const void* x, int64_t n, int64_t V, int64_t ld, float scale, co
   return Rows<T>{static_cast<const T*>(x), n, V, ld, base_of(scale), y};
 }
 
+// Whether a warp does a row, or a block (or cluster) does. A block's barriers and merge cost
+// as much as 10 KB of a row or more, a lone warp reads its row at 5 GB/s or so: warps where
+// rows are short and there are enough of them for the last ones not to matter. The sums of
+// bf16 rows, and the gradients, in us, by blocks and by warps:
+//   rows   length     sums       gradients        rows   length     sums       gradients
+//    620    2,048   3.7  3.3     3.7  3.4        2,000   8,192   9.1  7.4    12.1 11.1
+//    620    8,192   4.3  6.0     5.3  6.9        2,000  16,384  12.7 11.7    21.0 29.4
+//    900    4,096   4.8  4.3     5.5  4.7        8,000   4,096  29.1 11.5    38.9 22.4
+//    900   12,000   6.6  7.7     7.0  9.2        8,192  16,384  53.4 49.1    75.2 86.2
+bool by_warps(int64_t n, int64_t row_bytes) { return n >= 600 && row_bytes <= 24576 && row_bytes <= 12 * n; }
+// Blocks of groups of G that do n rows.
+template <int G>
+int64_t blocks_for(int64_t n) {
+  return (n + Group<G>::kRows - 1) / Group<G>::kRows;
+}
+
+template <typename T>
+cudaError_t launch_grad(const Rows<T>& R, const float2* stats, const float* g, const PairArgs& P, T* dx, int64_t dld,
+                        cudaStream_t s) {
+  const int64_t bytes = R.V * (int64_t)sizeof(T);
+  if (by_warps(R.n, bytes))
+    return launch(k_grad<T, 32>, blocks_for<32>(R.n), kLossThreads, 1, s, R, stats, g, P, dx, dld, 1);
+  const int parts = parts_for(R.n, bytes);
+  return launch(k_grad<T, kLossThreads>, R.n * parts, kLossThreads, 1, s, R, stats, g, P, dx, dld, parts);
+}
+
 int done(cudaError_t err) { return err == cudaSuccess ? GMC_OK : GMC_ECUDA; }
 
 }  // namespace
@@ -269,10 +339,14 @@ int gmc_token_logp(const void* logits_dev, int32_t dtype, int64_t n, int64_t voc
   if (!logp_dev) return GMC_EINVAL;
   return done(by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    return with_parts(parts_for(n, vocab * (int64_t)sizeof(T)), [&](int parts) {
-      return launch(k_stats<T>, n * parts, kLossThreads, parts, static_cast<cudaStream_t>(stream),
-                    rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev), logp_dev,
-                    reinterpret_cast<float2*>(stats_dev), parts);
+    const Rows<T> R = rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev);
+    const int64_t bytes = vocab * (int64_t)sizeof(T);
+    const cudaStream_t on = static_cast<cudaStream_t>(stream);
+    float2* stats = reinterpret_cast<float2*>(stats_dev);
+    if (by_warps(n, bytes))
+      return launch(k_stats<T, 32>, blocks_for<32>(n), kLossThreads, 1, on, R, logp_dev, stats, 1);
+    return with_parts(parts_for(n, bytes), [&](int parts) {
+      return launch(k_stats<T, kLossThreads>, n * parts, kLossThreads, parts, on, R, logp_dev, stats, parts);
     });
   }));
 }
@@ -287,11 +361,9 @@ int gmc_token_logp_backward(const void* logits_dev, int32_t dtype, int64_t n, in
   if (!stats_dev || !dlogp_dev || !dlogits_dev) return GMC_EINVAL;
   return done(by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    const int parts = parts_for(n, vocab * (int64_t)sizeof(T));
-    return launch(k_grad<T>, n * parts, kLossThreads, 1, static_cast<cudaStream_t>(stream),
-                  rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev),
-                  reinterpret_cast<const float2*>(stats_dev), dlogp_dev, PairArgs{},
-                  static_cast<T*>(dlogits_dev), dld, parts);
+    return launch_grad(rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev),
+                       reinterpret_cast<const float2*>(stats_dev), dlogp_dev, PairArgs{}, static_cast<T*>(dlogits_dev), dld,
+                       static_cast<cudaStream_t>(stream));
   }));
 }
 
@@ -398,13 +470,17 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
   cudaError_t err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
     const Rows<T> R = rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev);
-    const int most = parts_for(n, vocab * (int64_t)sizeof(T));
-    const cudaError_t e = with_parts(most, [&](int parts) {
-      return launch(k_pair_stats<T>, (n + 1) * parts, kLossThreads, parts, s, R, P, logp, h->stats, parts, !grad);
-    });
+    const int64_t bytes = vocab * (int64_t)sizeof(T);
+    cudaError_t e;
+    if (by_warps(n, bytes))
+      e = launch(k_pair_stats<T, 32>, blocks_for<32>(n) + 1, kLossThreads, 1, s, R, P, logp, h->stats, 1, !grad);
+    else
+      e = with_parts(parts_for(n, bytes), [&](int parts) {
+        return launch(k_pair_stats<T, kLossThreads>, (n + 1) * parts, kLossThreads, parts, s, R, P, logp, h->stats, parts,
+                      !grad);
+      });
     if (e != cudaSuccess || !grad) return e;
-    return launch(k_grad<T>, n * most, kLossThreads, 1, s, R, (const float2*)h->stats, (const float*)nullptr, P,
-                  static_cast<T*>(dlogits_dev), dld, most);
+    return launch_grad(R, (const float2*)h->stats, (const float*)nullptr, P, static_cast<T*>(dlogits_dev), dld, s);
   });
   if (err == cudaSuccess && !grad) err = cudaMemsetAsync(h->count, 0, sizeof(uint32_t) * (size_t)(pairs + 1), s);
   return done(err);

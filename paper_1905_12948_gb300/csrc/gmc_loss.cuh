@@ -193,10 +193,11 @@ __device__ __forceinline__ MaxSum cluster_merge(MaxSum a, int parts, const Base&
   return r;
 }
 
-// One block's share (`part` of `parts`) of a row's maximum and sum: the row's 32-byte
-// vectors, U at a time a thread, and its edges by a few threads of part 0.
+// One group's share (`part` of `parts`) of a row's maximum and sum, thread `tid` of
+// `threads`: the row's 32-byte vectors, U at a time a thread, and its edges by a few threads of
+// part 0.
 template <typename T>
-__device__ __forceinline__ MaxSum sweep(const T* x, int64_t V, const Base& b, int part, int parts) {
+__device__ __forceinline__ MaxSum sweep(const T* x, int64_t V, const Base& b, int part, int parts, int tid, int threads) {
   constexpr int N = Wide<T>::N, U = kSweepVecs;
   MaxSum a;
   const int head = wide_head(x, V);
@@ -205,11 +206,11 @@ __device__ __forceinline__ MaxSum sweep(const T* x, int64_t V, const Base& b, in
   const T* q = x + head;
   const int64_t per = (nv + parts - 1) / parts;
   const int64_t lo = per * part, hi = lo + per < nv ? lo + per : nv;
-  for (int64_t i0 = lo + threadIdx.x; i0 < hi; i0 += U * (int64_t)blockDim.x) {
+  for (int64_t i0 = lo + tid; i0 < hi; i0 += U * threads) {
     uint4 v[2 * U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t i = i0 + u * (int64_t)blockDim.x;
+      const int64_t i = i0 + u * threads;
       v[2 * u] = v[2 * u + 1] = make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
       if (i < hi) {
         const Wide<T> w = load_wide(q + i * N, true);
@@ -219,10 +220,8 @@ __device__ __forceinline__ MaxSum sweep(const T* x, int64_t V, const Base& b, in
     }
     add<T>(&a, v, b);
   }
-  if (part == 0) {
-    const int t = (int)threadIdx.x;
-    if (t < head + tail) add_one(&a, Vec<T>::one(x[t < head ? (int64_t)t : V - tail + (t - head)]), b);
-  }
+  if (part == 0 && tid < head + tail)
+    add_one(&a, Vec<T>::one(x[tid < head ? (int64_t)tid : V - tail + (tid - head)]), b);
   return a;
 }
 
@@ -298,11 +297,11 @@ __device__ __forceinline__ uint4 grad_vec(const uint4& v, const RowGrad& g, cons
 }
 
 // A share (`part` of `parts`) of a row's gradient, or of zeros (skip: x is not read, it may
-// hold anything), by a block: 32-byte loads, kSweepVecs at a time a thread, and, where
+// hold anything), by thread `tid` of `threads`: 32-byte loads, kSweepVecs at a time, and, where
 // the output row lies at the same offset from a 32-byte boundary, stores.
 template <typename T>
 __device__ __forceinline__ void write_gradient(const T* x, T* dx, int64_t V, const RowGrad& g, const Base& b, bool skip,
-                                               int64_t part, int64_t parts) {
+                                               int64_t part, int64_t parts, int tid, int threads) {
   constexpr int N = Wide<T>::N, U = kSweepVecs;
   const int head = wide_head(x, V);
   const int64_t nv = (V - head) / N;
@@ -311,17 +310,17 @@ __device__ __forceinline__ void write_gradient(const T* x, T* dx, int64_t V, con
   const int64_t per = (nv + parts - 1) / parts;
   const int64_t lo = per * part, hi = lo + per < nv ? lo + per : nv;
   const int64_t vy = g.y >= head ? (g.y - head) / N : -1;  // the target's vector (none of [lo, hi) where it is at an edge)
-  for (int64_t i0 = lo + threadIdx.x; i0 < hi; i0 += U * (int64_t)blockDim.x) {
+  for (int64_t i0 = lo + tid; i0 < hi; i0 += U * threads) {
     Wide<T> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t i = i0 + u * (int64_t)blockDim.x;
+      const int64_t i = i0 + u * threads;
       v[u].a = v[u].b = make_uint4(0, 0, 0, 0);
       if (!skip && i < hi) v[u] = load_wide(x + head + i * N, true);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t i = i0 + u * (int64_t)blockDim.x;
+      const int64_t i = i0 + u * threads;
       if (i >= hi) continue;
       T* to = dx + head + i * N;
       // (x may be dx: the target's logit is taken before its place is written)
@@ -334,9 +333,8 @@ __device__ __forceinline__ void write_gradient(const T* x, T* dx, int64_t V, con
       if (!skip && i == vy) dx[g.y] = Vec<T>::round(fy);
     }
   }
-  if (part == 0 && (int)threadIdx.x < head + tail) {
-    const int t = (int)threadIdx.x;
-    const int64_t j = t < head ? (int64_t)t : V - tail + (t - head);
+  if (part == 0 && tid < head + tail) {
+    const int64_t j = tid < head ? (int64_t)tid : V - tail + (tid - head);
     float f = 0.f;
     if (!skip) {
       const float v = Vec<T>::one(x[j]);

@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(kLossThreads) k_policy(Rows<T> R, PolicyArgs P
     const bool counts = y >= 0 && w != 0.f;
     if (counts) {
       const float xy = target_logit(x, R.V, y);
-      MaxSum a = block_merge(sweep(x, R.V, R.b, part, parts), R.b, ws);
+      MaxSum a = block_merge(sweep(x, R.V, R.b, part, parts, (int)threadIdx.x, kLossThreads), R.b, ws);
       a = cluster_merge(a, parts, R.b, cs);
       r = finish(a, xy, R.b);
       if (!r.empty)
@@ -683,7 +683,7 @@ __global__ void __launch_bounds__(kLossThreads) k_policy(Rows<T> R, PolicyArgs P
     }
     if (dx)
       write_gradient(x, dx + row * dld, R.V, grad_of(r.h, r.ls, w * slope, y, R.b), R.b,
-                     !counts || slope == 0.f || r.empty, part, parts);
+                     !counts || slope == 0.f || r.empty, part, parts, (int)threadIdx.x, kLossThreads);
   }
   if (part == 0 && threadIdx.x < 32) reduce_loss(P, total, (uint32_t)cluster, (uint32_t)clusters);
 }

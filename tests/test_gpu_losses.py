@@ -580,3 +580,74 @@ def test_withhold_refusals():
     for row, ns in ((-1, 1000), (10, 1000), (0, 0), (0, 2_000_000_001)):
         assert lib.gmc_test_withhold_row(h.h, row, ns) == GMC_EINVAL
     h.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,V,pad,shift", [(601, 1, 0, 0), (640, 2, 1, 0), (999, 15, 0, 1), (1_024, 61, 3, 5),
+                                           (777, 1_021, 0, 0), (2_051, 5_003, 0, 0)])
+def test_many_short_rows(n, V, pad, shift, kind):
+    """Rows that a warp does: every offset from a 32-byte boundary, the last warps without
+    a row, marked targets, masked logits, rows of nothing, nothing written beside the rows."""
+    import torch
+    from paper_1905_12948_gb300 import token_logp, token_logp_backward
+    rng = np.random.default_rng([17, n, V])
+    x, y = rng.standard_normal((n, V)) * 2.5, rng.integers(0, V, n)
+    x[5, 1:] = -np.inf
+    x[6] = -np.inf
+    x[7] = np.nan
+    y[5], y[7], y[n - 1] = 0, -1, -1
+    t, x = _place(x, kind, pad, shift)
+    logp, stats = token_logp(t, _dev(y), return_stats=True)
+    with np.errstate(invalid="ignore"):
+        want = ref.token_logp(x, y, 1.0)
+    _check_logp(logp.double().cpu().numpy(), want)
+    g = _f32(rng.standard_normal(n))
+    g[[3, 6, 7]] = 0.0
+    stride = V + pad + 1
+    buf = torch.full((n * stride,), 7.0, dtype=_torch_type(kind), device="cuda")
+    out = buf.as_strided((n, V), (stride, 1))
+    token_logp_backward(t, _dev(y), stats, _dev(g, torch.float32), out=out)
+    got = out.double().cpu().numpy()
+    assert (got[[3, 6, 7, n - 1]] == 0).all()
+    rows = np.setdiff1d(np.arange(n), [3, 6, 7, n - 1])
+    _check_gradient(out[torch.from_numpy(rows).cuda()], x[rows], y[rows], g[rows], np.zeros(len(rows)), 1.0, kind)
+    assert (buf.view(n, stride)[:, V:] == 7.0).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("lengths,V", [([1] * 700, 33), ([0, 0] + [7, 3] * 65 + [0, 1, 0, 0], 257), ([900, 0], 1_021),
+                                       ([0, 0] * 400 + [511, 513] + [0, 0] * 40, 5)])
+def test_pairs_of_many_short_rows(lengths, V, kind):
+    """A warp does a row, and the last one of a pair the pair: pairs with and without rows,
+    with and without the gradient, the same bits each time."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    n, pairs, f = sum(lengths), len(lengths) // 2, torch.float32
+    rng, t, x, y = _logits(n, V, 18, kind)
+    y[rng.random(n) < 0.2] = -1
+    beta, eps = 0.1, 0.05
+    lp = ref.token_logp(x, y, 1.0)
+    off = np.concatenate([[0], np.cumsum(lengths)])
+    rf, w = _f32(lp + rng.standard_normal(n) * 0.4), _f32(rng.uniform(0.1, 1.0, pairs))
+    w[0] = 0.0 if pairs > 1 else w[0]
+    h = TokenLoss(n, pairs)
+    args = dict(beta=beta, smoothing=eps, ref_logp=_dev(rf, f), weights=_dev(w, f))
+    r = h.preference(t, _dev(y), _dev(off), **args)
+    loss, each, ratio, coef = ref.preference(lp, y, off, rf, w, beta, eps, np.zeros(n, bool))
+    row = np.where(y >= 0, ref.LOGP + 2 * ref.U * np.abs(lp), 0.0)
+    off_ratio = np.array([row[off[s]: off[s + 1]].sum() for s in range(2 * pairs)])
+    dm = beta * (off_ratio[0::2] + off_ratio[1::2]) + 2 * ref.U * beta * np.abs(ratio).max()
+    _check_logp(r.logp.double().cpu().numpy(), lp)
+    assert (np.abs(r.seq_ratio.double().cpu().numpy() - ratio) <= off_ratio + ref.U * np.abs(ratio)).all()
+    assert (np.abs(r.pair_loss.double().cpu().numpy() - each) <= dm + 8 * ref.U * (1 + each)).all()
+    assert abs(float(r.loss) - loss) <= (w * (dm + 8 * ref.U * (1 + each))).sum() + ref.U * loss
+    dc = np.zeros(n)
+    for s in range(2 * pairs):
+        dc[off[s]: off[s + 1]] = w[s // 2] * beta * (dm[s // 2] / 4 + 8 * ref.U)
+    _check_gradient(r.dlogits, x, y, coef, dc, 1.0, kind)
+    for _ in range(3):
+        again = h.preference(t, _dev(y), _dev(off), grad=False, **args)
+        assert torch.equal(again.loss, r.loss) and torch.equal(again.seq_ratio, r.seq_ratio)
+        again = h.preference(t, _dev(y), _dev(off), **args)
+        assert torch.equal(again.loss, r.loss) and torch.equal(again.dlogits, r.dlogits)
+    h.close()
