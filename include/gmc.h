@@ -469,7 +469,7 @@ int gmc_token_logp_backward(const void* logits_dev, int32_t dtype, int64_t n, in
                             void* dlogits_dev, int64_t dld, void* stream);
 
 /* Workspace of the two losses below, for calls of at most max_rows rows and
- * max_pairs pairs: allocated once on the current device (20 bytes a row, 16 a pair, and
+ * max_pairs pairs: allocated once on the current device (20 bytes a row, 12 a pair, and
  * 64 KB). Calls with one handle are ordered by the caller (one stream, or events between
  * streams); distinct handles are independent. gmc_loss_destroy synchronises the
  * device; NULL is ignored. GMC_EINVAL, GMC_ENOMEM or GMC_ECUDA, with *out set to

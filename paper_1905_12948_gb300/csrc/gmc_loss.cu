@@ -15,9 +15,6 @@ namespace {
 
 // The threads that work on a row: a block (G = kLossThreads), of which up to 8 share a row as
 // a cluster, or a warp (G = 32).
-struct Halves {
-  double a, b;
-};
 template <int G>
 struct Group {
   static_assert(G == 32 || G == kLossThreads, "a warp or a block");
@@ -31,42 +28,6 @@ struct Group {
     } else {
       __shared__ MaxSum ws[32];
       return block_merge(a, b, ws);
-    }
-  }
-  // Sums over the first and the second half of the group, in a fixed order.
-  __device__ static Halves sums(double s) {
-    Halves h{0., 0.};
-    if constexpr (G == 32) {
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      h.a = __shfl_sync(0xffffffffu, s, 0);
-      h.b = __shfl_sync(0xffffffffu, s, 16);
-    } else {
-      __shared__ double ws[kLossThreads / 32];
-      s = warp_sum(s);
-      __syncthreads();
-      if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = s;
-      __syncthreads();
-      for (int i = 0; i < kLossThreads / 64; ++i) h.a += ws[i], h.b += ws[kLossThreads / 64 + i];
-    }
-    return h;
-  }
-  // Thread 0 adds to a count that other groups add to; every thread returns whether it has
-  // reached `all`. What the groups wrote before is then visible to this one.
-  __device__ static bool last_of(uint32_t* count, uint32_t mine, int64_t all) {
-    if constexpr (G == 32) {
-      __syncwarp();
-      int last = 0;
-      if (tid() == 0) last = (int64_t)count_add(count, mine) + mine == all;
-      last = __shfl_sync(0xffffffffu, last, 0);
-      __syncwarp();  // what thread 0 acquired holds for all
-      return last != 0;
-    } else {
-      __shared__ int last;
-      __syncthreads();
-      if (threadIdx.x == 0) last = (int64_t)count_add(count, mine) + mine == all;
-      __syncthreads();
-      return last != 0;
     }
   }
 };
@@ -108,13 +69,16 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
 // Bound by memory: a block of 256 threads loads 16 KB at once, and six of them share an SM.
 // 8,192 rows of 32,000 bf16 logits: 84 us, 6.2 TB/s; by warps, 8,000 rows of 4,096: 11.3 us,
 // 5.8 TB/s, and 40,000 of 2,048: 39.6 us with 48 registers (five blocks an SM), 46 with 54.
-template <typename T, int G>
+// kRatio: the log ratios are wanted (the code for them, where they are not, cost 10% of short
+// rows' time).
+template <typename T, int G, bool kRatio>
 __global__ void __launch_bounds__(kLossThreads, G == 32 ? 5 : 6) k_stats(Rows<T> R, float* logp, float2* stats,
-                                                                         int parts) {
+                                                                         const float* ref, double* ratio, int parts) {
   griddep_wait();
   const int64_t at = blockIdx.x / parts, row = at * Group<G>::kRows + Group<G>::of_block();
   if (row < R.n)
-    row_stats<G>(R, row, (int)(blockIdx.x - at * parts), parts, logp, stats, (const float*)nullptr, (double*)nullptr);
+    row_stats<G>(R, row, (int)(blockIdx.x - at * parts), parts, logp, stats, kRatio ? ref : nullptr,
+                 kRatio ? ratio : nullptr);
 }
 
 struct PairArgs {
@@ -126,15 +90,20 @@ struct PairArgs {
   float *loss, *pair_loss, *seq_ratio;    // the last two may be NULL
   float* slope;                           // beta w dl/dmargin of each pair
   double* wloss;                          // weighted loss of each pair
-  uint32_t* count;                        // rows done of each pair, then pairs done; 0 between calls
+  uint32_t* ticket;                       // 0 between calls
 };
-// The sequence that row is in (the last one that starts at or before it), -1: none.
+// The sequence that row is in (the last one that starts at or before it), -1: none. By a
+// warp, 32 offsets at a time: one read for 16 pairs, two for 500.
 __device__ __forceinline__ int64_t sequence_of(const PairArgs& P, int64_t row) {
-  int64_t lo = 0, hi = 2 * P.pairs;
+  const int lane = (int)threadIdx.x & 31;
+  int64_t lo = 0, hi = 2 * P.pairs;  // the first offset past the row is in [lo, hi]
   while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (P.offsets[mid] <= row) lo = mid + 1;
-    else hi = mid;
+    const int64_t step = (hi - lo + 31) >> 5, i = lo + (lane + 1) * step - 1;
+    const uint32_t past = __ballot_sync(0xffffffffu, i >= hi || P.offsets[i] > row);
+    const int64_t before = (past ? __ffs((int)past) - 1 : 32) * step;  // so many start at or before the row
+    const int64_t end = lo + before + step - 1;
+    lo = lo + before < hi ? lo + before : hi;
+    hi = end < hi ? end : hi;
   }
   return lo > 0 && row < P.offsets[lo] ? lo - 1 : -1;
 }
@@ -152,69 +121,62 @@ __device__ __forceinline__ void finish_pair(const PairArgs& P, int64_t p, float 
   if (P.seq_ratio) P.seq_ratio[2 * p] = (float)chosen, P.seq_ratio[2 * p + 1] = (float)other;
 }
 __device__ __forceinline__ float weight_of(const PairArgs& P, int64_t p) { return P.weights ? P.weights[p] : P.weight; }
-// By one group, half of it a sequence: the log ratios of a pair whose rows are all done.
-template <int G>
-__device__ __forceinline__ void pair_of_rows(const PairArgs& P, int64_t p) {
-  constexpr int half = G / 2;
-  const int tid = Group<G>::tid(), side = tid / half;
-  const float w = weight_of(P, p);
-  int64_t lo = P.offsets[2 * p + side], hi = P.offsets[2 * p + side + 1];
-  lo = lo < 0 ? 0 : lo;
-  hi = hi > P.n ? P.n : hi;
-  double s = 0.;
-  for (int64_t i = lo + tid % half; i < hi; i += half) s += __ldcg(P.ratio + i);
-  const Halves h = Group<G>::sums(s);
-  if (tid == 0) finish_pair(P, p, w, h.a, h.b);
+// Sums over the first and the second half of the block, in a fixed order.
+struct Halves {
+  double a, b;
+};
+__device__ __forceinline__ Halves block_sums(double s) {
+  __shared__ double ws[kLossThreads / 32];
+  s = warp_sum(s);
+  if ((threadIdx.x & 31) == 0) ws[threadIdx.x >> 5] = s;
+  __syncthreads();
+  Halves h{0., 0.};
+  for (int i = 0; i < kLossThreads / 64; ++i) h.a += ws[i], h.b += ws[kLossThreads / 64 + i];
+  return h;
 }
-// The pairs' weighted losses added up, by one group.
-template <int G>
+// The pairs' weighted losses added up, by one block.
 __device__ __forceinline__ void sum_pairs(const PairArgs& P) {
   double s = 0.;
-  for (int64_t p = Group<G>::tid(); p < P.pairs; p += G) s += __ldcg(P.wloss + p);
-  const Halves h = Group<G>::sums(s);
-  if (Group<G>::tid() == 0) *P.loss = (float)(h.a + h.b);
+  for (int64_t p = threadIdx.x; p < P.pairs; p += kLossThreads) s += __ldcg(P.wloss + p);
+  const Halves h = block_sums(s);
+  if (threadIdx.x == 0) *P.loss = (float)(h.a + h.b);
 }
 
-// k_stats, and the pairs' losses and slopes: the group that does a pair's last row does the
-// pair. The block (or cluster) past the last row does the pairs that have no rows. total:
-// the group that does the last pair adds up the loss (k_grad does so where it follows).
-// Six blocks an SM (40 registers): the pairs' part would take 58, and the sums' loads four
-// blocks at once (16 pairs of 50,257: 391 us instead of 363).
-template <typename T, int G>
-__global__ void __launch_bounds__(kLossThreads, 6) k_pair_stats(Rows<T> R, PairArgs P, float* logp, float2* stats,
-                                                                int parts, bool total) {
+// The pairs' losses and slopes from their rows' log ratios: G threads a pair, half of them a
+// sequence. total: the last block adds up the loss (k_grad does so where it follows).
+// A chain of reads, 3 us; in the sums' kernel, by the block that counts the pair's last row,
+// it took 5 to 7.
+template <int G>
+__global__ void __launch_bounds__(kLossThreads) k_pairs(PairArgs P, bool total) {
+  constexpr int half = G / 2;
   griddep_wait();
-  const int64_t at = blockIdx.x / parts, row = at * Group<G>::kRows + Group<G>::of_block();
-  const int part = (int)(blockIdx.x - at * parts);
-  uint32_t done = 1;
-  if ((at + 1) * parts == gridDim.x) {
-    if (part != 0 || Group<G>::of_block() != 0) return;
-    uint32_t empty = 0;
-    for (int64_t p = Group<G>::tid(); p < P.pairs; p += G)
-      if (P.offsets[2 * p] >= P.offsets[2 * p + 2]) {
-        finish_pair(P, p, weight_of(P, p), 0., 0.);
-        ++empty;
-      }
-    const Halves h = Group<G>::sums((double)empty);
-    done = (uint32_t)(h.a + h.b);
-  } else {
-    if (row >= R.n) return;
-    int64_t p = -1, rows = 0;
-    if (part == 0) {
-      p = sequence_of(P, row);
-      if (p >= 0) {
-        p >>= 1;
-        rows = P.offsets[2 * p + 2] - P.offsets[2 * p];
-      }
+  const int tid = Group<G>::tid();
+  const int64_t p = blockIdx.x * (int64_t)Group<G>::kRows + Group<G>::of_block();
+  if (p < P.pairs) {
+    const int side = tid / half;
+    const float w = weight_of(P, p);
+    int64_t lo = P.offsets[2 * p + side], hi = P.offsets[2 * p + side + 1];
+    lo = lo < 0 ? 0 : lo;
+    hi = hi > P.n ? P.n : hi;
+    double s = 0.;
+#pragma unroll 4
+    for (int64_t i = lo + tid % half; i < hi; i += half) s += P.ratio[i];
+    Halves h;
+    if constexpr (G == 32) {
+#pragma unroll
+      for (int o = half / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      h = Halves{s, __shfl_sync(0xffffffffu, s, half)};
+    } else {
+      h = block_sums(s);
     }
-    row_stats<G>(R, row, part, parts, logp, stats, P.ref_logp, P.ratio);
-    if (p < 0 || !Group<G>::last_of(P.count + p, 1, rows)) return;
-    pair_of_rows<G>(P, p);
-    if (Group<G>::tid() == 0) P.count[p] = 0;
+    if (tid == 0) finish_pair(P, p, w, h.a, h.b);
   }
-  if (!total || !Group<G>::last_of(P.count + P.pairs, done, P.pairs)) return;
-  sum_pairs<G>(P);
-  if (Group<G>::tid() == 0) P.count[P.pairs] = 0;
+  if (!total) return;
+  __shared__ bool last;
+  __syncthreads();
+  if (threadIdx.x == 0) last = count_inc(P.ticket, gridDim.x - 1) == gridDim.x - 1;
+  __syncthreads();
+  if (last) sum_pairs(P);
 }
 
 // dx = g s ([v = y] - p) of each row from its saved (m, log S). Without g, a row's is the
@@ -227,25 +189,22 @@ __global__ void __launch_bounds__(kLossThreads, G == 32 ? 4 : 6) k_grad(Rows<T> 
   const int64_t row = R.n - 1 - (blockIdx.x / parts * Group<G>::kRows + Group<G>::of_block());
   const int part = (int)(blockIdx.x % parts);
   if (row >= 0) {
+    // all that the row needs to know, in as few reads behind each other as can be
     const int64_t y = R.y[row];
+    const float2 st = stats[row];
     float coef = 0.f;
-    if (y >= 0) {
-      if (!g) {
-        const int64_t q = sequence_of(P, row);
-        if (q >= 0) coef = q & 1 ? -P.slope[q >> 1] : P.slope[q >> 1];
-      } else {
-        coef = g[row];
-      }
-      if (y >= R.V) coef = __uint_as_float(kNan);
+    if (g) {
+      coef = g[row];
+    } else {
+      const int64_t q = sequence_of(P, row);
+      if (q >= 0) coef = q & 1 ? -P.slope[q >> 1] : P.slope[q >> 1];
     }
-    const float2 st = coef != 0.f ? stats[row] : make_float2(0.f, 0.f);
+    if (y >= R.V) coef = __uint_as_float(kNan);
+    if (y < 0) coef = 0.f;
     write_gradient(R.x + row * R.ld, dx + row * dld, R.V, grad_of(shift_of(st.x, R.b), st.y, coef, y, R.b), R.b,
                    coef == 0.f || st.y == INFINITY, part, parts, Group<G>::tid(), G);
   }
-  if (g || blockIdx.x != 0 || Group<G>::of_block() != 0) return;
-  sum_pairs<G>(P);
-  // whatever the offsets were, the next call finds the counts at 0
-  for (int64_t i = Group<G>::tid(); i <= P.pairs; i += G) P.count[i] = 0;
+  if (!g && blockIdx.x == 0) sum_pairs(P);
 }
 
 }  // namespace
@@ -264,7 +223,6 @@ struct gmc_loss_ctx {
   float* logp = nullptr;     // max_rows
   double* ratio = nullptr;   // max_rows
   float* slope = nullptr;    // max_pairs
-  uint32_t* count = nullptr; // max_pairs + 1, zero between calls
 };
 
 namespace {
@@ -315,6 +273,22 @@ int64_t blocks_for(int64_t n) {
   return (n + Group<G>::kRows - 1) / Group<G>::kRows;
 }
 
+template <bool kRatio, typename T>
+cudaError_t launch_stats(const Rows<T>& R, float* logp, float2* stats, const float* ref, double* ratio, cudaStream_t s) {
+  const int64_t bytes = R.V * (int64_t)sizeof(T);
+  if (by_warps(R.n, bytes))
+    return launch(k_stats<T, 32, kRatio>, blocks_for<32>(R.n), kLossThreads, 1, s, R, logp, stats, ref, ratio, 1);
+  return with_parts(parts_for(R.n, bytes), [&](int parts) {
+    return launch(k_stats<T, kLossThreads, kRatio>, R.n * parts, kLossThreads, parts, s, R, logp, stats, ref, ratio, parts);
+  });
+}
+// A warp a pair where that is two reads a thread or so: 10,000 pairs of single rows of 512
+// logits 114 -> 53 us; one pair of 30,000 rows 160 us by a warp, 72 by a block.
+cudaError_t launch_pairs(const PairArgs& P, bool total, cudaStream_t s) {
+  if (P.pairs > 0 && P.n / P.pairs <= 64)
+    return launch(k_pairs<32>, blocks_for<32>(P.pairs), kLossThreads, 1, s, P, total);
+  return launch(k_pairs<kLossThreads>, P.pairs ? P.pairs : 1, kLossThreads, 1, s, P, total);
+}
 template <typename T>
 cudaError_t launch_grad(const Rows<T>& R, const float2* stats, const float* g, const PairArgs& P, T* dx, int64_t dld,
                         cudaStream_t s) {
@@ -339,15 +313,9 @@ int gmc_token_logp(const void* logits_dev, int32_t dtype, int64_t n, int64_t voc
   if (!logp_dev) return GMC_EINVAL;
   return done(by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    const Rows<T> R = rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev);
-    const int64_t bytes = vocab * (int64_t)sizeof(T);
-    const cudaStream_t on = static_cast<cudaStream_t>(stream);
-    float2* stats = reinterpret_cast<float2*>(stats_dev);
-    if (by_warps(n, bytes))
-      return launch(k_stats<T, 32>, blocks_for<32>(n), kLossThreads, 1, on, R, logp_dev, stats, 1);
-    return with_parts(parts_for(n, bytes), [&](int parts) {
-      return launch(k_stats<T, kLossThreads>, n * parts, kLossThreads, parts, on, R, logp_dev, stats, parts);
-    });
+    return launch_stats<false>(rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev), logp_dev,
+                        reinterpret_cast<float2*>(stats_dev), (const float*)nullptr, (double*)nullptr,
+                        static_cast<cudaStream_t>(stream));
   }));
 }
 
@@ -377,7 +345,7 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   h->max_rows = max_rows;
   h->max_pairs = max_pairs;
   const size_t bytes =
-      8 * (size_t)(kMostClusters + 1 + max_pairs + 2 * max_rows) + 4 * (size_t)(max_rows + 2 * max_pairs + 1);
+      8 * (size_t)(kMostClusters + 1 + max_pairs + 2 * max_rows) + 4 * (size_t)(max_rows + max_pairs);
   cudaError_t err = cudaGetDevice(&h->device);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&h->resident.sms, cudaDevAttrMultiProcessorCount, h->device);
   if (err == cudaSuccess) err = lib_malloc(&h->mem, bytes);
@@ -396,7 +364,6 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   h->ratio = reinterpret_cast<double*>(h->stats + max_rows);
   h->logp = reinterpret_cast<float*>(h->ratio + max_rows);
   h->slope = h->logp + max_rows;
-  h->count = reinterpret_cast<uint32_t*>(h->slope + max_pairs);
   *out = h;
   return GMC_OK;
 }
@@ -465,24 +432,16 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
   float* logp = logp_dev ? logp_dev : h->logp;
   const float weight = pairs ? (float)(1.0 / (double)pairs) : 0.f;
   const PairArgs P{offsets_dev, n, pairs, ref_logp_dev, weights_dev, h->ratio, weight, beta, smoothing,
-                   loss_dev, pair_loss_dev, seq_ratio_dev, h->slope, h->wloss, h->count};
+                   loss_dev, pair_loss_dev, seq_ratio_dev, h->slope, h->wloss, h->ticket};
   const bool grad = n > 0 && dlogits_dev;
   cudaError_t err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
     const Rows<T> R = rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev);
-    const int64_t bytes = vocab * (int64_t)sizeof(T);
-    cudaError_t e;
-    if (by_warps(n, bytes))
-      e = launch(k_pair_stats<T, 32>, blocks_for<32>(n) + 1, kLossThreads, 1, s, R, P, logp, h->stats, 1, !grad);
-    else
-      e = with_parts(parts_for(n, bytes), [&](int parts) {
-        return launch(k_pair_stats<T, kLossThreads>, (n + 1) * parts, kLossThreads, parts, s, R, P, logp, h->stats, parts,
-                      !grad);
-      });
+    cudaError_t e = n ? launch_stats<true>(R, logp, h->stats, ref_logp_dev, h->ratio, s) : cudaSuccess;
+    if (e == cudaSuccess && (pairs || !grad)) e = launch_pairs(P, !grad, s);
     if (e != cudaSuccess || !grad) return e;
     return launch_grad(R, (const float2*)h->stats, (const float*)nullptr, P, static_cast<T*>(dlogits_dev), dld, s);
   });
-  if (err == cudaSuccess && !grad) err = cudaMemsetAsync(h->count, 0, sizeof(uint32_t) * (size_t)(pairs + 1), s);
   return done(err);
 }
 

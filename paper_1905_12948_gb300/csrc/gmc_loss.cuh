@@ -157,11 +157,6 @@ __device__ __forceinline__ MaxSum block_merge(MaxSum a, const Base& b, MaxSum* w
 }
 // Counts that tell the last of several blocks: what a block (or a warp) wrote before it
 // counts is visible to the one that is told it is the last.
-__device__ __forceinline__ uint32_t count_add(uint32_t* p, uint32_t v) {
-  uint32_t before;
-  asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], %2;" : "=r"(before) : "l"(p), "r"(v) : "memory");
-  return before;
-}
 __device__ __forceinline__ uint32_t count_inc(uint32_t* p, uint32_t last) {  // back to 0 after `last`
   uint32_t before;
   asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(before) : "l"(p), "r"(last) : "memory");
