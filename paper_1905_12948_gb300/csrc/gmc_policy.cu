@@ -733,7 +733,7 @@ cudaError_t Residency::clusters(const void* f, const LaunchConfig& l, int parts,
       return cudaSuccess;
     }
   cudaError_t err = cudaSuccess;
-  if (smem > 48 * 1024)  // (of the 227 KB, leaving room for static shared memory)
+  if (smem > 32 * 1024)  // 48 KB, with the static shared memory, are had without; of 227 KB this leaves that room too
     err = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, 224 * 1024);
   int n = 0;
   if (err == cudaSuccess)

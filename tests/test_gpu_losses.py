@@ -651,3 +651,28 @@ def test_pairs_of_many_short_rows(lengths, V, kind):
         again = h.preference(t, _dev(y), _dev(off), **args)
         assert torch.equal(again.loss, r.loss) and torch.equal(again.dlogits, r.dlogits)
     h.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("V", [60, 121, 200, 251, 256, 310, 500, 512, 700, 1_000, 1_024, 1_990, 2_048, 3_990])
+def test_policy_of_many_short_rows(V, kind):
+    """Rows that a warp does, over the sizes of its buffers: a block's shared memory goes from a
+    few KB, over what a kernel has without asking, to all there is."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    n, f = 700, torch.float32
+    rng, t, x, y = _logits(n, V, 19, kind)
+    y[rng.random(n) < 0.2] = -1
+    lp = ref.token_logp(x, y, 1.0)
+    old, rf = _f32(lp + 0.1 * rng.standard_normal(n)), _f32(lp - 0.2)
+    adv, w = _f32(rng.uniform(-1.5, 1.5, n)), _f32(rng.uniform(0.1, 1.0, n))
+    # no ratio within the rounding of its bounds
+    close = np.abs(np.exp(lp - old)[:, None] - [1 - LO, 1 + HI]).min(1) < 1e-3
+    old[close] = _f32(lp[close])
+    h = TokenLoss(n)
+    r = h.policy(t, _dev(y), _dev(old, f), _dev(adv, f), weights=_dev(w, f), ref_logp=_dev(rf, f), clip_low=LO,
+                 clip_high=HI, kl=0.1)
+    _check_logp(r.logp.double().cpu().numpy(), lp)
+    _, _, coef = ref.policy(lp, y, old, adv, w, rf, LO, HI, 0.1)
+    _check_gradient(r.dlogits, x, y, coef, w * ref.policy_bound(lp, old, adv, rf, 0.1), 1.0, kind)
+    h.close()
