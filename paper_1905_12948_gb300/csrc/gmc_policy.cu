@@ -493,12 +493,13 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
 // ---------------------------------------------------------------------------
 // Short rows, one a warp
 // ---------------------------------------------------------------------------
-// Each warp has two buffers of a row and takes rows by itself: while it works on one, the
-// next but one's bulk copy is under way. Nothing is shared with another warp but the sum of
-// the losses at the end. cap: vectors of a buffer.
-constexpr int kShortWarps = 24;  // of a block at most
+// Each warp has a buffer of a row and takes rows by itself: the other warps work while it
+// waits for its bulk copy. (Two buffers a warp, and half as many warps: 13,463 bf16 rows of
+// 4,999 72 us instead of 62.) Nothing is shared with another warp but the sum of the losses at
+// the end. cap: vectors of a buffer.
+constexpr int kShortWarps = 28;  // of a block at most
 constexpr int kShortBatch = 4;   // vectors that a lane takes at once
-constexpr int64_t kShortVecs = 960;          // vectors of a row at most (15 KB)
+constexpr int64_t kShortVecs = 1440;         // vectors of a row at most (22.5 KB)
 constexpr int64_t kShortBytes = 220 * 1024;  // of all buffers of a block
 
 template <typename T>
@@ -506,53 +507,49 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
     k_policy_short(Rows<T> R, PolicyArgs P, T* dx, int64_t dld, int cap) {
   constexpr int N = Vec<T>::N;
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ uint64_t full[kShortWarps][2];
+  __shared__ uint64_t full[kShortWarps];
   __shared__ double totals[kShortWarps];
   __shared__ int dead;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  uint4* mine = reinterpret_cast<uint4*>(smem) + (int64_t)warp * 2 * cap;
+  uint4* mine = reinterpret_cast<uint4*>(smem) + (int64_t)warp * cap;
   if (threadIdx.x == 0) dead = 0;
   if (lane == 0) {
-    mbar_init(&full[warp][0], 1);
-    mbar_init(&full[warp][1], 1);
+    mbar_init(&full[warp], 1);
     fence_mbar_init();
   }
   __syncthreads();
   griddep_wait();
   const int64_t first = (int64_t)warp * gridDim.x + blockIdx.x, step = (int64_t)warps * gridDim.x;
   double total = 0.;
-  uint32_t loaded[2] = {0, 0};
-  // begin the copy of a row that counts into buffer b
-  auto load = [&](int64_t row, const Facts& f, int b) {
+  uint32_t loaded = 0;
+  // begin the copy of a row that counts
+  auto load = [&](int64_t row, const Facts& f) {
     if (row >= R.n || !f.count()) return;
-    ++loaded[b];
+    ++loaded;
     if (row == P.hold_row) return;
     const T* x = R.x + row * R.ld;
     const Cover<T> c(x, R.V);
-    uint4* to = mine + b * cap;
     const int64_t v0 = c.first ? 1 : 0, v1 = c.last ? c.nv - 1 : c.nv;
     if (lane == 0 && v1 > v0) {
       const uint32_t bytes = (uint32_t)(v1 - v0) * 16u;
-      mbar_expect_tx(&full[warp][b], bytes);
-      bulk_load(to + v0, x - c.ph + v0 * N, bytes, &full[warp][b]);
+      mbar_expect_tx(&full[warp], bytes);
+      bulk_load(mine + v0, x - c.ph + v0 * N, bytes, &full[warp]);
     }
     if (c.first && lane < N) {
       const int64_t j = (int64_t)lane - c.ph;
-      reinterpret_cast<T*>(to)[lane] = j >= 0 && j < R.V ? x[j] : Vec<T>::round(-INFINITY);
+      reinterpret_cast<T*>(mine)[lane] = j >= 0 && j < R.V ? x[j] : Vec<T>::round(-INFINITY);
     }
     if (c.last && v1 >= v0 && lane < N) {
       const int64_t j = v1 * N - c.ph + lane;
-      reinterpret_cast<T*>(to + v1)[lane] = j < R.V ? x[j] : Vec<T>::round(-INFINITY);
+      reinterpret_cast<T*>(mine + v1)[lane] = j < R.V ? x[j] : Vec<T>::round(-INFINITY);
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(&full[warp][b]);
+    if (lane == 0) mbar_arrive(&full[warp]);
   };
-  Facts now = facts_of(R, P, first), next = facts_of(R, P, first + step);
-  load(first, now, 0);
-  load(first + step, next, 1);
-  int b = 0;
-  for (int64_t row = first; row < R.n; row += step, b ^= 1) {
-    const Facts after = facts_of(R, P, row + 2 * step);
+  Facts now = facts_of(R, P, first);
+  load(first, now);
+  for (int64_t row = first; row < R.n; row += step) {
+    const Facts next = facts_of(R, P, row + step);
     const int64_t y = now.y;
     const float w = now.w;
     const bool counts = now.count();
@@ -560,13 +557,13 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
     T* out = dx + row * dld;
     const Cover<T> c(x, R.V);
     const int nv = (int)c.nv;
-    const uint4* v = mine + b * cap;
+    const uint4* v = mine;
     RowStats st = {};
     float loss = 0.f, slope = 0.f;
     if (counts) {
       const float xy = target_logit(x, R.V, y);
       const float adv = P.adv[row], old_logp = P.old_logp[row], ref_logp = P.ref_logp ? P.ref_logp[row] : 0.f;
-      if (!warp_wait(&full[warp][b], (loaded[b] - 1) & 1, P.wait_ns)) {
+      if (!warp_wait(&full[warp], (loaded - 1) & 1, P.wait_ns)) {
         dead = 1;
         break;
       }
@@ -624,12 +621,11 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
       if (lane == 0 && !skip && y < R.V) out[y] = Vec<T>::round(g.k * -expm1f(st.logp));
     }
     __syncwarp();  // every lane has read the buffer
-    load(row + 2 * step, after, b);
+    load(row + step, next);
     now = next;
-    next = after;
   }
-  for (int i = 0; i < 2; ++i)  // no copy is under way when the block ends
-    if (loaded[i]) warp_wait(&full[warp][i], (loaded[i] - 1) & 1, P.wait_ns);
+  // no copy is under way when the block ends
+  if (loaded) warp_wait(&full[warp], (loaded - 1) & 1, P.wait_ns);
   if (lane == 0) totals[warp] = total;
   __syncthreads();
   if (warp == 0) {
@@ -755,14 +751,15 @@ template <typename T>
 cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, Residency* device, cudaStream_t s) {
   const int64_t nv = most_vecs(R);
   const int sms = device->sms;
-  // Short rows, and more of them than the ring kernel's blocks see twice: a warp a row. bf16
-  // 16,384 x 2,221 43 us (by the ring 128), 4,000 x 6,001 28 (40), 1,000 x 2,500 10 (14); the ring is
-  // the faster from 16 KB a row: 4,000 x 4,096 fp32 32 us (36), 9,689 x 8,696 88 (91), 4,000 x 12,001 49 (72).
-  if (nv <= kShortVecs && R.n > 2 * sms) {
+  // Short rows, and so many that a lone warp's 10 us for 20 KB do not matter: a warp a row.
+  // bf16, in us, by a warp and by the ring: 30,000 x 2,000 51 201, 16,384 x 2,221 43 140, 30,000 x 10,000
+  // 198 290, 8,000 x 11,000 74 83, 4,000 x 12,001 51 50, 1,000 x 2,500 8.7 12.0, 1,000 x 10,000 12.9 14.8,
+  // 600 x 7,000 9.7 9.2, 310 x 2,500 8.1 8.0, 310 x 7,000 9.5 8.2.
+  if (nv <= kShortVecs && R.n > 2 * sms && nv * 16 <= 20 * R.n) {
     const int cap = (int)(nv + 7) / 8 * 8;
-    int warps = (int)(kShortBytes / (cap * 32));
+    int warps = (int)(kShortBytes / (cap * 16));
     if (warps > kShortWarps) warps = kShortWarps;
-    LaunchConfig l(1, warps * 32, 1, (size_t)warps * cap * 32, s);
+    LaunchConfig l(1, warps * 32, 1, (size_t)warps * cap * 16, s);
     int64_t blocks = 1;
     const cudaError_t err = device->clusters((const void*)k_policy_short<T>, l, 1, &blocks);
     if (err != cudaSuccess) return err;
