@@ -295,7 +295,11 @@ cudaError_t launch_grad(const Rows<T>& R, const float2* stats, const float* g, c
   const int64_t bytes = R.V * (int64_t)sizeof(T);
   if (by_warps(R.n, bytes))
     return launch(k_grad<T, 32>, blocks_for<32>(R.n), kLossThreads, 1, s, R, stats, g, P, dx, dld, 1);
-  const int parts = parts_for(R.n, bytes);
+  // pieces of up to 56 KB (they need no cluster): the last blocks end together. 4,096 rows of
+  // 50,257 fp32 248 us whole, 239 in pieces of 50 KB, 269 of 13; 1,024 rows 73, 65 and 71; 300 of
+  // 50,257 bf16 8.3 in pieces of 50 KB, 9.1 of 25.
+  int parts = parts_for(R.n, bytes);
+  while (bytes / parts > 57344) parts *= 2;
   return launch(k_grad<T, kLossThreads>, R.n * parts, kLossThreads, 1, s, R, stats, g, P, dx, dld, parts);
 }
 
