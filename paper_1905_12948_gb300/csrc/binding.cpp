@@ -1,6 +1,6 @@
 // Python module _tokens: the operators of tokens.py on torch tensors. It checks and
 // marshals arguments, allocates outputs and calls the C ABI (through the addresses that
-// init() is given); nothing is computed here. As compiled code it takes 3 to 10 us of
+// init() is given); nothing is computed here. As compiled code it takes 4 to 12 us of
 // host time a call, allocations and launch included, where ctypes and the same checks in
 // Python took 10 to 20: small calls are bound by that.
 #define PY_SSIZE_T_CLEAN

@@ -14,10 +14,10 @@
 // so that nothing in a row's long chain of small steps (3 to 4 us) holds up another row's
 // traffic: 192 KB of ring cover about 40 KB in flight from HBM, the chain, and a row's
 // share of up to 64 KB (128 KB for the longest rows). Bound by HBM at shares of 64 KB (8,192 x
-// 131,072 bf16: 610 us, 6.7 TB/s read and written), by what the SMs issue where a share is an
-// odd number of batches (12,160 x 50,257: 400 us, 6.1 TB/s), and by the first and last row's
-// chains where there are few rows (64 x 32,000: 9 us).
-// k_policy_short: short rows, one a warp. k_policy: rows over 1 MB, swept twice from global
+// 131,072 bf16: 606 us, 6.7 TB/s read and written), by the gradient warps at smaller ones (12,160
+// x 50,257, shares of 49 KB: 400 us, 6.1 TB/s), and by the first and last row's chains where
+// there are few rows (64 x 32,000: 7.3 us).
+// k_policy_short: many short rows, one a warp. k_policy: rows over 1 MB, swept twice from global
 // memory.
 #include <new>
 
