@@ -265,8 +265,12 @@ Rows<T> rows_of(const void* x, int64_t n, int64_t V, int64_t ld, float scale, co
 //    620    2,048   3.7  3.3     3.7  3.4        2,000   8,192   9.1  7.4    12.1 11.1
 //    620    8,192   4.3  6.0     5.3  6.9        2,000  16,384  12.7 11.7    21.0 29.4
 //    900    4,096   4.8  4.3     5.5  4.7        8,000   4,096  29.1 11.5    38.9 22.4
-//    900   12,000   6.6  7.7     7.0  9.2        8,192  16,384  53.4 49.1    75.2 86.2
-bool by_warps(int64_t n, int64_t row_bytes) { return n >= 600 && row_bytes <= 24576 && row_bytes <= 12 * n; }
+//    900   12,000   6.6  7.7     7.0  9.2        4,000  12,000  23.4 16.9    33.4 35.9
+//  1,300    8,192   6.7  7.3     8.2  8.4        8,192  16,384  53.4 49.1    75.2 86.2
+constexpr int64_t kWarpStats = 32768, kWarpGrad = 18432;  // bytes of a row at most
+bool by_warps(int64_t n, int64_t row_bytes, int64_t most) {
+  return n >= 600 && row_bytes <= most && row_bytes <= 12 * n;
+}
 // Blocks of groups of G that do n rows.
 template <int G>
 int64_t blocks_for(int64_t n) {
@@ -276,7 +280,7 @@ int64_t blocks_for(int64_t n) {
 template <bool kRatio, typename T>
 cudaError_t launch_stats(const Rows<T>& R, float* logp, float2* stats, const float* ref, double* ratio, cudaStream_t s) {
   const int64_t bytes = R.V * (int64_t)sizeof(T);
-  if (by_warps(R.n, bytes))
+  if (by_warps(R.n, bytes, kWarpStats))
     return launch(k_stats<T, 32, kRatio>, blocks_for<32>(R.n), kLossThreads, 1, s, R, logp, stats, ref, ratio, 1);
   return with_parts(parts_for(R.n, bytes), [&](int parts) {
     return launch(k_stats<T, kLossThreads, kRatio>, R.n * parts, kLossThreads, parts, s, R, logp, stats, ref, ratio, parts);
@@ -293,7 +297,7 @@ template <typename T>
 cudaError_t launch_grad(const Rows<T>& R, const float2* stats, const float* g, const PairArgs& P, T* dx, int64_t dld,
                         cudaStream_t s) {
   const int64_t bytes = R.V * (int64_t)sizeof(T);
-  if (by_warps(R.n, bytes))
+  if (by_warps(R.n, bytes, kWarpGrad))
     return launch(k_grad<T, 32>, blocks_for<32>(R.n), kLossThreads, 1, s, R, stats, g, P, dx, dld, 1);
   // pieces of up to 56 KB (they need no cluster): the last blocks end together. 4,096 rows of
   // 50,257 fp32 248 us whole, 239 in pieces of 50 KB, 269 of 13; 1,024 rows 73, 65 and 71; 300 of
