@@ -180,7 +180,8 @@ __global__ void __launch_bounds__(kLossThreads) k_pairs(PairArgs P, bool total) 
 }
 
 // dx = g s ([v = y] - p) of each row from its saved (m, log S). Without g, a row's is the
-// slope of its pair (negated in the sequence not preferred).
+// slope of its pair (negated in the sequence not preferred). Bound by memory, read and written:
+// 4,096 rows of 50,257 fp32 239 us, 6.9 TB/s; by warps, 8,000 rows of 4,096 bf16 22 us, 5.9 TB/s.
 template <typename T, int G>
 __global__ void __launch_bounds__(kLossThreads, G == 32 ? 4 : 6) k_grad(Rows<T> R, const float2* stats, const float* g,
                                                                         PairArgs P, T* dx, int64_t dld, int parts) {
@@ -322,8 +323,8 @@ int gmc_token_logp(const void* logits_dev, int32_t dtype, int64_t n, int64_t voc
   return done(by_type(dtype, [&](auto t) {
     using T = decltype(t);
     return launch_stats<false>(rows_of<T>(logits_dev, n, vocab, ld, scale, targets_dev), logp_dev,
-                        reinterpret_cast<float2*>(stats_dev), (const float*)nullptr, (double*)nullptr,
-                        static_cast<cudaStream_t>(stream));
+                               reinterpret_cast<float2*>(stats_dev), (const float*)nullptr, (double*)nullptr,
+                               static_cast<cudaStream_t>(stream));
   }));
 }
 
