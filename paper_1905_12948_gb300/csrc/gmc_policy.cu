@@ -51,6 +51,7 @@ __device__ __forceinline__ void reduce_loss(const PolicyArgs& P, double mine, ui
     last = count_inc(P.ticket, clusters - 1) == clusters - 1;
   }
   if (!__shfl_sync(0xffffffffu, last, 0)) return;
+  __syncwarp();  // what lane 0's count acquired is there for the other lanes too: a shuffle orders no memory
   double s = 0.;
   for (uint32_t i = lane; i < clusters; i += 32) s += __ldcg(P.partial + i);
   s = warp_sum(s);
