@@ -473,6 +473,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
           const int64_t j = b * N - c.ph + lane;
           reinterpret_cast<T*>(chunk + (b - v0))[lane] = j < R.V ? x[j] : Vec<T>::round(-INFINITY);
         }
+        fence_proxy_async();  // these come before a later bulk copy into the same bytes
         __syncwarp();
         if (lane == 0) mbar_arrive(&S.full[at.i]);
         at.next(chunks);
@@ -544,6 +545,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
       const int64_t j = v1 * N - c.ph + lane;
       reinterpret_cast<T*>(mine + v1)[lane] = j < R.V ? x[j] : Vec<T>::round(-INFINITY);
     }
+    fence_proxy_async();  // these come before a later bulk copy into the same bytes
     __syncwarp();
     if (lane == 0) mbar_arrive(&full[warp]);
   };

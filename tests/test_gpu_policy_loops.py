@@ -49,3 +49,74 @@ def test_loss_of_alternating_calls(n, V):
     for pair in losses:
         assert torch.equal(pair[0], first[0]) and torch.equal(pair[1], first[1])
     h.close()
+
+
+def _check(r, x, y, old, adv, args, kind):
+    """A call's outputs against the 64-bit statement."""
+    import torch
+    n = x.shape[0]
+    weights, rf = args["weights"].double().cpu().numpy(), args["ref_logp"].double().cpu().numpy()
+    lp = torch.cat([torch.log_softmax(p.double(), 1).gather(1, q.clamp(min=0)[:, None])[:, 0]
+                    for p, q in zip(x.split(256), y.split(256))]).cpu().numpy()
+    yn, o, a = y.cpu().numpy(), old.double().cpu().numpy(), adv.double().cpu().numpy()
+    loss, each, coef = ref.policy(lp, yn, o, a, weights, rf, args["clip_low"], args["clip_high"], args["kl"])
+    bound = ref.policy_bound(lp, o, a, rf, args["kl"])
+    counts = yn >= 0
+    got = r.logp.double().cpu().numpy()
+    assert (abs(got - lp)[counts] <= (ref.LOGP + 2 * ref.U * abs(lp))[counts]).all() and (got[~counts] == 0).all()
+    assert (abs(r.token_loss.double().cpu().numpy() - each) <= bound).all()
+    assert abs(float(r.loss) - loss) <= (weights * bound)[counts].sum() + 2 * ref.U * abs(loss)
+    rel, low = ref.ROUND[kind]
+    k_all, dk_all = torch.from_numpy(coef).cuda(), torch.from_numpy(abs(weights * bound) * counts).cuda()
+    for i in range(0, n, 256):      # ref.gradient and ref.gradient_bound, on the device
+        p = torch.softmax(x[i: i + 256].double(), 1)
+        k, dk, at = k_all[i: i + 256, None], dk_all[i: i + 256, None], y[i: i + 256].clamp(min=0)[:, None]
+        want = -k * p
+        want.scatter_add_(1, at, k)
+        away = p.scatter(1, at, 1 - p.gather(1, at))
+        off = dk * away + k.abs() * (ref.P * p + 2.0 ** -126)
+        off.scatter_add_(1, at, k.abs() * (2 * ref.LOGP + 4 * ref.U))
+        off = off + rel * (k.abs() * away + off) + low
+        d = r.dlogits[i: i + 256].double()
+        bad = ~((d - want).abs() <= off)
+        assert not bad.any(), (i, bad.nonzero()[:5], d[bad][:5], want[bad][:5], off[bad][:5])
+        assert (d[(y[i: i + 256] < 0)] == 0).all()
+
+
+# parts: the blocks that share a row at these lengths; each takes more than 16 rows, so that its
+# eight row slots, its ring and the two sets of messages are used again and again
+RING = [(3_000, 15_001, "bf16", 1), (2_600, 15_000, "f16", 1), (2_600, 7_503, "f32", 1), (1_500, 50_257, "bf16", 2),
+        (720, 70_003, "f16", 4), (360, 131_073, "f32", 8)]
+
+
+@pytest.mark.parametrize("masked", [0.0, 0.2])
+@pytest.mark.parametrize("n,V,kind,parts", RING)
+def test_many_rows_a_cluster(n, V, kind, parts, masked):
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert n * parts > 16 * sms
+    x, y, old, adv, args = _inputs(n, V, kind, 3, masked)
+    h = TokenLoss(n)
+    r = h.policy(x, y, old, adv, **args)
+    _check(r, x, y, old, adv, args, kind)
+    again = h.policy(x, y, old, adv, **args)
+    assert torch.equal(again.loss, r.loss) and torch.equal(again.dlogits, r.dlogits)
+    h.close()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,V,most", [(30_000, 301, 56), (20_000, 1_021, 56), (11_000, 4_999, 22)])
+def test_many_rows_a_warp(n, V, most, kind):
+    """most: warps of an SM at most, so that each takes rows in turn from one buffer."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert n > 2 * most * sms
+    x, y, old, adv, args = _inputs(n, V, kind, 4, 0.2)
+    h = TokenLoss(n)
+    r = h.policy(x, y, old, adv, **args)
+    _check(r, x, y, old, adv, args, kind)
+    again = h.policy(x, y, old, adv, **args)
+    assert torch.equal(again.loss, r.loss) and torch.equal(again.dlogits, r.dlogits)
+    h.close()
