@@ -379,6 +379,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       if (alive && counts) {
         MaxSum a = block_of(S.ws[slot], lane, R.b);
         if (parts > 1) {
+          // Where dx is x, the block that holds x[y] writes its gradient there as soon as it has
+          // heard from all. So the sums that it waits for are made of xy: a target that is NaN
+          // makes them NaN (as it does the row), and no block sends before it has xy.
+          if (__any_sync(0xffffffffu, xy != xy)) a.s = __uint_as_float(kNan);
           // two sets of slots in turn: a block sends its next but one row's sums only after
           // it has heard this one's next, which this one sends after it has read these
           const int set = trades & 1;

@@ -120,3 +120,40 @@ def test_many_rows_a_warp(n, V, most, kind):
     again = h.policy(x, y, old, adv, **args)
     assert torch.equal(again.loss, r.loss) and torch.equal(again.dlogits, r.dlogits)
     h.close()
+
+
+@pytest.mark.parametrize("n,V,kind", [c[:3] for c in RING] + [(11_000, 4_999, "bf16"), (20_000, 301, "f16")])
+def test_many_rows_in_place(n, V, kind):
+    """The gradient in the logits' place: the same bits as beside them, call after call."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    x, y, old, adv, args = _inputs(n, V, kind, 5, 0.2)
+    h = TokenLoss(n)
+    want = h.policy(x, y, old, adv, **args)
+    for _ in range(5):
+        t = x.clone()
+        r = h.policy(t, y, old, adv, out=t, **args)
+        assert r.dlogits is t and torch.equal(t, want.dlogits)
+        assert torch.equal(r.loss, want.loss) and torch.equal(r.logp, want.logp)
+    h.close()
+
+
+@pytest.mark.parametrize("y", [0, 69_000])
+def test_marked_targets_and_nan_targets_of_a_cluster(y):
+    """A target outside the vocabulary, and one whose logit is NaN, in a row that several blocks
+    share: the row is NaN in all of its blocks' shares, the others are as they were."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    n, V = 4, 70_003
+    x, tgt, old, adv, args = _inputs(n, V, "bf16", 6)
+    h = TokenLoss(n)
+    want = h.policy(x, tgt, old, adv, **args)
+    bad = x.clone()
+    bad[1, y] = float("nan")
+    marked = tgt.clone()
+    marked[1], marked[2] = y, V
+    r = h.policy(bad, marked, old, adv, **args)
+    assert torch.isnan(r.dlogits[1:3]).all() and torch.isnan(r.token_loss[1:3]).all() and torch.isnan(r.loss)
+    for i in (0, 3):
+        assert torch.equal(r.dlogits[i], want.dlogits[i]) and torch.equal(r.token_loss[i], want.token_loss[i])
+    h.close()
