@@ -52,6 +52,7 @@ struct Rows {
 // 5e-8 low on the mean, kExp2Low, which a second one would double). x c - m c is one fused
 // operation as long as m c is not so large that its rounding matters (masks of the type's
 // lowest value in a whole row); then the difference x - m is taken first.
+constexpr float kFar = 1048576.f;  // 2^20
 struct Shift {
   float h, hc;  // m (0 where nothing but -inf was seen), and m c rounded up
   bool far;
@@ -60,16 +61,20 @@ __device__ __forceinline__ Shift shift_of(float m, const Base& b) {
   Shift s;
   s.h = m == -INFINITY ? 0.f : m;
   s.hc = ceilf(s.h * b.c);
-  s.far = !(fabsf(s.hc) < 1048576.f);
+  s.far = !(fabsf(s.hc) < kFar);
   return s;
 }
 // Exponent of x (of x - h, with 0 for hc, where the shift is far).
 __device__ __forceinline__ float exponent(float x, float hc, const Base& b) {
   return __fmaf_rn(x, b.lo, __fmaf_rn(x, b.c, -hc));
 }
-// Of a maximum m's own shift below s.
+// By how much the shift of a sum kept under its maximum m lies below s, in exponents. Each of the
+// two may be far or not: a sum under a far maximum is 2^0 at m itself, any other at m c rounded up.
 __device__ __forceinline__ float between(float m, const Shift& s, const Base& b) {
-  return s.far ? (m - s.h) * b.c : ceilf(m * b.c) - s.hc;
+  const float hc = ceilf(m * b.c);
+  const bool far = !(fabsf(hc) < kFar);
+  if (!s.far) return far ? exponent(m, s.hc, b) : hc - s.hc;
+  return far ? (m - s.h) * b.c : __fmaf_rn(-s.h, b.c, hc) - s.h * b.lo;
 }
 
 // A maximum and the sum of the exponentials below its shift. m = -inf: nothing yet.

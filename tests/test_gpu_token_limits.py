@@ -1,0 +1,67 @@
+"""Values at the limits of what the post-training operators take."""
+import numpy as np
+import pytest
+
+import token_ref as ref
+
+pytestmark = pytest.mark.gpu
+# Of a logp whose exponents are near 2^20, token_ref's bound with one term more: an exponent's rounding
+# is that of its distance from the maximum (below 8 here) and of the last place of s log2 e in two
+# words, 2^-46 of 2^20. logp itself is below 16 there.
+LIMIT = ref.LOGP + 2.0 ** -24
+
+
+def _type(kind):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[kind]
+
+
+def _dev(a, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def _around(V, scale, sign, order, seed):
+    """A row of float32 logits whose exponents scale * log2(e) * x lie on both sides of 2^20 (or
+    -2^20), from which on the kernels take the difference to the maximum first: within 0.7 of it
+    below, 0.05 to 1 of it above. order: where those above lie."""
+    rng = np.random.default_rng(seed)
+    limit = 2.0 ** 20 / (scale * np.log2(np.e))
+    near, past = rng.uniform(0.05, 0.7, V) / scale, rng.uniform(0.05, 1.0, V) / scale
+    above = {"first": np.arange(V) < V // 2, "last": np.arange(V) >= V // 2, "one": np.arange(V) == V // 3,
+             "but one": np.arange(V) != V // 3, "mixed": rng.random(V) < 0.5}[order]
+    return (sign * (limit + np.where(above, past, -near))).astype(np.float32)
+
+
+@pytest.mark.parametrize("order", ["first", "last", "one", "but one", "mixed"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** 20, 2.0 ** -20, 1e5])
+@pytest.mark.parametrize("n,V", [(5, 2), (5, 40), (3, 129), (2, 5_003), (1, 70_001), (700, 37), (700, 1_021)])
+def test_rows_around_the_limit_of_the_exponents(n, V, scale, sign, order):
+    """In a thread, across lanes, warps and blocks."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss, token_logp, token_logp_backward
+    rng = np.random.default_rng([21, n, V])
+    rows = min(n, 7)
+    x = np.stack([_around(V, scale, sign, order, [i, V]) for i in range(rows)])[np.arange(n) % rows]
+    y = rng.integers(0, V, n)
+    t, tgt, f = _dev(x), _dev(y), torch.float32
+    x = x.astype(np.float64)
+    scale = float(np.float32(scale))
+    lp = ref.token_logp(x, y, scale)
+    logp, stats = token_logp(t, tgt, scale=scale, return_stats=True)
+    off = abs(logp.double().cpu().numpy() - lp)
+    assert (off <= LIMIT).all(), off.max()
+    g = np.ones(n)
+    d = token_logp_backward(t, tgt, stats, _dev(g, f), scale=scale).double().cpu().numpy()
+    bound = ref.gradient_bound(x, y, g, np.zeros(n), scale, "f32")
+    assert (abs(d - ref.gradient(x, y, g, scale)) <= bound).all()
+    h = TokenLoss(n, 1)
+    old = np.float32(lp + 0.05).astype(np.float64)
+    r = h.policy(t, tgt, _dev(old, f), _dev(g, f), scale=scale, out=torch.empty_like(t))
+    assert (abs(r.logp.double().cpu().numpy() - lp) <= LIMIT).all()
+    _, _, coef = ref.policy(lp, y, old, g, g / n, lp, 0.2, 0.2, 0.0)
+    bound = ref.gradient_bound(x, y, coef, ref.policy_bound(lp, old, g, lp, 0.0) / n, scale, "f32")
+    assert (abs(r.dlogits.double().cpu().numpy() - ref.gradient(x, y, coef, scale)) <= bound).all()
+    h.close()
