@@ -22,12 +22,13 @@ struct Group {
   __device__ static int tid() { return G == 32 ? (int)threadIdx.x % 32 : (int)threadIdx.x; }
   __device__ static int of_block() { return G == 32 ? (int)threadIdx.x / 32 : 0; }  // of the block's rows
   // Over the group; every thread returns the result.
+  template <typename T>
   __device__ static MaxSum merge(const MaxSum& a, const Base& b) {
     if constexpr (G == 32) {
-      return warp_merge(a, b);
+      return warp_merge<T>(a, b);
     } else {
       __shared__ MaxSum ws[32];
-      return block_merge(a, b, ws);
+      return block_merge<T>(a, b, ws);
     }
   }
 };
@@ -53,10 +54,10 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
   const T* x = R.x + row * R.ld;
   const float xy = target_logit(x, R.V, y);
   const double less = ref ? (double)ref[row] : 0.;
-  MaxSum a = Group<G>::merge(sweep(x, R.V, R.b, part, parts, Group<G>::tid(), G), R.b);
+  MaxSum a = Group<G>::template merge<T>(sweep(x, R.V, R.b, part, parts, Group<G>::tid(), G), R.b);
   if (G != 32 && parts > 1) {
     cluster_wait();  // every block has begun
-    a = cluster_merge(a, parts, R.b, cs);
+    a = cluster_merge<T>(a, parts, R.b, cs);
   }
   if (writes) {
     const RowStats r = finish(a, xy, R.b);

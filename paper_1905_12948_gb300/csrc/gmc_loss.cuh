@@ -68,33 +68,42 @@ __device__ __forceinline__ Shift shift_of(float m, const Base& b) {
 __device__ __forceinline__ float exponent(float x, float hc, const Base& b) {
   return __fmaf_rn(x, b.lo, __fmaf_rn(x, b.c, -hc));
 }
-// By how much the shift of a sum kept under its maximum m lies below s, in exponents. Each of the
-// two may be far or not: a sum under a far maximum is 2^0 at m itself, any other at m c rounded up.
+// By how much the shift of a sum kept under its maximum m lies below s, in exponents. Either may be
+// far or not: a sum under a far maximum is 2^0 at m itself, any other at m c rounded up. For logits
+// of 16 bits one rule does: two maxima on either side of 2^20 are 2^9 exponents apart, and
+// the lower one's sum is nothing.
+template <typename T>
 __device__ __forceinline__ float between(float m, const Shift& s, const Base& b) {
   const float hc = ceilf(m * b.c);
-  const bool far = !(fabsf(hc) < kFar);
-  if (!s.far) return far ? exponent(m, s.hc, b) : hc - s.hc;
-  return far ? (m - s.h) * b.c : __fmaf_rn(-s.h, b.c, hc) - s.h * b.lo;
+  if constexpr (sizeof(T) == 4) {
+    const bool far = !(fabsf(hc) < kFar);
+    if (s.far) return far ? (m - s.h) * b.c : __fmaf_rn(-s.h, b.c, hc) - s.h * b.lo;
+    return far ? exponent(m, s.hc, b) : hc - s.hc;
+  } else {
+    return s.far ? (m - s.h) * b.c : hc - s.hc;
+  }
 }
 
 // A maximum and the sum of the exponentials below its shift. m = -inf: nothing yet.
 struct alignas(8) MaxSum {  // one 8-byte message
   float m = -INFINITY, s = 0.f;
 };
+template <typename T>
 __device__ __forceinline__ MaxSum merge(const MaxSum& a, const MaxSum& o, const Base& b) {
   MaxSum r;
   r.m = fmaxf(a.m, o.m);
   const Shift h = shift_of(r.m, b);
-  r.s = a.s * exp2_fast(between(a.m, h, b)) + o.s * exp2_fast(between(o.m, h, b));
+  r.s = a.s * exp2_fast(between<T>(a.m, h, b)) + o.s * exp2_fast(between<T>(o.m, h, b));
   return r;
 }
 // One value into a, and U vectors. Sums are kept four to a thread, and no NaN hides in a
 // maximum's shadow: its exponential is NaN.
+template <typename T>
 __device__ __forceinline__ void add_one(MaxSum* a, float x, const Base& b) {
   const float m = fmaxf(a->m, x);
   const Shift h = shift_of(m, b);
   const float e = h.far ? exponent(x - h.h, 0.f, b) : exponent(x, h.hc, b);
-  a->s = a->s * exp2_fast(between(a->m, h, b)) + exp2_fast(e);
+  a->s = a->s * exp2_fast(between<T>(a->m, h, b)) + exp2_fast(e);
   a->m = m;
 }
 template <typename T, int U>
@@ -107,7 +116,7 @@ __device__ __forceinline__ void add(MaxSum* a, const uint4 (&v)[U], const Base& 
   const float m = fmaxf(a->m, Vec<T>::top_of(top));
   const Shift h = shift_of(m, b);
   const Pair c = pair_of(b.c, b.c), lo = pair_of(b.lo, b.lo), hc = pair_of(-h.hc, -h.hc);
-  Pair s0 = pair_of(a->s * exp2_fast(between(a->m, h, b)), 0.f), s1 = pair_of(0.f, 0.f);
+  Pair s0 = pair_of(a->s * exp2_fast(between<T>(a->m, h, b)), 0.f), s1 = pair_of(0.f, 0.f);
   if (!h.far) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -144,21 +153,23 @@ __device__ __forceinline__ void add(MaxSum* a, const uint4 (&v)[U], const Base& 
   a->m = m;
 }
 // Over a warp; every lane returns the result.
+template <typename T>
 __device__ __forceinline__ MaxSum warp_merge(MaxSum a, const Base& b) {
   MaxSum r;
   r.m = a.m;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
-  r.s = warp_sum(a.s * exp2_fast(between(a.m, shift_of(r.m, b), b)));
+  r.s = warp_sum(a.s * exp2_fast(between<T>(a.m, shift_of(r.m, b), b)));
   return r;
 }
 // Over the block; every thread returns the result. ws: 32 entries of shared memory.
+template <typename T>
 __device__ __forceinline__ MaxSum block_merge(MaxSum a, const Base& b, MaxSum* ws) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  a = warp_merge(a, b);
+  a = warp_merge<T>(a, b);
   if (lane == 0) ws[warp] = a;
   __syncthreads();
-  return warp_merge(lane < warps ? ws[lane] : MaxSum(), b);
+  return warp_merge<T>(lane < warps ? ws[lane] : MaxSum(), b);
 }
 // Counts that tell the last of several blocks: what a block (or a warp) wrote before it
 // counts is visible to the one that is told it is the last.
@@ -178,6 +189,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // Over the blocks of a cluster, in rank order: a is the block's, the same in all its
 // threads. The caller has passed the cluster's barrier once before, so that none
 // writes into a block that has not begun.
+template <typename T>
 __device__ __forceinline__ MaxSum cluster_merge(MaxSum a, int parts, const Base& b, MaxSum* ws) {
   if (parts == 1) return a;
   if (threadIdx.x < (unsigned)parts) {  // into slot `rank` of every block
@@ -189,7 +201,7 @@ __device__ __forceinline__ MaxSum cluster_merge(MaxSum a, int parts, const Base&
   cluster_arrive();
   cluster_wait();
   MaxSum r = ws[0];
-  for (int i = 1; i < parts; ++i) r = merge(r, ws[i], b);
+  for (int i = 1; i < parts; ++i) r = merge<T>(r, ws[i], b);
   return r;
 }
 
@@ -221,7 +233,7 @@ __device__ __forceinline__ MaxSum sweep(const T* x, int64_t V, const Base& b, in
     add<T>(&a, v, b);
   }
   if (part == 0 && tid < head + tail)
-    add_one(&a, Vec<T>::one(x[tid < head ? (int64_t)tid : V - tail + (tid - head)]), b);
+    add_one<T>(&a, Vec<T>::one(x[tid < head ? (int64_t)tid : V - tail + (tid - head)]), b);
   return a;
 }
 

@@ -145,6 +145,7 @@ __device__ __forceinline__ void add_some(MaxSum* a, const uint4* q, int left, co
   add<T>(a, v, b);
 }
 // A warp's merge of all stats threads' maxima and sums.
+template <typename T>
 __device__ __forceinline__ MaxSum block_of(const MaxSum* ws, int lane, const Base& b) {
   MaxSum t[kStatsWarps], r;
 #pragma unroll
@@ -156,7 +157,7 @@ __device__ __forceinline__ MaxSum block_of(const MaxSum* ws, int lane, const Bas
   for (int o = 16; o > 0; o >>= 1) r.m = fmaxf(r.m, __shfl_xor_sync(0xffffffffu, r.m, o));
   const Shift h = shift_of(r.m, b);
 #pragma unroll
-  for (int i = 0; i < kStatsWarps; ++i) r.s += t[i].s * exp2_fast(between(t[i].m, h, b));
+  for (int i = 0; i < kStatsWarps; ++i) r.s += t[i].s * exp2_fast(between<T>(t[i].m, h, b));
   r.s = warp_sum(r.s);
   return r;
 }
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       float loss = 0.f;
       alive = (!turn || warp_wait(&S.free[slot], (turn - 1) & 1, limit)) && warp_wait(&S.summed[slot], turn & 1, limit);
       if (alive && counts) {
-        MaxSum a = block_of(S.ws[slot], lane, R.b);
+        MaxSum a = block_of<T>(S.ws[slot], lane, R.b);
         if (parts > 1) {
           // Where dx is x, the block that holds x[y] writes its gradient there as soon as it has
           // heard from all. So the sums that it waits for are made of xy: a target that is NaN
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
             a.m = __uint_as_float((uint32_t)v);
             a.s = __uint_as_float((uint32_t)(v >> 32));
           }
-          a = warp_merge(a, R.b);
+          a = warp_merge<T>(a, R.b);
         }
         st = finish(a, xy, R.b);
         float slope = 0.f;
@@ -583,7 +584,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
           q[u] = k0 + 32 * u < nv ? v[k0 + 32 * u] : make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
         add<T>(&a, q, R.b);
       }
-      st = finish(warp_merge(a, R.b), xy, R.b);
+      st = finish(warp_merge<T>(a, R.b), xy, R.b);
       if (!st.empty) policy_terms(P, adv, old_logp, ref_logp, st.logp, &loss, &slope);
     }
     if (lane == 0) {
@@ -665,8 +666,8 @@ __global__ void __launch_bounds__(kLossThreads) k_policy(Rows<T> R, PolicyArgs P
     const bool counts = y >= 0 && w != 0.f;
     if (counts) {
       const float xy = target_logit(x, R.V, y);
-      MaxSum a = block_merge(sweep(x, R.V, R.b, part, parts, (int)threadIdx.x, kLossThreads), R.b, ws);
-      a = cluster_merge(a, parts, R.b, cs);
+      MaxSum a = block_merge<T>(sweep(x, R.V, R.b, part, parts, (int)threadIdx.x, kLossThreads), R.b, ws);
+      a = cluster_merge<T>(a, parts, R.b, cs);
       r = finish(a, xy, R.b);
       if (!r.empty)
         policy_terms(P, P.adv[row], P.old_logp[row], P.ref_logp ? P.ref_logp[row] : 0.f, r.logp, &loss, &slope);

@@ -65,3 +65,23 @@ def test_rows_around_the_limit_of_the_exponents(n, V, scale, sign, order):
     bound = ref.gradient_bound(x, y, coef, ref.policy_bound(lp, old, g, lp, 0.0) / n, scale, "f32")
     assert (abs(r.dlogits.double().cpu().numpy() - ref.gradient(x, y, coef, scale)) <= bound).all()
     h.close()
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("scale", [100.0, 2.0 ** 9])
+@pytest.mark.parametrize("n,V,kind", [(3, 130, "bf16"), (2, 5_003, "f16"), (1, 70_001, "bf16"), (700, 1_021, "f16")])
+def test_rows_around_the_limit_in_16_bits(n, V, kind, scale, sign):
+    """The type's values on either side of 2^20 exponents lie hundreds of exponents apart."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss, token_logp
+    limit = 2.0 ** 20 / (scale * np.log2(np.e))
+    ulp = 2.0 ** (np.floor(np.log2(limit)) - {"bf16": 7, "f16": 10}[kind])
+    rng = np.random.default_rng([23, n, V])
+    x = sign * ulp * (np.floor(limit / ulp) + rng.integers(-1, 3, (n, V)))
+    y = rng.integers(0, V, n)
+    t = _dev(x).to(_type(kind))
+    assert np.array_equal(t.double().cpu().numpy(), x)
+    lp = ref.token_logp(x, y, scale)
+    one = torch.ones(n, device="cuda")
+    for logp in (token_logp(t, _dev(y), scale=scale), TokenLoss(n).policy(t, _dev(y), -one, one, scale=scale).logp):
+        assert (abs(logp.double().cpu().numpy() - lp) <= LIMIT + 2 * ref.U * abs(lp)).all()
