@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
         g.at_y = k * -expm1f(st.logp);
         g.y = y;
         g.go = slope != 0.f && !st.empty;
-        total += (double)w * (double)loss;
+        if (!st.empty) total += (double)w * (double)loss;
       }
       if (!alive) {
         S.dead = 1;
@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
       if (!st.empty) policy_terms(P, adv, old_logp, ref_logp, st.logp, &loss, &slope);
     }
     if (lane == 0) {
-      total += (double)w * (double)loss;
+      if (counts && !st.empty) total += (double)w * (double)loss;  // (w may be inf or NaN where nothing counts)
       if (P.token_loss) P.token_loss[row] = loss;
       if (P.logp) P.logp[row] = st.logp;
     }
@@ -673,7 +673,7 @@ __global__ void __launch_bounds__(kLossThreads) k_policy(Rows<T> R, PolicyArgs P
         policy_terms(P, P.adv[row], P.old_logp[row], P.ref_logp ? P.ref_logp[row] : 0.f, r.logp, &loss, &slope);
     }
     if (part == 0 && threadIdx.x == 0) {
-      total += (double)w * (double)loss;
+      if (counts && !r.empty) total += (double)w * (double)loss;
       if (P.token_loss) P.token_loss[row] = loss;
       if (P.logp) P.logp[row] = r.logp;
     }

@@ -85,3 +85,25 @@ def test_rows_around_the_limit_in_16_bits(n, V, kind, scale, sign):
     one = torch.ones(n, device="cuda")
     for logp in (token_logp(t, _dev(y), scale=scale), TokenLoss(n).policy(t, _dev(y), -one, one, scale=scale).logp):
         assert (abs(logp.double().cpu().numpy() - lp) <= LIMIT + 2 * ref.U * abs(lp)).all()
+
+
+@pytest.mark.parametrize("n,V,kind", [(400, 300, "bf16"), (9, 300, "f32"), (6, 50_257, "bf16"), (3, 300_001, "f32")])
+def test_weights_that_are_not_finite_on_rows_that_add_nothing(n, V, kind):
+    """A warp a row, the ring by one block and by several, and rows swept twice."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.randn((n, V), generator=g, device="cuda").to(_type(kind))
+    y = torch.randint(0, V, (n,), generator=g, device="cuda")
+    old, adv, w = torch.full((n,), -8.0, device="cuda"), torch.ones(n, device="cuda"), torch.ones(n, device="cuda")
+    y[1] = -1
+    x[n - 1] = -float("inf")          # no distribution
+    h = TokenLoss(n)
+    want = h.policy(x, y, old, adv, weights=w)
+    assert torch.isfinite(want.loss)
+    for bad in (float("inf"), float("nan")):
+        w[1] = w[n - 1] = bad
+        r = h.policy(x, y, old, adv, weights=w)
+        assert torch.equal(r.loss, want.loss) and torch.equal(r.dlogits, want.dlogits), bad
+        assert torch.equal(r.token_loss, want.token_loss)
+    h.close()
