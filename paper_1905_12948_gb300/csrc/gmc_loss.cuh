@@ -368,6 +368,20 @@ struct PolicyArgs {
   int64_t hold_row;                       // test hook: no copy of this row is made; -1: none
 };
 
+// exp(d) - 1 - d, its slope expm1(d) given. Where d is small the difference cancels (at 1e-3 to 1e-4 of
+// itself): below 1/2 it is d^2 sum_n d^n / (n + 2)!, whose terms from n = 8 on are below 2^-28 of the sum.
+__device__ __forceinline__ float kl_term(float d, float slope) {
+  if (!(fabsf(d) < 0.5f)) return slope - d;
+  float s = 1.f / 362880.f;
+  s = __fmaf_rn(s, d, 1.f / 40320.f);
+  s = __fmaf_rn(s, d, 1.f / 5040.f);
+  s = __fmaf_rn(s, d, 1.f / 720.f);
+  s = __fmaf_rn(s, d, 1.f / 120.f);
+  s = __fmaf_rn(s, d, 1.f / 24.f);
+  s = __fmaf_rn(s, d, 1.f / 6.f);
+  s = __fmaf_rn(s, d, 0.5f);
+  return d * d * s;
+}
 // The token's loss and its slope in logp.
 __device__ __forceinline__ void policy_terms(const PolicyArgs& P, float adv, float old_logp, float ref_logp, float logp,
                                              float* loss, float* slope) {
@@ -378,9 +392,9 @@ __device__ __forceinline__ void policy_terms(const PolicyArgs& P, float adv, flo
   float l = plain <= clipped ? -plain : -clipped;
   float d = plain <= clipped ? -plain : 0.f;
   if (P.ref_logp) {
-    const float far = ref_logp - logp, ef = expf(far);
-    l += P.kl * (ef - far - 1.f);
-    d += P.kl * (1.f - ef);
+    const float off = ref_logp - logp, up = expm1f(off);
+    l += P.kl * kl_term(off, up);
+    d -= P.kl * up;
   }
   if (l != l) d = l;
   *loss = l;

@@ -107,3 +107,42 @@ def test_weights_that_are_not_finite_on_rows_that_add_nothing(n, V, kind):
         assert torch.equal(r.loss, want.loss) and torch.equal(r.dlogits, want.dlogits), bad
         assert torch.equal(r.token_loss, want.token_loss)
     h.close()
+
+
+@pytest.mark.parametrize("n", [60, 700])
+def test_kl_term_near_the_reference(n):
+    """Advantages of 0 leave the KL term alone: f(d) = exp(d) - d - 1 of d = ref - logp, and its
+    slope, as good as 32 bits hold them at any distance. d is the kernel's own: the difference of two
+    floats within a factor of two of each other (exact), or rounded once (u of d, which f'/f d, below
+    2 + |d|, multiplies). f's series or difference takes some ten roundings, none larger than u of f
+    (where it is a difference, from |d| = 1/2 on, of terms that are below 9 f): 40u of f cover them."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    rng = np.random.default_rng(22)
+    V, kl, f = 50, 0.25, torch.float32
+    x = rng.standard_normal((n, V)).astype(np.float32)
+    y = rng.integers(0, V, n)
+    x[np.arange(n), y] += np.where(np.arange(n) % 2, 12.0, 0.0).astype(np.float32)     # confident tokens too
+    t, tgt, zero = _dev(x), _dev(y), torch.zeros(n, device="cuda")
+    h = TokenLoss(n)
+    logp = h.policy(t, tgt, zero, zero).logp.cpu().numpy()
+    d = rng.choice([-1, 1], n) * 10.0 ** rng.uniform(-7.5, 1, n)
+    d[:6] = 0.0, 0.5, -0.5, 0.4999, -0.4999, 1e-7
+    rf = (logp.astype(np.float64) + d).astype(np.float32)
+    r = h.policy(t, tgt, _dev(logp), zero, ref_logp=_dev(rf), kl=kl, weights=torch.ones(n, device="cuda"))
+    assert np.array_equal(r.logp.cpu().numpy(), logp)
+    d = rf.astype(np.float64) - logp.astype(np.float64)
+    # to 64 bits: the series, or expm1 where its difference from d loses no more than 4 bits
+    k = np.where(abs(d) < 0.5, d * d / 2 * sum(2.0 * d ** i / _factorial(i + 2) for i in range(20)), np.expm1(d) - d)
+    got = r.token_loss.double().cpu().numpy()
+    assert (got >= 0).all()
+    assert (abs(got - kl * k) <= kl * k * (40 + abs(d)) * ref.U + 1e-44).all()
+    coef = -kl * np.expm1(d)
+    bound = ref.gradient_bound(x, y, coef, abs(kl * np.exp(d) * d) * 2 * ref.U + 8 * ref.U * abs(coef), 1.0, "f32")
+    assert (abs(r.dlogits.double().cpu().numpy() - ref.gradient(x.astype(np.float64), y, coef, 1.0)) <= bound).all()
+    h.close()
+
+
+def _factorial(n):
+    import math
+    return math.factorial(n)
