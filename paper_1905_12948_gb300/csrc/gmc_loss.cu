@@ -114,7 +114,8 @@ __device__ __forceinline__ float softplus(float x) { return fmaxf(x, 0.f) + log1
 __device__ __forceinline__ void finish_pair(const PairArgs& P, int64_t p, float w, double chosen, double other) {
   const float margin = (float)((double)P.beta * (chosen - other));
   const float up = softplus(-margin), down = softplus(margin);  // -log sigmoid(margin), -log sigmoid(-margin)
-  const float loss = (1.f - P.smoothing) * up + P.smoothing * down;
+  // a term with no weight is left out: the margin of a sequence with a masked token is infinite
+  const float loss = (P.smoothing < 1.f ? (1.f - P.smoothing) * up : 0.f) + (P.smoothing > 0.f ? P.smoothing * down : 0.f);
   const float sig_up = 1.f / (1.f + expf(-margin)), sig_down = 1.f / (1.f + expf(margin));
   P.slope[p] = w == 0.f ? 0.f : w * P.beta * (P.smoothing * sig_up - (1.f - P.smoothing) * sig_down);
   P.wloss[p] = w == 0.f ? 0. : (double)w * (double)loss;

@@ -146,3 +146,25 @@ def test_kl_term_near_the_reference(n):
 def _factorial(n):
     import math
     return math.factorial(n)
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+def test_pairs_whose_margin_is_infinite(smoothing):
+    """A token masked by -inf in one of a pair's sequences: the margin is inf or -inf. What is not
+    asked for (a weight of 0 on one of the two terms) does not make the loss NaN."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss
+    x = torch.zeros((4, 8), device="cuda")
+    y = torch.zeros(4, dtype=torch.int64, device="cuda")
+    x[1, 0] = -float("inf")          # the first pair's other answer: margin inf
+    x[2, 0] = -float("inf")          # the second pair's preferred one: margin -inf
+    h = TokenLoss(4, 2)
+    r = h.preference(x, y, torch.arange(5, device="cuda"), beta=0.5, smoothing=smoothing)
+    up, down = (0.0 if smoothing == 0 else np.inf), (0.0 if smoothing == 1 else np.inf)
+    assert np.array_equal(r.pair_loss.cpu().numpy(), np.array([up, down]))
+    assert np.array_equal(r.seq_ratio.cpu().numpy()[[1, 2]], [-np.inf, -np.inf])
+    assert float(r.loss) == np.inf
+    assert torch.isfinite(r.dlogits).all()
+    one = h.preference(x[:2], y[:2], torch.arange(3, device="cuda"), beta=0.5, smoothing=smoothing)
+    assert float(one.loss) == up
+    h.close()
