@@ -254,13 +254,13 @@ __device__ __forceinline__ float logp_of(float xy, const Shift& h, float ls, con
 __device__ __forceinline__ RowStats finish(const MaxSum& a, float xy, const Base& b) {
   RowStats r;
   r.h = shift_of(a.m, b);
-  r.empty = a.m == -INFINITY && a.s == 0.f;
+  r.empty = a.m == -INFINITY && a.s == 0.f && xy == xy;  // a target outside the vocabulary marks this row too
   r.ls = r.empty ? 0.f : logf(a.s);
   r.low = 0.f;
   if (r.h.far || r.empty) {
     r.logp = logp_of(xy, r.h, r.ls, b);
   } else {
-    const uint32_t bits = __float_as_uint(a.s);  // at least 1/2: the maximum's own term
+    const uint32_t bits = __float_as_uint(a.s);  // at least 1/2, the maximum's own term, or NaN (0: xy is NaN)
     const float power = (float)((int)(bits >> 23) - 127);
     const float rest = logf(__uint_as_float((bits & 0x007fffffu) | 0x3f800000u));
     const double full =

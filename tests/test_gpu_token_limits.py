@@ -109,6 +109,26 @@ def test_weights_that_are_not_finite_on_rows_that_add_nothing(n, V, kind):
     h.close()
 
 
+@pytest.mark.parametrize("n,V", [(400, 300), (4, 300), (4, 50_257), (3, 300_001)])
+def test_target_outside_the_vocabulary_in_a_row_of_nothing(n, V):
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss, token_logp, token_logp_backward
+    x = torch.zeros((n, V), device="cuda")
+    x[1] = -float("inf")
+    y = torch.zeros(n, dtype=torch.int64, device="cuda")
+    y[1] = V
+    one = torch.ones(n, device="cuda")
+    logp, stats = token_logp(x, y, return_stats=True)
+    h = TokenLoss(n, 1)
+    r = h.policy(x, y, logp.nan_to_num(), one)
+    q = h.preference(x, y, torch.tensor([0, 2, 3], device="cuda"), beta=0.1)
+    assert torch.isnan(logp[1]) and torch.isnan(token_logp_backward(x, y, stats, one)[1]).all()
+    assert torch.isnan(r.token_loss[1]) and torch.isnan(r.loss) and torch.isnan(r.dlogits[1]).all()
+    assert torch.isfinite(r.token_loss[[0, 2]]).all() and torch.isfinite(r.dlogits[[0, 2]]).all()
+    assert torch.isnan(q.seq_ratio[0]) and torch.isfinite(q.seq_ratio[1]) and torch.isnan(q.loss)
+    h.close()
+
+
 @pytest.mark.parametrize("n", [60, 700])
 def test_kl_term_near_the_reference(n):
     """Advantages of 0 leave the KL term alone: f(d) = exp(d) - d - 1 of d = ref - logp, and its
