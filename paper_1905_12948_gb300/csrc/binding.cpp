@@ -146,6 +146,12 @@ Tensor gradient(PyObject* o, const Tensor& logits, const Rows& r, int64_t* ld) {
   return t;
 }
 
+// What torch's own writes in place do: a backward pass that saved the tensor then refuses it.
+// (Inference tensors have no version, and are never saved.)
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // `sizes` elements of a 1-D tensor from `at` on, as a tensor of its own.
 Tensor part(const Tensor& whole, at::IntArrayRef sizes, int64_t at) {
   Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
@@ -220,6 +226,7 @@ PyObject* token_logp_backward(Args a, Py_ssize_t na) {
   const Tensor out = gradient(a[5], x, r, &dld);
   check(g_abi.token_logp_backward(x.data_ptr(), k, r.n, r.v, r.ld, scale, y, stats, g, out.data_ptr(), dld, stream_of(x)),
         "gmc_token_logp_backward");
+  if (a[5] != Py_None) written(out);
   return wrap(out);
 }
 
@@ -256,6 +263,7 @@ PyObject* policy(Args a, Py_ssize_t na) {
                           loss.data_ptr<float>(), each.data_ptr<float>(), logp.data_ptr<float>(),
                           grad ? out.data_ptr() : nullptr, dld, stream_of(x)),
         "gmc_policy_loss");
+  if (grad && a[13] != Py_None) written(out);
   return tuple_of({wrap(loss), wrap(each), wrap(logp), grad ? wrap(out) : none()});
 }
 
@@ -289,6 +297,7 @@ PyObject* preference(Args a, Py_ssize_t na) {
                               loss.data_ptr<float>(), each.data_ptr<float>(), ratio.data_ptr<float>(),
                               logp.data_ptr<float>(), grad ? out.data_ptr() : nullptr, dld, stream_of(x)),
         "gmc_preference_loss");
+  if (grad && a[11] != Py_None) written(out);
   return tuple_of({wrap(loss), wrap(each), wrap(ratio), wrap(logp), grad ? wrap(out) : none()});
 }
 
@@ -328,6 +337,7 @@ PyObject* dropout(Args a, Py_ssize_t na) {
   const int64_t ldo = worker_stride(out, x, K, n, "out");
   check(g_abi.dropout(x.data_ptr(), ldx, res, ldr, out.data_ptr(), ldo, k, worker, K, n, p, seed, t, site, stream_of(x)),
         "gmc_dropout");
+  if (a[7] != Py_None) written(out);
   return wrap(out);
 }
 

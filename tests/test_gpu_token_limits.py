@@ -188,3 +188,34 @@ def test_pairs_whose_margin_is_infinite(smoothing):
     one = h.preference(x[:2], y[:2], torch.arange(3, device="cuda"), beta=0.5, smoothing=smoothing)
     assert float(one.loss) == up
     h.close()
+
+
+@pytest.mark.parametrize("call", ["backward", "policy", "preference", "dropout"])
+def test_autograd_is_told_of_writes_in_place(call):
+    """Logits that a layer's backward pass has saved, and that an operator overwrote: backward refuses."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss, dropout, token_logp, token_logp_backward
+    z = torch.randn((4, 32), device="cuda", requires_grad=True)
+    logits = torch.tanh(z)            # its backward pass takes its output
+    y = torch.arange(4, device="cuda")
+    one, h = torch.ones(4, device="cuda"), TokenLoss(4, 1)
+    before = logits._version
+    if call == "backward":
+        _, stats = token_logp(logits, y, return_stats=True)
+        token_logp_backward(logits, y, stats, one, out=torch.empty_like(logits))
+        assert logits._version == before
+        d = token_logp_backward(logits, y, stats, one, out=logits)
+    elif call == "policy":
+        d = h.policy(logits, y, -one, one, out=logits).dlogits
+    elif call == "preference":
+        d = h.preference(logits, y, torch.tensor([0, 2, 4], device="cuda"), beta=0.1, out=logits).dlogits
+    else:
+        d = dropout(logits, 0.5, seed=1, out=logits)
+    assert d is logits and logits._version > before
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        logits.backward(torch.ones_like(d))
+    with torch.inference_mode():      # tensors without a version
+        v = torch.randn((4, 32), device="cuda")
+        h.policy(v, y, -one, one, out=v)
+    h.policy(v, y, -one, one, out=v)
+    h.close()
