@@ -152,6 +152,8 @@ extern "C" int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_
   if (!x_dev || !out_dev) return GMC_EINVAL;
   for (const void* q : {x_dev, residual_dev, (const void*)out_dev})
     if (reinterpret_cast<uintptr_t>(q) % size) return GMC_EINVAL;
+  // in place: the same rows
+  if (K > 1 && ((out_dev == x_dev && ldo != ldx) || (out_dev == residual_dev && ldo != ldr))) return GMC_EINVAL;
   const uint32_t q = (uint32_t)std::lrint(p * 65536.0);
   const float gain = q < 65536u ? 65536.f / (float)(65536u - q) : 0.f;
   const cudaError_t err = by_type(dtype, [&](auto z) {
