@@ -99,6 +99,8 @@ class TokenLoss:
             _load()
         self.lib = load()
         self.device = torch.device(device if device is not None else "cuda")
+        if self.device.type != "cuda":
+            raise ValueError("device must be a CUDA device")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index

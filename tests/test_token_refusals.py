@@ -25,3 +25,10 @@ def test_dropout_in_place_with_another_stride(lib):
     # (K = 0: nothing to do)
     for right in ((p, 8, None, 0, p, 8, 0), (p, 8, p + 1024, 9, p + 1024, 8, 0)):
         assert call(*right) == 0
+
+
+def test_token_loss_wants_a_cuda_device(lib):
+    pytest.importorskip("torch")
+    from paper_1905_12948_gb300 import TokenLoss
+    with pytest.raises(ValueError, match="CUDA device"):
+        TokenLoss(4, device="cpu")
