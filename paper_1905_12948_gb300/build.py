@@ -5,7 +5,8 @@
 Each CUDA translation unit is compiled in parallel into ``_build/`` and linked
 into ``paper_1905_12948_gb300/libgmc.so`` (static CUDA runtime); beside it
 ``_tokens.so``, the Python module of the operators on torch tensors, is compiled
-against the torch that is installed. Floating-point
+against the torch that is installed (where there is none, or one without CUDA, the
+library alone is built). Floating-point
 flags keep one IEEE rounding per operation: no FMA contraction (-fmad=false on
 the device, -ffp-contract=off on the host), no flush-to-zero, IEEE division.
 """
@@ -55,10 +56,16 @@ def _stale(target, deps):
 
 
 def _tokens_command(cc: str, out: str):
-    """The compiler's command for the Python module, and a line that tells what it was built for."""
+    """The compiler's command for the Python module, and a line that tells what it was built for;
+    None without a torch to build against."""
     import sysconfig
 
-    import torch
+    try:
+        import torch
+    except ImportError:
+        return None
+    if torch.version.cuda is None:
+        return None
     home = os.path.dirname(torch.__file__)
     cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(cc))), "include")
     abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
@@ -83,10 +90,10 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         if force or _stale(o, [s, *headers, __file__]):
             jobs.append([cc, *FLAGS, *extra_flags, "-c", s, "-o", o])
 
-    tokens, made_for = _tokens_command(cc, TOKENS + f".{os.getpid()}.tmp")
+    tokens, made_for = _tokens_command(cc, TOKENS + f".{os.getpid()}.tmp") or (None, "")
     stamp = os.path.join(BUILD, "tokens.txt")
     known = open(stamp).read() if os.path.exists(stamp) else ""
-    if force or known != made_for or _stale(TOKENS, [os.path.join(CSRC, "binding.cpp"), *headers, __file__]):
+    if tokens and (force or known != made_for or _stale(TOKENS, [os.path.join(CSRC, "binding.cpp"), *headers, __file__])):
         jobs.append(tokens)
 
     def run(cmd):
