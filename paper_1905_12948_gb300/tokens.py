@@ -45,13 +45,17 @@ def _load():
     return module
 
 
-def _on(stream, t, name: str):
-    """The context of a call on another stream than the current one: the outputs belong to it too."""
+def _on(stream, t, name: str, *others):
+    """The context of a call on another stream than the current one: the outputs belong to it, and the
+    memory of t and the others is not handed out again before the call is done."""
     torch = _import_torch()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if stream.device_index != t.device.index:
         raise TypeError(f"stream must be one of {t.device}")
+    for tensor in (t, *others):
+        if isinstance(tensor, torch.Tensor) and tensor.is_cuda:
+            tensor.record_stream(stream)
     return torch.cuda.stream(stream)
 
 
@@ -60,7 +64,7 @@ def token_logp(logits, targets, *, scale: float = 1.0, return_stats: bool = Fals
     (gmc_token_logp). With ``return_stats`` also the (n, 2) float32 that
     ``token_logp_backward`` takes."""
     if stream is not None:
-        with _on(stream, logits, "logits"):
+        with _on(stream, logits, "logits", targets):
             return token_logp(logits, targets, scale=scale, return_stats=return_stats)
     return (_ops or _load()).token_logp(logits, targets, scale, return_stats)
 
@@ -69,7 +73,7 @@ def token_logp_backward(logits, targets, stats, dlogp, *, scale: float = 1.0, ou
     """Gradient of sum(dlogp * logp) in the logits (gmc_token_logp_backward), of the
     logits' dtype; ``out`` may be the logits themselves."""
     if stream is not None:
-        with _on(stream, logits, "logits"):
+        with _on(stream, logits, "logits", targets, stats, dlogp, out):
             return token_logp_backward(logits, targets, stats, dlogp, scale=scale, out=out)
     return (_ops or _load()).token_logp_backward(logits, targets, stats, dlogp, scale, out)
 
@@ -127,7 +131,7 @@ class TokenLoss:
         """Clipped policy loss with a KL term, and its gradient in the logits
         (gmc_policy_loss). ``out`` may be the logits themselves."""
         if stream is not None:
-            with _on(stream, logits, "logits"):
+            with _on(stream, logits, "logits", targets, old_logp, advantages, weights, ref_logp, out):
                 return self.policy(logits, targets, old_logp, advantages, weights=weights, ref_logp=ref_logp,
                                    clip_low=clip_low, clip_high=clip_high, kl=kl, scale=scale, grad=grad, out=out)
         return PolicyLoss(*_ops.policy(self._h, self._index, logits, targets, old_logp, advantages, weights, ref_logp,
@@ -140,7 +144,7 @@ class TokenLoss:
         device, the preferred sequence of a pair first. ``out`` may be the logits
         themselves."""
         if stream is not None:
-            with _on(stream, logits, "logits"):
+            with _on(stream, logits, "logits", targets, offsets, ref_logp, weights, out):
                 return self.preference(logits, targets, offsets, beta=beta, smoothing=smoothing, ref_logp=ref_logp,
                                        weights=weights, scale=scale, grad=grad, out=out)
         return PreferenceLoss(*_ops.preference(self._h, self._index, logits, targets, offsets, beta, smoothing,
@@ -155,7 +159,7 @@ def dropout(x, p: float, *, seed: int, t: int = 0, worker: int = 0, site: int = 
     multiple of 2**-16 and the kept elements are divided by the share kept. ``out`` may
     be x or the residual."""
     if stream is not None:
-        with _on(stream, x, "x"):
+        with _on(stream, x, "x", residual, out):
             return dropout(x, p, seed=seed, t=t, worker=worker, site=site, residual=residual, out=out)
     return (_ops or _load()).dropout(x, p, seed, t, worker, site, residual, out)
 
