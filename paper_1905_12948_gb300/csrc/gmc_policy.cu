@@ -106,6 +106,10 @@ __device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity)
       : "memory");
   return ok != 0;
 }
+// What a block that gave up leaves to copies and messages under way before its shared memory may be
+// another's: they land within microseconds.
+constexpr uint64_t kLandNs = 1000000;
+__device__ __forceinline__ uint64_t landing(uint64_t limit_ns) { return limit_ns > kLandNs ? limit_ns : kLandNs; }
 // A warp's waits: bounded, with one answer for all its lanes.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, uint64_t limit_ns) {
   return __all_sync(0xffffffffu, wait_bounded(bar, parity, limit_ns));
@@ -487,13 +491,17 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
     // no copy is under way when the block ends, whatever became of its readers
     for (int i = 0; i < chunks; ++i) {
       const uint32_t uses = i < at.i ? at.turn + 1 : at.turn;
-      if (uses) wait_bounded(&S.full[i], (uses - 1) & 1, limit);
+      if (uses) wait_bounded(&S.full[i], (uses - 1) & 1, landing(limit));
     }
   }
   if (parts > 1) {  // no block ends while another may still send to it
     __syncthreads();
     cluster_arrive();
     cluster_wait();
+    if (S.dead) {  // all is sent, but nobody waits for it here
+      const uint64_t t0 = global_ns();
+      while (global_ns() - t0 < kLandNs) __nanosleep(1000);
+    }
   }
 }
 
@@ -633,7 +641,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, 1)
     now = next;
   }
   // no copy is under way when the block ends
-  if (loaded) warp_wait(&full[warp], (loaded - 1) & 1, P.wait_ns);
+  if (loaded) warp_wait(&full[warp], (loaded - 1) & 1, landing(P.wait_ns));
   if (lane == 0) totals[warp] = total;
   __syncthreads();
   if (warp == 0) {
