@@ -221,7 +221,7 @@ struct gmc_loss_ctx {
   void* mem = nullptr;
   float2* stats = nullptr;   // max_rows
   double* wloss = nullptr;   // max_pairs
-  double* partial = nullptr; // kMostClusters
+  double* partial = nullptr; // kMostBlocks
   uint32_t* ticket = nullptr;
   float* logp = nullptr;     // max_rows
   double* ratio = nullptr;   // max_rows
@@ -356,7 +356,7 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
   h->max_rows = max_rows;
   h->max_pairs = max_pairs;
   const size_t bytes =
-      8 * (size_t)(kMostClusters + 1 + max_pairs + 2 * max_rows) + 4 * (size_t)(max_rows + max_pairs);
+      8 * (size_t)(kMostBlocks + 1 + max_pairs + 2 * max_rows) + 4 * (size_t)(max_rows + max_pairs);
   cudaError_t err = cudaGetDevice(&h->device);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&h->resident.sms, cudaDevAttrMultiProcessorCount, h->device);
   if (err == cudaSuccess) err = lib_malloc(&h->mem, bytes);
@@ -369,8 +369,8 @@ int gmc_loss_create(gmc_loss_t* out, int64_t max_rows, int64_t max_pairs) {
     return err == cudaErrorMemoryAllocation ? GMC_ENOMEM : GMC_ECUDA;
   }
   h->partial = static_cast<double*>(h->mem);
-  h->ticket = reinterpret_cast<uint32_t*>(h->partial + kMostClusters);
-  h->wloss = h->partial + kMostClusters + 1;
+  h->ticket = reinterpret_cast<uint32_t*>(h->partial + kMostBlocks);
+  h->wloss = h->partial + kMostBlocks + 1;
   h->stats = reinterpret_cast<float2*>(h->wloss + max_pairs);
   h->ratio = reinterpret_cast<double*>(h->stats + max_rows);
   h->logp = reinterpret_cast<float*>(h->ratio + max_rows);

@@ -362,8 +362,8 @@ struct PolicyArgs {
   float clip_low, clip_high, kl, weight;  // weight: of every row, where weights is NULL
   float *token_loss, *logp;               // either may be NULL
   float* loss;
-  double* partial;                        // the clusters' sums of weighted losses
-  uint32_t* ticket;                       // counts the clusters that are done; 0 between calls
+  double* partial;                        // the blocks' sums of weighted losses
+  uint32_t* ticket;                       // counts the blocks that are done; 0 between calls
   uint64_t wait_ns;                       // bound of the waits on mbarriers
   int64_t hold_row;                       // test hook: no copy of this row is made; -1: none
 };
@@ -458,8 +458,8 @@ struct Residency {
   cudaError_t clusters(const void* f, const LaunchConfig& l, int parts, int64_t* out);
 };
 
-// The policy loss over n > 0 rows (gmc_policy.cu). A.partial has kMostClusters slots.
-constexpr int kMostClusters = 8192;
+// The policy loss over n > 0 rows (gmc_policy.cu). A.partial has kMostBlocks slots.
+constexpr int kMostBlocks = 8192;
 template <typename T>
 cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dld, Residency* device, cudaStream_t s);
 }  // namespace gmc

@@ -41,19 +41,19 @@ static_assert(kChunkVecs % (kStatsWarps * 32 * kStatsBatch) == 0, "whole batches
 static_assert(kChunkVecs % (kGradWarps * 32 * kGradBatch) == 0, "whole batches");
 static_assert(kRowSlots % kFinishers == 0, "a slot's rows have one finisher");
 
-// The weighted losses' sum in cluster order, by the last of `clusters` to be done (lane
-// 0 of a warp of each calls with its sum; the lanes of the last warp add).
-__device__ __forceinline__ void reduce_loss(const PolicyArgs& P, double mine, uint32_t cluster, uint32_t clusters) {
+// The weighted losses' sum in block order, by the last of `blocks` to be done (lane 0 of a
+// warp of each calls with its sum, NaN where a wait gave up; the lanes of the last warp add).
+__device__ __forceinline__ void reduce_loss(const PolicyArgs& P, double mine, uint32_t block, uint32_t blocks) {
   const int lane = threadIdx.x & 31;
   uint32_t last = 0;
   if (lane == 0) {
-    P.partial[cluster] = mine;
-    last = count_inc(P.ticket, clusters - 1) == clusters - 1;
+    P.partial[block] = mine;
+    last = count_inc(P.ticket, blocks - 1) == blocks - 1;
   }
   if (!__shfl_sync(0xffffffffu, last, 0)) return;
   __syncwarp();  // what lane 0's count acquired is there for the other lanes too: a shuffle orders no memory
   double s = 0.;
-  for (uint32_t i = lane; i < clusters; i += 32) s += __ldcg(P.partial + i);
+  for (uint32_t i = lane; i < blocks; i += 32) s += __ldcg(P.partial + i);
   s = warp_sum(s);
   if (lane == 0) *P.loss = (float)s;
 }
@@ -278,8 +278,16 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       const bool now = next.count();
       next = facts_at(row + clusters);
       const int slot = r % kRowSlots;
-      // the result comes after the sums, and these after the row's chunks
-      if (!warp_wait(&S.ready[slot], (r / kRowSlots) & 1, limit)) {
+      // The result comes after the sums, and these after the row's chunks. It comes, or a wait that
+      // it depends on gives up, here or in the finisher, and S.dead says so: a block whose gradient is
+      // not complete is one whose finishers know of it. (A finisher waits three times at most for a row.)
+      bool ok = warp_wait(&S.ready[slot], (r / kRowSlots) & 1, limit);
+      for (const uint64_t t0 = global_ns(); !ok;) {
+        const bool over = *(volatile int*)&S.dead || global_ns() - t0 > 4 * kWaitLimitNs;
+        if (__any_sync(0xffffffffu, over)) break;
+        ok = warp_wait(&S.ready[slot], (r / kRowSlots) & 1, limit);
+      }
+      if (!ok) {
         S.dead = 1;
         break;
       }
@@ -434,15 +442,17 @@ __global__ void __launch_bounds__(kRowsThreads, 1)
       }
     }
     // The loss, before the last gradients are out. A wait that gave up anywhere in the block
-    // ends, or has ended, a finisher's too.
+    // ends, or has ended, a finisher's too; and every block counts, since only its own finishers
+    // may know of it.
     if (lane == 0) S.total[me] = total;
     __syncwarp();
     asm volatile("bar.sync 1, %0;" ::"n"(kFinishers * 32) : "memory");
-    if (me == 0 && rank == 0) {
+    if (me == 0) {
       total = 0.;
       for (int i = 0; i < kFinishers; ++i) total += S.total[i];
+      if (rank > 0) total = 0.;  // its cluster's first block has them
       if (*(volatile int*)&S.dead) total = (double)__uint_as_float(kNan);
-      reduce_loss(P, total, (uint32_t)cluster, (uint32_t)clusters);
+      reduce_loss(P, total, blockIdx.x, gridDim.x);
     }
   } else {
     RingAt at;
@@ -729,7 +739,7 @@ cudaError_t launch_rows(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t dl
   const cudaError_t err = device->clusters((const void*)k_policy_rows<T>, l, parts, &clusters);
   if (err != cudaSuccess) return err;
   if (clusters > R.n) clusters = R.n;
-  if (clusters > kMostClusters) clusters = kMostClusters;
+  if (clusters > kMostBlocks / parts) clusters = kMostBlocks / parts;
   l.cfg.gridDim.x = (unsigned)(clusters * parts);
   return cudaLaunchKernelEx(&l.cfg, k_policy_rows<T>, R, A, dx, dld, parts, per, chunks);
 }

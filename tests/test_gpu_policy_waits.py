@@ -38,3 +38,20 @@ def test_the_next_call_is_right(n, V, kind):
         for got, right in zip(call(), want):
             assert torch.equal(got, right), limit
     h.close()
+
+
+@pytest.mark.parametrize("n,V,kind", SHAPES)
+def test_a_loss_that_is_a_number_has_its_gradient(n, V, kind):
+    """Whichever waits give up (few: the hardware holds a wait for microseconds before it is asked again), in
+    whichever block of a cluster: the loss is NaN, or every output is what it is without a limit."""
+    import torch
+    h, call, row = _call(n, V, kind)
+    want = [t.clone() for t in call()]
+    for limit in [int(10 * 1.3 ** i) for i in range(44)] * 3:      # 10 ns to 0.8 ms
+        assert h.lib.gmc_test_withhold_row(h.h, row, limit) == 0
+        got = call()
+        if torch.isnan(got.loss):
+            continue
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), limit
+    h.close()
