@@ -157,3 +157,23 @@ def test_marked_targets_and_nan_targets_of_a_cluster(y):
     for i in (0, 3):
         assert torch.equal(r.dlogits[i], want.dlogits[i]) and torch.equal(r.token_loss[i], want.token_loss[i])
     h.close()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("n,V,kind,refuse", [(400, 50_257, "bf16", True),
+                                             (130, 300_001, "f32", False), (130, 540_003, "bf16", False)])
+def test_many_rows_swept_twice(n, V, kind, refuse, in_place):
+    """Rows over 1 MB by clusters of 8, and shorter ones where a launch of clusters is refused: more rows than
+    two blocks an SM take at once."""
+    import torch
+    from paper_1905_12948_gb300 import TokenLoss, gmc
+    x, y, old, adv, args = _inputs(n, V, kind, 8, 0.2)
+    h = TokenLoss(n)
+    t = x.clone()
+    try:
+        assert gmc.load().gmc_test_refuse_cooperative(int(refuse)) == 0
+        r = h.policy(t, y, old, adv, out=t if in_place else None, **args)
+    finally:
+        gmc.load().gmc_test_refuse_cooperative(0)
+    _check(r, x, y, old, adv, args, kind)
+    h.close()
