@@ -166,13 +166,6 @@ struct Vec<__half> {
   __device__ static __half round(float v) { return __float2half_rn(v); }
 };
 
-// The elements of a row that lie before its first 16-byte boundary.
-template <typename T>
-__device__ __forceinline__ int head_of(const T* p, int64_t V) {
-  const int h = (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / (int)sizeof(T);
-  return V < h ? (int)V : h;
-}
-
 // 32 bytes of a row: the widest load and store there is. N elements.
 template <typename T>
 struct Wide {
