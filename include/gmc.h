@@ -439,7 +439,8 @@ int gmc_topk_noalloc(const float* x_dev, int64_t n, int64_t k, uint32_t* idx_dev
  * targets_dev holds n int64. A row with a negative target is not scored: it is not
  * read, its logp is 0, and it adds nothing to a loss or a gradient (its gradient
  * row is written as zeros). A target >= vocab marks its row: logp, loss and the
- * row's gradient are NaN. Logits may be -inf (p_v = 0); a row of -inf alone has
+ * row's gradient are NaN, the gradient also where its coefficient is 0 (a pair's weight,
+ * dlogp). Logits may be -inf (p_v = 0); any other row of -inf alone has
  * no distribution: its logp is -inf, and it adds nothing to a loss or a gradient.
  * +inf and NaN among the logits of a row that counts make its outputs NaN.
  * Sums and exponentials are formed in 32 bits whatever the type, and a gradient
@@ -463,7 +464,7 @@ int gmc_token_logp(const void* logits_dev, int32_t dtype, int64_t n, int64_t voc
 
 /* gmc_token_logp_backward -- the gradient of sum_r dlogp[r]*logp[r] in the logits,
  * from the logits, scale, targets and stats of a gmc_token_logp call. A row with
- * dlogp = 0 is written as zeros and not read. */
+ * dlogp = 0 is written as zeros and not read (but for one that its target marks). */
 int gmc_token_logp_backward(const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, float scale,
                             const int64_t* targets_dev, const float* stats_dev, const float* dlogp_dev,
                             void* dlogits_dev, int64_t dld, void* stream);
@@ -487,7 +488,8 @@ void gmc_loss_destroy(gmc_loss_t h);
  * count as unclipped) and 0 elsewhere, plus kl*(1 - exp(ref_logp - logp)).
  * old_logp_dev, advantages_dev: n floats; ref_logp_dev: n floats, read only when
  * kl > 0 (else it may be NULL); weights_dev: n floats, or NULL for 1/n each. A row with
- * weight 0 is not scored, as one with a negative target. loss_dev receives one
+ * weight 0 is not scored, as one with a negative target (a weight of inf or NaN on a row that
+ * adds nothing adds nothing). loss_dev receives one
  * float; token_loss_dev (l_r, 0 for rows not scored), logp_dev and dlogits_dev may
  * be NULL. 0 <= clip_low <= 1, clip_high >= 0, kl >= 0, all finite. The blocks that share a
  * row wait for one another (they run together, as one cluster); should such a wait give up
@@ -511,7 +513,8 @@ int gmc_test_withhold_row(gmc_loss_t h, int64_t row, uint64_t wait_limit_ns);
  * be empty); pair p prefers sequence 2p over 2p + 1:
  *   S_s = sum of logp - ref_logp over the sequence's rows with a target >= 0,
  *   margin = beta*(S_{2p} - S_{2p+1}),
- *   l = -(1 - smoothing)*log sigmoid(margin) - smoothing*log sigmoid(-margin),
+ *   l = -(1 - smoothing)*log sigmoid(margin) - smoothing*log sigmoid(-margin)
+ *       (a term whose factor is 0 is 0, also where the margin is infinite),
  *   loss = sum_p weights[p]*l_p.
  * ref_logp_dev: n floats, or NULL for zeros; weights_dev: `pairs` floats, or NULL
  * for 1/pairs each (a pair with weight 0 has zero gradients; its l is still given).
@@ -528,7 +531,8 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
 /* gmc_dropout -- out = residual + x*65536/(65536 - q) where kept, residual + 0
  * elsewhere, for K workers' rows of n elements (row strides ldx, ldr, ldo elements,
  * ignored when K = 1), q = p*65536 rounded to nearest even, 0 <= p <= 1; residual_dev may
- * be NULL (zeros) and out_dev may be x_dev or residual_dev (same stride). Dropped
+ * be NULL (zeros) and out_dev may be x_dev or residual_dev (of the same stride, else
+ * GMC_EINVAL). Dropped
  * elements are not computed with: a NaN or Inf there leaves the residual.
  * Element i of row k is kept iff b >= q, b being bits 16*(i mod 4) .. +15 of
  * draw i/4 of the SplitMix64 stream (the library's counter stream, as for RBGS)

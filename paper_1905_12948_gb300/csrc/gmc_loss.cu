@@ -68,7 +68,7 @@ __device__ __forceinline__ void row_stats(const Rows<T>& R, int64_t row, int par
 }
 
 // Bound by memory: a block of 256 threads loads 16 KB at once, and six of them share an SM.
-// 8,192 rows of 32,000 bf16 logits: 84 us, 6.2 TB/s; by warps, 8,000 rows of 4,096: 11.3 us,
+// 8,192 rows of 32,000 bf16 logits: 83 us, 6.3 TB/s; by warps, 8,000 rows of 4,096: 11.3 us,
 // 5.8 TB/s, and 40,000 of 2,048: 39.6 us with 48 registers (five blocks an SM), 46 with 54.
 // kRatio: the log ratios are wanted (the code for them, where they are not, cost 10% of short
 // rows' time).

@@ -14,9 +14,9 @@
 // so that nothing in a row's long chain of small steps (3 to 4 us) holds up another row's
 // traffic: 192 KB of ring cover about 40 KB in flight from HBM, the chain, and a row's
 // share of up to 64 KB (128 KB for the longest rows). Bound by HBM at shares of 64 KB (8,192 x
-// 131,072 bf16: 606 us, 6.7 TB/s read and written), by the gradient warps at smaller ones (12,160
-// x 50,257, shares of 49 KB: 400 us, 6.1 TB/s), and by the first and last row's chains where
-// there are few rows (64 x 32,000: 7.3 us).
+// 131,072 bf16: 603 us, 6.7 TB/s read and written), by the gradient warps at smaller ones (12,160
+// x 50,257, shares of 49 KB: 401 us, 6.1 TB/s), and by the first and last row's chains where
+// there are few rows (64 x 32,000: 7.9 us).
 // k_policy_short: many short rows, one a warp. k_policy: rows over 1 MB, swept twice from global
 // memory.
 #include <new>
@@ -772,8 +772,8 @@ cudaError_t launch_policy(const Rows<T>& R, const PolicyArgs& A, T* dx, int64_t 
   const int64_t nv = most_vecs(R);
   const int sms = device->sms;
   // Short rows, and so many that a lone warp's 10 us for 20 KB do not matter: a warp a row.
-  // bf16, in us, by a warp and by the ring: 30,000 x 2,000 51 201, 16,384 x 2,221 43 140, 30,000 x 10,000
-  // 198 290, 8,000 x 11,000 74 83, 4,000 x 12,001 51 50, 1,000 x 2,500 8.7 12.0, 1,000 x 10,000 12.9 14.8,
+  // bf16, in us, by a warp and by the ring: 30,000 x 2,000 52 201, 16,384 x 2,221 44 140, 30,000 x 10,000
+  // 200 290, 8,000 x 11,000 74 83, 4,000 x 12,001 51 50, 1,000 x 2,500 9.1 12.0, 1,000 x 10,000 12.7 14.8,
   // 600 x 7,000 9.7 9.2, 310 x 2,500 8.1 8.0, 310 x 7,000 9.5 8.2.
   if (nv <= kShortVecs && R.n > 2 * sms && nv * 16 <= 20 * R.n) {
     const int cap = (int)(nv + 7) / 8 * 8;

@@ -11,6 +11,13 @@ contiguous; a row stride larger than vocab is fine. Targets are int64, negative
 where a token is not scored. Outputs are allocated on the stream of the call. A
 gradient is contiguous where the logits are; beside a view with padded rows its rows
 lie as the view's do, a few elements apart.
+
+Nothing here is recorded by autograd: outputs have no grad_fn, also for logits that
+require a gradient. It is had by ``logits.backward(result.dlogits)``, or from
+``token_logp_backward``; a loss that is added to another one adds no gradient. Writing
+into ``out`` raises that tensor's version, as torch's own writes in place do. With
+``stream=`` the inputs are recorded on that stream (their memory is kept until the call
+has run); what follows on another stream waits for it by the caller's own events.
 """
 from __future__ import annotations
 
@@ -79,6 +86,7 @@ def token_logp_backward(logits, targets, stats, dlogp, *, scale: float = 1.0, ou
 
 
 class PolicyLoss(NamedTuple):
+    """loss, token_loss and logp share one allocation: clone what is kept beyond the others."""
     loss: object         # float32 scalar tensor: sum of weights * token_loss
     token_loss: object   # (n,) float32, 0 where a token is not scored
     logp: object         # (n,) float32, 0 where a token is not scored
@@ -86,6 +94,7 @@ class PolicyLoss(NamedTuple):
 
 
 class PreferenceLoss(NamedTuple):
+    """All but dlogits share one allocation: clone what is kept beyond the others."""
     loss: object         # float32 scalar tensor: sum of weights * pair_loss
     pair_loss: object    # (pairs,) float32
     seq_ratio: object    # (2 * pairs,) float32: summed log ratio of each sequence
