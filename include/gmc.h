@@ -469,6 +469,34 @@ int gmc_token_logp_backward(const void* logits_dev, int32_t dtype, int64_t n, in
                             const int64_t* targets_dev, const float* stats_dev, const float* dlogp_dev,
                             void* dlogits_dev, int64_t dld, void* stream);
 
+/* gmc_token_scores -- log-probabilities of given tokens, the entropy and the top
+ * alternatives of each row, in one pass. targets_dev holds n x given int64 (0 <= given
+ * <= 64; NULL for given = 0, where every row counts). A row counts if one of its targets is not
+ * negative; the others are not read, and get 0 (top_index -1). With lp_v the
+ * log-probability of token v:
+ *   logp[r, j] = lp of targets[r, j] (0 where that is negative, NaN where it is >= vocab),
+ *   entropy[r] = -sum_v exp(lp_v) lp_v (a logit of -inf adds nothing),
+ *   top_index[r, :] = the `top` (0 <= top <= 64, top <= vocab) largest logits' places,
+ *       larger ones first and the lower place first among equal ones, top_logp their lp.
+ * A row of -inf alone has lp = -inf, entropy 0. +inf or NaN in a row that counts makes its
+ * outputs NaN, its top_index -1. logp_dev, entropy_dev and stats_dev (4n floats, 16-byte
+ * aligned, for gmc_token_scores_backward) may be NULL, top_logp_dev and top_index_dev where
+ * top = 0. Takes no handle, runs on the current device, stream-ordered. */
+int gmc_token_scores(const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, float scale,
+                     const int64_t* targets_dev, int32_t given, int32_t top, float* logp_dev, float* entropy_dev,
+                     float* top_logp_dev, int64_t* top_index_dev, float* stats_dev, void* stream);
+
+/* gmc_token_scores_backward -- the gradient of
+ *   sum_r (sum_j dlogp[r, j] logp[r, j] + dentropy[r] entropy[r])
+ * in the logits, from the logits, scale and stats of a gmc_token_scores call; targets and
+ * given as there or others (those of the top alternatives, say), as long as the same rows
+ * count. A token that is given twice gets both slopes. dlogp_dev: n x given floats,
+ * dentropy_dev: n floats; NULL for zeros. A row whose slopes are all 0 is written as zeros and not
+ * read; one with a target >= vocab is NaN. dlogits_dev may be logits_dev itself. */
+int gmc_token_scores_backward(const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, float scale,
+                              const int64_t* targets_dev, int32_t given, const float* stats_dev, const float* dlogp_dev,
+                              const float* dentropy_dev, void* dlogits_dev, int64_t dld, void* stream);
+
 /* Workspace of the two losses below, for calls of at most max_rows rows and
  * max_pairs pairs: allocated once on the current device (20 bytes a row, 12 a pair, and
  * 64 KB). Calls with one handle are ordered by the caller (one stream, or events between
@@ -545,6 +573,34 @@ int gmc_preference_loss(gmc_loss_t h, const void* logits_dev, int32_t dtype, int
 int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_t ldr, void* out_dev, int64_t ldo,
                 int32_t dtype, int64_t worker0, int64_t K, int64_t n, double p, uint64_t seed, int64_t t,
                 int64_t site, void* stream);
+
+/*
+ * gmc_orthogonalize -- K matrices of m x n, each replaced by what Newton-Schulz products
+ * make of it: with X = G / |G| (the Frobenius norm), `steps` times
+ *   X <- a X + (b A + c A^2) X,  A = X X',
+ * and out = scale * X. Each singular value of G / |G| goes through the same odd polynomials; the
+ * singular vectors stay. With the coefficients 3.4445, -4.7750, 2.0315 (those of the Muon
+ * optimiser) and 5 steps they come to lie between about 0.7 and 1.2. The paper has no counterpart:
+ * a worker's gradient of a weight matrix is orthogonalised so before gmc_step takes it.
+ *
+ * Matrix k's row i is n contiguous elements at x_dev + k*ldk + i*ld (out_dev likewise, by its
+ * own strides; ldk is ignored where K = 1, ld where m = 1), of type `dtype`. out_dev may be x_dev, or overlap it in
+ * any way: x is read before out is written. coefficients_host: 3*steps floats, a, b, c of each step;
+ * 1 <= steps <= 16. A matrix of zeros gives zeros; one that holds inf or NaN gives NaN. The
+ * singular values have to stay below 4 on the way, else a matrix may become NaN.
+ * |G| is summed in 64 bits, products in 32. Their factors are halves: one for bfloat16
+ * matrices, whose result is off by less than its own rounding, and the sum of two (22 bits) for float and half;
+ * X itself is kept in 22 bits and the diagonals of A and B in 32.
+ * The same call gives the same bits.
+ * workspace_dev: gmc_orthogonalize_workspace(dtype, K, m, n) bytes, 256-byte aligned, whose
+ * contents do not matter; it belongs to the call until the stream has passed it. K <= 65535, m, n <= 2^20, K*m*n <= 2^36
+ * (the workspace call answers -1 otherwise). Takes no handle, runs on the current device,
+ * stream-ordered. GMC_EINVAL for a bad argument, GMC_ECUDA if a launch fails.
+ */
+int64_t gmc_orthogonalize_workspace(int32_t dtype, int64_t K, int64_t m, int64_t n);
+int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev, int64_t out_ldk, int64_t out_ld,
+                      int32_t dtype, int64_t K, int64_t m, int64_t n, int32_t steps, const float* coefficients_host,
+                      float scale, void* workspace_dev, int64_t workspace_bytes, void* stream);
 
 /* gmc_strerror -- a static message for a status code. */
 const char* gmc_strerror(int status);

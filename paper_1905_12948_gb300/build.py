@@ -28,7 +28,7 @@ LIB = os.path.join(PKG, "libgmc.so")
 TOKENS = os.path.join(PKG, "_tokens.so")
 
 SOURCES = ["gmc_api.cu", "gmc_topk.cu", "gmc_small.cu", "gmc_rbgs.cu", "gmc_noalloc.cu",
-           "gmc_loss.cu", "gmc_policy.cu", "gmc_dropout.cu"]
+           "gmc_loss.cu", "gmc_policy.cu", "gmc_dropout.cu", "gmc_scores.cu", "gmc_ortho.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", *ARCH,
          "-fmad=false", "-ftz=false", "-prec-div=true", "-prec-sqrt=true",

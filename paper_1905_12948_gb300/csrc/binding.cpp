@@ -24,6 +24,10 @@ struct Abi {
   decltype(&gmc_policy_loss) policy_loss = nullptr;
   decltype(&gmc_preference_loss) preference_loss = nullptr;
   decltype(&gmc_dropout) dropout = nullptr;
+  decltype(&gmc_token_scores) token_scores = nullptr;
+  decltype(&gmc_token_scores_backward) token_scores_backward = nullptr;
+  decltype(&gmc_orthogonalize_workspace) orthogonalize_workspace = nullptr;
+  decltype(&gmc_orthogonalize) orthogonalize = nullptr;
 } g_abi;
 PyObject* g_error = nullptr;  // GMCError
 
@@ -341,7 +345,139 @@ PyObject* dropout(Args a, Py_ssize_t na) {
   return wrap(out);
 }
 
-// (GMCError, the five entry points' addresses in Abi's order)
+// The targets of n rows: (n,) or (n, given) int64, or None.
+struct Given {
+  const int64_t* y = nullptr;
+  int32_t given = 0;
+  std::vector<int64_t> shape;
+};
+Given given_of(PyObject* o, int64_t n, const Tensor& like) {
+  Given g;
+  if (o == Py_None) return g;
+  const Tensor& t = tensor(o, "targets");
+  if (t.dim() < 1 || t.dim() > 2 || t.size(0) != n) fail(PyExc_ValueError, "targets", "must be (n,) or (n, given)");
+  const int64_t each = t.dim() == 1 ? 1 : t.size(1);
+  if (each < 1 || each > 64) fail(PyExc_ValueError, "targets", "must be 1 to 64 a row");
+  g.y = vector<const int64_t>(o, n * each, at::kLong, like, "targets");
+  g.given = (int32_t)each;
+  g.shape.assign(t.sizes().begin(), t.sizes().end());
+  return g;
+}
+
+// (logits, targets, top, scale, return_stats)
+PyObject* token_scores(Args a, Py_ssize_t na) {
+  arguments(na, 5);
+  const Tensor& x = tensor(a[0], "logits");
+  const Rows r = rows(x, "logits");
+  const int32_t k = kind(x, "logits");
+  const Given g = given_of(a[1], r.n, x);
+  const int64_t top = integer(a[2]);
+  if (top < 0 || top > 64 || top > r.v) fail(PyExc_ValueError, "top", "must be 0 to 64, and at most the vocabulary");
+  const float scale = (float)number(a[3]);
+  const bool with_stats = truth(a[4]);
+  const c10::cuda::OptionalCUDAGuard guard(x.device());
+  const auto f32 = x.options().dtype(at::kFloat);
+  Tensor logp, entropy = at::empty({r.n}, f32), best, index, stats;
+  if (g.given) logp = at::empty(g.shape, f32);
+  if (top) best = at::empty({r.n, top}, f32), index = at::empty({r.n, top}, x.options().dtype(at::kLong));
+  if (with_stats) stats = at::empty({r.n, 4}, f32);
+  check(g_abi.token_scores(x.data_ptr(), k, r.n, r.v, r.ld, scale, g.y, g.given, (int32_t)top,
+                           g.given ? logp.data_ptr<float>() : nullptr, entropy.data_ptr<float>(),
+                           top ? best.data_ptr<float>() : nullptr, top ? index.data_ptr<int64_t>() : nullptr,
+                           with_stats ? stats.data_ptr<float>() : nullptr, stream_of(x)),
+        "gmc_token_scores");
+  return tuple_of({g.given ? wrap(logp) : none(), wrap(entropy), top ? wrap(best) : none(), top ? wrap(index) : none(),
+                   with_stats ? wrap(stats) : none()});
+}
+
+// (logits, targets, stats, dlogp, dentropy, scale, out)
+PyObject* token_scores_backward(Args a, Py_ssize_t na) {
+  arguments(na, 7);
+  const Tensor& x = tensor(a[0], "logits");
+  const Rows r = rows(x, "logits");
+  const int32_t k = kind(x, "logits");
+  const Given g = given_of(a[1], r.n, x);
+  const float* stats = floats(a[2], 4 * r.n, x, "stats");
+  if (a[3] == Py_None && a[4] == Py_None) fail(PyExc_ValueError, "dlogp", "or dentropy must be given");
+  if (!g.given && a[3] != Py_None) fail(PyExc_ValueError, "dlogp", "is that of targets: there are none");
+  const c10::cuda::OptionalCUDAGuard guard(x.device());
+  const float* dlogp = floats(a[3], r.n * g.given, x, "dlogp");
+  const float* dentropy = floats(a[4], r.n, x, "dentropy");
+  const float scale = (float)number(a[5]);
+  int64_t dld = 0;
+  const Tensor out = gradient(a[6], x, r, &dld);
+  check(g_abi.token_scores_backward(x.data_ptr(), k, r.n, r.v, r.ld, scale, g.y, g.given, stats, dlogp, dentropy,
+                                    out.data_ptr(), dld, stream_of(x)),
+        "gmc_token_scores_backward");
+  if (a[6] != Py_None) written(out);
+  return wrap(out);
+}
+
+// Strides of K matrices (one: a 2-D tensor), their rows contiguous.
+struct Matrices {
+  int64_t K, m, n, ldk, ld;
+};
+Matrices matrices(const Tensor& t, const char* name) {
+  const int64_t d = t.dim();
+  if (d != 2 && d != 3) fail(PyExc_TypeError, name, "must be a matrix, or the workers' matrices");
+  Matrices s{d == 3 ? t.size(0) : 1, t.size(d - 2), t.size(d - 1), d == 3 ? t.stride(0) : 0, t.stride(d - 2)};
+  if (s.n > 1 && t.stride(d - 1) != 1) fail(PyExc_TypeError, name, "must have contiguous rows");
+  if (s.m <= 1) s.ld = s.n;
+  if (s.K <= 1) s.ldk = s.m * s.ld;
+  if (s.ld < s.n || s.ldk < (s.m - 1) * s.ld + s.n) fail(PyExc_TypeError, name, "must have rows that do not overlap");
+  return s;
+}
+
+// (x, steps, coefficients, scale, out)
+PyObject* orthogonalize(Args a, Py_ssize_t na) {
+  arguments(na, 5);
+  const Tensor& x = tensor(a[0], "x");
+  const int32_t k = kind(x, "x");
+  const Matrices s = matrices(x, "x");
+  const int64_t steps = integer(a[1]);
+  if (steps < 1 || steps > 16) fail(PyExc_ValueError, "steps", "must be 1 to 16");
+  float coef[48];
+  PyObject* seq = PySequence_Fast(a[2], "coefficients must be (a, b, c), or one such triple for each step");
+  if (!seq) throw PythonError();
+  struct Release {
+    PyObject* o;
+    ~Release() { Py_DECREF(o); }
+  } release{seq};
+  const Py_ssize_t count = PySequence_Fast_GET_SIZE(seq);
+  const bool single = count == 3 && PyNumber_Check(PySequence_Fast_GET_ITEM(seq, 0));
+  if (!single && count != steps) fail(PyExc_ValueError, "coefficients", "must be (a, b, c), or one such triple for each step");
+  for (int64_t i = 0; i < steps; ++i) {
+    PyObject* three = single ? (Py_INCREF(seq), seq)
+                             : PySequence_Fast(PySequence_Fast_GET_ITEM(seq, i), "coefficients must hold triples");
+    if (!three) throw PythonError();
+    Release also{three};
+    if (PySequence_Fast_GET_SIZE(three) != 3) fail(PyExc_ValueError, "coefficients", "must hold triples");
+    for (int j = 0; j < 3; ++j) coef[3 * i + j] = (float)number(PySequence_Fast_GET_ITEM(three, j));
+  }
+  const float scale = (float)number(a[3]);
+  const c10::cuda::OptionalCUDAGuard guard(x.device());
+  Tensor out;
+  Matrices o = s;
+  if (a[4] == Py_None) {
+    out = at::empty(x.sizes(), x.options());
+    o.ld = s.n, o.ldk = s.m * s.n;
+  } else {
+    out = tensor(a[4], "out");
+    if (out.sizes() != x.sizes() || out.scalar_type() != x.scalar_type() || out.device() != x.device())
+      fail(PyExc_TypeError, "out", "must have x's shape, dtype and device");
+    o = matrices(out, "out");
+  }
+  const int64_t bytes = g_abi.orthogonalize_workspace(k, s.K, s.m, s.n);
+  if (bytes < 0) check(GMC_EINVAL, "gmc_orthogonalize");
+  const Tensor work = at::empty({bytes}, x.options().dtype(at::kByte));
+  check(g_abi.orthogonalize(x.data_ptr(), s.ldk, s.ld, out.data_ptr(), o.ldk, o.ld, k, s.K, s.m, s.n, (int32_t)steps, coef,
+                            scale, work.data_ptr(), bytes, stream_of(x)),
+        "gmc_orthogonalize");
+  if (a[4] != Py_None) written(out);
+  return wrap(out);
+}
+
+// (GMCError, the first five entry points' addresses in Abi's order)
 PyObject* init(Args a, Py_ssize_t na) {
   arguments(na, 6);
   void* p[5];
@@ -362,13 +498,31 @@ PyObject* init(Args a, Py_ssize_t na) {
   return none();
 }
 
+// (the other entry points' addresses in Abi's order)
+PyObject* init_more(Args a, Py_ssize_t na) {
+  arguments(na, 4);
+  void* p[4];
+  for (int i = 0; i < 4; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a NULL entry point");
+      throw PythonError();
+    }
+  }
+  g_abi.token_scores = reinterpret_cast<decltype(g_abi.token_scores)>(p[0]);
+  g_abi.token_scores_backward = reinterpret_cast<decltype(g_abi.token_scores_backward)>(p[1]);
+  g_abi.orthogonalize_workspace = reinterpret_cast<decltype(g_abi.orthogonalize_workspace)>(p[2]);
+  g_abi.orthogonalize = reinterpret_cast<decltype(g_abi.orthogonalize)>(p[3]);
+  return none();
+}
+
 // No C++ exception leaves the module: a Python error that is set, or torch's own.
 template <PyObject* (*F)(Args, Py_ssize_t)>
 PyObject* entry(PyObject*, Args a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   try {
-    if (F != init && !g_error) {
-      PyErr_SetString(PyExc_RuntimeError, "init() comes first");
+    if (F != init && !(g_error && (F == init_more || g_abi.orthogonalize))) {
+      PyErr_SetString(PyExc_RuntimeError, "init() and init_more() come first");
       return nullptr;
     }
     return F(a, n);
@@ -382,6 +536,8 @@ PyObject* entry(PyObject*, Args a, Py_ssize_t n) {
   {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<f>)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {GMC_METHOD(init),       GMC_METHOD(token_logp), GMC_METHOD(token_logp_backward),
                            GMC_METHOD(policy),     GMC_METHOD(preference), GMC_METHOD(dropout),
+                           GMC_METHOD(init_more),  GMC_METHOD(token_scores), GMC_METHOD(token_scores_backward),
+                           GMC_METHOD(orthogonalize),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_tokens", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -79,6 +79,13 @@ _SIGNATURES = {
                                            _c_p]),
     "gmc_dropout": (ctypes.c_int, [_c_p, _i64, _c_p, _i64, _c_p, _i64, _i32, _i64, _i64, _i64, _f64, _u64,
                                    _i64, _i64, _c_p]),
+    "gmc_token_scores": (ctypes.c_int, [_c_p, _i32, _i64, _i64, _i64, _f32, _c_p, _i32, _i32, _c_p, _c_p, _c_p,
+                                        _c_p, _c_p, _c_p]),
+    "gmc_token_scores_backward": (ctypes.c_int, [_c_p, _i32, _i64, _i64, _i64, _f32, _c_p, _i32, _c_p, _c_p,
+                                                 _c_p, _c_p, _i64, _c_p]),
+    "gmc_orthogonalize_workspace": (_i64, [_i32, _i64, _i64, _i64]),
+    "gmc_orthogonalize": (ctypes.c_int, [_c_p, _i64, _i64, _c_p, _i64, _i64, _i32, _i64, _i64, _i64, _i32, _c_p,
+                                         _f32, _c_p, _i64, _c_p]),
     "gmc_test_fail_alloc": (_i64, [_i64]),
     "gmc_test_withhold_copy": (ctypes.c_int, [_c_p, _i64, _i32, _u64]),
     "gmc_test_pass": (ctypes.c_int, [_c_p]),

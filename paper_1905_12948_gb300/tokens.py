@@ -48,6 +48,8 @@ def _load():
     module.init(GMCError, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.gmc_token_logp, lib.gmc_token_logp_backward, lib.gmc_policy_loss, lib.gmc_preference_loss,
         lib.gmc_dropout)))
+    module.init_more(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.gmc_token_scores, lib.gmc_token_scores_backward, lib.gmc_orthogonalize_workspace, lib.gmc_orthogonalize)))
     _ops = module
     return module
 
@@ -83,6 +85,38 @@ def token_logp_backward(logits, targets, stats, dlogp, *, scale: float = 1.0, ou
         with _on(stream, logits, "logits", targets, stats, dlogp, out):
             return token_logp_backward(logits, targets, stats, dlogp, scale=scale, out=out)
     return (_ops or _load()).token_logp_backward(logits, targets, stats, dlogp, scale, out)
+
+
+class TokenScores(NamedTuple):
+    """What token_scores gives: None in the place of what was not asked for."""
+    logp: object         # float32 of the targets' shape, 0 where a token is not scored
+    entropy: object      # (n,) float32
+    top_logp: object     # (n, top) float32, larger ones first
+    top_index: object    # (n, top) int64, the lower one first among equal logits
+    stats: object        # (n, 4) float32, for token_scores_backward
+
+
+def token_scores(logits, targets=None, *, top: int = 0, scale: float = 1.0, return_stats: bool = False,
+                 stream=None) -> TokenScores:
+    """Log-probabilities of given tokens, the entropy and the ``top`` most probable tokens of
+    each row under softmax(scale * logits), in one pass (gmc_token_scores). ``targets``: (n,) or
+    (n, given) int64, up to 64 a row; a row whose targets are all negative is not scored.
+    Without targets every row is."""
+    if stream is not None:
+        with _on(stream, logits, "logits", targets):
+            return token_scores(logits, targets, top=top, scale=scale, return_stats=return_stats)
+    return TokenScores(*(_ops or _load()).token_scores(logits, targets, top, scale, return_stats))
+
+
+def token_scores_backward(logits, targets, stats, dlogp=None, dentropy=None, *, scale: float = 1.0, out=None,
+                          stream=None):
+    """Gradient of sum(dlogp * logp) + sum(dentropy * entropy) in the logits
+    (gmc_token_scores_backward), of the logits' dtype; ``out`` may be the logits themselves. The
+    slopes of top alternatives are given as those of tokens: ``targets=scores.top_index``."""
+    if stream is not None:
+        with _on(stream, logits, "logits", targets, stats, dlogp, dentropy, out):
+            return token_scores_backward(logits, targets, stats, dlogp, dentropy, scale=scale, out=out)
+    return (_ops or _load()).token_scores_backward(logits, targets, stats, dlogp, dentropy, scale, out)
 
 
 class PolicyLoss(NamedTuple):
