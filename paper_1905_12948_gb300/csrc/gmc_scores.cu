@@ -19,19 +19,51 @@ using namespace gmc;
 namespace {
 
 constexpr int kMostGiven = 64, kMostTop = 64;
-constexpr int kHeld = kLossThreads;  // candidates of a block
+constexpr int kBatches = 16;  // of a sweep, before its candidates are looked for
 
-// A maximum and the two sums under its shift. m = -inf: nothing yet.
+// Exponents to base 2 are x c less a shift, c the float next to scale log2 e: all of them, the given tokens' too, so that
+// a log-probability is off by 2^-25 of itself, and no second word of c is wanted.
+inline Base score_base(float scale) { return Base{scale, (float)((double)scale * kLog2e), 0.f}; }
+
+// The threads that work on a row: a block, of which up to 8 share a row as a cluster, or a warp.
+template <int G>
+struct Team {
+  static_assert(G == 32 || G == kLossThreads, "a warp or a block");
+  static constexpr int kRows = kLossThreads / G;  // rows of a block
+  __device__ static int tid() { return G == 32 ? (int)threadIdx.x % 32 : (int)threadIdx.x; }
+  __device__ static int of_block() { return G == 32 ? (int)threadIdx.x / 32 : 0; }
+  __device__ static void sync() {
+    if constexpr (G == 32) __syncwarp();
+    else __syncthreads();
+  }
+  __device__ static bool any(bool p) {
+    if constexpr (G == 32) return __any_sync(0xffffffffu, p);
+    else return __syncthreads_or(p);
+  }
+};
+
+// What is summed below a shift: that of m, which is -inf where nothing has been seen, and at most
+// kAbove exponents below the largest logit seen.
 struct alignas(16) Moments {
   float m = -INFINITY, s = 0.f, t = 0.f, none = 0.f;
 };
+constexpr float kAbove = 8.f;
 // Where 2^e is 0 (a logit of -inf, a sum that is too low to matter) e may be -inf, and e 2^e is not
 // a number; below 2^-126 the exponential is 0. (NaN passes through the exponential itself.)
 __device__ __forceinline__ float low(float e) { return fmaxf(e, -256.f); }
 
+// By how much the shift of m lies below s, in exponents; as in gmc_loss.cuh, with one word of c.
+template <typename T>
+__device__ __forceinline__ float below(float m, const Shift& s, const Base& b) {
+  if (m == -INFINITY) return m;
+  const float hc = ceilf(m * b.c);
+  const bool far = !(fabsf(hc) < kFar);
+  if (sizeof(T) == 2 || far == s.far) return s.far ? (m - s.h) * b.c : hc - s.hc;
+  return s.far ? __fmaf_rn(-s.h, b.c, hc) : __fmaf_rn(m, b.c, -s.hc);
+}
 template <typename T>
 __device__ __forceinline__ void move(Moments* a, const Shift& to, const Base& b) {
-  const float d = between<T>(a->m, to, b), f = exp2_fast(d);
+  const float d = below<T>(a->m, to, b), f = exp2_fast(d);
   a->t = (a->t + low(d) * a->s) * f;
   a->s *= f;
 }
@@ -48,50 +80,110 @@ __device__ __forceinline__ Moments merge(Moments a, Moments o, const Base& b) {
   return r;
 }
 template <typename T>
-__device__ __forceinline__ void add_one(Moments* a, float x, const Base& b) {
-  const float m = fmaxf(a->m, x);
-  const Shift h = shift_of(m, b);
-  move<T>(a, h, b);
-  const float e = h.far ? exponent(x - h.h, 0.f, b) : exponent(x, h.hc, b), p = exp2_fast(e);
-  a->s += p;
-  a->t = __fmaf_rn(low(e), p, a->t);
-  a->m = m;
-}
-// U vectors whose largest value is `top`.
-template <typename T, int U>
-__device__ __forceinline__ void add(Moments* a, const uint4 (&v)[U], float top, const Base& b) {
-  constexpr int P = Vec<T>::N / 2;
-  const float m = fmaxf(a->m, top);
-  const Shift h = shift_of(m, b);
-  move<T>(a, h, b);
-  a->m = m;
-  const float sh = h.far ? -h.h : 0.f, off = h.far ? 0.f : -h.hc;
-  const Pair by = pair_of(sh, sh), c = pair_of(b.c, b.c), lo = pair_of(b.lo, b.lo), hc = pair_of(off, off);
-  Pair s = pair_of(a->s, 0.f), t = pair_of(a->t, 0.f);
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    Pair x[P];
-    Vec<T>::pairs(v[u], x);
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      if (h.far) x[i] = add_pair(x[i], by);
-      const Pair e = fma_pair(x[i], lo, fma_pair(x[i], c, hc)), p = exp2_pair(e);
-      float e0, e1;
-      split(e, &e0, &e1);
-      s = add_pair(s, p);
-      t = fma_pair(pair_of(low(e0), low(e1)), p, t);
-    }
-  }
-  float s0, s1;
-  split(s, &s0, &s1);
-  a->s = s0 + s1;
-  split(t, &s0, &s1);
-  a->t = s0 + s1;
-}
-template <typename T>
 __device__ __forceinline__ float largest(const uint4& v) {
   return Vec<T>::top_of(Vec<T>::top(Vec<T>::top(v.x, v.y), Vec<T>::top(v.z, v.w)));
 }
+// The word's two values, no less than those of `floor` (NaN stays NaN).
+__device__ __forceinline__ uint32_t at_least(uint32_t w, uint32_t floor, __nv_bfloat16) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(floor));
+  return r;
+}
+__device__ __forceinline__ uint32_t at_least(uint32_t w, uint32_t floor, __half) {
+  uint32_t r;
+  asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(floor));
+  return r;
+}
+
+// A thread's running sums. The shift moves only when a logit lies kAbove exponents above it: hardly ever
+// after the first batch, and sums are as exact at any shift.
+template <typename T>
+struct Running {
+  Moments a;
+  Pair s = 0, t = 0;                     // of a's shift
+  Shift h{0.f, 0.f, false};
+  float limit = -INFINITY;               // the largest logit that the shift is good for
+  uint32_t floor = Vec<T>::kLow;         // 16-bit types: a logit, twice, whose exponential is 0
+  bool clamp = true;                     // exponents are held above -256 one by one
+
+  __device__ __forceinline__ void shift_to(float top, const Base& b) {
+    split_sums();
+    const float m = fmaxf(a.m, top);
+    h = shift_of(m, b);
+    move<T>(&a, h, b);
+    a.m = m;
+    limit = h.far ? m : (h.hc + kAbove) / b.c;
+    s = pair_of(a.s, 0.f);
+    t = pair_of(a.t, 0.f);
+    clamp = true;
+    if constexpr (sizeof(T) == 2) {
+      // its exponent is -200, give or take a rounding to the type: at most 9 where the shift is below 2^12
+      const float f = (h.hc - 200.f) / b.c;
+      clamp = h.far || fabsf(h.hc) > 4096.f || !(f > -60000.f);
+      const T lowest = Vec<T>::round(f);
+      const uint32_t half = *reinterpret_cast<const uint16_t*>(&lowest);
+      floor = clamp ? Vec<T>::kLow : half << 16 | half;
+    }
+  }
+  __device__ __forceinline__ void split_sums() {
+    float x, y;
+    split(s, &x, &y);
+    a.s = x + y;
+    split(t, &x, &y);
+    a.t = x + y;
+  }
+  // U vectors whose largest value is `top`.
+  template <int U>
+  __device__ __forceinline__ void add(const uint4 (&v)[U], float top, const Base& b) {
+    constexpr int P = Vec<T>::N / 2;
+    if (top > limit) shift_to(top, b);
+    const float off = h.far ? 0.f : -h.hc;
+    const Pair c = pair_of(b.c, b.c), hc = pair_of(off, off);
+    if (sizeof(T) == 2 && !clamp) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        uint4 w = v[u];
+        if constexpr (sizeof(T) == 2)
+          w = make_uint4(at_least(w.x, floor, T()), at_least(w.y, floor, T()), at_least(w.z, floor, T()), at_least(w.w, floor, T()));
+        Pair x[P];
+        Vec<T>::pairs(w, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const Pair e = fma_pair(x[i], c, hc), p = exp2_pair(e);
+          s = add_pair(s, p);
+          t = fma_pair(e, p, t);
+        }
+      }
+    } else {
+      const float sh = h.far ? -h.h : 0.f;
+      const Pair by = pair_of(sh, sh);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        Pair x[P];
+        Vec<T>::pairs(v[u], x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          if (h.far) x[i] = add_pair(x[i], by);
+          const Pair e = fma_pair(x[i], c, hc), p = exp2_pair(e);
+          float e0, e1;
+          split(e, &e0, &e1);
+          s = add_pair(s, p);
+          t = fma_pair(pair_of(low(e0), low(e1)), p, t);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void add_one(float x, const Base& b) {
+    if (x > limit) shift_to(x, b);
+    const float e = h.far ? (x - h.h) * b.c : __fmaf_rn(x, b.c, -h.hc), p = exp2_fast(e);
+    s = add_pair(s, pair_of(p, 0.f));
+    t = fma_pair(pair_of(low(e), 0.f), pair_of(p, 0.f), t);
+  }
+  __device__ __forceinline__ Moments sums() {
+    split_sums();
+    return a;
+  }
+};
 template <typename T>
 __device__ __forceinline__ Moments warp_merge(Moments a, const Base& b) {
   float m = a.m;
@@ -104,54 +196,100 @@ __device__ __forceinline__ Moments warp_merge(Moments a, const Base& b) {
   r.t = warp_sum(a.t);
   return r;
 }
-template <typename T>
-__device__ __forceinline__ Moments block_merge(Moments a, const Base& b, Moments* ws) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+template <typename T, int G>
+__device__ __forceinline__ Moments team_merge(Moments a, const Base& b) {
   a = warp_merge<T>(a, b);
-  if (lane == 0) ws[warp] = a;
-  __syncthreads();
-  return warp_merge<T>(lane < warps ? ws[lane] : Moments(), b);
+  if constexpr (G != 32) {
+    __shared__ Moments ws[G / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (lane == 0) ws[warp] = a;
+    __syncthreads();
+    a = warp_merge<T>(lane < G / 32 ? ws[lane] : Moments(), b);
+  }
+  return a;
+}
+// The log-probability of a logit, from its row's sums.
+__device__ __forceinline__ float score_of(const Moments& a, float x, const Base& b) {
+  const Shift h = shift_of(a.m, b);
+  if (h.far || (a.m == -INFINITY && a.s == 0.f)) {
+    if (x != x) return x;
+    return a.s == 0.f ? -INFINITY : (x - h.h) * b.scale - logf(a.s);
+  }
+  // log S in two parts, the power of two and the rest
+  const uint32_t bits = __float_as_uint(a.s);
+  const float power = (float)((int)(bits >> 23) - 127);
+  const float rest = logf(__uint_as_float((bits & 0x007fffffu) | 0x3f800000u));
+  const double full = ((double)x * (double)b.c - (double)(h.hc + power)) * kLn2 - ((double)rest + kExp2Low);
+  return a.s != a.s ? a.s : (float)full;
 }
 
-// A logit and its place as one number: larger logits first, and lower places among equal ones
-// (zeros of either sign are equal; any NaN is above all). No key is 0.
-__device__ __forceinline__ uint64_t key_of(float x, int64_t at) {
-  uint32_t u = __float_as_uint(x + 0.f);
-  u = x != x ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
-  return (uint64_t)u << 32 | (uint32_t)~(uint32_t)at;
+// A logit as a number that is larger where it is (zeros of either sign are equal; any NaN is above
+// all), never 0; with its place as one number: lower places first among equal ones.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.f);
+  return x != x ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(uint64_t key) {
-  const uint32_t u = (uint32_t)(key >> 32);
-  return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+__device__ __forceinline__ float value_of(uint32_t order) {
+  return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
 }
+__device__ __forceinline__ uint64_t key_of(float x, int64_t at) { return (uint64_t)order_of(x) << 32 | (uint32_t)~(uint32_t)at; }
 __device__ __forceinline__ int64_t place_of(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
 
-// The best `top` keys seen by a block: an unordered list that takes every key above the
-// last bound, cut back to its best whenever it is half full.
+// The best keys seen by a team: an unordered list that takes every key above the last
+// bound, cut back to its best whenever it is full.
+template <int G>
 struct Held {
-  uint64_t key[kHeld];
-  uint64_t bound;        // no key at or below it is among the best
+  static constexpr int N = G == 32 ? 128 : 256;
+  uint64_t key[N];
+  uint64_t bound;             // no key at or below it is among the best
   int n;
+  uint32_t least[G / 32];     // of a sweep, by warps
+  float most[kBatches][G];    // the threads' largest logits, by batches
 };
-// All threads: the list's best `top`, in order, and the bound that follows.
-__device__ __forceinline__ void cut(Held* H, int top) {
-  __syncthreads();
-  const int n = H->n < kHeld ? H->n : kHeld, tid = (int)threadIdx.x;
-  const uint64_t mine = tid < n ? H->key[tid] : 0;
-  int rank = 0;
+// The whole team: the list's best `top`, in order, and the bound that follows.
+template <int G>
+__device__ __forceinline__ void cut(Held<G>* H, int top) {
+  constexpr int N = Held<G>::N, per = N / G;  // keys of a thread
+  Team<G>::sync();
+  const int n = H->n < N ? H->n : N, tid = Team<G>::tid();
+  uint64_t mine[per];
+  int rank[per];
+#pragma unroll
+  for (int u = 0; u < per; ++u) {
+    mine[u] = tid + u * G < n ? H->key[tid + u * G] : 0;
+    rank[u] = 0;
+  }
   if (tid < n)
-    for (int i = 0; i < n; ++i) rank += H->key[i] > mine;
-  __syncthreads();
-  if (tid < n && rank < top) H->key[rank] = mine;
+    for (int i = 0; i < n; ++i) {
+      const uint64_t other = H->key[i];
+#pragma unroll
+      for (int u = 0; u < per; ++u) rank[u] += other > mine[u];
+    }
+  Team<G>::sync();
+#pragma unroll
+  for (int u = 0; u < per; ++u) {
+    const bool in = tid + u * G < n;
+    if (in && rank[u] < top) H->key[rank[u]] = mine[u];
+    if (in && rank[u] == top - 1) H->bound = mine[u];
+  }
   if (tid == 0) H->n = n < top ? n : top;
-  if (tid < n && rank == top - 1) H->bound = mine;
-  __syncthreads();
+  Team<G>::sync();
 }
-// Into the list; the place that the key got (kHeld or more: none, before the next cut).
-__device__ __forceinline__ int offer(Held* H, uint64_t key) {
+// Into the list; false: there is no room before the next cut.
+template <int G>
+__device__ __forceinline__ bool offer(Held<G>* H, uint64_t key) {
   const int at = atomicAdd(&H->n, 1);
-  if (at < kHeld) H->key[at] = key;
-  return at;
+  if (at < Held<G>::N) H->key[at] = key;
+  return at < Held<G>::N;
+}
+// The j-th largest of a warp's numbers.
+__device__ __forceinline__ uint32_t jth_largest(uint32_t u, int j) {
+  for (int i = 1; i < j; ++i) {
+    const uint32_t most = __reduce_max_sync(0xffffffffu, u);
+    const uint32_t who = __ballot_sync(0xffffffffu, u == most);
+    if (((int)threadIdx.x & 31) == __ffs((int)who) - 1) u = 0;
+  }
+  return __reduce_max_sync(0xffffffffu, u);
 }
 
 struct ScoreArgs {
@@ -171,127 +309,204 @@ __device__ __forceinline__ bool counts(const int64_t* y, int given) {
   return __any_sync(0xffffffffu, some);
 }
 
-// A row by a block. Bound by memory.
-template <typename T, bool kTop>
-__global__ void __launch_bounds__(kLossThreads) k_scores(Rows<T> R, ScoreArgs A) {
+// A team's share (`part` of `parts`) of a row. Its best `top` logits are found by bounds: of the
+// largest logits of some groups of its elements the top-th is a bound from below. A sweep of kBatches
+// batches leaves the threads' largest ones behind; the few batches that reach the bound are then read
+// again, and what is above it goes into the list.
+template <typename T, int G, bool kTop>
+__device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base& b, int part, int parts, int top, Held<G>* H) {
   constexpr int N = Wide<T>::N, U = kSweepVecs, M = Vec<T>::N;
-  __shared__ Moments ws[32];
-  __shared__ Held H;
-  __shared__ float first[kLossThreads];
-  griddep_wait();
-  const int64_t row = blockIdx.x;
-  const int tid = (int)threadIdx.x;
-  const int64_t* y = A.y + row * A.given;
-  if (!counts(y, A.given)) {
-    if (tid < A.given && A.logp) A.logp[row * A.given + tid] = 0.f;
-    if (tid < A.top) A.top_logp[row * A.top + tid] = 0.f, A.top_index[row * A.top + tid] = -1;
-    if (tid == 0 && A.entropy) A.entropy[row] = 0.f;
-    if (tid == 0 && A.stats) A.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
-    return;
-  }
-  const T* x = R.x + row * R.ld;
-  const int64_t V = R.V;
-  const int64_t yj = tid < A.given ? y[tid] : -1;
-  const float xy = yj >= 0 ? target_logit(x, V, yj) : 0.f;
-
+  const int tid = Team<G>::tid();
   const int head = wide_head(x, V);
   const int64_t nv = (V - head) / N;
   const int tail = (int)(V - head - nv * N);
   const T* q = x + head;
-  Moments a;
-  if (kTop && tid == 0) H.n = 0, H.bound = 0;
-  uint64_t edge = 0;  // the row's ends, by a few threads
-  if (tid < head + tail) {
+  const int64_t per = (nv + parts - 1) / parts;
+  const int64_t lo = per * part < nv ? per * part : nv, hi = lo + per < nv ? lo + per : nv;
+  Running<T> a;
+  uint64_t edge = 0;  // the row's ends, by a few threads of the first part
+  if (part == 0 && tid < head + tail) {
     const int64_t i = tid < head ? (int64_t)tid : V - tail + (tid - head);
     const float v = Vec<T>::one(x[i]);
-    add_one<T>(&a, v, R.b);
+    a.add_one(v, b);
     edge = key_of(v, i);
   }
-  for (int64_t i0 = tid, block0 = 0; block0 < nv || (kTop && block0 == 0); i0 += U * kLossThreads, block0 += U * kLossThreads) {
-    float top = -INFINITY;
-    {
+  if (kTop) {
+    if (tid == 0) H->n = 0, H->bound = 0;
+    Team<G>::sync();
+  }
+  int64_t begin = lo;
+  do {
+    float first = -INFINITY, second = -INFINITY;  // the largest logits of the thread's two vectors
+    int batches = 0;
+    for (; batches < kBatches && begin + batches * (U * G) < hi; ++batches) {
+      const int64_t i0 = begin + batches * (U * G) + tid;
       uint4 v[2 * U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t i = i0 + u * kLossThreads;
+        const int64_t i = i0 + u * G;
         v[2 * u] = v[2 * u + 1] = make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
-        if (i < nv) {
+        if (i < hi) {
           const Wide<T> w = load_wide(q + i * N, true);
           v[2 * u] = w.a;
           v[2 * u + 1] = w.b;
         }
       }
-#pragma unroll
-      for (int u = 0; u < 2 * U; ++u) top = fmaxf(top, largest<T>(v[u]));
-      add<T>(&a, v, top, R.b);
+      static_assert(U == 2, "two vectors a thread");
+      const float m0 = fmaxf(largest<T>(v[0]), largest<T>(v[1])), m1 = fmaxf(largest<T>(v[2]), largest<T>(v[3]));
+      a.add(v, fmaxf(m0, m1), b);
+      if constexpr (kTop) {
+        H->most[batches][tid] = fmaxf(m0, m1);
+        first = fmaxf(first, m0);
+        second = fmaxf(second, m1);
+      }
     }
     if constexpr (kTop) {
-      if (block0 == 0) {
-        // Of the threads' largest values the top-th is a bound from below: so many are not less.
-        first[tid] = top;
+      uint32_t least;
+      if constexpr (G == 32) {
+        least = top <= 32 ? jth_largest(order_of(fmaxf(first, second)), top)
+                          : __reduce_min_sync(0xffffffffu, order_of(fminf(first, second)));
+      } else {
+        // (of each warp's so many that the warps have `top` together)
+        const uint32_t of_warp = jth_largest(order_of(fmaxf(first, second)), (top + G / 32 - 1) / (G / 32));
+        if (tid % 32 == 0) H->least[tid / 32] = of_warp;
         __syncthreads();
-        int above = 0;
-        for (int i = 0; i < kLossThreads; ++i) above += first[i] > top || (first[i] == top && i < tid);
-        if (above == A.top - 1 && top > -INFINITY) H.bound = (key_of(top, 0) >> 32 << 32) - 1;
-        __syncthreads();
+        least = H->least[0];
+#pragma unroll
+        for (int i = 1; i < G / 32; ++i) least = H->least[i] < least ? H->least[i] : least;
       }
-      int done = 0;  // so many elements of this thread are in the list
+      const uint32_t none = order_of(-INFINITY);
+      int batch = 0, done = 0;  // elements of a batch before `done` have been offered
       for (bool again = true; again;) {
-        const uint64_t bound = H.bound;
-        const float least = bound ? value_of(bound) : -INFINITY;
-        bool full = false, left = false;
-        if (edge > bound) {
-          const int at = offer(&H, edge);
-          full = at >= kHeld / 2;
-          left = at >= kHeld;
-          if (!left) edge = 0;
-        }
-        if (top >= least) {  // (rare: these vectors are read a second time)
+        uint64_t bound = H->bound;
+        if (least > none && bound < ((uint64_t)least << 32) - 1) bound = ((uint64_t)least << 32) - 1;
+        const float from = bound ? value_of((uint32_t)((bound + 1) >> 32)) : -INFINITY;
+        bool left = false;
+        if (edge > bound) left = !offer(H, edge);
+        if (!left) edge = 0;
+        for (; batch < batches && !left; batch += !left) {
+          if (!(H->most[batch][tid] >= from)) continue;
 #pragma unroll 1
-          for (int u = 0; u < 2 * U; ++u) {
-            const int64_t vec = i0 + u / 2 * kLossThreads;
-            if (vec >= nv || done >= (u + 1) * M || left) continue;
+          for (int u = done / M; u < 2 * U && !left; ++u) {
+            const int64_t vec = begin + batch * (U * G) + tid + u / 2 * G;
+            if (vec >= hi) break;
             const int64_t at0 = head + vec * N + (u & 1) * M;
             const uint4 w = *reinterpret_cast<const uint4*>(x + at0);
-            if (!(largest<T>(w) >= least)) continue;
+            if (!(largest<T>(w) >= from)) continue;
             float f[M];
             Vec<T>::get(w, f);
 #pragma unroll
             for (int i = 0; i < M; ++i)
-              if (f[i] >= least && !left && done <= u * M + i) {
+              if (f[i] >= from && !left && done <= u * M + i) {
                 const uint64_t key = key_of(f[i], at0 + i);
-                if (key > bound) {
-                  const int at = offer(&H, key);
-                  full |= at >= kHeld / 2;
-                  left = at >= kHeld;
-                  if (!left) done = u * M + i + 1;
-                }
+                if (key > bound) left = !offer(H, key);
+                if (!left) done = u * M + i + 1;
               }
           }
+          if (!left) done = 0;
         }
-        again = __syncthreads_or(full);
-        if (again) cut(&H, A.top);
+        again = Team<G>::any(left);
+        if (again) cut(H, top);
       }
     }
+    begin += kBatches * (U * G);
+  } while (begin < hi);
+  return a.sums();
+}
+
+// What a row that does not count gets.
+__device__ __forceinline__ void no_score(const ScoreArgs& A, int64_t row, int tid, int threads) {
+  for (int j = tid; j < A.given; j += threads)
+    if (A.logp) A.logp[row * A.given + j] = 0.f;
+  for (int j = tid; j < A.top; j += threads) A.top_logp[row * A.top + j] = 0.f, A.top_index[row * A.top + j] = -1;
+  if (tid == 0 && A.entropy) A.entropy[row] = 0.f;
+  if (tid == 0 && A.stats) A.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+__device__ __forceinline__ void write_scores(const ScoreArgs& A, const Moments& a, int64_t row, const Base& b) {
+  const bool empty = a.m == -INFINITY && a.s == 0.f;
+  const Shift h = shift_of(a.m, b);
+  const float ls = empty ? 0.f : logf(a.s);
+  float e = empty ? 0.f : (float)((double)ls - kLn2 * ((double)a.t / (double)a.s));
+  e = e < 0.f ? 0.f : e;  // (kExp2Low of S is left: a row of one token has no entropy)
+  if (A.entropy) A.entropy[row] = e;
+  if (A.stats) A.stats[row] = make_float4(h.h, empty ? INFINITY : ls, e, 0.f);
+}
+
+// Rows by blocks, by clusters of `parts` blocks where there are few, by warps where there are many
+// short ones. Bound by memory.
+template <typename T, int G, bool kTop>
+__global__ void __launch_bounds__(kLossThreads, G == 32 && kTop ? 4 : 5) k_scores(Rows<T> R, ScoreArgs A, int parts) {
+  using Te = Team<G>;
+  __shared__ Held<G> held[kTop ? Te::kRows : 1];
+  __shared__ Moments cs[kMaxParts];
+  __shared__ uint64_t ck[kTop && G != 32 ? kMaxParts : 1][kMostTop];
+  griddep_wait();
+  const int64_t at = blockIdx.x / parts, row = at * Te::kRows + Te::of_block();
+  const int part = (int)(blockIdx.x - at * parts), tid = Te::tid();
+  if (G == 32 && row >= R.n) return;
+  const int64_t* y = A.y + row * A.given;
+  if (!counts(y, A.given)) {  // (all blocks of a cluster)
+    if (part == 0) no_score(A, row, tid, G);
+    return;
   }
-  a = block_merge<T>(a, R.b, ws);
-  const MaxSum ms{a.m, a.s};
-  if (tid < A.given && A.logp) A.logp[row * A.given + tid] = yj >= 0 ? finish(ms, xy, R.b).logp : 0.f;
-  if (kTop) {
-    cut(&H, A.top);
-    if (tid < A.top) {
-      const uint64_t key = H.key[tid];
-      A.top_logp[row * A.top + tid] = finish(ms, value_of(key), R.b).logp;
-      A.top_index[row * A.top + tid] = a.s != a.s ? -1 : place_of(key);
+  if (G != 32 && parts > 1) cluster_arrive();
+  const T* x = R.x + row * R.ld;
+  Held<G>* H = &held[kTop ? Te::of_block() : 0];
+  Moments a = score_sweep<T, G, kTop>(x, R.V, R.b, part, parts, A.top, H);
+  a = team_merge<T, G>(a, R.b);
+  const uint64_t* best = H->key;
+  if (kTop) cut(H, A.top);
+  if (G != 32 && parts > 1) {
+    cluster_wait();  // every block has begun
+    // into slot `part` of the first block: the sums, and the best keys (0: none)
+    const uint32_t here = smem_addr(cs + part), keys = smem_addr(ck[kTop ? part : 0]);
+    uint32_t there;
+    if (tid == 0) {
+      asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(here));
+      asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(a.m), "f"(a.s), "f"(a.t), "f"(0.f) : "memory");
+    }
+    if (kTop && tid < A.top) {
+      const uint64_t key = tid < H->n ? H->key[tid] : 0;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(there) : "r"(keys + tid * 8));
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(there), "l"(key) : "memory");
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (part != 0) return;
+    a = cs[0];
+    for (int i = 1; i < parts; ++i) a = merge<T>(a, cs[i], R.b);
+    if (kTop) {
+      // each key's place: its own in its list, and how many of the others' are above it
+      for (int i = tid; i < parts * A.top; i += G) {
+        const int list = i / A.top, own = i % A.top;
+        const uint64_t key = ck[list][own];
+        int rank = own;
+        for (int l = 0; l < parts; ++l) {
+          if (l == list) continue;
+          int from = 0, to = A.top;  // so many are above
+          while (from < to) {
+            const int mid = (from + to) / 2;
+            if (ck[l][mid] > key) from = mid + 1;
+            else to = mid;
+          }
+          rank += from;
+        }
+        if (key && rank < A.top) H->key[rank] = key;
+      }
+      __syncthreads();
     }
   }
-  if (tid == 0) {
-    const RowStats r = finish(ms, 0.f, R.b);
-    float h = r.empty ? 0.f : (float)((double)r.ls - kLn2 * ((double)a.t / (double)a.s));
-    h = h < 0.f ? 0.f : h;  // (kExp2Low of S is left: a row of one token has no entropy)
-    if (A.entropy) A.entropy[row] = h;
-    if (A.stats) A.stats[row] = make_float4(r.h.h, r.empty ? INFINITY : r.ls, h, 0.f);
+  for (int j = tid; j < A.given; j += G) {
+    const int64_t t = y[j];
+    if (A.logp) A.logp[row * A.given + j] = t < 0 ? 0.f : score_of(a, target_logit(x, R.V, t), R.b);
   }
+  if (kTop)
+    for (int j = tid; j < A.top; j += G) {
+      const uint64_t key = best[j];
+      A.top_logp[row * A.top + j] = score_of(a, value_of((uint32_t)(key >> 32)), R.b);
+      A.top_index[row * A.top + j] = a.s != a.s ? -1 : place_of(key);
+    }
+  if (tid == 0) write_scores(A, a, row, R.b);
 }
 
 // What a row's gradient is made of, in exponents: p_v (G + h (lp_v + H)) s = 2^e (c0 + c1 e).
@@ -303,14 +518,14 @@ template <typename T>
 __device__ __forceinline__ uint4 grad_vec(const uint4& v, const ScoreGrad& g, const Base& b) {
   constexpr int P = Vec<T>::N / 2;
   const float sh = g.h.far ? -g.h.h : 0.f, hc = g.h.far ? 0.f : -g.h.hc;
-  const Pair by = pair_of(sh, sh), c = pair_of(b.c, b.c), lo = pair_of(b.lo, b.lo), off = pair_of(hc, hc),
+  const Pair by = pair_of(sh, sh), c = pair_of(b.c, b.c), off = pair_of(hc, hc),
              c0 = pair_of(g.c0, g.c0), c1 = pair_of(g.c1, g.c1);
   Pair x[P];
   Vec<T>::pairs(v, x);
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     x[i] = add_pair(x[i], by);
-    const Pair e = fma_pair(x[i], lo, fma_pair(x[i], c, off));
+    const Pair e = fma_pair(x[i], c, off);
     float e0, e1;
     split(e, &e0, &e1);
     x[i] = mul_pair(exp2_pair(e), fma_pair(pair_of(low(e0), low(e1)), c1, c0));
@@ -319,7 +534,7 @@ __device__ __forceinline__ uint4 grad_vec(const uint4& v, const ScoreGrad& g, co
 }
 template <typename T>
 __device__ __forceinline__ float grad_one(float x, const ScoreGrad& g, const Base& b) {
-  const float e = g.h.far ? exponent(x - g.h.h, 0.f, b) : exponent(x, g.h.hc, b);
+  const float e = g.h.far ? (x - g.h.h) * b.c : __fmaf_rn(x, b.c, -g.h.hc);
   return exp2_fast(e) * __fmaf_rn(low(e), g.c1, g.c0);
 }
 
@@ -376,7 +591,9 @@ __global__ void __launch_bounds__(kLossThreads, 6) k_scores_grad(Rows<T> R, int 
       if (j < tid && ys[j] == y) mine = false;
     }
     if (mine) {
-      const float lp = logp_of(Vec<T>::one(x[y]), q.h, st.y, R.b);
+      const float v = Vec<T>::one(x[y]);
+      const float lp = q.h.far ? (v - q.h.h) * R.b.scale - st.y
+                               : (float)(((double)v * (double)R.b.c - (double)q.h.hc) * kLn2 - ((double)st.y + kExp2Low));
       const float p = lp == -INFINITY ? 0.f : expf(lp), more = p == 0.f ? 0.f : p * (G - gy + h * (lp + st.z));
       at_y = R.b.scale * (gy * -expm1f(lp) - more);
       if (wrong) at_y = G;
@@ -411,6 +628,16 @@ __global__ void __launch_bounds__(kLossThreads, 6) k_scores_grad(Rows<T> R, int 
   if (mine) out[ys[tid]] = Vec<T>::round(at_y);
 }
 
+template <typename T, bool kTop>
+cudaError_t launch_scores(const Rows<T>& R, const ScoreArgs& A, cudaStream_t s) {
+  const int64_t bytes = R.V * (int64_t)sizeof(T);
+  if (R.n >= 600 && bytes <= 32768 && bytes <= 12 * R.n)
+    return launch(k_scores<T, 32, kTop>, (R.n + 7) / 8, kLossThreads, 1, s, R, A, 1);
+  return with_parts(parts_for(R.n, bytes), [&](int parts) {
+    return launch(k_scores<T, kLossThreads, kTop>, R.n * parts, kLossThreads, parts, s, R, A, parts);
+  });
+}
+
 bool ok(const void* x, int32_t dtype, int64_t n, int64_t V, int64_t ld, float scale, const int64_t* y, int32_t given) {
   if (dtype != GMC_F32 && dtype != GMC_BF16 && dtype != GMC_F16) return false;
   const uintptr_t size = dtype == GMC_F32 ? 4 : 2;
@@ -437,10 +664,11 @@ int gmc_token_scores(const void* logits_dev, int32_t dtype, int64_t n, int64_t v
   if (top > 0 && (!top_logp_dev || !top_index_dev)) return GMC_EINVAL;
   const cudaError_t err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    const Rows<T> R{static_cast<const T*>(logits_dev), n, vocab, ld, base_of(scale), targets_dev};
+    const Rows<T> R{static_cast<const T*>(logits_dev), n, vocab, ld, score_base(scale), targets_dev};
     const ScoreArgs A{targets_dev, given, top, logp_dev, entropy_dev, top_logp_dev, top_index_dev,
                       reinterpret_cast<float4*>(stats_dev)};
-    return launch(top ? k_scores<T, true> : k_scores<T, false>, n, kLossThreads, 1, static_cast<cudaStream_t>(stream), R, A);
+    const cudaStream_t q = static_cast<cudaStream_t>(stream);
+    return top ? launch_scores<T, true>(R, A, q) : launch_scores<T, false>(R, A, q);
   });
   return err == cudaSuccess ? GMC_OK : GMC_ECUDA;
 }
@@ -456,7 +684,7 @@ int gmc_token_scores_backward(const void* logits_dev, int32_t dtype, int64_t n, 
   if (!stats_dev || !dlogits_dev) return GMC_EINVAL;
   const cudaError_t err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    const Rows<T> R{static_cast<const T*>(logits_dev), n, vocab, ld, base_of(scale), targets_dev};
+    const Rows<T> R{static_cast<const T*>(logits_dev), n, vocab, ld, score_base(scale), targets_dev};
     const int64_t bytes = vocab * (int64_t)sizeof(T);
     int parts = parts_for(n, bytes);
     while (bytes / parts > 57344) parts *= 2;
