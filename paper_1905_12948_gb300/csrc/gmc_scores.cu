@@ -244,6 +244,7 @@ struct Held {
   uint64_t bound;             // no key at or below it is among the best
   int n;
   uint32_t least[G / 32];     // of a sweep, by warps
+  uint16_t list[G / 32][kBatches * 32];
   float most[kBatches][G];    // the threads' largest logits, by batches
 };
 // The whole team: the list's best `top`, in order, and the bound that follows.
@@ -376,37 +377,59 @@ __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base
         for (int i = 1; i < G / 32; ++i) least = H->least[i] < least ? H->least[i] : least;
       }
       const uint32_t none = order_of(-INFINITY);
-      int batch = 0, done = 0;  // elements of a batch before `done` have been offered
-      for (bool again = true; again;) {
-        uint64_t bound = H->bound;
-        if (least > none && bound < ((uint64_t)least << 32) - 1) bound = ((uint64_t)least << 32) - 1;
-        const float from = bound ? value_of((uint32_t)((bound + 1) >> 32)) : -INFINITY;
+      // The batches of this warp's lanes that reach the bound: four lanes read one of them again, a
+      // vector each, eight batches at a time, the next eight already under way.
+      uint64_t bound = H->bound;
+      if (least > none && bound < ((uint64_t)least << 32) - 1) bound = ((uint64_t)least << 32) - 1;
+      float from = bound ? value_of((uint32_t)((bound + 1) >> 32)) : -INFINITY;
+      uint16_t* list = H->list[tid / 32];
+      int found = 0;
+      for (int i = 0; i < batches; ++i) {
+        const bool hit = H->most[i][tid] >= from;
+        const uint32_t who = __ballot_sync(0xffffffffu, hit);
+        if (hit) list[found + __popc(who & lanemask_lt())] = (uint16_t)(i * G + tid);
+        found += __popc(who);
+      }
+      __syncwarp();
+      auto vector_at = [&](int i) {  // this lane's one of batch i of the list: its first place, -1: none
+        if (i >= found) return (int64_t)-1;
+        const int entry = list[i], u = tid & 3;
+        const int64_t vec = begin + (int64_t)(entry / G) * (U * G) + entry % G + u / 2 * G;
+        return vec < hi ? head + vec * N + (u & 1) * M : (int64_t)-1;
+      };
+      int i = tid % 32 / 4, done = 0;  // elements of this vector before `done` have been offered
+      int64_t at0 = vector_at(i), at1 = vector_at(i + 8);
+      uint4 w = make_uint4(0, 0, 0, 0), next = w;
+      if (at0 >= 0) w = *reinterpret_cast<const uint4*>(x + at0);
+      for (int rest = found;;) {
         bool left = false;
         if (edge > bound) left = !offer(H, edge);
         if (!left) edge = 0;
-        for (; batch < batches && !left; batch += !left) {
-          if (!(H->most[batch][tid] >= from)) continue;
-#pragma unroll 1
-          for (int u = done / M; u < 2 * U && !left; ++u) {
-            const int64_t vec = begin + batch * (U * G) + tid + u / 2 * G;
-            if (vec >= hi) break;
-            const int64_t at0 = head + vec * N + (u & 1) * M;
-            const uint4 w = *reinterpret_cast<const uint4*>(x + at0);
-            if (!(largest<T>(w) >= from)) continue;
+        while (rest > 0) {
+          if (at1 >= 0) next = *reinterpret_cast<const uint4*>(x + at1);
+          if (at0 >= 0 && largest<T>(w) >= from) {
             float f[M];
             Vec<T>::get(w, f);
 #pragma unroll
-            for (int i = 0; i < M; ++i)
-              if (f[i] >= from && !left && done <= u * M + i) {
-                const uint64_t key = key_of(f[i], at0 + i);
+            for (int j = 0; j < M; ++j)
+              if (f[j] >= from && !left && done <= j) {
+                const uint64_t key = key_of(f[j], at0 + j);
                 if (key > bound) left = !offer(H, key);
-                if (!left) done = u * M + i + 1;
+                if (!left) done = j + 1;
               }
           }
-          if (!left) done = 0;
+          if (__any_sync(0xffffffffu, left)) break;
+          rest -= 8;
+          i += 8;
+          done = 0;
+          at0 = at1;
+          w = next;
+          at1 = vector_at(i + 8);
         }
-        again = Team<G>::any(left);
-        if (again) cut(H, top);
+        if (!Team<G>::any(left)) break;
+        cut(H, top);
+        bound = H->bound > bound ? H->bound : bound;
+        from = value_of((uint32_t)((bound + 1) >> 32));
       }
     }
     begin += kBatches * (U * G);

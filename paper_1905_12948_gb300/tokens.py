@@ -88,7 +88,8 @@ def token_logp_backward(logits, targets, stats, dlogp, *, scale: float = 1.0, ou
 
 
 class TokenScores(NamedTuple):
-    """What token_scores gives: None in the place of what was not asked for."""
+    """None in the place of what was not asked for. All share one allocation: clone what is kept
+    beyond the others."""
     logp: object         # float32 of the targets' shape, 0 where a token is not scored
     entropy: object      # (n,) float32
     top_logp: object     # (n, top) float32, larger ones first
