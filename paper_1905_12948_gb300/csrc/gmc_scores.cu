@@ -225,6 +225,7 @@ __device__ __forceinline__ float score_of(const Moments& a, float x, const Base&
 
 // A logit as a number that is larger where it is (zeros of either sign are equal; any NaN is above
 // all), never 0; with its place as one number: lower places first among equal ones.
+__device__ __forceinline__ uint32_t max(uint32_t a, uint32_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return x != x ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
@@ -245,7 +246,7 @@ struct Held {
   int n;
   uint32_t least[G / 32];     // of a sweep, by warps
   uint16_t list[G / 32][kBatches * 32];
-  float most[kBatches][G];    // the threads' largest logits, by batches
+  uint32_t most[kBatches][G]; // the threads' largest logits of a batch's two vectors, their orders' upper halves
 };
 // The whole team: the list's best `top`, in order, and the bound that follows.
 template <int G>
@@ -338,7 +339,7 @@ __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base
   }
   int64_t begin = lo;
   do {
-    float first = -INFINITY, second = -INFINITY;  // the largest logits of the thread's two vectors
+    uint32_t best = 0;  // the order of the thread's largest logit
     int batches = 0;
     for (; batches < kBatches && begin + batches * (U * G) < hi; ++batches) {
       const int64_t i0 = begin + batches * (U * G) + tid;
@@ -357,19 +358,33 @@ __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base
       const float m0 = fmaxf(largest<T>(v[0]), largest<T>(v[1])), m1 = fmaxf(largest<T>(v[2]), largest<T>(v[3]));
       a.add(v, fmaxf(m0, m1), b);
       if constexpr (kTop) {
-        H->most[batches][tid] = fmaxf(m0, m1);
-        first = fmaxf(first, m0);
-        second = fmaxf(second, m1);
+        const uint32_t o0 = order_of(m0), o1 = order_of(m1);
+        H->most[batches][tid] = (o0 & 0xffff0000u) | o1 >> 16;
+        best = max(best, max(o0, o1));
       }
     }
     if constexpr (kTop) {
       uint32_t least;
       if constexpr (G == 32) {
-        least = top <= 32 ? jth_largest(order_of(fmaxf(first, second)), top)
-                          : __reduce_min_sync(0xffffffffu, order_of(fminf(first, second)));
+        if (top <= 8) {
+          least = jth_largest(best, top);
+        } else {
+          // the largest upper half that `top` of the vectors reach
+          uint32_t half = 0;
+          for (uint32_t bit = 0x8000; bit; bit >>= 1) {
+            const uint32_t trial = half | bit;
+            int reach = 0;
+            for (int i = 0; i < batches; ++i) {
+              const uint32_t w = H->most[i][tid];
+              reach += (int)(w >> 16 >= trial) + (int)((w & 0xffff) >= trial);
+            }
+            if (__reduce_add_sync(0xffffffffu, reach) >= top) half = trial;
+          }
+          least = half << 16;
+        }
       } else {
         // (of each warp's so many that the warps have `top` together)
-        const uint32_t of_warp = jth_largest(order_of(fmaxf(first, second)), (top + G / 32 - 1) / (G / 32));
+        const uint32_t of_warp = jth_largest(best, (top + G / 32 - 1) / (G / 32));
         if (tid % 32 == 0) H->least[tid / 32] = of_warp;
         __syncthreads();
         least = H->least[0];
@@ -382,10 +397,12 @@ __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base
       uint64_t bound = H->bound;
       if (least > none && bound < ((uint64_t)least << 32) - 1) bound = ((uint64_t)least << 32) - 1;
       float from = bound ? value_of((uint32_t)((bound + 1) >> 32)) : -INFINITY;
+      const uint32_t from_half = bound ? (uint32_t)((bound + 1) >> 48) : 0;
       uint16_t* list = H->list[tid / 32];
       int found = 0;
       for (int i = 0; i < batches; ++i) {
-        const bool hit = H->most[i][tid] >= from;
+        const uint32_t most = H->most[i][tid];
+        const bool hit = most >> 16 >= from_half || (most & 0xffff) >= from_half;
         const uint32_t who = __ballot_sync(0xffffffffu, hit);
         if (hit) list[found + __popc(who & lanemask_lt())] = (uint16_t)(i * G + tid);
         found += __popc(who);
@@ -449,7 +466,7 @@ __device__ __forceinline__ void write_scores(const ScoreArgs& A, const Moments& 
   const bool empty = a.m == -INFINITY && a.s == 0.f;
   const Shift h = shift_of(a.m, b);
   const float ls = empty ? 0.f : logf(a.s);
-  float e = empty ? 0.f : (float)((double)ls - kLn2 * ((double)a.t / (double)a.s));
+  float e = empty ? 0.f : __fmaf_rn(-(float)kLn2, a.t / a.s, ls);
   e = e < 0.f ? 0.f : e;  // (kExp2Low of S is left: a row of one token has no entropy)
   if (A.entropy) A.entropy[row] = e;
   if (A.stats) A.stats[row] = make_float4(h.h, empty ? INFINITY : ls, e, 0.f);
@@ -561,17 +578,22 @@ __device__ __forceinline__ float grad_one(float x, const ScoreGrad& g, const Bas
   return exp2_fast(e) * __fmaf_rn(low(e), g.c1, g.c0);
 }
 
-// dx of a row, or a part of it, by a block. Bound by memory, read and written.
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads, 6) k_scores_grad(Rows<T> R, int given, const float4* stats, const float* g,
-                                                                 const float* dh, T* dx, int64_t dld, int parts) {
-  constexpr int N = Wide<T>::N, U = kSweepVecs;
-  __shared__ int64_t ys[kMostGiven];
-  __shared__ float gs[kMostGiven];
+// dx of a row, or a part of it, by a block or a warp. Bound by memory, read and written.
+template <typename T, int G>
+__global__ void __launch_bounds__(kLossThreads, G == 32 ? 4 : 5) k_scores_grad(Rows<T> R, int given, const float4* stats,
+                                                                               const float* g, const float* dh, T* dx,
+                                                                               int64_t dld, int parts) {
+  using Te = Team<G>;
+  constexpr int N = Wide<T>::N, U = kSweepVecs, kOwn = G == 32 ? kMostGiven / 32 : 1;
+  __shared__ int64_t all_ys[Te::kRows][kMostGiven];
+  __shared__ float all_gs[Te::kRows][kMostGiven];
   griddep_wait();
   // from the last row to the first: the logits read last are still in the L2 cache
-  const int64_t row = R.n - 1 - blockIdx.x / parts;
-  const int part = (int)(blockIdx.x % parts), tid = (int)threadIdx.x;
+  const int64_t row = R.n - 1 - (blockIdx.x / parts * Te::kRows + Te::of_block());
+  if (G == 32 && row < 0) return;
+  const int part = (int)(blockIdx.x % parts), tid = Te::tid();
+  int64_t* ys = all_ys[Te::of_block()];
+  float* gs = all_gs[Te::of_block()];
   const T* x = R.x + row * R.ld;
   T* out = dx + row * dld;
   const int64_t V = R.V;
@@ -582,59 +604,64 @@ __global__ void __launch_bounds__(kLossThreads, 6) k_scores_grad(Rows<T> R, int 
   const int64_t lo = per * part < nv ? per * part : nv, hi = lo + per < nv ? lo + per : nv;
 
   const float4 st = stats[row];
-  const bool counted = counts(R.y + row * given, given);
-  bool wrong = false, any = false;
-  if (tid < given) {
-    const int64_t y = R.y[row * given + tid];
-    ys[tid] = y;
-    gs[tid] = y >= 0 && g ? g[row * given + tid] : 0.f;
-    wrong = y >= V;
-    any = y >= 0 && gs[tid] != 0.f;
+  float h = dh ? dh[row] : 0.f;
+  bool wrong = false, some = given == 0, any = false;
+  for (int j = tid; j < given; j += G) {
+    const int64_t y = R.y[row * given + j];
+    const float gy = y >= 0 && g ? g[row * given + j] : 0.f;
+    ys[j] = y;
+    gs[j] = gy;
+    wrong |= y >= V;
+    some |= y >= 0;
+    any |= gy != 0.f;
   }
-  wrong = __syncthreads_or(wrong);
-  const float h = dh && counted ? dh[row] : 0.f;
-  any = __syncthreads_or(any) || h != 0.f;
+  wrong = Te::any(wrong);
+  if (!Te::any(some)) h = 0.f;  // the row does not count
+  any = Te::any(any) || h != 0.f;
   const bool skip = !wrong && (!any || st.y == INFINITY);
-  float G = 0.f;
-  for (int j = 0; j < given; ++j) G += gs[j];
-  if (wrong) G = __uint_as_float(kNan);
+  float sum = 0.f;
+  for (int j = 0; j < given; ++j) sum += gs[j];
+  if (wrong) sum = __uint_as_float(kNan);
   const float k = -R.b.scale * expf(-st.y);
-  const ScoreGrad q{shift_of(st.x, R.b), k * (G + h * (st.z - st.y)), k * h * (float)kLn2};
+  const ScoreGrad q{shift_of(st.x, R.b), k * (sum + h * (st.z - st.y)), k * h * (float)kLn2};
 
   // The given tokens in this part, taken before their places are written (out may be x):
   // g_y (1 - p_y) - p_y (G - g_y + h (lp_y + H)), the first without cancellation.
-  float at_y = 0.f;
-  bool mine = false;
-  if (tid < given && !skip) {
-    const int64_t y = ys[tid], v = y >= head ? (y - head) / N : -1;
-    mine = y >= 0 && y < V && (y < head || v >= nv ? part == 0 : v >= lo && v < hi);
+  float at_y[kOwn];
+  bool mine[kOwn];
+#pragma unroll
+  for (int o = 0; o < kOwn; ++o) {
+    const int own = tid + o * G;
+    mine[o] = false;
+    if (own >= given || skip) continue;
+    const int64_t y = ys[own], v = y >= head ? (y - head) / N : -1;
+    mine[o] = y >= 0 && y < V && (y < head || v >= nv ? part == 0 : v >= lo && v < hi);
+    if (!mine[o]) continue;
     float gy = 0.f;
     for (int j = 0; j < given; ++j) {
-      if (ys[j] == y) gy += gs[j];
-      if (j < tid && ys[j] == y) mine = false;
+      if (ys[j] != y) continue;
+      gy += gs[j];
+      if (j < own) mine[o] = false;  // (the first of equal ones writes)
     }
-    if (mine) {
-      const float v = Vec<T>::one(x[y]);
-      const float lp = q.h.far ? (v - q.h.h) * R.b.scale - st.y
-                               : (float)(((double)v * (double)R.b.c - (double)q.h.hc) * kLn2 - ((double)st.y + kExp2Low));
-      const float p = lp == -INFINITY ? 0.f : expf(lp), more = p == 0.f ? 0.f : p * (G - gy + h * (lp + st.z));
-      at_y = R.b.scale * (gy * -expm1f(lp) - more);
-      if (wrong) at_y = G;
-    }
+    const float xy = Vec<T>::one(x[y]);
+    const float lp = q.h.far ? (xy - q.h.h) * R.b.scale - st.y
+                             : (float)(((double)xy * (double)R.b.c - (double)q.h.hc) * kLn2 - ((double)st.y + kExp2Low));
+    const float p = lp == -INFINITY ? 0.f : expf(lp), more = p == 0.f ? 0.f : p * (sum - gy + h * (lp + st.z));
+    at_y[o] = wrong ? sum : R.b.scale * (gy * -expm1f(lp) - more);
   }
-  __syncthreads();
+  if (given) Te::sync();
   const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(out)) & 31) == 0;
-  for (int64_t i0 = lo + tid; i0 < hi; i0 += U * kLossThreads) {
+  for (int64_t i0 = lo + tid; i0 < hi; i0 += U * G) {
     Wide<T> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t i = i0 + u * kLossThreads;
+      const int64_t i = i0 + u * G;
       v[u].a = v[u].b = make_uint4(0, 0, 0, 0);
       if (!skip && i < hi) v[u] = load_wide(x + head + i * N, true);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t i = i0 + u * kLossThreads;
+      const int64_t i = i0 + u * G;
       if (i >= hi) continue;
       if (!skip) {
         v[u].a = grad_vec<T>(v[u].a, q, R.b);
@@ -647,14 +674,19 @@ __global__ void __launch_bounds__(kLossThreads, 6) k_scores_grad(Rows<T> R, int 
     const int64_t j = tid < head ? (int64_t)tid : V - tail + (tid - head);
     out[j] = Vec<T>::round(skip ? 0.f : grad_one<T>(Vec<T>::one(x[j]), q, R.b));
   }
-  __syncthreads();
-  if (mine) out[ys[tid]] = Vec<T>::round(at_y);
+  if (given) Te::sync();
+#pragma unroll
+  for (int o = 0; o < kOwn; ++o)
+    if (mine[o]) out[ys[tid + o * G]] = Vec<T>::round(at_y[o]);
 }
+
+constexpr int64_t kWarpScores = 32768, kWarpGrad = 18432;  // bytes of a row at most
+bool by_warps(int64_t n, int64_t row_bytes, int64_t most) { return n >= 600 && row_bytes <= most && row_bytes <= 12 * n; }
 
 template <typename T, bool kTop>
 cudaError_t launch_scores(const Rows<T>& R, const ScoreArgs& A, cudaStream_t s) {
   const int64_t bytes = R.V * (int64_t)sizeof(T);
-  if (R.n >= 600 && bytes <= 32768 && bytes <= 12 * R.n)
+  if (by_warps(R.n, bytes, kWarpScores))
     return launch(k_scores<T, 32, kTop>, (R.n + 7) / 8, kLossThreads, 1, s, R, A, 1);
   return with_parts(parts_for(R.n, bytes), [&](int parts) {
     return launch(k_scores<T, kLossThreads, kTop>, R.n * parts, kLossThreads, parts, s, R, A, parts);
@@ -709,11 +741,15 @@ int gmc_token_scores_backward(const void* logits_dev, int32_t dtype, int64_t n, 
     using T = decltype(t);
     const Rows<T> R{static_cast<const T*>(logits_dev), n, vocab, ld, score_base(scale), targets_dev};
     const int64_t bytes = vocab * (int64_t)sizeof(T);
+    const float4* st = reinterpret_cast<const float4*>(stats_dev);
+    const cudaStream_t q = static_cast<cudaStream_t>(stream);
+    if (by_warps(n, bytes, kWarpGrad))
+      return launch(k_scores_grad<T, 32>, (n + 7) / 8, kLossThreads, 1, q, R, (int)given, st, dlogp_dev, dentropy_dev,
+                    static_cast<T*>(dlogits_dev), dld, 1);
     int parts = parts_for(n, bytes);
     while (bytes / parts > 57344) parts *= 2;
-    return launch(k_scores_grad<T>, n * parts, kLossThreads, 1, static_cast<cudaStream_t>(stream), R, (int)given,
-                  reinterpret_cast<const float4*>(stats_dev), dlogp_dev, dentropy_dev, static_cast<T*>(dlogits_dev), dld,
-                  parts);
+    return launch(k_scores_grad<T, kLossThreads>, n * parts, kLossThreads, 1, q, R, (int)given, st, dlogp_dev, dentropy_dev,
+                  static_cast<T*>(dlogits_dev), dld, parts);
   });
   return err == cudaSuccess ? GMC_OK : GMC_ECUDA;
 }
