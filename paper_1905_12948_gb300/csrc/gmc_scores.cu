@@ -80,8 +80,12 @@ __device__ __forceinline__ Moments merge(Moments a, Moments o, const Base& b) {
   return r;
 }
 template <typename T>
+__device__ __forceinline__ uint32_t largest_word(const uint4& v) {
+  return Vec<T>::top(Vec<T>::top(v.x, v.y), Vec<T>::top(v.z, v.w));
+}
+template <typename T>
 __device__ __forceinline__ float largest(const uint4& v) {
-  return Vec<T>::top_of(Vec<T>::top(Vec<T>::top(v.x, v.y), Vec<T>::top(v.z, v.w)));
+  return Vec<T>::top_of(largest_word<T>(v));
 }
 // The word's two values, no less than those of `floor` (NaN stays NaN).
 __device__ __forceinline__ uint32_t at_least(uint32_t w, uint32_t floor, __nv_bfloat16) {
@@ -109,8 +113,17 @@ struct Running {
   __device__ __forceinline__ void shift_to(float top, const Base& b) {
     split_sums();
     const float m = fmaxf(a.m, top);
-    h = shift_of(m, b);
-    move<T>(&a, h, b);
+    const Shift to = shift_of(m, b);
+    if (a.m == -INFINITY) {
+      // nothing but -inf and NaN so far: sums of 0 or NaN, at any shift
+    } else if (!to.far && !h.far) {
+      const float d = h.hc - to.hc, f = exp2_fast(d);
+      a.t = (a.t + d * a.s) * f;
+      a.s *= f;
+    } else {
+      move<T>(&a, to, b);
+    }
+    h = to;
     a.m = m;
     limit = h.far ? m : (h.hc + kAbove) / b.c;
     s = pair_of(a.s, 0.f);
@@ -196,15 +209,16 @@ __device__ __forceinline__ Moments warp_merge(Moments a, const Base& b) {
   r.t = warp_sum(a.t);
   return r;
 }
+// (by the warps that need it: the others may go on)
 template <typename T, int G>
-__device__ __forceinline__ Moments team_merge(Moments a, const Base& b) {
+__device__ __forceinline__ Moments team_merge(Moments a, const Base& b, bool needed) {
   a = warp_merge<T>(a, b);
   if constexpr (G != 32) {
     __shared__ Moments ws[G / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (lane == 0) ws[warp] = a;
     __syncthreads();
-    a = warp_merge<T>(lane < G / 32 ? ws[lane] : Moments(), b);
+    if (needed) a = warp_merge<T>(lane < G / 32 ? ws[lane] : Moments(), b);
   }
   return a;
 }
@@ -225,7 +239,6 @@ __device__ __forceinline__ float score_of(const Moments& a, float x, const Base&
 
 // A logit as a number that is larger where it is (zeros of either sign are equal; any NaN is above
 // all), never 0; with its place as one number: lower places first among equal ones.
-__device__ __forceinline__ uint32_t max(uint32_t a, uint32_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.f);
   return x != x ? 0xffffffffu : (u & 0x80000000u) ? ~u : u | 0x80000000u;
@@ -246,7 +259,7 @@ struct Held {
   int n;
   uint32_t least[G / 32];     // of a sweep, by warps
   uint16_t list[G / 32][kBatches * 32];
-  uint32_t most[kBatches][G]; // the threads' largest logits of a batch's two vectors, their orders' upper halves
+  uint32_t most[kBatches][G]; // the threads' marks, by batches
 };
 // The whole team: the list's best `top`, in order, and the bound that follows.
 template <int G>
@@ -262,6 +275,7 @@ __device__ __forceinline__ void cut(Held<G>* H, int top) {
     rank[u] = 0;
   }
   if (tid < n)
+#pragma unroll 4
     for (int i = 0; i < n; ++i) {
       const uint64_t other = H->key[i];
 #pragma unroll
@@ -284,6 +298,58 @@ __device__ __forceinline__ bool offer(Held<G>* H, uint64_t key) {
   if (at < Held<G>::N) H->key[at] = key;
   return at < Held<G>::N;
 }
+// What a batch leaves behind of a thread's two vectors: of 16-bit types both vectors' largest logits, of float
+// the larger one.
+template <typename T>
+struct Mark {
+  static constexpr uint32_t kNone = Vec<T>::kLow;
+  // of two words of pairwise largest logits
+  __device__ static uint32_t of(uint32_t t0, uint32_t t1) {
+    return Vec<T>::top(__byte_perm(t0, t1, 0x5410), __byte_perm(t0, t1, 0x7632));
+  }
+  __device__ static bool reaches(uint32_t w, uint32_t from);
+  // upper halves of the orders of its logits, and back
+  __device__ static uint32_t ordered(uint32_t w) {
+    const uint32_t sign = (w >> 15 & 0x00010001u) * 0x7fffu;  // 0x7fff where negative
+    return w ^ (sign | 0x80008000u);
+  }
+  __device__ static uint32_t raw(uint32_t w) {
+    const uint32_t sign = (~w >> 15 & 0x00010001u) * 0x7fffu;
+    return w ^ (sign | 0x80008000u);
+  }
+  __device__ static int reach(uint32_t ordered, uint32_t half) {
+    return (int)(ordered >> 16 >= half) + (int)((ordered & 0xffff) >= half);
+  }
+  // the order of the logit whose order's upper half that is
+  __device__ static uint32_t order(uint32_t half) {
+    const uint16_t bits = (uint16_t)raw(half);
+    return order_of(Vec<T>::one(*reinterpret_cast<const T*>(&bits)));
+  }
+  __device__ static uint32_t word(float from) {
+    const T t = Vec<T>::round(from);
+    const uint32_t b = *reinterpret_cast<const uint16_t*>(&t);
+    return b << 16 | b;
+  }
+};
+template <>
+__device__ __forceinline__ bool Mark<__nv_bfloat16>::reaches(uint32_t w, uint32_t from) {
+  return __hge2_mask(*reinterpret_cast<__nv_bfloat162*>(&w), *reinterpret_cast<__nv_bfloat162*>(&from)) != 0;
+}
+template <>
+__device__ __forceinline__ bool Mark<__half>::reaches(uint32_t w, uint32_t from) {
+  return __hge2_mask(*reinterpret_cast<__half2*>(&w), *reinterpret_cast<__half2*>(&from)) != 0;
+}
+template <>
+struct Mark<float> {
+  static constexpr uint32_t kNone = Vec<float>::kLow;
+  __device__ static uint32_t of(uint32_t t0, uint32_t t1) { return Vec<float>::top(t0, t1); }
+  __device__ static bool reaches(uint32_t w, uint32_t from) { return __uint_as_float(w) >= __uint_as_float(from); }
+  __device__ static uint32_t ordered(uint32_t w) { return order_of(__uint_as_float(w)); }
+  __device__ static uint32_t raw(uint32_t w) { return __float_as_uint(value_of(w)); }
+  __device__ static int reach(uint32_t ordered, uint32_t half) { return ordered >> 16 >= half; }
+  __device__ static uint32_t order(uint32_t half) { return half << 16; }
+  __device__ static uint32_t word(float from) { return __float_as_uint(from); }
+};
 // The j-th largest of a warp's numbers.
 __device__ __forceinline__ uint32_t jth_largest(uint32_t u, int j) {
   for (int i = 1; i < j; ++i) {
@@ -339,7 +405,7 @@ __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base
   }
   int64_t begin = lo;
   do {
-    uint32_t best = 0;  // the order of the thread's largest logit
+    uint32_t best = Mark<T>::kNone;
     int batches = 0;
     for (; batches < kBatches && begin + batches * (U * G) < hi; ++batches) {
       const int64_t i0 = begin + batches * (U * G) + tid;
@@ -355,36 +421,34 @@ __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base
         }
       }
       static_assert(U == 2, "two vectors a thread");
-      const float m0 = fmaxf(largest<T>(v[0]), largest<T>(v[1])), m1 = fmaxf(largest<T>(v[2]), largest<T>(v[3]));
-      a.add(v, fmaxf(m0, m1), b);
+      const uint32_t mark = Mark<T>::of(Vec<T>::top(largest_word<T>(v[0]), largest_word<T>(v[1])),
+                                        Vec<T>::top(largest_word<T>(v[2]), largest_word<T>(v[3])));
+      a.add(v, Vec<T>::top_of(mark), b);
       if constexpr (kTop) {
-        const uint32_t o0 = order_of(m0), o1 = order_of(m1);
-        H->most[batches][tid] = (o0 & 0xffff0000u) | o1 >> 16;
-        best = max(best, max(o0, o1));
+        H->most[batches][tid] = mark;
+        best = Vec<T>::top(best, mark);
       }
     }
     if constexpr (kTop) {
       uint32_t least;
       if constexpr (G == 32) {
         if (top <= 8) {
-          least = jth_largest(best, top);
+          least = jth_largest(order_of(Vec<T>::top_of(best)), top);
         } else {
-          // the largest upper half that `top` of the vectors reach
+          // the largest upper half of an order that `top` of the vectors reach
+          for (int i = 0; i < batches; ++i) H->most[i][tid] = Mark<T>::ordered(H->most[i][tid]);
           uint32_t half = 0;
           for (uint32_t bit = 0x8000; bit; bit >>= 1) {
-            const uint32_t trial = half | bit;
             int reach = 0;
-            for (int i = 0; i < batches; ++i) {
-              const uint32_t w = H->most[i][tid];
-              reach += (int)(w >> 16 >= trial) + (int)((w & 0xffff) >= trial);
-            }
-            if (__reduce_add_sync(0xffffffffu, reach) >= top) half = trial;
+            for (int i = 0; i < batches; ++i) reach += Mark<T>::reach(H->most[i][tid], half | bit);
+            if (__reduce_add_sync(0xffffffffu, reach) >= top) half |= bit;
           }
-          least = half << 16;
+          for (int i = 0; i < batches; ++i) H->most[i][tid] = Mark<T>::raw(H->most[i][tid]);
+          least = half ? Mark<T>::order(half) : 0;
         }
       } else {
         // (of each warp's so many that the warps have `top` together)
-        const uint32_t of_warp = jth_largest(best, (top + G / 32 - 1) / (G / 32));
+        const uint32_t of_warp = jth_largest(order_of(Vec<T>::top_of(best)), (top + G / 32 - 1) / (G / 32));
         if (tid % 32 == 0) H->least[tid / 32] = of_warp;
         __syncthreads();
         least = H->least[0];
@@ -397,12 +461,11 @@ __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base
       uint64_t bound = H->bound;
       if (least > none && bound < ((uint64_t)least << 32) - 1) bound = ((uint64_t)least << 32) - 1;
       float from = bound ? value_of((uint32_t)((bound + 1) >> 32)) : -INFINITY;
-      const uint32_t from_half = bound ? (uint32_t)((bound + 1) >> 48) : 0;
+      const uint32_t from_word = Mark<T>::word(from);
       uint16_t* list = H->list[tid / 32];
       int found = 0;
       for (int i = 0; i < batches; ++i) {
-        const uint32_t most = H->most[i][tid];
-        const bool hit = most >> 16 >= from_half || (most & 0xffff) >= from_half;
+        const bool hit = Mark<T>::reaches(H->most[i][tid], from_word);
         const uint32_t who = __ballot_sync(0xffffffffu, hit);
         if (hit) list[found + __popc(who & lanemask_lt())] = (uint16_t)(i * G + tid);
         found += __popc(who);
@@ -491,9 +554,23 @@ __global__ void __launch_bounds__(kLossThreads, G == 32 && kTop ? 4 : 5) k_score
   }
   if (G != 32 && parts > 1) cluster_arrive();
   const T* x = R.x + row * R.ld;
+  // the given tokens' logits, read while there is time; by threads that have no alternative to finish
+  constexpr int kOwn = G == 32 ? kMostGiven / 32 : 1;
+  const int mine = G == 32 ? tid : tid - kMostTop;
+  float xy[kOwn];
+  bool scored[kOwn];
+#pragma unroll
+  for (int o = 0; o < kOwn; ++o) {
+    const int j = mine + o * G;
+    const int64_t t = j >= 0 && j < A.given ? y[j] : -1;
+    scored[o] = t >= 0;
+    xy[o] = t >= 0 ? target_logit(x, R.V, t) : 0.f;
+  }
   Held<G>* H = &held[kTop ? Te::of_block() : 0];
   Moments a = score_sweep<T, G, kTop>(x, R.V, R.b, part, parts, A.top, H);
-  a = team_merge<T, G>(a, R.b);
+  // alternatives are finished by the first two warps, given tokens by the next two, the row by the last
+  const int warp = (int)threadIdx.x / 32;
+  a = team_merge<T, G>(a, R.b, warp == G / 32 - 1 || (warp < 4 && warp * 32 < (warp < 2 ? A.top : A.given + kMostTop)) || warp == 0);
   const uint64_t* best = H->key;
   if (kTop) cut(H, A.top);
   if (G != 32 && parts > 1) {
@@ -536,9 +613,10 @@ __global__ void __launch_bounds__(kLossThreads, G == 32 && kTop ? 4 : 5) k_score
       __syncthreads();
     }
   }
-  for (int j = tid; j < A.given; j += G) {
-    const int64_t t = y[j];
-    if (A.logp) A.logp[row * A.given + j] = t < 0 ? 0.f : score_of(a, target_logit(x, R.V, t), R.b);
+#pragma unroll
+  for (int o = 0; o < kOwn; ++o) {
+    const int j = mine + o * G;
+    if (j >= 0 && j < A.given && A.logp) A.logp[row * A.given + j] = scored[o] ? score_of(a, xy[o], R.b) : 0.f;
   }
   if (kTop)
     for (int j = tid; j < A.top; j += G) {
@@ -546,7 +624,7 @@ __global__ void __launch_bounds__(kLossThreads, G == 32 && kTop ? 4 : 5) k_score
       A.top_logp[row * A.top + j] = score_of(a, value_of((uint32_t)(key >> 32)), R.b);
       A.top_index[row * A.top + j] = a.s != a.s ? -1 : place_of(key);
     }
-  if (tid == 0) write_scores(A, a, row, R.b);
+  if (tid == G - 1) write_scores(A, a, row, R.b);
 }
 
 // What a row's gradient is made of, in exponents: p_v (G + h (lp_v + H)) s = 2^e (c0 + c1 e).
