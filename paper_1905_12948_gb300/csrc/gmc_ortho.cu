@@ -51,58 +51,71 @@ struct Halves2 {
 };
 // What this thread wrote is seen by copies that follow (another launch's).
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
-__device__ __forceinline__ void two_halves(float x, __half* hi, __half* lo) {
-  *hi = __float2half_rn(x);
-  *lo = __float2half_rn(x - __half2float(*hi));
+// Two numbers as sums of two halves each.
+__device__ __forceinline__ void two_halves(float x, float y, __half2* hi, __half2* lo) {
+  *hi = __floats2half2_rn(x, y);
+  const float2 back = __half22float2(*hi);
+  *lo = __floats2half2_rn(x - back.x, y - back.y);
 }
 
-// v with a power of two that puts its norm near 1 taken out, in two steps (either may be large).
+// What makes v of a matrix X: a power of two that puts the norm near 1 is taken out, in two steps (either
+// may be large), then the rest, 1 / [1, 2), in two words: an error of the norm is one of all singular values,
+// which five steps may multiply by tens.
 struct Scaled {
-  float p1, p2, q;  // x = ((v p1) p2) q
+  float p1, p2, q, low;
+  __device__ __forceinline__ float operator()(float v) const {
+    v = v * p1 * p2;
+    return __fmaf_rn(v, q, v * low);
+  }
 };
 __device__ __forceinline__ float power2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
-__device__ __forceinline__ Scaled scaled_by(double size) {
-  if (!(size < (double)INFINITY)) return Scaled{1.f, 1.f, __uint_as_float(kNan)};
-  if (size == 0.) return Scaled{1.f, 1.f, 0.f};
-  int e;
-  const double f = frexp(size, &e);
-  return Scaled{power2(-(e / 2)), power2(-(e - e / 2)), (float)((double)kX / f)};
+__device__ __forceinline__ Scaled scaled_by(double squares) {
+  const uint64_t bits = (uint64_t)__double_as_longlong(squares);
+  const int biased = (int)(bits >> 52);  // (no sum of squares of floats is below 2^-298 but 0)
+  if (biased >= 0x7ff) return Scaled{1.f, 1.f, __uint_as_float(kNan), 0.f};
+  if (biased == 0) return Scaled{1.f, 1.f, 0.f, 0.f};
+  const int e = (biased - 1023) >> 1;  // squares = 4^e r, r in [1, 4)
+  const double r = __longlong_as_double((long long)((bits & 0xfffffffffffffull) | (uint64_t)(biased - 2 * e) << 52));
+  // r^(-1/2): that of 32 bits, off by some 2^-23, and a step of Newton's
+  const double y = (double)rsqrtf((float)r), q = (double)kX * __fma_rn(0.5 * y, __fma_rn(-(r * y), y, 1.), y);
+  return Scaled{power2(-(e / 2)), power2(-(e - e / 2)), (float)q, (float)(q - (double)(float)q)};
 }
 
 // The squares of N numbers added up: in 32 bits, with a power of two taken out where they would
 // not fit, so that the sum is the same at any magnitude.
 template <int N>
-__device__ __forceinline__ double squares(const float* f) {
-  float s = 0.f, most = 0.f;
+__device__ __forceinline__ float sum_squares(const float* f) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    s = __fmaf_rn(f[i], f[i], s);
-    most = fmaxf(most, fabsf(f[i]));
-  }
+  for (int i = 0; i < N; ++i) s[i % 4] = __fmaf_rn(f[i], f[i], s[i % 4]);
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+template <int N>
+__device__ __forceinline__ double squares(float* f) {
+  float s = sum_squares<N>(f);
   if (s > 0x1p-90f && s < 0x1p100f) return (double)s;
+  float most = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(f[i]));
   if (s != s || most == INFINITY) return (double)s;
   if (most == 0.f) return 0.;
   int e;
   frexpf(most, &e);
   const float p1 = power2(-(e / 2)), p2 = power2(-(e - e / 2));
-  s = 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float v = f[i] * p1 * p2;
-    s = __fmaf_rn(v, v, s);
-  }
-  return ldexp((double)s, 2 * e);
+  for (int i = 0; i < N; ++i) f[i] = f[i] * p1 * p2;
+  return ldexp((double)sum_squares<N>(f), 2 * e);
 }
 // Sums of squares of parts of each matrix G (as it is given: m rows of n), in a fixed order: warps
 // take rows, or pieces of 4,096 elements of them.
 constexpr int kMostSizeParts = 256, kSizePiece = 4096;
 template <typename T>
 __global__ void __launch_bounds__(256) k_size(const T* g, int64_t sk, int64_t ld, int64_t m, int64_t n, double* part,
-                                              uint32_t* gave_up) {
+                                              uint32_t* counts) {
   constexpr int N = Vec<T>::N;
   __shared__ double ws[8];
   griddep_wait();
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *gave_up = 0;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) counts[threadIdx.x] = 0;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int64_t pieces = (n + kSizePiece - 1) / kSizePiece;
   double s = 0.;
@@ -114,14 +127,18 @@ __global__ void __launch_bounds__(256) k_size(const T* g, int64_t sk, int64_t ld
     if (head > len) head = len;
     const int nv = (len - head) / N, tail = len - head - nv * N;
     if (lane < head + tail) {
-      const float v = Vec<T>::one(x[lane < head ? lane : len - tail + (lane - head)]);
+      float v = Vec<T>::one(x[lane < head ? lane : len - tail + (lane - head)]);
       s += squares<1>(&v);
     }
-#pragma unroll 4
-    for (int i = lane; i < nv; i += 32) {
-      float f[N];
-      Vec<T>::get(*reinterpret_cast<const uint4*>(x + head + i * N), f);
-      s += squares<N>(f);
+    for (int i = lane; i < nv; i += 4 * 32) {
+      uint4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        v[u] = i + u * 32 < nv ? *reinterpret_cast<const uint4*>(x + head + (i + u * 32) * N) : make_uint4(0, 0, 0, 0);
+      float f[4 * N];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) Vec<T>::get(v[u], f + u * N);
+      s += squares<4 * N>(f);
     }
   }
   s = warp_sum(s);
@@ -132,14 +149,11 @@ __global__ void __launch_bounds__(256) k_size(const T* g, int64_t sk, int64_t ld
     part[blockIdx.y * kMostSizeParts + blockIdx.x] = s;
   }
 }
-__device__ __forceinline__ double size_of(const double* part, int parts) {  // by a block of 256
-  __shared__ double ws[8];
-  const double s = warp_sum((int)threadIdx.x < parts ? part[threadIdx.x] : 0.);
-  if (threadIdx.x % 32 == 0) ws[threadIdx.x / 32] = s;
-  __syncthreads();
-  double t = 0.;
-  for (int i = 0; i < 8; ++i) t += ws[i];
-  return sqrt(t);
+// The parts of a matrix added up, by a warp, in a fixed order.
+__device__ __forceinline__ double squares_of(const double* part, int parts) {
+  double s = 0.;
+  for (int i = (int)threadIdx.x % 32; i < parts; i += 32) s += part[i];
+  return warp_sum(s);
 }
 // The four pieces (8 columns of a row) of a block of halves that are a thread's: neighbours along a row
 // of G, whichever way X lies.
@@ -154,36 +168,44 @@ template <typename T, bool kTurned>
 __global__ void __launch_bounds__(256) k_first(const T* g, int64_t sk, int64_t ld, Shape S, const double* part, int parts,
                                                Halves2 X) {
   griddep_wait();
-  const int64_t k = blockIdx.y, xc = S.np / 64, rb = blockIdx.x / xc, cb = blockIdx.x % xc;
-  const Scaled by = scaled_by(size_of(part + k * kMostSizeParts, parts));
-  const int64_t to = k * S.x() + blockIdx.x * (int64_t)kBlock;
+  const int64_t k = blockIdx.y, xc = S.np / 64, blocks = S.x() / kBlock;
+  const Scaled by = scaled_by(squares_of(part + k * kMostSizeParts, parts));
   const bool vectors = !kTurned && ((reinterpret_cast<uintptr_t>(g) | (uintptr_t)(ld * sizeof(T)) | (uintptr_t)(sk * sizeof(T))) & 15) == 0;
+  for (int64_t block = blockIdx.x; block < blocks; block += gridDim.x) {
+    const int64_t rb = block / xc, cb = block % xc, to = k * S.x() + block * kBlock;
+    float f[4][8];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    int row, piece;
-    piece_of<kTurned>(u, &row, &piece);
-    const int64_t i = rb * 128 + row, j0 = cb * 64 + piece * 8;
-    float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (i < S.m) {
+    for (int u = 0; u < 4; ++u) {
+      int row, piece;
+      piece_of<kTurned>(u, &row, &piece);
+      const int64_t i = rb * 128 + row, j0 = cb * 64 + piece * 8;
       const T* x = g + k * sk + (kTurned ? j0 * ld + i : i * ld + j0);
-      if (vectors && j0 + 8 <= S.n) {
+      if (vectors && i < S.m && j0 + 8 <= S.n) {
 #pragma unroll
-        for (int v = 0; v < 8; v += Vec<T>::N) Vec<T>::get(*reinterpret_cast<const uint4*>(x + v), f + v);
+        for (int v = 0; v < 8; v += Vec<T>::N) Vec<T>::get(*reinterpret_cast<const uint4*>(x + v), f[u] + v);
       } else {
 #pragma unroll
-        for (int v = 0; v < 8; ++v)
-          if (j0 + v < S.n) f[v] = Vec<T>::one(x[v * (kTurned ? ld : 1)]);
+        for (int v = 0; v < 8; ++v) f[u][v] = i < S.m && j0 + v < S.n ? Vec<T>::one(x[v * (kTurned ? ld : 1)]) : 0.f;
       }
-#pragma unroll
-      for (int v = 0; v < 8; ++v)
-        if (j0 + v < S.n) f[v] = f[v] * by.p1 * by.p2 * by.q;
     }
-    alignas(16) __half hi[8], lo[8];
 #pragma unroll
-    for (int v = 0; v < 8; ++v) two_halves(f[v], hi + v, lo + v);
-    const uint32_t in = piece_at((uint32_t)row, (uint32_t)piece);
-    *reinterpret_cast<uint4*>(reinterpret_cast<char*>(X.hi + to) + in) = *reinterpret_cast<uint4*>(hi);
-    *reinterpret_cast<uint4*>(reinterpret_cast<char*>(X.lo + to) + in) = *reinterpret_cast<uint4*>(lo);
+    for (int u = 0; u < 4; ++u) {
+      int row, piece;
+      piece_of<kTurned>(u, &row, &piece);
+      const int64_t i = rb * 128 + row, j0 = cb * 64 + piece * 8;
+      alignas(16) __half2 hi[4], lo[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        float x[2];
+#pragma unroll
+        for (int o = 0; o < 2; ++o)  // (what pads a matrix that is NaN stays 0)
+          x[o] = i < S.m && j0 + 2 * v + o < S.n ? by(f[u][2 * v + o]) : 0.f;
+        two_halves(x[0], x[1], hi + v, lo + v);
+      }
+      const uint32_t in = piece_at((uint32_t)row, (uint32_t)piece);
+      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(X.hi + to) + in) = *reinterpret_cast<uint4*>(hi);
+      *reinterpret_cast<uint4*>(reinterpret_cast<char*>(X.lo + to) + in) = *reinterpret_cast<uint4*>(lo);
+    }
   }
   fence_proxy_async_all();
 }
@@ -258,6 +280,24 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatil
   return true;
 }
 
+// Until a count that others raise has come to `to`.
+__device__ __forceinline__ bool wait_count(const uint32_t* p, uint32_t to, volatile uint32_t* dead) {
+  uint64_t t0 = 0;
+  for (uint32_t n = 1;; ++n) {
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    if (v >= to) return true;
+    if (n % 64) continue;
+    if (*dead) return false;
+    const uint64_t now = global_ns();
+    if (t0 == 0) t0 = now;
+    if (now - t0 > kWaitLimitNs) {
+      *dead = 1;
+      return false;
+    }
+  }
+}
+
 template <int CG>
 __device__ __forceinline__ void tmem_alloc(uint32_t* to, uint32_t columns) {
   if constexpr (CG == 1) {
@@ -298,18 +338,29 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
                  "h"((uint16_t)3)
                  : "memory");
 }
-__device__ __forceinline__ void tmem_load32(uint32_t at, float* f) {
+__device__ __forceinline__ void tmem_load16(uint32_t at, float* f) {
   uint32_t* r = reinterpret_cast<uint32_t*>(f);
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(at));
 }
-__device__ __forceinline__ void tmem_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_store16(uint32_t at, const float* f) {
+  const uint32_t* r = reinterpret_cast<const uint32_t*>(f);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// (The registers are named: nothing may look at them before.)
+__device__ __forceinline__ void tmem_loaded(float (&f)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]), "+f"(f[8]),
+                 "+f"(f[9]), "+f"(f[10]), "+f"(f[11]), "+f"(f[12]), "+f"(f[13]), "+f"(f[14]), "+f"(f[15])::"memory");
+}
 // Shared memory of a factor: rows of 128 bytes, eight of them (1 KB) a group; `stride` bytes
 // from one 64-column block to the next where the factor's rows are the sum's index.
 __device__ __forceinline__ uint64_t factor(uint32_t addr, uint32_t stride) {
@@ -321,7 +372,11 @@ __device__ __forceinline__ void bulk_store(void* to, const void* from, uint32_t 
                : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void bulk_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+// Until all stores but the last kLeft have read what they store.
+template <int kLeft>
+__device__ __forceinline__ void bulk_read() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory");
+}
 __device__ __forceinline__ void bulk_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // A copy of 64 rows of 128 bytes; row `at` of the workspace. With pairs of blocks the bytes are counted by the barrier of the
@@ -347,11 +402,17 @@ enum Phase { kGram, kSquare, kUpdate };  // A = X X';  B = b A + c A^2;  X <- a 
 struct ProductArgs {
   Shape S;
   int64_t K;
-  const __half* base;  // of the workspace, which the map is of
-  Halves2 x, o, r, y;  // X, O, R; the new X
-  float *d, *e;        // diagonals of A and B, mp each
-  float a, b, c;
+  const __half* base;   // of the workspace, which the map is of
+  Halves2 x[2], o, r;   // X before and after each step, in turn; O, R
+  float *d, *e;         // diagonals of A and B, mp each
+  int begin, end;       // phases of this launch, three a step
+  uint32_t* phases;     // counts the blocks that are done with each
   uint32_t* gave_up;
+  float coef[3 * kMostSteps];
+};
+template <int P>
+struct PhaseOf {
+  static constexpr int value = P;
 };
 
 constexpr int kFactorBytes = 16384;  // of a stage: 128 rows, or columns, by 64
@@ -407,13 +468,14 @@ struct Tiles {
   }
 };
 
-// One product of all K matrices. A block holds 128 rows of the left factor and 128 rows (columns
+// The phases of all steps, with a barrier over the grid between two of them (the blocks are resident together);
+// or one of them. A block holds 128 rows of the left factor and 128 rows (columns
 // in kUpdate) of the right one, 64 of the sum at a time; a pair of blocks (CG = 2) shares them, and its tile
 // is 256 x 256, 128 x 256 of it in each block's tensor memory; CG = 1: 128 x 128.
 // Warp 0 issues the copies, warp 1 the products; the others read the sums back (the tensor memory
 // holds two tiles) and put the new halves where the next product takes them from.
-template <int CG, bool kFine, int kPhase>
-__global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_product(const __grid_constant__ CUtensorMap map, ProductArgs P) {
+template <int CG, bool kFine>
+__global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const __grid_constant__ CUtensorMap map, const __grid_constant__ ProductArgs P) {
   using Pl = Plan<CG, kFine>;
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -425,9 +487,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_product(const 
 
   const Shape S = P.S;
   const int64_t xc = S.np / 64, oc = S.mp / 64;  // blocks in a row of blocks
-  const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
   const int64_t first = blockIdx.x / CG, step = gridDim.x / CG;
-  const int kblocks = (int)(((kPhase == kGram ? S.n : S.m) + 63) / 64);
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < Pl::kStages; ++i) {
@@ -454,46 +514,69 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_product(const 
   volatile uint32_t* dead = &bars.dead;
   griddep_wait();
 
+  auto kblocks_of = [&](auto phase) { return (int)(((decltype(phase)::value == kGram ? S.n : S.m) + 63) / 64); };
+  // Until every block is done with the phases before this one.
+  auto wait_phase = [&](int index) {
+    if (index == P.begin) return true;
+    const bool there = wait_count(P.phases, (uint32_t)(index - P.begin) * gridDim.x, dead);
+    fence_proxy_async_all();
+    return there;
+  };
+  auto each_phase = [&](auto&& f) {
+    for (int i = P.begin; i < P.end; ++i) {
+      const Halves2& x = P.x[i / 3 & 1];
+      if (i % 3 == kGram) f(PhaseOf<kGram>(), i, x);
+      else if (i % 3 == kSquare) f(PhaseOf<kSquare>(), i, x);
+      else f(PhaseOf<kUpdate>(), i, x);
+    }
+  };
+
   if (warp == 0) {
     if (lane == 0) {
-      const Halves2 left = kPhase == kGram ? P.x : kPhase == kSquare ? P.o : P.r;
-      const Halves2 right = kPhase == kSquare ? P.o : P.x;
-      // rows of 64 halves from the workspace's beginning
-      const int64_t lh = (left.hi - P.base) / 64, rh = (right.hi - P.base) / 64;
-      const int64_t ll = kFine ? (left.lo - left.hi) / 64 : 0, rl = kFine ? (right.lo - right.hi) / 64 : 0;
-      const int64_t lk = (kPhase == kGram ? S.x() : S.o()) / 64, rk = (kPhase == kSquare ? S.o() : S.x()) / 64;
-      const int64_t lc = kPhase == kGram ? xc : oc, rc = kPhase == kSquare ? oc : xc;
       uint32_t n = 0;  // stages filled
       bool going = true;
-      for (int64_t t = first; t < tiles.all && going; t += step) {
-        int64_t k;
-        int row, col;
-        tiles.at(t, &k, &row, &col);
-        const int64_t ra = (int64_t)row * CG + rank, rb = (int64_t)col * CG + rank;
-        for (int kb = 0; kb < kblocks; ++kb, ++n) {
-          const int s = (int)(n % Pl::kStages);
-          if (n >= Pl::kStages && !wait_for(&bars.empty[s], (n / Pl::kStages - 1) & 1, dead)) {
-            going = false;
-            break;
-          }
-          char* to = smem + s * Pl::kStageBytes;
-          const uint32_t bar = CG == 1 ? smem_addr(&bars.full[s]) : remote(smem_addr(&bars.full[s]), 0);
-          if (rank == 0) mbar_arrive_expect_tx(&bars.full[s], CG * Pl::kStageBytes);
+      each_phase([&](auto phase, int index, const Halves2& x) {
+        constexpr int kPhase = decltype(phase)::value;
+        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
+        const int kblocks = kblocks_of(phase);
+        going = going && wait_phase(index);
+        const Halves2 left = kPhase == kGram ? x : kPhase == kSquare ? P.o : P.r;
+        const Halves2 right = kPhase == kSquare ? P.o : x;
+        // rows of 64 halves from the workspace's beginning
+        const int64_t lh = (left.hi - P.base) / 64, rh = (right.hi - P.base) / 64;
+        const int64_t ll = kFine ? (left.lo - left.hi) / 64 : 0, rl = kFine ? (right.lo - right.hi) / 64 : 0;
+        const int64_t lk = (kPhase == kGram ? S.x() : S.o()) / 64, rk = (kPhase == kSquare ? S.o() : S.x()) / 64;
+        const int64_t lc = kPhase == kGram ? xc : oc, rc = kPhase == kSquare ? oc : xc;
+        for (int64_t t = first; t < tiles.all && going; t += step) {
+          int64_t k;
+          int row, col;
+          tiles.at(t, &k, &row, &col);
+          const int64_t ra = (int64_t)row * CG + rank, rb = (int64_t)col * CG + rank;
+          for (int kb = 0; kb < kblocks; ++kb, ++n) {
+            const int s = (int)(n % Pl::kStages);
+            if (n >= Pl::kStages && !wait_for(&bars.empty[s], (n / Pl::kStages - 1) & 1, dead)) {
+              going = false;
+              break;
+            }
+            char* to = smem + s * Pl::kStageBytes;
+            const uint32_t bar = CG == 1 ? smem_addr(&bars.full[s]) : remote(smem_addr(&bars.full[s]), 0);
+            if (rank == 0) mbar_arrive_expect_tx(&bars.full[s], CG * Pl::kStageBytes);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {  // 64 rows each
-            char* at = to + h * (kFactorBytes / 2);
-            const int64_t l = lh + lk * k + (ra * lc + kb) * 128 + h * 64;
-            const int64_t r = rh + rk * k + (kPhase == kUpdate ? ((kb / 2) * rc + rb * 2 + h) * 128 + (kb & 1) * 64
-                                                               : (rb * rc + kb) * 128 + h * 64);
-            tile_load<CG>(at, &map, l, bar);
-            tile_load<CG>(at + kFactorBytes, &map, r, bar);
-            if (kFine) {
-              tile_load<CG>(at + 2 * kFactorBytes, &map, l + ll, bar);
-              tile_load<CG>(at + 3 * kFactorBytes, &map, r + rl, bar);
+            for (int h = 0; h < 2; ++h) {  // 64 rows each
+              char* at = to + h * (kFactorBytes / 2);
+              const int64_t l = lh + lk * k + (ra * lc + kb) * 128 + h * 64;
+              const int64_t r = rh + rk * k + (kPhase == kUpdate ? ((kb / 2) * rc + rb * 2 + h) * 128 + (kb & 1) * 64
+                                                                 : (rb * rc + kb) * 128 + h * 64);
+              tile_load<CG>(at, &map, l, bar);
+              tile_load<CG>(at + kFactorBytes, &map, r, bar);
+              if (kFine) {
+                tile_load<CG>(at + 2 * kFactorBytes, &map, l + ll, bar);
+                tile_load<CG>(at + 3 * kFactorBytes, &map, r + rl, bar);
+              }
             }
           }
         }
-      }
+      });
       // what is under way has landed before the block ends
       if (rank == 0)
         for (uint32_t i = n > Pl::kStages ? n - Pl::kStages : 0; i < n; ++i)
@@ -503,39 +586,44 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_product(const 
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      // 32-bit sums of halves; the right factor's rows are the sum's index in kUpdate
-      constexpr uint32_t what = 1u << 4 | (kPhase == kUpdate ? 1u << 16 : 0) | (CG * 128 / 8) << 17 | (CG * 128 / 16) << 24;
       uint32_t n = 0, it = 0;
       bool going = true;
-      for (int64_t t = first; t < tiles.all && going; t += step) {
-        for (int kb = 0; kb < kblocks && going; ++it) {
-          const uint32_t acc = tmem + (it & 1) * kColumns;
-          going = it < 2 || wait_for(&bars.taken[it & 1], (it / 2 - 1) & 1, dead);
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const int begin = kb, end = kblocks - kb > Pl::kChunk ? kb + Pl::kChunk : kblocks;
-          for (; kb < end && going; ++kb, ++n) {
-            const int s = (int)(n % Pl::kStages);
-            going = wait_for(&bars.full[s], (n / Pl::kStages) & 1, dead);
-            if (!going) break;
+      each_phase([&](auto phase, int, const Halves2&) {
+        constexpr int kPhase = decltype(phase)::value;
+        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
+        const int kblocks = kblocks_of(phase);
+        // 32-bit sums of halves; the right factor's rows are the sum's index in kUpdate
+        constexpr uint32_t what = 1u << 4 | (kPhase == kUpdate ? 1u << 16 : 0) | (CG * 128 / 8) << 17 | (CG * 128 / 16) << 24;
+        for (int64_t t = first; t < tiles.all && going; t += step) {
+          for (int kb = 0; kb < kblocks && going; ++it) {
+            const uint32_t acc = tmem + (it & 1) * kColumns;
+            going = it < 2 || wait_for(&bars.taken[it & 1], (it / 2 - 1) & 1, dead);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t at = smem_addr(smem + s * Pl::kStageBytes);
-            constexpr uint32_t apart = kPhase == kUpdate ? kFactorBytes / 2 : 0;
-            const uint64_t l = factor(at, 0), r = factor(at + kFactorBytes, apart);
-            constexpr uint64_t lo = (2 * kFactorBytes) >> 4;
+            const int begin = kb, end = kblocks - kb > Pl::kChunk ? kb + Pl::kChunk : kblocks;
+            for (; kb < end && going; ++kb, ++n) {
+              const int s = (int)(n % Pl::kStages);
+              going = wait_for(&bars.full[s], (n / Pl::kStages) & 1, dead);
+              if (!going) break;
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              const uint32_t at = smem_addr(smem + s * Pl::kStageBytes);
+              constexpr uint32_t apart = kPhase == kUpdate ? kFactorBytes / 2 : 0;
+              const uint64_t l = factor(at, 0), r = factor(at + kFactorBytes, apart);
+              constexpr uint64_t lo = (2 * kFactorBytes) >> 4;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {  // 16 of the sum: 32 bytes of each row, or 16 rows
-              const uint64_t dl = q * 32 >> 4, dr = (kPhase == kUpdate ? q * 2048 : q * 32) >> 4;
-              if (kFine) {  // the small terms first, while there is less to cut off
-                mma<CG>(acc, l + dl, r + dr + lo, what, kb > begin || q > 0);
-                mma<CG>(acc, l + dl + lo, r + dr, what, true);
+              for (int q = 0; q < 4; ++q) {  // 16 of the sum: 32 bytes of each row, or 16 rows
+                const uint64_t dl = q * 32 >> 4, dr = (kPhase == kUpdate ? q * 2048 : q * 32) >> 4;
+                if (kFine) {  // the small terms first, while there is less to cut off
+                  mma<CG>(acc, l + dl, r + dr + lo, what, kb > begin || q > 0);
+                  mma<CG>(acc, l + dl + lo, r + dr, what, true);
+                }
+                mma<CG>(acc, l + dl, r + dr, what, kFine || kb > begin || q > 0);
               }
-              mma<CG>(acc, l + dl, r + dr, what, kFine || kb > begin || q > 0);
+              commit<CG>(&bars.empty[s]);
             }
-            commit<CG>(&bars.empty[s]);
+            if (going) commit<CG>(&bars.sums[it & 1]);
           }
-          if (going) commit<CG>(&bars.sums[it & 1]);
         }
-      }
+      });
       // the last products are done before the tensor memory is given back
       for (uint32_t i = n > Pl::kStages ? n - Pl::kStages : 0; i < n; ++i)
         wait_bounded(&bars.empty[i % Pl::kStages], (i / Pl::kStages) & 1, kWaitLimitNs);
@@ -544,176 +632,226 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_product(const 
     const int w = warp & 3, e = warp - 2;   // 32 rows of the block's part of the tile, and 128 columns
     char* mine = held + e * Pl::kBuffers * 2 * kHeldBytes;
     uint64_t* in = bars.held[e];
-    constexpr bool kLow = kPhase == kUpdate || kFine;  // two halves are kept
-    const Halves2 from = kPhase == kUpdate ? P.x : P.o, to = kPhase == kGram ? P.o : kPhase == kSquare ? P.r : P.y;
-    const int64_t bc = kPhase == kUpdate ? xc : oc, plane = kPhase == kUpdate ? S.x() : S.o();
-    // where this warp's part of a block of halves lies
-    auto part_of = [&](int64_t k, int row, int col, int c) {
-      const int64_t rb = (int64_t)row * CG + rank, cb = (int64_t)col * (2 * CG) + e / 4 * 2 + c;
-      return k * plane + (rb * bc + cb) * kBlock + w * (kHeldBytes / 2);
-    };
-    uint32_t fetched = 0;
-    auto fetch = [&](int64_t t, int c) {  // the next one
-      if (kPhase == kGram || t >= tiles.all) return;
-      int64_t k;
-      int row, col;
-      tiles.at(t, &k, &row, &col);
-      const int64_t at = part_of(k, row, col, c);
-      char* b = mine + fetched % Pl::kBuffers * 2 * kHeldBytes;
-      uint64_t* bar = &in[fetched % Pl::kBuffers];
-      mbar_arrive_expect_tx(bar, (kLow ? 2 : 1) * kHeldBytes);
-      bulk_load(b, from.hi + at, kHeldBytes, bar);
-      if (kLow) bulk_load(b + kHeldBytes, from.lo + at, kHeldBytes, bar);
-      ++fetched;
-    };
-    uint32_t q = 0, it = 0;
+    uint32_t fetched = 0, q = 0, it = 0;  // parts of blocks on their way or read, read; accumulators read
     bool going = true;
-    if (lane == 0) fetch(first, 0);
-    for (int64_t t = first; t < tiles.all && going; t += step) {
-      int64_t k;
-      int tr, tc;
-      tiles.at(t, &k, &tr, &tc);
-      const int64_t row = ((int64_t)tr * CG + rank) * 128 + w * 32 + lane;
-      const float* D = P.d + k * S.mp;
-      const float di = kPhase == kSquare ? D[row] : 0.f, ei = kPhase == kUpdate ? P.a + P.e[k * S.mp + row] : 0.f;
-      float sum[kFine ? 128 : 1];
-      if constexpr (kFine) {
+    each_phase([&](auto phase, int index, const Halves2& x) {
+      constexpr int kPhase = decltype(phase)::value;
+      const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
+      const int kblocks = kblocks_of(phase);
+      const float c1 = P.coef[index / 3 * 3], c3 = P.coef[index / 3 * 3 + 1], c5 = P.coef[index / 3 * 3 + 2];
+      going = __all_sync(0xffffffffu, going && (lane != 0 || wait_phase(index)));
+      constexpr bool kLow = kPhase == kUpdate || kFine;  // two halves are kept
+      const Halves2 from = kPhase == kUpdate ? x : P.o;
+      const Halves2 to = kPhase == kGram ? P.o : kPhase == kSquare ? P.r : P.x[(index / 3 + 1) & 1];
+      const int64_t bc = kPhase == kUpdate ? xc : oc, plane = kPhase == kUpdate ? S.x() : S.o();
+      // where this warp's part of a block of halves lies
+      auto part_of = [&](int64_t k, int row, int col, int c) {
+        const int64_t rb = (int64_t)row * CG + rank, cb = (int64_t)col * (2 * CG) + e / 4 * 2 + c;
+        return k * plane + (rb * bc + cb) * kBlock + w * (kHeldBytes / 2);
+      };
+      auto fetch = [&](int64_t t, int c) {  // the next one
+        if (kPhase == kGram || t >= tiles.all) return;
+        int64_t k;
+        int row, col;
+        tiles.at(t, &k, &row, &col);
+        const int64_t at = part_of(k, row, col, c);
+        char* b = mine + fetched % Pl::kBuffers * 2 * kHeldBytes;
+        uint64_t* bar = &in[fetched % Pl::kBuffers];
+        mbar_arrive_expect_tx(bar, (kLow ? 2 : 1) * kHeldBytes);
+        bulk_load(b, from.hi + at, kHeldBytes, bar);
+        if (kLow) bulk_load(b + kHeldBytes, from.lo + at, kHeldBytes, bar);
+        ++fetched;
+      };
+      if (lane == 0 && going) fetch(first, 0);
+      for (int64_t t = first; t < tiles.all && going; t += step) {
+        int64_t k;
+        int tr, tc;
+        tiles.at(t, &k, &tr, &tc);
+        const int64_t row = ((int64_t)tr * CG + rank) * 128 + w * 32 + lane;
+        const uint32_t acc_at = tmem + e / 4 * 128 + ((uint32_t)w << 21);  // this warp's part of the first accumulator
+        if (Pl::kBuffers == 2) {
+          __syncwarp();  // the buffer's last tile has been read
+          if (lane == 0) {
+            bulk_read<0>();
+            fetch(t, 1);
+          }
+        }
+        // D and E of the row, D of the warp's columns: 32 at a time, a lane each
+        const float* D = P.d + k * S.mp;
+        const float di = kPhase == kSquare ? c3 + c5 * D[row] : 0.f, ei = kPhase == kUpdate ? c1 + P.e[k * S.mp + row] : 0.f;
+        const int64_t cols = ((int64_t)tc * CG + e / 4) * 128;  // the warp's first column
+        float dj[4] = {0.f, 0.f, 0.f, 0.f};
+        if (kPhase == kSquare)
 #pragma unroll
-        for (int i = 0; i < 128; ++i) sum[i] = 0.f;
-        for (int kb = 0; kb < kblocks && going; kb += Pl::kChunk, ++it) {
+          for (int i = 0; i < 4; ++i) dj[i] = c5 * D[cols + i * 32 + lane];
+        if constexpr (kFine) {
+          float sum[128];
+#pragma unroll
+          for (int i = 0; i < 128; ++i) sum[i] = 0.f;
+          for (int kb = 0; kb < kblocks; kb += Pl::kChunk) {
+            going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
+            if (!going) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+              float one[16], two[16];
+              tmem_load16(acc_at + (it & 1) * kColumns + i * 16, one);
+              tmem_load16(acc_at + (it & 1) * kColumns + i * 16 + 16, two);
+              tmem_loaded(one);
+              tmem_loaded(two);
+#pragma unroll
+              for (int u = 0; u < 16; ++u) sum[i * 16 + u] += one[u], sum[i * 16 + 16 + u] += two[u];
+            }
+            if (kb + Pl::kChunk < kblocks) {
+              asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) arrive_at(remote(smem_addr(&bars.taken[it & 1]), 0));
+              ++it;
+            }
+          }
+          // back into the last accumulator: what follows takes them from there in a loop
+#pragma unroll
+          for (int i = 0; i < 8; ++i) tmem_store16(acc_at + (it & 1) * kColumns + i * 16, sum + i * 16);
+          tmem_stored();
+        } else {
           going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
-          if (!going) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float acc[32];
-            tmem_load32(tmem + (it & 1) * kColumns + e / 4 * 128 + i * 32 + ((uint32_t)w << 21), acc);
-            tmem_loaded();
-#pragma unroll
-            for (int u = 0; u < 32; ++u) sum[i * 32 + u] += acc[u];
-          }
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) arrive_at(remote(smem_addr(&bars.taken[it & 1]), 0));
         }
-      } else {
-        going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      }
-      if (!going) break;
-#pragma unroll
-      for (int c = 0; c < 2; ++c, ++q) {
-        char* b = mine + q % Pl::kBuffers * 2 * kHeldBytes;
-        if (lane == 0) {
-          bulk_read();  // earlier stores: what they were read from may be written again
-          if (Pl::kBuffers == 2) fetch(c == 0 ? t : t + step, c ^ 1);
-        }
-        __syncwarp();
-        if (kPhase != kGram)
-          going = __all_sync(0xffffffffu, wait_for(&in[q % Pl::kBuffers], (q / Pl::kBuffers) & 1, dead));
         if (!going) break;
-        const int64_t col0 = ((int64_t)tc * (2 * CG) + e / 4 * 2 + c) * 64;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float acc[32];
-          if constexpr (kFine) {
-#pragma unroll
-            for (int u = 0; u < 32; ++u) acc[u] = sum[c * 64 + half * 32 + u];
+        // (Loops that are not unrolled: each tile goes through this code once, and instructions have to be
+        // fetched. 64 columns took 4,500 to 9,000 cycles unrolled.)
+        float next[16];
+        tmem_load16(acc_at + (it & 1) * kColumns, next);
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          char* b = mine + (kPhase == kGram ? c : (int)q) % Pl::kBuffers * 2 * kHeldBytes;
+          if (kPhase == kGram) {
+            if (lane == 0) bulk_read<Pl::kBuffers - 1>();  // what is stored from here has been read
+            __syncwarp();
           } else {
-            tmem_load32(tmem + (it & 1) * kColumns + e / 4 * 128 + c * 64 + half * 32 + ((uint32_t)w << 21), acc);
-            tmem_loaded();
+            going = __all_sync(0xffffffffu, wait_for(&in[q % Pl::kBuffers], (q / Pl::kBuffers) & 1, dead));
+            ++q;
           }
+          if (!going) break;
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {  // 16 columns
+            float acc[16];
+            tmem_loaded(next);
 #pragma unroll
-          for (int p = 0; p < 4; ++p) {
-            char* at = b + piece_at((uint32_t)lane, (uint32_t)(half * 4 + p));
-            float was[8];
-            if (kPhase != kGram) {
-              Vec<__half>::get(*reinterpret_cast<const uint4*>(at), was);
-              if (kLow) {
+            for (int u = 0; u < 16; ++u) acc[u] = next[u];
+            if (c == 0 || h < 3) tmem_load16(acc_at + (it & 1) * kColumns + c * 64 + h * 16 + 16, next);
+            const float dh = c == 0 ? (h < 2 ? dj[0] : dj[1]) : (h < 2 ? dj[2] : dj[3]);
+            float was[16];
+            char* at[2];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              at[p] = b + piece_at((uint32_t)lane, (uint32_t)(h * 2 + p));
+              if (kPhase != kGram) Vec<__half>::get(*reinterpret_cast<const uint4*>(at[p]), was + p * 8);
+              if (kPhase != kGram && kLow) {
                 float low[8];
-                Vec<__half>::get(*reinterpret_cast<const uint4*>(at + kHeldBytes), low);
+                Vec<__half>::get(*reinterpret_cast<const uint4*>(at[p] + kHeldBytes), low);
 #pragma unroll
-                for (int u = 0; u < 8; ++u) was[u] += low[u];
+                for (int u = 0; u < 8; ++u) was[p * 8 + u] += low[u];
               }
             }
-            alignas(16) __half nh[8], nl[8];
-            const int64_t col = col0 + half * 32 + p * 8;
+            // (acc: X X' 2^28 times, O^2 2^22 times, R X 2^25 times)
+            alignas(16) __half2 nh[8], nl[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              float v = acc[p * 8 + u];
-              if constexpr (kPhase == kGram) {
-                v *= kO / (kX * kX);
-                if (col + u == row) P.d[k * S.mp + row] = v * (1.f / kO), v = 0.f;
-              } else if constexpr (kPhase == kSquare) {
-                v *= 1.f / kO;  // O^2, 2^11 times
-                if (col + u == row) {
-                  P.e[k * S.mp + row] = P.b * di + P.c * __fmaf_rn(di, di, v * (1.f / kO));
-                  v = 0.f;
+            for (int u = 0; u < 16; u += 2) {
+              float v[2];
+#pragma unroll
+              for (int o = 0; o < 2; ++o) {
+                if constexpr (kPhase == kGram) {
+                  v[o] = acc[u + o] * (kO / (kX * kX));
+                } else if constexpr (kPhase == kSquare) {  // b O + c (O^2 + (D_i + D_j) O)
+                  const float by = di + __shfl_sync(0xffffffffu, dh, (h & 1) * 16 + u + o);
+                  v[o] = __fmaf_rn(by, was[u + o], acc[u + o] * (c5 / kO));
                 } else {
-                  v = P.b * was[u] + P.c * __fmaf_rn(di + D[col + u], was[u], v);
+                  v[o] = __fmaf_rn(ei, was[u + o], acc[u + o] * (1.f / kO));
                 }
+              }
+              two_halves(v[0], v[1], nh + u / 2, nl + u / 2);
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              *reinterpret_cast<uint4*>(at[p]) = *reinterpret_cast<const uint4*>(nh + p * 4);
+              if (kLow) *reinterpret_cast<uint4*>(at[p] + kHeldBytes) = *reinterpret_cast<const uint4*>(nl + p * 4);
+            }
+            const int on = (int)(row - (cols + c * 64 + h * 16));  // the column that is on the diagonal
+            if (kPhase != kUpdate && tr == tc && on >= 0 && on < 16) {
+              float mid = 0.f;
+#pragma unroll
+              for (int u = 0; u < 16; ++u) mid = u == on ? acc[u] : mid;
+              if (kPhase == kGram) {
+                P.d[k * S.mp + row] = mid * (1.f / (kX * kX));
               } else {
-                v = __fmaf_rn(ei, was[u], v * (1.f / kO));
+                const float d = D[row];
+                P.e[k * S.mp + row] = c3 * d + c5 * __fmaf_rn(d, d, mid * (1.f / (kO * kO)));
               }
-              two_halves(v, nh + u, nl + u);
-            }
-            *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(nh);
-            if (kLow) *reinterpret_cast<uint4*>(at + kHeldBytes) = *reinterpret_cast<const uint4*>(nl);
-          }
-        }
-        if (!kFine && c == 1) {  // the sums are read
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) arrive_at(remote(smem_addr(&bars.taken[it & 1]), 0));
-        }
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) {
-          const int64_t at = part_of(k, tr, tc, c);
-          bulk_store(to.hi + at, b, kHeldBytes);
-          if (kLow) bulk_store(to.lo + at, b + kHeldBytes, kHeldBytes);
-          bulk_commit();
-        }
-        if (kPhase != kUpdate && tr != tc) {
-          // the same above the diagonal: this warp's 64 columns are rows there, two of them a lane, its rows
-          // 32 columns, four pieces
-          const int64_t rb = ((int64_t)tc * (2 * CG) + e / 4 * 2 + c) / 2;  // (64 columns: half a block's rows)
-          const int64_t cb = ((int64_t)tr * CG + rank) * 2 + w / 2;
-          const int64_t block = k * plane + (rb * bc + cb) * kBlock;
-#pragma unroll
-          for (int low = 0; low < (kLow ? 2 : 1); ++low) {
-            const char* plane_at = b + low * kHeldBytes;
-            char* out = reinterpret_cast<char*>((low ? to.lo : to.hi) + block);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t j = h * 32 + lane, r = c * 64 + j;  // column here, row there
-#pragma unroll
-              for (int p = 0; p < 4; ++p) {
-                alignas(16) uint16_t v[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u)
-                  v[u] = *reinterpret_cast<const uint16_t*>(plane_at + piece_at((uint32_t)(p * 8 + u), j / 8) + j % 8 * 2);
-                *reinterpret_cast<uint4*>(out + piece_at(r, (uint32_t)(w % 2 * 4 + p))) = *reinterpret_cast<const uint4*>(v);
-              }
+              char* place = on < 8 ? at[0] : at[1];
+              *reinterpret_cast<uint16_t*>(place + on % 8 * 2) = 0;
+              if (kLow) *reinterpret_cast<uint16_t*>(place + kHeldBytes + on % 8 * 2) = 0;
             }
           }
-        }
-        if (Pl::kBuffers == 1) {
+          if (c == 1) {  // the sums are read
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) arrive_at(remote(smem_addr(&bars.taken[it & 1]), 0));
+          }
+          fence_proxy_async();
           __syncwarp();
           if (lane == 0) {
-            bulk_read();
-            fetch(c == 0 ? t : t + step, c ^ 1);
+            if (Pl::kBuffers == 2 && c == 1 && kPhase != kGram) {
+              bulk_read<0>();  // the first part's store, a while ago
+              fetch(t + step, 0);
+            }
+            const int64_t at = part_of(k, tr, tc, c);
+            bulk_store(to.hi + at, b, kHeldBytes);
+            if (kLow) bulk_store(to.lo + at, b + kHeldBytes, kHeldBytes);
+            bulk_commit();
+          }
+          if (kPhase != kUpdate && tr != tc) {
+            // the same above the diagonal: this warp's 64 columns are rows there, two of them a lane, its rows
+            // 32 columns, four pieces
+            const int64_t rb = (int64_t)tc * CG + e / 4;  // (64 columns: half a block's rows)
+            const int64_t cb = ((int64_t)tr * CG + rank) * 2 + w / 2;
+            const int64_t block = k * plane + (rb * bc + cb) * kBlock;
+#pragma unroll 1
+            for (int i = 0; i < (kLow ? 16 : 8); ++i) {
+              const int low = i / 8, h = i / 4 % 2, p = i % 4;
+              const char* plane_at = b + low * kHeldBytes;
+              char* out = reinterpret_cast<char*>((low ? to.lo : to.hi) + block);
+              const uint32_t j = h * 32 + lane, r = c * 64 + j;  // column here, row there
+              alignas(16) uint16_t v[8];
+#pragma unroll
+              for (int u = 0; u < 8; ++u)
+                v[u] = *reinterpret_cast<const uint16_t*>(plane_at + piece_at((uint32_t)(p * 8 + u), j / 8) + j % 8 * 2);
+              *reinterpret_cast<uint4*>(out + piece_at(r, (uint32_t)(w % 2 * 4 + p))) = *reinterpret_cast<const uint4*>(v);
+            }
+          }
+          if (Pl::kBuffers == 1) {
+            __syncwarp();
+            if (lane == 0) {
+              bulk_read<0>();
+              fetch(c == 0 ? t : t + step, c ^ 1);
+            }
           }
         }
+        tmem_loaded(next);  // (nothing is on its way, but where a wait gave up)
+        ++it;
       }
-      if (!kFine) ++it;
-    }
-    if (kPhase != kUpdate) fence_proxy_async_all();
-    if (lane == 0) {
-      bulk_done();
+      // what this block wrote is there for the next phase (which orders its copies after it)
+      if (lane == 0) bulk_done();
+      if (index + 1 == P.end) {
+        fence_proxy_async_all();
+      } else {
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * Pl::kWarps) : "memory");
+        if (e == 0 && lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(P.phases) : "memory");
+      }
+    });
+    if (lane == 0)
       for (uint32_t i = fetched > Pl::kBuffers ? fetched - Pl::kBuffers : 0; i < fetched; ++i)
         wait_bounded(&in[i % Pl::kBuffers], (i / Pl::kBuffers) & 1, kWaitLimitNs);
-    }
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -727,29 +865,41 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_product(const 
   if (threadIdx.x == 0 && bars.dead) atomicExch(P.gave_up, 1u);
 }
 
-template <int CG, bool kFine, int kPhase>
-cudaError_t launch_product(const CUtensorMap& map, const ProductArgs& P, int device, int sms, cudaStream_t s) {
+// The phases [P.begin, P.end) in one launch: more than one need all blocks resident at once.
+template <int CG, bool kFine>
+cudaError_t launch_phases(const CUtensorMap& map, const ProductArgs& P, int device, int sms, cudaStream_t s) {
   using Pl = Plan<CG, kFine>;
   constexpr int smem = product_smem<CG, kFine>();
   static_assert(smem <= 232448, "shared memory of a block");
-  auto* f = k_product<CG, kFine, kPhase>;
+  auto* f = k_products<CG, kFine>;
   static std::atomic<uint64_t> known{0};  // devices whose limit is raised
   if (device >= 64 || !(known.load(std::memory_order_relaxed) >> device & 1)) {
     const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     if (device < 64) known.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
   }
+  const bool together = P.end - P.begin > 1;
+  if ((CG > 1 || together) && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
   const int64_t rows = P.S.mp / (128 * CG), cols = P.S.np / (128 * CG);
-  const int64_t most = sms / CG, tiles = P.K * (kPhase == kUpdate ? rows * cols : rows * (rows + 1) / 2);
-  if (CG > 1 && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
+  const int64_t most = sms / CG, tiles = P.K * std::max(rows * cols, rows * (rows + 1) / 2);
   LaunchConfig l((tiles < most ? tiles : most) * CG, Pl::kThreads, CG, smem, s);
+  if (together) {  // in the place of programmatic serialization
+    l.at[0].id = cudaLaunchAttributeCooperative;
+    l.at[0].val.cooperative = 1;
+  }
   return cudaLaunchKernelEx(&l.cfg, f, map, P);
 }
+// All steps: in one launch, or, where the context has no room for all blocks, phase by phase.
 template <int CG, bool kFine>
-cudaError_t one_step(const CUtensorMap& map, const ProductArgs& P, int device, int sms, cudaStream_t s) {
-  cudaError_t e = launch_product<CG, kFine, kGram>(map, P, device, sms, s);
-  if (e == cudaSuccess) e = launch_product<CG, kFine, kSquare>(map, P, device, sms, s);
-  if (e == cudaSuccess) e = launch_product<CG, kFine, kUpdate>(map, P, device, sms, s);
+cudaError_t all_steps(const CUtensorMap& map, ProductArgs P, int device, int sms, cudaStream_t s) {
+  cudaError_t e = launch_phases<CG, kFine>(map, P, device, sms, s);
+  if (!too_large_here(e)) return e;
+  cudaGetLastError();  // this launch's
+  const int end = P.end;
+  for (e = cudaSuccess; P.begin < end && e == cudaSuccess; ++P.begin) {
+    P.end = P.begin + 1;
+    e = launch_phases<CG, kFine>(map, P, device, sms, s);
+  }
   return e;
 }
 
@@ -777,7 +927,7 @@ cudaError_t map_of(void* base, int64_t bytes, CUtensorMap* map) {
 
 struct Work {
   double* part;
-  uint32_t* gave_up;
+  uint32_t* counts;  // gave up, phases
   float *d, *e;
   Halves2 x, y, o, r;
 };
@@ -802,7 +952,7 @@ int64_t work_of(int32_t dtype, int64_t K, const Shape& S, char* at, Work* w) {
   };
   Work v;
   v.part = reinterpret_cast<double*>(take(8 * K * kMostSizeParts));
-  v.gave_up = reinterpret_cast<uint32_t*>(take(4));
+  v.counts = reinterpret_cast<uint32_t*>(take(8));
   v.d = reinterpret_cast<float*>(take(4 * K * S.mp));
   v.e = reinterpret_cast<float*>(take(4 * K * S.mp));
   const bool fine = dtype != GMC_BF16;
@@ -866,32 +1016,29 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
   // parts of |G|^2: as many blocks as are resident at once, of eight rows or pieces each
   const int64_t rows8 = (m * ((n + kSizePiece - 1) / kSizePiece) + 7) / 8, share = (sms * 8 + K - 1) / K;
   const int parts = (int)std::min({rows8, share, (int64_t)kMostSizeParts});
-  const dim3 blocks((unsigned)(S.x() / kBlock), (unsigned)K);
+  const dim3 blocks((unsigned)(S.x() / kBlock), (unsigned)K), some((unsigned)std::min(S.x() / kBlock, share), (unsigned)K);
   err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
     constexpr bool fine = !std::is_same<T, __nv_bfloat16>::value;
     const T* g = static_cast<const T*>(x_dev);
     T* o = static_cast<T*>(out_dev);
-    cudaError_t e = launch_pdl(k_size<T>, dim3((unsigned)parts, (unsigned)K), dim3(256), 0, s, g, ldk, ld, m, n, w.part, w.gave_up);
+    cudaError_t e = launch_pdl(k_size<T>, dim3((unsigned)parts, (unsigned)K), dim3(256), 0, s, g, ldk, ld, m, n, w.part, w.counts);
     if (e != cudaSuccess) return e;
-    e = launch_pdl(turned ? k_first<T, true> : k_first<T, false>, blocks, dim3(256), 0, s, g, ldk, ld, S, (const double*)w.part,
+    e = launch_pdl(turned ? k_first<T, true> : k_first<T, false>, some, dim3(256), 0, s, g, ldk, ld, S, (const double*)w.part,
                    parts, w.x);
-    for (int i = 0; i < steps && e == cudaSuccess; ++i) {
-      const float* c = coefficients_host + 3 * i;
-      const ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), w.x, w.o, w.r, w.y, w.d, w.e, c[0], c[1], c[2], w.gave_up};
-      if (pairs) e = one_step<2, fine>(map, P, device, sms, s);
-      if (pairs && too_large_here(e)) {  // a context without room for clusters
-        cudaGetLastError();              // this launch's
-        pairs = false;
-      }
-      if (!pairs) e = one_step<1, fine>(map, P, device, sms, s);
-      const Halves2 was = w.x;
-      w.x = w.y;
-      w.y = was;
-    }
     if (e != cudaSuccess) return e;
-    return launch_pdl(turned ? k_last<T, true> : k_last<T, false>, blocks, dim3(256), 0, s, o, out_ldk, out_ld, S, w.x, scale,
-                      (const uint32_t*)w.gave_up);
+    ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps, w.counts + 1,
+                  w.counts, {}};
+    std::copy(coefficients_host, coefficients_host + 3 * steps, P.coef);
+    if (pairs) e = all_steps<2, fine>(map, P, device, sms, s);
+    if (pairs && too_large_here(e)) {  // a context without room for clusters
+      cudaGetLastError();
+      pairs = false;
+    }
+    if (!pairs) e = all_steps<1, fine>(map, P, device, sms, s);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(turned ? k_last<T, true> : k_last<T, false>, blocks, dim3(256), 0, s, o, out_ldk, out_ld, S,
+                      steps % 2 ? w.y : w.x, scale, (const uint32_t*)w.counts);
   });
   return err == cudaSuccess ? GMC_OK : GMC_ECUDA;
 }
