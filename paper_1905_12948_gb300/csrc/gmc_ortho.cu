@@ -111,11 +111,13 @@ __device__ __forceinline__ double squares(float* f) {
 constexpr int kMostSizeParts = 256, kSizePiece = 4096;
 template <typename T>
 __global__ void __launch_bounds__(256) k_size(const T* g, int64_t sk, int64_t ld, int64_t m, int64_t n, double* part,
-                                              uint32_t* counts) {
+                                              uint32_t* counts, int64_t counters) {
   constexpr int N = Vec<T>::N;
   __shared__ double ws[8];
   griddep_wait();
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2) counts[threadIdx.x] = 0;
+  for (int64_t i = (blockIdx.y * (int64_t)gridDim.x + blockIdx.x) * 256 + threadIdx.x; i < counters;
+       i += (int64_t)gridDim.x * gridDim.y * 256)
+    counts[i] = 0;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int64_t pieces = (n + kSizePiece - 1) / kSizePiece;
   double s = 0.;
@@ -248,8 +250,13 @@ __device__ __forceinline__ uint32_t remote(uint32_t addr, uint32_t rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ void arrive_at(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+// Says that an accumulator was read, to the block that issues the products. Across blocks without a release: what comes
+// before it are reads of tensor memory, which have ended, and a release would wait for all of the thread's stores
+// (1,000 cycles).
+template <int CG>
+__device__ __forceinline__ void arrive_first(uint64_t* bar) {
+  if constexpr (CG == 1) mbar_arrive(bar);
+  else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(remote(smem_addr(bar), 0)) : "memory");
 }
 __device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
   uint32_t ok;
@@ -372,11 +379,8 @@ __device__ __forceinline__ void bulk_store(void* to, const void* from, uint32_t 
                : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-// Until all stores but the last kLeft have read what they store.
-template <int kLeft>
-__device__ __forceinline__ void bulk_read() {
-  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory");
-}
+// Until all stores have read what they store.
+__device__ __forceinline__ void bulk_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // A copy of 64 rows of 128 bytes; row `at` of the workspace. With pairs of blocks the bytes are counted by the barrier of the
@@ -406,6 +410,9 @@ struct ProductArgs {
   Halves2 x[2], o, r;   // X before and after each step, in turn; O, R
   float *d, *e;         // diagonals of A and B, mp each
   int begin, end;       // phases of this launch, three a step
+  int splits;           // shares of a tile's sum over X's columns
+  float* shares;        // their sums,
+  uint32_t* shared;     // and how many of them are there, by warps
   uint32_t* phases;     // counts the blocks that are done with each
   uint32_t* gave_up;
   float coef[3 * kMostSteps];
@@ -421,10 +428,9 @@ template <int CG, bool kFine>
 struct Plan {
   static constexpr int kStages = kFine ? 2 : 5;
   static constexpr int kStageBytes = (kFine ? 4 : 2) * kFactorBytes;
-  static constexpr int kWarps = 4 * CG;                // that read the sums back
+  static constexpr int kWarps = 8;         // that read the sums back: 32 rows, and 64 CG columns each
   static constexpr int kThreads = 64 + 32 * kWarps;
-  static constexpr int kBuffers = CG == 1 ? 2 : 1;     // of such a warp, two parts of a block each
-  static constexpr int kHeld = kWarps * kBuffers * 2 * kHeldBytes;
+  static constexpr int kHeld = kWarps * 2 * kHeldBytes;  // a part of a block, two halves, for each
   // Sums in the tensor cores are cut off, not rounded: by a quarter of a last place an addition where
   // all terms have one sign (4,608 columns of fp32 matrices: 2.8e-5 off the result, by three additions for
   // 16 columns). They are added up in registers after 128.
@@ -433,7 +439,7 @@ struct Plan {
 struct alignas(8) ProductBars {
   uint64_t full[5], empty[5];
   uint64_t sums[2], taken[2];  // accumulators: written, read back
-  uint64_t held[8][2];
+  uint64_t held[8];
   uint32_t tmem, dead;
 };
 template <int CG, bool kFine>
@@ -468,6 +474,24 @@ struct Tiles {
   }
 };
 
+// The units of work of a phase: tiles, or shares of them, the columns of X in `splits` parts.
+struct Parts {
+  int splits, kblocks, per;
+  int64_t all;
+  __device__ Parts(const ProductArgs& P, const Tiles& tiles, int phase) {
+    splits = phase == kGram ? P.splits : 1;
+    kblocks = (int)(((phase == kGram ? P.S.n : P.S.m) + 63) / 64);
+    per = (kblocks + splits - 1) / splits;
+    all = tiles.all * splits;
+  }
+  // its tile, and blocks of 64 of the sum (none for the last ones where they do not go round: not planned)
+  __device__ void at(int64_t unit, int64_t* t, int* begin, int* end) const {
+    *t = unit / splits;
+    *begin = (int)(unit % splits) * per;
+    *end = *begin + per < kblocks ? *begin + per : kblocks;
+  }
+};
+
 // The phases of all steps, with a barrier over the grid between two of them (the blocks are resident together);
 // or one of them. A block holds 128 rows of the left factor and 128 rows (columns
 // in kUpdate) of the right one, 64 of the sum at a time; a pair of blocks (CG = 2) shares them, and its tile
@@ -497,8 +521,8 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.sums[i], 1);
       mbar_init(&bars.taken[i], Pl::kWarps * CG);
-      for (int w = 0; w < Pl::kWarps; ++w) mbar_init(&bars.held[w][i], 1);
     }
+    for (int w = 0; w < Pl::kWarps; ++w) mbar_init(&bars.held[w], 1);
     bars.dead = 0;
     fence_mbar_init();
   }
@@ -514,7 +538,6 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
   volatile uint32_t* dead = &bars.dead;
   griddep_wait();
 
-  auto kblocks_of = [&](auto phase) { return (int)(((decltype(phase)::value == kGram ? S.n : S.m) + 63) / 64); };
   // Until every block is done with the phases before this one.
   auto wait_phase = [&](int index) {
     if (index == P.begin) return true;
@@ -538,7 +561,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       each_phase([&](auto phase, int index, const Halves2& x) {
         constexpr int kPhase = decltype(phase)::value;
         const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
-        const int kblocks = kblocks_of(phase);
+        const Parts parts(P, tiles, kPhase);
         going = going && wait_phase(index);
         const Halves2 left = kPhase == kGram ? x : kPhase == kSquare ? P.o : P.r;
         const Halves2 right = kPhase == kSquare ? P.o : x;
@@ -547,12 +570,13 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         const int64_t ll = kFine ? (left.lo - left.hi) / 64 : 0, rl = kFine ? (right.lo - right.hi) / 64 : 0;
         const int64_t lk = (kPhase == kGram ? S.x() : S.o()) / 64, rk = (kPhase == kSquare ? S.o() : S.x()) / 64;
         const int64_t lc = kPhase == kGram ? xc : oc, rc = kPhase == kSquare ? oc : xc;
-        for (int64_t t = first; t < tiles.all && going; t += step) {
-          int64_t k;
-          int row, col;
+        for (int64_t unit = first; unit < parts.all && going; unit += step) {
+          int64_t t, k;
+          int begin, end, row, col;
+          parts.at(unit, &t, &begin, &end);
           tiles.at(t, &k, &row, &col);
           const int64_t ra = (int64_t)row * CG + rank, rb = (int64_t)col * CG + rank;
-          for (int kb = 0; kb < kblocks; ++kb, ++n) {
+          for (int kb = begin; kb < end; ++kb, ++n) {
             const int s = (int)(n % Pl::kStages);
             if (n >= Pl::kStages && !wait_for(&bars.empty[s], (n / Pl::kStages - 1) & 1, dead)) {
               going = false;
@@ -591,15 +615,18 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       each_phase([&](auto phase, int, const Halves2&) {
         constexpr int kPhase = decltype(phase)::value;
         const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
-        const int kblocks = kblocks_of(phase);
+        const Parts parts(P, tiles, kPhase);
         // 32-bit sums of halves; the right factor's rows are the sum's index in kUpdate
         constexpr uint32_t what = 1u << 4 | (kPhase == kUpdate ? 1u << 16 : 0) | (CG * 128 / 8) << 17 | (CG * 128 / 16) << 24;
-        for (int64_t t = first; t < tiles.all && going; t += step) {
-          for (int kb = 0; kb < kblocks && going; ++it) {
+        for (int64_t unit = first; unit < parts.all && going; unit += step) {
+          int64_t t;
+          int kb, last;
+          parts.at(unit, &t, &kb, &last);
+          while (kb < last && going) {
             const uint32_t acc = tmem + (it & 1) * kColumns;
             going = it < 2 || wait_for(&bars.taken[it & 1], (it / 2 - 1) & 1, dead);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const int begin = kb, end = kblocks - kb > Pl::kChunk ? kb + Pl::kChunk : kblocks;
+            const int begin = kb, end = last - kb > Pl::kChunk ? kb + Pl::kChunk : last;
             for (; kb < end && going; ++kb, ++n) {
               const int s = (int)(n % Pl::kStages);
               going = wait_for(&bars.full[s], (n / Pl::kStages) & 1, dead);
@@ -621,6 +648,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
               commit<CG>(&bars.empty[s]);
             }
             if (going) commit<CG>(&bars.sums[it & 1]);
+            ++it;
           }
         }
       });
@@ -629,15 +657,15 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         wait_bounded(&bars.empty[i % Pl::kStages], (i / Pl::kStages) & 1, kWaitLimitNs);
     }
   } else {
-    const int w = warp & 3, e = warp - 2;   // 32 rows of the block's part of the tile, and 128 columns
-    char* mine = held + e * Pl::kBuffers * 2 * kHeldBytes;
-    uint64_t* in = bars.held[e];
+    const int w = warp & 3, e = (warp - 2) / 4;  // rows 32 w of the block's part of the tile, columns 64 CG e
+    char* b = held + (warp - 2) * 2 * kHeldBytes;
+    uint64_t* in = &bars.held[warp - 2];
     uint32_t fetched = 0, q = 0, it = 0;  // parts of blocks on their way or read, read; accumulators read
     bool going = true;
     each_phase([&](auto phase, int index, const Halves2& x) {
       constexpr int kPhase = decltype(phase)::value;
       const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
-      const int kblocks = kblocks_of(phase);
+      const Parts parts(P, tiles, kPhase);
       const float c1 = P.coef[index / 3 * 3], c3 = P.coef[index / 3 * 3 + 1], c5 = P.coef[index / 3 * 3 + 2];
       going = __all_sync(0xffffffffu, going && (lane != 0 || wait_phase(index)));
       constexpr bool kLow = kPhase == kUpdate || kFine;  // two halves are kept
@@ -646,7 +674,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       const int64_t bc = kPhase == kUpdate ? xc : oc, plane = kPhase == kUpdate ? S.x() : S.o();
       // where this warp's part of a block of halves lies
       auto part_of = [&](int64_t k, int row, int col, int c) {
-        const int64_t rb = (int64_t)row * CG + rank, cb = (int64_t)col * (2 * CG) + e / 4 * 2 + c;
+        const int64_t rb = (int64_t)row * CG + rank, cb = ((int64_t)col * 2 + e) * CG + c;
         return k * plane + (rb * bc + cb) * kBlock + w * (kHeldBytes / 2);
       };
       auto fetch = [&](int64_t t, int c) {  // the next one
@@ -655,92 +683,48 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         int row, col;
         tiles.at(t, &k, &row, &col);
         const int64_t at = part_of(k, row, col, c);
-        char* b = mine + fetched % Pl::kBuffers * 2 * kHeldBytes;
-        uint64_t* bar = &in[fetched % Pl::kBuffers];
-        mbar_arrive_expect_tx(bar, (kLow ? 2 : 1) * kHeldBytes);
-        bulk_load(b, from.hi + at, kHeldBytes, bar);
-        if (kLow) bulk_load(b + kHeldBytes, from.lo + at, kHeldBytes, bar);
+        mbar_arrive_expect_tx(in, (kLow ? 2 : 1) * kHeldBytes);
+        bulk_load(b, from.hi + at, kHeldBytes, in);
+        if (kLow) bulk_load(b + kHeldBytes, from.lo + at, kHeldBytes, in);
         ++fetched;
       };
+      // this warp's sums of one share of tile t, 64 CG columns of 32 rows
+      auto share_of = [&](int64_t t, int split) {
+        return P.shares + ((((t * parts.splits + split) * CG + rank) * Pl::kWarps + warp - 2) * (64 * CG)) * 32 + lane;
+      };
       if (lane == 0 && going) fetch(first, 0);
-      for (int64_t t = first; t < tiles.all && going; t += step) {
+
+      // One tile: `sums(c, h, acc)` gives 16 columns of its sums, in the order of the columns, `done()` says that all were given.
+      auto finish = [&](int64_t t, auto&& sums, auto&& done) {
         int64_t k;
         int tr, tc;
         tiles.at(t, &k, &tr, &tc);
         const int64_t row = ((int64_t)tr * CG + rank) * 128 + w * 32 + lane;
-        const uint32_t acc_at = tmem + e / 4 * 128 + ((uint32_t)w << 21);  // this warp's part of the first accumulator
-        if (Pl::kBuffers == 2) {
-          __syncwarp();  // the buffer's last tile has been read
-          if (lane == 0) {
-            bulk_read<0>();
-            fetch(t, 1);
-          }
-        }
         // D and E of the row, D of the warp's columns: 32 at a time, a lane each
         const float* D = P.d + k * S.mp;
-        const float di = kPhase == kSquare ? c3 + c5 * D[row] : 0.f, ei = kPhase == kUpdate ? c1 + P.e[k * S.mp + row] : 0.f;
-        const int64_t cols = ((int64_t)tc * CG + e / 4) * 128;  // the warp's first column
-        float dj[4] = {0.f, 0.f, 0.f, 0.f};
-        if (kPhase == kSquare)
+        [[maybe_unused]] const float dr = kPhase == kSquare ? D[row] : 0.f, di = c3 + c5 * dr;
+        [[maybe_unused]] const float ei = kPhase == kUpdate ? c1 + P.e[k * S.mp + row] : 0.f;
+        const int64_t cols = ((int64_t)tc * 2 + e) * (64 * CG);  // the warp's first column
+        float dj[2 * CG];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) dj[i] = c5 * D[cols + i * 32 + lane];
-        if constexpr (kFine) {
-          float sum[128];
-#pragma unroll
-          for (int i = 0; i < 128; ++i) sum[i] = 0.f;
-          for (int kb = 0; kb < kblocks; kb += Pl::kChunk) {
-            going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
-            if (!going) break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              float one[16], two[16];
-              tmem_load16(acc_at + (it & 1) * kColumns + i * 16, one);
-              tmem_load16(acc_at + (it & 1) * kColumns + i * 16 + 16, two);
-              tmem_loaded(one);
-              tmem_loaded(two);
-#pragma unroll
-              for (int u = 0; u < 16; ++u) sum[i * 16 + u] += one[u], sum[i * 16 + 16 + u] += two[u];
-            }
-            if (kb + Pl::kChunk < kblocks) {
-              asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-              __syncwarp();
-              if (lane == 0) arrive_at(remote(smem_addr(&bars.taken[it & 1]), 0));
-              ++it;
-            }
-          }
-          // back into the last accumulator: what follows takes them from there in a loop
-#pragma unroll
-          for (int i = 0; i < 8; ++i) tmem_store16(acc_at + (it & 1) * kColumns + i * 16, sum + i * 16);
-          tmem_stored();
-        } else {
-          going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        }
-        if (!going) break;
+        for (int i = 0; i < 2 * CG; ++i) dj[i] = kPhase == kSquare ? c5 * D[cols + i * 32 + lane] : 0.f;
         // (Loops that are not unrolled: each tile goes through this code once, and instructions have to be
-        // fetched. 64 columns took 4,500 to 9,000 cycles unrolled.)
-        float next[16];
-        tmem_load16(acc_at + (it & 1) * kColumns, next);
+        // fetched. 64 columns took 4,500 to 9,000 cycles unrolled, 1,200 to 2,200 in loops of 16.)
 #pragma unroll 1
-        for (int c = 0; c < 2; ++c) {
-          char* b = mine + (kPhase == kGram ? c : (int)q) % Pl::kBuffers * 2 * kHeldBytes;
+        for (int c = 0; c < CG; ++c) {
           if (kPhase == kGram) {
-            if (lane == 0) bulk_read<Pl::kBuffers - 1>();  // what is stored from here has been read
+            if (lane == 0) bulk_read();  // the last store from here
             __syncwarp();
           } else {
-            going = __all_sync(0xffffffffu, wait_for(&in[q % Pl::kBuffers], (q / Pl::kBuffers) & 1, dead));
+            going = __all_sync(0xffffffffu, wait_for(in, q & 1, dead));
             ++q;
           }
-          if (!going) break;
+          if (!going) return;
 #pragma unroll 1
           for (int h = 0; h < 4; ++h) {  // 16 columns
             float acc[16];
-            tmem_loaded(next);
-#pragma unroll
-            for (int u = 0; u < 16; ++u) acc[u] = next[u];
-            if (c == 0 || h < 3) tmem_load16(acc_at + (it & 1) * kColumns + c * 64 + h * 16 + 16, next);
-            const float dh = c == 0 ? (h < 2 ? dj[0] : dj[1]) : (h < 2 ? dj[2] : dj[3]);
+            sums(c, h, acc);
+            [[maybe_unused]] const float dh = c == 0 ? (h < 2 ? dj[0] : dj[1]) : (h < 2 ? dj[2 * CG - 2] : dj[2 * CG - 1]);
             float was[16];
             char* at[2];
 #pragma unroll
@@ -782,29 +766,17 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
               float mid = 0.f;
 #pragma unroll
               for (int u = 0; u < 16; ++u) mid = u == on ? acc[u] : mid;
-              if (kPhase == kGram) {
-                P.d[k * S.mp + row] = mid * (1.f / (kX * kX));
-              } else {
-                const float d = D[row];
-                P.e[k * S.mp + row] = c3 * d + c5 * __fmaf_rn(d, d, mid * (1.f / (kO * kO)));
-              }
+              if (kPhase == kGram) P.d[k * S.mp + row] = mid * (1.f / (kX * kX));
+              else P.e[k * S.mp + row] = c3 * dr + c5 * __fmaf_rn(dr, dr, mid * (1.f / (kO * kO)));
               char* place = on < 8 ? at[0] : at[1];
               *reinterpret_cast<uint16_t*>(place + on % 8 * 2) = 0;
               if (kLow) *reinterpret_cast<uint16_t*>(place + kHeldBytes + on % 8 * 2) = 0;
             }
           }
-          if (c == 1) {  // the sums are read
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) arrive_at(remote(smem_addr(&bars.taken[it & 1]), 0));
-          }
+          if (c == CG - 1) done();
           fence_proxy_async();
           __syncwarp();
           if (lane == 0) {
-            if (Pl::kBuffers == 2 && c == 1 && kPhase != kGram) {
-              bulk_read<0>();  // the first part's store, a while ago
-              fetch(t + step, 0);
-            }
             const int64_t at = part_of(k, tr, tc, c);
             bulk_store(to.hi + at, b, kHeldBytes);
             if (kLow) bulk_store(to.lo + at, b + kHeldBytes, kHeldBytes);
@@ -813,15 +785,15 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
           if (kPhase != kUpdate && tr != tc) {
             // the same above the diagonal: this warp's 64 columns are rows there, two of them a lane, its rows
             // 32 columns, four pieces
-            const int64_t rb = (int64_t)tc * CG + e / 4;  // (64 columns: half a block's rows)
+            const int64_t first_row = cols + c * 64;
             const int64_t cb = ((int64_t)tr * CG + rank) * 2 + w / 2;
-            const int64_t block = k * plane + (rb * bc + cb) * kBlock;
+            const int64_t block = k * plane + (first_row / 128 * bc + cb) * kBlock;
 #pragma unroll 1
             for (int i = 0; i < (kLow ? 16 : 8); ++i) {
               const int low = i / 8, h = i / 4 % 2, p = i % 4;
               const char* plane_at = b + low * kHeldBytes;
               char* out = reinterpret_cast<char*>((low ? to.lo : to.hi) + block);
-              const uint32_t j = h * 32 + lane, r = c * 64 + j;  // column here, row there
+              const uint32_t j = h * 32 + lane, r = (uint32_t)(first_row % 128) + j;  // column here, row there
               alignas(16) uint16_t v[8];
 #pragma unroll
               for (int u = 0; u < 8; ++u)
@@ -829,16 +801,113 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
               *reinterpret_cast<uint4*>(out + piece_at(r, (uint32_t)(w % 2 * 4 + p))) = *reinterpret_cast<const uint4*>(v);
             }
           }
-          if (Pl::kBuffers == 1) {
-            __syncwarp();
-            if (lane == 0) {
-              bulk_read<0>();
-              fetch(c == 0 ? t : t + step, c ^ 1);
+          __syncwarp();
+          if (lane == 0 && kPhase != kGram) {
+            bulk_read();
+            fetch(c + 1 < CG ? t : t + step, c + 1 < CG ? c + 1 : 0);
+          }
+        }
+      };
+
+      for (int64_t unit = first; unit < parts.all && going; unit += step) {
+        const uint32_t acc_at = tmem + e * (64 * CG) + ((uint32_t)w << 21);  // this warp's part of the first accumulator
+        int64_t t;
+        int begin, end;
+        parts.at(unit, &t, &begin, &end);
+        if constexpr (kFine) {
+          float sum[64 * CG];
+#pragma unroll
+          for (int i = 0; i < 64 * CG; ++i) sum[i] = 0.f;
+          for (int kb = begin; kb < end; kb += Pl::kChunk) {
+            going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
+            if (!going) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < 4 * CG; i += 2) {
+              float one[16], two[16];
+              tmem_load16(acc_at + (it & 1) * kColumns + i * 16, one);
+              tmem_load16(acc_at + (it & 1) * kColumns + i * 16 + 16, two);
+              tmem_loaded(one);
+              tmem_loaded(two);
+#pragma unroll
+              for (int u = 0; u < 16; ++u) sum[i * 16 + u] += one[u], sum[i * 16 + 16 + u] += two[u];
+            }
+            if (kb + Pl::kChunk < end) {
+              asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) arrive_first<CG>(&bars.taken[it & 1]);
+              ++it;
             }
           }
+          // back into the last accumulator: what follows takes them from there in a loop
+#pragma unroll
+          for (int i = 0; i < 4 * CG; ++i) tmem_store16(acc_at + (it & 1) * kColumns + i * 16, sum + i * 16);
+          tmem_stored();
+        } else {
+          going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        }
+        if (!going) break;
+        float next[16];
+        tmem_load16(acc_at + (it & 1) * kColumns, next);
+        auto sums = [&](int c, int h, float (&acc)[16]) {
+          tmem_loaded(next);
+#pragma unroll
+          for (int u = 0; u < 16; ++u) acc[u] = next[u];
+          if (c < CG - 1 || h < 3) tmem_load16(acc_at + (it & 1) * kColumns + c * 64 + h * 16 + 16, next);
+        };
+        auto done = [&] {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) arrive_first<CG>(&bars.taken[it & 1]);
+        };
+        if (kPhase == kGram && parts.splits > 1) {
+          float* share = share_of(t, (int)(unit % parts.splits));
+#pragma unroll 1
+          for (int i = 0; i < 4 * CG; ++i) {
+            float acc[16];
+            sums(i / 4, i % 4, acc);
+#pragma unroll
+            for (int u = 0; u < 16; ++u) share[(i * 16 + u) * 32] = acc[u];
+          }
+          done();  // (a barrier of the warp)
+          if (lane == 0)
+            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(P.shared + (t * CG + rank) * Pl::kWarps + warp - 2) : "memory");
+        } else {
+          finish(t, sums, done);
         }
         tmem_loaded(next);  // (nothing is on its way, but where a wait gave up)
         ++it;
+      }
+      if constexpr (kPhase == kGram) {
+        // Shares of tiles are added up, in their order, by the warps that have the same place in the tile: of
+        // eight, each share's block takes its part. (None waits before all its own shares are out.)
+        if (parts.splits > 1)
+          for (int64_t unit = first; unit < parts.all && going; unit += step) {
+            const int64_t t = unit / parts.splits;
+            if ((warp - 2) % parts.splits != (int)(unit % parts.splits)) continue;
+            const uint32_t* count = P.shared + (t * CG + rank) * Pl::kWarps + warp - 2;
+            going = __all_sync(0xffffffffu, lane != 0 || wait_count(count, (uint32_t)parts.splits * (index / 3 + 1), dead));
+            if (!going) break;
+            auto sums = [&](int c, int h, float (&acc)[16]) {
+#pragma unroll
+              for (int u = 0; u < 16; ++u) acc[u] = 0.f;
+              for (int split = 0; split < parts.splits; split += 4) {
+                float of[4][16];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                  const float* share = share_of(t, split + v) + (c * 64 + h * 16) * 32;
+#pragma unroll
+                  for (int u = 0; u < 16; ++u) of[v][u] = split + v < parts.splits ? __ldcg(share + u * 32) : 0.f;
+                }
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                  for (int u = 0; u < 16; ++u) acc[u] += of[v][u];
+              }
+            };
+            finish(t, sums, [] {});
+          }
       }
       // what this block wrote is there for the next phase (which orders its copies after it)
       if (lane == 0) bulk_done();
@@ -846,12 +915,10 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         fence_proxy_async_all();
       } else {
         asm volatile("bar.sync 1, %0;" ::"n"(32 * Pl::kWarps) : "memory");
-        if (e == 0 && lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(P.phases) : "memory");
+        if (warp == 2 && lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(P.phases) : "memory");
       }
     });
-    if (lane == 0)
-      for (uint32_t i = fetched > Pl::kBuffers ? fetched - Pl::kBuffers : 0; i < fetched; ++i)
-        wait_bounded(&in[i % Pl::kBuffers], (i / Pl::kBuffers) & 1, kWaitLimitNs);
+    if (lane == 0 && fetched) wait_bounded(in, (fetched - 1) & 1, kWaitLimitNs);
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -881,7 +948,7 @@ cudaError_t launch_phases(const CUtensorMap& map, const ProductArgs& P, int devi
   const bool together = P.end - P.begin > 1;
   if ((CG > 1 || together) && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
   const int64_t rows = P.S.mp / (128 * CG), cols = P.S.np / (128 * CG);
-  const int64_t most = sms / CG, tiles = P.K * std::max(rows * cols, rows * (rows + 1) / 2);
+  const int64_t most = sms / CG, tiles = P.K * std::max(rows * cols, rows * (rows + 1) / 2 * P.splits);
   LaunchConfig l((tiles < most ? tiles : most) * CG, Pl::kThreads, CG, smem, s);
   if (together) {  // in the place of programmatic serialization
     l.at[0].id = cudaLaunchAttributeCooperative;
@@ -896,6 +963,7 @@ cudaError_t all_steps(const CUtensorMap& map, ProductArgs P, int device, int sms
   if (!too_large_here(e)) return e;
   cudaGetLastError();  // this launch's
   const int end = P.end;
+  P.splits = 1;  // (shares wait for each other)
   for (e = cudaSuccess; P.begin < end && e == cudaSuccess; ++P.begin) {
     P.end = P.begin + 1;
     e = launch_phases<CG, kFine>(map, P, device, sms, s);
@@ -925,37 +993,68 @@ cudaError_t map_of(void* base, int64_t bytes, CUtensorMap* map) {
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// How a call is carried out: tiles of one block or of a pair, and the shares that X's columns are
+// taken in. By what the phases take, in cycles.
+struct Course {
+  Shape S;
+  bool pairs;
+  int splits;
+};
+constexpr int kSms = 152, kMostSplits = 16;
+int64_t phase_cycles(int64_t units, int slots, int64_t kblocks, int64_t per_kblock, int64_t finish) {
+  return (units + slots - 1) / slots * std::max(kblocks * per_kblock, finish) + finish;
+}
+Course course_of(int64_t K, int64_t m, int64_t n, bool fine) {
+  if (m > n) std::swap(m, n);
+  Course best{};
+  int64_t least = INT64_MAX;
+  for (int cg = 1; cg <= 2; ++cg) {
+    const int unit = 128 * cg, slots = kSms / cg;
+    const int64_t per = cg == 1 ? (fine ? 1130 : 560) : (fine ? 1560 : 560), finish = cg == 1 ? 2500 : 4500;
+    const Shape S{m, n, up(m, unit), up(n, unit)};
+    const int64_t R = S.mp / unit, C = S.np / unit, half = K * (R * (R + 1) / 2), kn = (n + 63) / 64, km = (m + 63) / 64;
+    int splits = 1;
+    int64_t gram = phase_cycles(half, slots, kn, per, finish);
+    for (int64_t s = 2; s <= kMostSplits && s <= kn; ++s) {
+      if ((s - 1) * ((kn + s - 1) / s) >= kn) continue;  // a share without columns
+      const int64_t sum = (half * s + slots - 1) / slots * (1500 + 4000 * cg * ((s + 3) / 4));  // written, and added up
+      const int64_t t = phase_cycles(half * s, slots, (kn + s - 1) / s, per, finish) + sum;
+      if (t < gram) gram = t, splits = (int)s;
+    }
+    const int64_t all = gram + phase_cycles(half, slots, km, per, finish) + phase_cycles(K * R * C, slots, km, per, finish);
+    if (all < least) least = all, best = Course{S, cg == 2, splits};
+  }
+  return best;
+}
+
 struct Work {
   double* part;
   uint32_t* counts;  // gave up, phases
-  float *d, *e;
+  uint32_t* shared;
+  int64_t counters;  // of all these
+  float *shares, *d, *e;
   Halves2 x, y, o, r;
 };
-int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
-// Whether pairs of blocks take tiles of 256 x 256.
-bool by_pairs(int64_t m, int64_t n) { return (m < n ? m : n) >= 512; }
-Shape shape_of(int64_t m, int64_t n) {
-  const int64_t whole = by_pairs(m, n) ? 256 : 128;
-  if (m > n) {
-    const int64_t t = m;
-    m = n;
-    n = t;
-  }
-  return Shape{m, n, up(m, whole), up(n, whole)};
-}
-int64_t work_of(int32_t dtype, int64_t K, const Shape& S, char* at, Work* w) {
+int64_t work_of(bool fine, int64_t K, const Course& c, char* at, Work* w) {
   int64_t bytes = 0;
   auto take = [&](int64_t n) {
     char* p = at + bytes;
     bytes += up(n, 1024);
     return p;
   };
+  const Shape& S = c.S;
+  const int cg = c.pairs ? 2 : 1;
+  const int64_t R = S.mp / (128 * cg), tiles = c.splits > 1 ? K * (R * (R + 1) / 2) : 0;
   Work v;
   v.part = reinterpret_cast<double*>(take(8 * K * kMostSizeParts));
-  v.counts = reinterpret_cast<uint32_t*>(take(8));
+  v.counters = 2 + tiles * cg * 8;
+  v.counts = reinterpret_cast<uint32_t*>(take(4 * v.counters));
+  v.shared = v.counts + 2;
+  v.shares = reinterpret_cast<float*>(take(4 * tiles * c.splits * (128 * cg) * (128 * cg)));
   v.d = reinterpret_cast<float*>(take(4 * K * S.mp));
   v.e = reinterpret_cast<float*>(take(4 * K * S.mp));
-  const bool fine = dtype != GMC_BF16;
   for (Halves2* h : {&v.x, &v.y, &v.o, &v.r}) {
     const bool is_x = h == &v.x || h == &v.y;
     const int64_t n = 2 * K * (is_x ? S.x() : S.o());
@@ -984,7 +1083,8 @@ extern "C" {
 
 int64_t gmc_orthogonalize_workspace(int32_t dtype, int64_t K, int64_t m, int64_t n) {
   if (!sizes_ok(dtype, K, m, n)) return -1;
-  const int64_t bytes = work_of(dtype, K, shape_of(m, n), nullptr, nullptr);
+  const bool fine = dtype != GMC_BF16;
+  const int64_t bytes = work_of(fine, K, course_of(K, m, n, fine), nullptr, nullptr);
   return bytes <= kMostWork ? bytes : -1;
 }
 
@@ -998,14 +1098,16 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
   if (K == 0 || m == 0 || n == 0) return GMC_OK;
   if (!strides_ok(x_dev, dtype, K, m, n, ldk, ld) || !strides_ok(out_dev, dtype, K, m, n, out_ldk, out_ld))
     return GMC_EINVAL;
-  const Shape S = shape_of(m, n);
+  const bool of_two = dtype != GMC_BF16;
+  const Course course = course_of(K, m, n, of_two);
+  const Shape S = course.S;
   Work w;
-  const int64_t need = work_of(dtype, K, S, static_cast<char*>(workspace_dev), &w);
+  const int64_t need = work_of(of_two, K, course, static_cast<char*>(workspace_dev), &w);
   if (!workspace_dev || reinterpret_cast<uintptr_t>(workspace_dev) % 256 || need > kMostWork || workspace_bytes < need)
     return GMC_EINVAL;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool turned = m > n;
-  bool pairs = by_pairs(m, n);
+  bool pairs = course.pairs;
   int device = 0, sms = 0;
   cudaError_t err = cudaGetDevice(&device);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
@@ -1022,18 +1124,20 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
     constexpr bool fine = !std::is_same<T, __nv_bfloat16>::value;
     const T* g = static_cast<const T*>(x_dev);
     T* o = static_cast<T*>(out_dev);
-    cudaError_t e = launch_pdl(k_size<T>, dim3((unsigned)parts, (unsigned)K), dim3(256), 0, s, g, ldk, ld, m, n, w.part, w.counts);
+    cudaError_t e = launch_pdl(k_size<T>, dim3((unsigned)parts, (unsigned)K), dim3(256), 0, s, g, ldk, ld, m, n, w.part, w.counts,
+                               w.counters);
     if (e != cudaSuccess) return e;
     e = launch_pdl(turned ? k_first<T, true> : k_first<T, false>, some, dim3(256), 0, s, g, ldk, ld, S, (const double*)w.part,
                    parts, w.x);
     if (e != cudaSuccess) return e;
-    ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps, w.counts + 1,
-                  w.counts, {}};
+    ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps,
+                  course.splits, w.shares, w.shared, w.counts + 1, w.counts, {}};
     std::copy(coefficients_host, coefficients_host + 3 * steps, P.coef);
     if (pairs) e = all_steps<2, fine>(map, P, device, sms, s);
     if (pairs && too_large_here(e)) {  // a context without room for clusters
       cudaGetLastError();
       pairs = false;
+      P.splits = 1;
     }
     if (!pairs) e = all_steps<1, fine>(map, P, device, sms, s);
     if (e != cudaSuccess) return e;
