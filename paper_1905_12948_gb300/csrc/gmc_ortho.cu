@@ -410,6 +410,7 @@ struct ProductArgs {
   Halves2 x[2], o, r;   // X before and after each step, in turn; O, R
   float *d, *e;         // diagonals of A and B, mp each
   int begin, end;       // phases of this launch, three a step
+  bool triangle;        // of A and B, tiles on and below the diagonal
   int splits;           // shares of a tile's sum over X's columns
   float* shares;        // their sums,
   uint32_t* shared;     // and how many of them are there, by warps
@@ -426,11 +427,12 @@ constexpr int kFactorBytes = 16384;  // of a stage: 128 rows, or columns, by 64
 constexpr int kHeldBytes = 4096;     // a warp's part of a block of halves
 template <int CG, bool kFine>
 struct Plan {
-  static constexpr int kStages = kFine ? 2 : 5;
+  static constexpr int kBuffers = CG == 1 && !kFine ? 2 : 1;  // of a warp that reads sums back
+  static constexpr int kStages = kFine ? 2 : kBuffers == 2 ? 3 : 5;
   static constexpr int kStageBytes = (kFine ? 4 : 2) * kFactorBytes;
   static constexpr int kWarps = 8;         // that read the sums back: 32 rows, and 64 CG columns each
   static constexpr int kThreads = 64 + 32 * kWarps;
-  static constexpr int kHeld = kWarps * 2 * kHeldBytes;  // a part of a block, two halves, for each
+  static constexpr int kHeld = kWarps * kBuffers * 2 * kHeldBytes;  // parts of a block, two halves, for each
   // Sums in the tensor cores are cut off, not rounded: by a quarter of a last place an addition where
   // all terms have one sign (4,608 columns of fp32 matrices: 2.8e-5 off the result, by three additions for
   // 16 columns). They are added up in registers after 128.
@@ -439,7 +441,7 @@ struct Plan {
 struct alignas(8) ProductBars {
   uint64_t full[5], empty[5];
   uint64_t sums[2], taken[2];  // accumulators: written, read back
-  uint64_t held[8];
+  uint64_t held[8][2];
   uint32_t tmem, dead;
 };
 template <int CG, bool kFine>
@@ -448,14 +450,15 @@ constexpr int product_smem() {
   return Pl::kStages * Pl::kStageBytes + Pl::kHeld + 1024 + (int)sizeof(ProductBars);
 }
 
-// Tiles of all K matrices. A and B are symmetric: the tiles on and below the diagonal.
+// Tiles of all K matrices. A and B are symmetric: the tiles on and below the diagonal do, where that
+// saves more than writing each of them twice takes.
 struct Tiles {
   int rows, cols;  // of a matrix; cols = 0: a triangle
   int64_t each, all;
-  __device__ Tiles(const Shape& S, int64_t K, int unit, bool triangle) {
+  __device__ Tiles(const Shape& S, int64_t K, int unit, bool symmetric, bool triangle) {
     rows = (int)(S.mp / unit);
-    cols = triangle ? 0 : (int)(S.np / unit);
-    each = triangle ? (int64_t)rows * (rows + 1) / 2 : (int64_t)rows * cols;
+    cols = !symmetric ? (int)(S.np / unit) : triangle ? 0 : rows;
+    each = cols ? (int64_t)rows * cols : (int64_t)rows * (rows + 1) / 2;
     all = each * K;
   }
   __device__ void at(int64_t t, int64_t* k, int* row, int* col) const {
@@ -522,7 +525,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       mbar_init(&bars.sums[i], 1);
       mbar_init(&bars.taken[i], Pl::kWarps * CG);
     }
-    for (int w = 0; w < Pl::kWarps; ++w) mbar_init(&bars.held[w], 1);
+    for (int w = 0; w < Pl::kWarps; ++w) mbar_init(&bars.held[w][0], 1), mbar_init(&bars.held[w][1], 1);
     bars.dead = 0;
     fence_mbar_init();
   }
@@ -560,7 +563,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       bool going = true;
       each_phase([&](auto phase, int index, const Halves2& x) {
         constexpr int kPhase = decltype(phase)::value;
-        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
+        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, P.triangle);
         const Parts parts(P, tiles, kPhase);
         going = going && wait_phase(index);
         const Halves2 left = kPhase == kGram ? x : kPhase == kSquare ? P.o : P.r;
@@ -614,7 +617,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       bool going = true;
       each_phase([&](auto phase, int, const Halves2&) {
         constexpr int kPhase = decltype(phase)::value;
-        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
+        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, P.triangle);
         const Parts parts(P, tiles, kPhase);
         // 32-bit sums of halves; the right factor's rows are the sum's index in kUpdate
         constexpr uint32_t what = 1u << 4 | (kPhase == kUpdate ? 1u << 16 : 0) | (CG * 128 / 8) << 17 | (CG * 128 / 16) << 24;
@@ -658,13 +661,13 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
     }
   } else {
     const int w = warp & 3, e = (warp - 2) / 4;  // rows 32 w of the block's part of the tile, columns 64 CG e
-    char* b = held + (warp - 2) * 2 * kHeldBytes;
-    uint64_t* in = &bars.held[warp - 2];
+    char* own = held + (warp - 2) * Pl::kBuffers * 2 * kHeldBytes;
+    uint64_t* in = bars.held[warp - 2];
     uint32_t fetched = 0, q = 0, it = 0;  // parts of blocks on their way or read, read; accumulators read
     bool going = true;
     each_phase([&](auto phase, int index, const Halves2& x) {
       constexpr int kPhase = decltype(phase)::value;
-      const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate);
+      const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, P.triangle);
       const Parts parts(P, tiles, kPhase);
       const float c1 = P.coef[index / 3 * 3], c3 = P.coef[index / 3 * 3 + 1], c5 = P.coef[index / 3 * 3 + 2];
       going = __all_sync(0xffffffffu, going && (lane != 0 || wait_phase(index)));
@@ -683,9 +686,11 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         int row, col;
         tiles.at(t, &k, &row, &col);
         const int64_t at = part_of(k, row, col, c);
-        mbar_arrive_expect_tx(in, (kLow ? 2 : 1) * kHeldBytes);
-        bulk_load(b, from.hi + at, kHeldBytes, in);
-        if (kLow) bulk_load(b + kHeldBytes, from.lo + at, kHeldBytes, in);
+        char* to = own + fetched % Pl::kBuffers * 2 * kHeldBytes;
+        uint64_t* bar = in + fetched % Pl::kBuffers;
+        mbar_arrive_expect_tx(bar, (kLow ? 2 : 1) * kHeldBytes);
+        bulk_load(to, from.hi + at, kHeldBytes, bar);
+        if (kLow) bulk_load(to + kHeldBytes, from.lo + at, kHeldBytes, bar);
         ++fetched;
       };
       // this warp's sums of one share of tile t, 64 CG columns of 32 rows
@@ -712,11 +717,15 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         // fetched. 64 columns took 4,500 to 9,000 cycles unrolled, 1,200 to 2,200 in loops of 16.)
 #pragma unroll 1
         for (int c = 0; c < CG; ++c) {
-          if (kPhase == kGram) {
-            if (lane == 0) bulk_read();  // the last store from here
+          char* b = own + (kPhase == kGram ? 0 : q % Pl::kBuffers) * 2 * kHeldBytes;
+          if (kPhase == kGram || Pl::kBuffers == 2) {
+            __syncwarp();                // (the last tile's mirror has been read)
+            if (lane == 0) bulk_read();  // the last store
+            if (lane == 0 && Pl::kBuffers == 2) fetch(c + 1 < CG ? t : t + step, c + 1 < CG ? c + 1 : 0);
             __syncwarp();
-          } else {
-            going = __all_sync(0xffffffffu, wait_for(in, q & 1, dead));
+          }
+          if (kPhase != kGram) {
+            going = __all_sync(0xffffffffu, wait_for(in + q % Pl::kBuffers, (q / Pl::kBuffers) & 1, dead));
             ++q;
           }
           if (!going) return;
@@ -782,7 +791,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
             if (kLow) bulk_store(to.lo + at, b + kHeldBytes, kHeldBytes);
             bulk_commit();
           }
-          if (kPhase != kUpdate && tr != tc) {
+          if (kPhase != kUpdate && P.triangle && tr != tc) {
             // the same above the diagonal: this warp's 64 columns are rows there, two of them a lane, its rows
             // 32 columns, four pieces
             const int64_t first_row = cols + c * 64;
@@ -802,7 +811,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
             }
           }
           __syncwarp();
-          if (lane == 0 && kPhase != kGram) {
+          if (lane == 0 && kPhase != kGram && Pl::kBuffers == 1) {
             bulk_read();
             fetch(c + 1 < CG ? t : t + step, c + 1 < CG ? c + 1 : 0);
           }
@@ -918,7 +927,9 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         if (warp == 2 && lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(P.phases) : "memory");
       }
     });
-    if (lane == 0 && fetched) wait_bounded(in, (fetched - 1) & 1, kWaitLimitNs);
+    if (lane == 0)
+      for (uint32_t i = fetched > Pl::kBuffers ? fetched - Pl::kBuffers : 0; i < fetched; ++i)
+        wait_bounded(in + i % Pl::kBuffers, (i / Pl::kBuffers) & 1, kWaitLimitNs);
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -948,7 +959,7 @@ cudaError_t launch_phases(const CUtensorMap& map, const ProductArgs& P, int devi
   const bool together = P.end - P.begin > 1;
   if ((CG > 1 || together) && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
   const int64_t rows = P.S.mp / (128 * CG), cols = P.S.np / (128 * CG);
-  const int64_t most = sms / CG, tiles = P.K * std::max(rows * cols, rows * (rows + 1) / 2 * P.splits);
+  const int64_t most = sms / CG, tiles = P.K * std::max(rows * cols, (P.triangle ? rows * (rows + 1) / 2 : rows * rows) * P.splits);
   LaunchConfig l((tiles < most ? tiles : most) * CG, Pl::kThreads, CG, smem, s);
   if (together) {  // in the place of programmatic serialization
     l.at[0].id = cudaLaunchAttributeCooperative;
@@ -999,8 +1010,12 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // taken in. By what the phases take, in cycles.
 struct Course {
   Shape S;
-  bool pairs;
+  bool pairs, triangle;
   int splits;
+  int64_t tiles() const {  // of a symmetric product
+    const int64_t R = S.mp / (pairs ? 256 : 128);
+    return triangle ? R * (R + 1) / 2 : R * R;
+  }
 };
 constexpr int kSms = 152, kMostSplits = 16;
 int64_t phase_cycles(int64_t units, int slots, int64_t kblocks, int64_t per_kblock, int64_t finish) {
@@ -1014,17 +1029,21 @@ Course course_of(int64_t K, int64_t m, int64_t n, bool fine) {
     const int unit = 128 * cg, slots = kSms / cg;
     const int64_t per = cg == 1 ? (fine ? 1130 : 560) : (fine ? 1560 : 560), finish = cg == 1 ? 2500 : 4500;
     const Shape S{m, n, up(m, unit), up(n, unit)};
-    const int64_t R = S.mp / unit, C = S.np / unit, half = K * (R * (R + 1) / 2), kn = (n + 63) / 64, km = (m + 63) / 64;
-    int splits = 1;
-    int64_t gram = phase_cycles(half, slots, kn, per, finish);
-    for (int64_t s = 2; s <= kMostSplits && s <= kn; ++s) {
-      if ((s - 1) * ((kn + s - 1) / s) >= kn) continue;  // a share without columns
-      const int64_t sum = (half * s + slots - 1) / slots * (1500 + 4000 * cg * ((s + 3) / 4));  // written, and added up
-      const int64_t t = phase_cycles(half * s, slots, (kn + s - 1) / s, per, finish) + sum;
-      if (t < gram) gram = t, splits = (int)s;
+    const int64_t R = S.mp / unit, C = S.np / unit, kn = (n + 63) / 64, km = (m + 63) / 64;
+    const int64_t update = phase_cycles(K * R * C, slots, km, per, finish);
+    for (int triangle = 0; triangle < 2; ++triangle) {
+      const int64_t tiles = K * (triangle ? R * (R + 1) / 2 : R * R), end = finish + (triangle && R > 1 ? 4000 * cg : 0);
+      const int64_t square = phase_cycles(tiles, slots, km, per, end);
+      int splits = 1;
+      int64_t gram = phase_cycles(tiles, slots, kn, per, end);
+      for (int64_t s = 2; s <= kMostSplits && s <= kn; ++s) {
+        if ((s - 1) * ((kn + s - 1) / s) >= kn) continue;  // a share without columns
+        const int64_t sum = (tiles * s + slots - 1) / slots * (1500 + 4000 * cg * ((s + 3) / 4));  // written, and added up
+        const int64_t t = phase_cycles(tiles * s, slots, (kn + s - 1) / s, per, end) + sum;
+        if (t < gram) gram = t, splits = (int)s;
+      }
+      if (gram + square + update < least) least = gram + square + update, best = Course{S, cg == 2, triangle == 1, splits};
     }
-    const int64_t all = gram + phase_cycles(half, slots, km, per, finish) + phase_cycles(K * R * C, slots, km, per, finish);
-    if (all < least) least = all, best = Course{S, cg == 2, splits};
   }
   return best;
 }
@@ -1046,7 +1065,7 @@ int64_t work_of(bool fine, int64_t K, const Course& c, char* at, Work* w) {
   };
   const Shape& S = c.S;
   const int cg = c.pairs ? 2 : 1;
-  const int64_t R = S.mp / (128 * cg), tiles = c.splits > 1 ? K * (R * (R + 1) / 2) : 0;
+  const int64_t tiles = c.splits > 1 ? K * c.tiles() : 0;
   Work v;
   v.part = reinterpret_cast<double*>(take(8 * K * kMostSizeParts));
   v.counters = 2 + tiles * cg * 8;
@@ -1131,7 +1150,7 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
                    parts, w.x);
     if (e != cudaSuccess) return e;
     ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps,
-                  course.splits, w.shares, w.shared, w.counts + 1, w.counts, {}};
+                  course.triangle, course.splits, w.shares, w.shared, w.counts + 1, w.counts, {}};
     std::copy(coefficients_host, coefficients_host + 3 * steps, P.coef);
     if (pairs) e = all_steps<2, fine>(map, P, device, sms, s);
     if (pairs && too_large_here(e)) {  // a context without room for clusters
