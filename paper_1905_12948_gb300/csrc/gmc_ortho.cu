@@ -345,28 +345,30 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
                  "h"((uint16_t)3)
                  : "memory");
 }
-__device__ __forceinline__ void tmem_load16(uint32_t at, float* f) {
-  uint32_t* r = reinterpret_cast<uint32_t*>(f);
+// kStep columns of a warp's 32 rows of tensor memory, and back.
+constexpr int kStep = 16;
+__device__ __forceinline__ void tmem_load(uint32_t at, float (&f)[kStep]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]), "=f"(f[8]),
+        "=f"(f[9]), "=f"(f[10]), "=f"(f[11]), "=f"(f[12]), "=f"(f[13]), "=f"(f[14]), "=f"(f[15])
       : "r"(at));
 }
-__device__ __forceinline__ void tmem_store16(uint32_t at, const float* f) {
-  const uint32_t* r = reinterpret_cast<const uint32_t*>(f);
+__device__ __forceinline__ void tmem_store(uint32_t at, const float* f) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(at),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]), "f"(f[8]), "f"(f[9]),
+      "f"(f[10]), "f"(f[11]), "f"(f[12]), "f"(f[13]), "f"(f[14]), "f"(f[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // (The registers are named: nothing may look at them before.)
-__device__ __forceinline__ void tmem_loaded(float (&f)[16]) {
+__device__ __forceinline__ void tmem_loaded(float (&f)[kStep]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]), "+f"(f[8]),
-                 "+f"(f[9]), "+f"(f[10]), "+f"(f[11]), "+f"(f[12]), "+f"(f[13]), "+f"(f[14]), "+f"(f[15])::"memory");
+               : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]), "+f"(f[4]), "+f"(f[5]), "+f"(f[6]), "+f"(f[7]),
+                 "+f"(f[8]), "+f"(f[9]), "+f"(f[10]), "+f"(f[11]), "+f"(f[12]), "+f"(f[13]), "+f"(f[14]), "+f"(f[15])
+               :
+               : "memory");
 }
 // Shared memory of a factor: rows of 128 bytes, eight of them (1 KB) a group; `stride` bytes
 // from one 64-column block to the next where the factor's rows are the sum's index.
@@ -410,8 +412,9 @@ struct ProductArgs {
   Halves2 x[2], o, r;   // X before and after each step, in turn; O, R
   float *d, *e;         // diagonals of A and B, mp each
   int begin, end;       // phases of this launch, three a step
-  bool triangle;        // of A and B, tiles on and below the diagonal
-  int splits;           // shares of a tile's sum over X's columns
+  bool triangle[2];     // of A, of B: tiles on and below the diagonal
+  int64_t whole;        // tiles of A that one block (or pair) sums alone,
+  int splits;           // and in how many shares the others are summed
   float* shares;        // their sums,
   uint32_t* shared;     // and how many of them are there, by warps
   uint32_t* phases;     // counts the blocks that are done with each
@@ -427,12 +430,15 @@ constexpr int kFactorBytes = 16384;  // of a stage: 128 rows, or columns, by 64
 constexpr int kHeldBytes = 4096;     // a warp's part of a block of halves
 template <int CG, bool kFine>
 struct Plan {
-  static constexpr int kBuffers = CG == 1 && !kFine ? 2 : 1;  // of a warp that reads sums back
-  static constexpr int kStages = kFine ? 2 : kBuffers == 2 ? 3 : 5;
+  // Warps that read the sums back, 32 rows each; 64 columns at a time, with as many parts of a block (two
+  // halves) on their way to it.
+  static constexpr int kWarps = CG == 2 && !kFine ? 4 : 8;
+  static constexpr int kBuffers = kFine ? 1 : 2;
+  static constexpr int kStages = kFine ? 2 : CG == 1 ? 3 : 5;
   static constexpr int kStageBytes = (kFine ? 4 : 2) * kFactorBytes;
-  static constexpr int kWarps = 8;         // that read the sums back: 32 rows, and 64 CG columns each
+  static constexpr int kItems = 8 * CG / kWarps;  // of a warp, 64 columns each
   static constexpr int kThreads = 64 + 32 * kWarps;
-  static constexpr int kHeld = kWarps * kBuffers * 2 * kHeldBytes;  // parts of a block, two halves, for each
+  static constexpr int kHeld = kWarps * kBuffers * 2 * kHeldBytes;
   // Sums in the tensor cores are cut off, not rounded: by a quarter of a last place an addition where
   // all terms have one sign (4,608 columns of fp32 matrices: 2.8e-5 off the result, by three additions for
   // 16 columns). They are added up in registers after 128.
@@ -461,9 +467,11 @@ struct Tiles {
     each = cols ? (int64_t)rows * cols : (int64_t)rows * (rows + 1) / 2;
     all = each * K;
   }
+  // (a workspace of kMostWork holds less than 2^24 of them)
   __device__ void at(int64_t t, int64_t* k, int* row, int* col) const {
-    *k = t / each;
-    const int i = (int)(t - *k * each);
+    const uint32_t n = (uint32_t)t / (uint32_t)each;
+    *k = n;
+    const int i = (int)((uint32_t)t - n * (uint32_t)each);
     if (cols) {
       *row = i % rows;
       *col = i / rows;
@@ -477,22 +485,25 @@ struct Tiles {
   }
 };
 
-// The units of work of a phase: tiles, or shares of them, the columns of X in `splits` parts.
+// The units of work of a phase: tiles, then, of A, shares of tiles, a part of X's columns each. (Tiles that are too
+// few for another round of all blocks are shared.)
 struct Parts {
   int splits, kblocks, per;
-  int64_t all;
+  int64_t whole, all;
   __device__ Parts(const ProductArgs& P, const Tiles& tiles, int phase) {
     splits = phase == kGram ? P.splits : 1;
     kblocks = (int)(((phase == kGram ? P.S.n : P.S.m) + 63) / 64);
     per = (kblocks + splits - 1) / splits;
-    all = tiles.all * splits;
+    whole = splits > 1 ? P.whole : tiles.all;
+    all = whole + (tiles.all - whole) * splits;
   }
-  // its tile, and blocks of 64 of the sum (none for the last ones where they do not go round: not planned)
+  // its tile, and blocks of 64 of the sum
   __device__ void at(int64_t unit, int64_t* t, int* begin, int* end) const {
-    *t = unit / splits;
-    *begin = (int)(unit % splits) * per;
-    *end = *begin + per < kblocks ? *begin + per : kblocks;
+    *t = unit < whole ? unit : whole + (uint32_t)(unit - whole) / (uint32_t)splits;
+    *begin = unit < whole ? 0 : split_of(unit) * per;
+    *end = unit < whole || *begin + per > kblocks ? kblocks : *begin + per;
   }
+  __device__ int split_of(int64_t unit) const { return (int)((uint32_t)(unit - whole) % (uint32_t)splits); }
 };
 
 // The phases of all steps, with a barrier over the grid between two of them (the blocks are resident together);
@@ -563,7 +574,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       bool going = true;
       each_phase([&](auto phase, int index, const Halves2& x) {
         constexpr int kPhase = decltype(phase)::value;
-        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, P.triangle);
+        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, kPhase != kUpdate && P.triangle[kPhase % kUpdate]);
         const Parts parts(P, tiles, kPhase);
         going = going && wait_phase(index);
         const Halves2 left = kPhase == kGram ? x : kPhase == kSquare ? P.o : P.r;
@@ -617,7 +628,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       bool going = true;
       each_phase([&](auto phase, int, const Halves2&) {
         constexpr int kPhase = decltype(phase)::value;
-        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, P.triangle);
+        const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, kPhase != kUpdate && P.triangle[kPhase % kUpdate]);
         const Parts parts(P, tiles, kPhase);
         // 32-bit sums of halves; the right factor's rows are the sum's index in kUpdate
         constexpr uint32_t what = 1u << 4 | (kPhase == kUpdate ? 1u << 16 : 0) | (CG * 128 / 8) << 17 | (CG * 128 / 16) << 24;
@@ -660,14 +671,14 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         wait_bounded(&bars.empty[i % Pl::kStages], (i / Pl::kStages) & 1, kWaitLimitNs);
     }
   } else {
-    const int w = warp & 3, e = (warp - 2) / 4;  // rows 32 w of the block's part of the tile, columns 64 CG e
+    const int w = warp & 3, e = (warp - 2) / 4;  // rows 32 w of the block's part of the tile, columns 64 kItems e
     char* own = held + (warp - 2) * Pl::kBuffers * 2 * kHeldBytes;
     uint64_t* in = bars.held[warp - 2];
     uint32_t fetched = 0, q = 0, it = 0;  // parts of blocks on their way or read, read; accumulators read
     bool going = true;
     each_phase([&](auto phase, int index, const Halves2& x) {
       constexpr int kPhase = decltype(phase)::value;
-      const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, P.triangle);
+      const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, kPhase != kUpdate && P.triangle[kPhase % kUpdate]);
       const Parts parts(P, tiles, kPhase);
       const float c1 = P.coef[index / 3 * 3], c3 = P.coef[index / 3 * 3 + 1], c5 = P.coef[index / 3 * 3 + 2];
       going = __all_sync(0xffffffffu, going && (lane != 0 || wait_phase(index)));
@@ -675,17 +686,16 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
       const Halves2 from = kPhase == kUpdate ? x : P.o;
       const Halves2 to = kPhase == kGram ? P.o : kPhase == kSquare ? P.r : P.x[(index / 3 + 1) & 1];
       const int64_t bc = kPhase == kUpdate ? xc : oc, plane = kPhase == kUpdate ? S.x() : S.o();
-      // where this warp's part of a block of halves lies
-      auto part_of = [&](int64_t k, int row, int col, int c) {
-        const int64_t rb = (int64_t)row * CG + rank, cb = ((int64_t)col * 2 + e) * CG + c;
-        return k * plane + (rb * bc + cb) * kBlock + w * (kHeldBytes / 2);
-      };
-      auto fetch = [&](int64_t t, int c) {  // the next one
-        if (kPhase == kGram || t >= tiles.all) return;
+      // where this warp's part of a tile's first block of halves lies (the next blocks follow it)
+      auto part_of = [&](int64_t t) {
         int64_t k;
         int row, col;
         tiles.at(t, &k, &row, &col);
-        const int64_t at = part_of(k, row, col, c);
+        const int64_t rb = (int64_t)row * CG + rank, cb = ((int64_t)col * (Pl::kWarps / 4) + e) * Pl::kItems;
+        return k * plane + (rb * bc + cb) * kBlock + w * (kHeldBytes / 2);
+      };
+      auto fetch = [&](int64_t at) {  // the next one
+        if (kPhase == kGram) return;
         char* to = own + fetched % Pl::kBuffers * 2 * kHeldBytes;
         uint64_t* bar = in + fetched % Pl::kBuffers;
         mbar_arrive_expect_tx(bar, (kLow ? 2 : 1) * kHeldBytes);
@@ -693,35 +703,45 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         if (kLow) bulk_load(to + kHeldBytes, from.lo + at, kHeldBytes, bar);
         ++fetched;
       };
-      // this warp's sums of one share of tile t, 64 CG columns of 32 rows
+      // this warp's sums of one share of tile t, 64 kItems columns of 32 rows
       auto share_of = [&](int64_t t, int split) {
-        return P.shares + ((((t * parts.splits + split) * CG + rank) * Pl::kWarps + warp - 2) * (64 * CG)) * 32 + lane;
+        return P.shares + (((((t - parts.whole) * parts.splits + split) * CG + rank) * Pl::kWarps + warp - 2) * (64 * Pl::kItems)) * 32 + lane;
       };
-      if (lane == 0 && going) fetch(first, 0);
+      // and the count of them
+      auto shared = [&](int64_t t) {
+        return P.shared + ((t - parts.whole) * CG + rank) * Pl::kWarps + warp - 2;
+      };
+      if (lane == 0 && going && first < parts.whole) fetch(part_of(first));
 
-      // One tile: `sums(c, h, acc)` gives 16 columns of its sums, in the order of the columns, `done()` says that all were given.
-      auto finish = [&](int64_t t, auto&& sums, auto&& done) {
+      // Items [item, items) of a tile, and `then` the next one (-1: none): `sums(at, acc)` gives kStep columns of its sums, in the order of the columns, `done()` says that all were given.
+      auto finish = [&](int64_t t, int64_t then, int item, int items, auto&& sums, auto&& done) {
         int64_t k;
         int tr, tc;
         tiles.at(t, &k, &tr, &tc);
         const int64_t row = ((int64_t)tr * CG + rank) * 128 + w * 32 + lane;
+        const int64_t part = part_of(t), next_part = then >= 0 ? part_of(then) : -1;
+        // the item after c
+        auto fetch_after = [&](int c) {
+          if (c + 1 < items) fetch(part + (c + 1) * kBlock);
+          else if (next_part >= 0) fetch(next_part);
+        };
         // D and E of the row, D of the warp's columns: 32 at a time, a lane each
         const float* D = P.d + k * S.mp;
         [[maybe_unused]] const float dr = kPhase == kSquare ? D[row] : 0.f, di = c3 + c5 * dr;
         [[maybe_unused]] const float ei = kPhase == kUpdate ? c1 + P.e[k * S.mp + row] : 0.f;
-        const int64_t cols = ((int64_t)tc * 2 + e) * (64 * CG);  // the warp's first column
-        float dj[2 * CG];
+        const int64_t cols = ((int64_t)tc * (Pl::kWarps / 4) + e) * (64 * Pl::kItems);  // the warp's first column
+        float dj[2 * Pl::kItems];
 #pragma unroll
-        for (int i = 0; i < 2 * CG; ++i) dj[i] = kPhase == kSquare ? c5 * D[cols + i * 32 + lane] : 0.f;
+        for (int i = 0; i < 2 * Pl::kItems; ++i) dj[i] = kPhase == kSquare ? c5 * D[cols + i * 32 + lane] : 0.f;
         // (Loops that are not unrolled: each tile goes through this code once, and instructions have to be
-        // fetched. 64 columns took 4,500 to 9,000 cycles unrolled, 1,200 to 2,200 in loops of 16.)
+        // fetched. 64 columns took 4,500 to 9,000 cycles unrolled.)
 #pragma unroll 1
-        for (int c = 0; c < CG; ++c) {
+        for (int c = item; c < items; ++c) {
           char* b = own + (kPhase == kGram ? 0 : q % Pl::kBuffers) * 2 * kHeldBytes;
           if (kPhase == kGram || Pl::kBuffers == 2) {
             __syncwarp();                // (the last tile's mirror has been read)
             if (lane == 0) bulk_read();  // the last store
-            if (lane == 0 && Pl::kBuffers == 2) fetch(c + 1 < CG ? t : t + step, c + 1 < CG ? c + 1 : 0);
+            if (lane == 0 && Pl::kBuffers == 2) fetch_after(c);
             __syncwarp();
           }
           if (kPhase != kGram) {
@@ -730,15 +750,12 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
           }
           if (!going) return;
 #pragma unroll 1
-          for (int h = 0; h < 4; ++h) {  // 16 columns
-            float acc[16];
-            sums(c, h, acc);
-            [[maybe_unused]] const float dh = c == 0 ? (h < 2 ? dj[0] : dj[1]) : (h < 2 ? dj[2 * CG - 2] : dj[2 * CG - 1]);
-            float was[16];
-            char* at[2];
+          for (int h = 0; h < 64; h += kStep) {  // so many columns, eight a piece
+            char* at[kStep / 8];
+            float was[kStep];
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-              at[p] = b + piece_at((uint32_t)lane, (uint32_t)(h * 2 + p));
+            for (int p = 0; p < kStep / 8; ++p) {
+              at[p] = b + piece_at((uint32_t)lane, (uint32_t)(h / 8 + p));
               if (kPhase != kGram) Vec<__half>::get(*reinterpret_cast<const uint4*>(at[p]), was + p * 8);
               if (kPhase != kGram && kLow) {
                 float low[8];
@@ -747,51 +764,58 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
                 for (int u = 0; u < 8; ++u) was[p * 8 + u] += low[u];
               }
             }
+            [[maybe_unused]] float dh = dj[0];
+#pragma unroll
+            for (int i = 1; i < 2 * Pl::kItems; ++i) dh = i == c * 2 + h / 32 ? dj[i] : dh;
+            float acc[kStep];
+            sums(c * 64 + h, acc);
             // (acc: X X' 2^28 times, O^2 2^22 times, R X 2^25 times)
-            alignas(16) __half2 nh[8], nl[8];
-#pragma unroll
-            for (int u = 0; u < 16; u += 2) {
-              float v[2];
-#pragma unroll
-              for (int o = 0; o < 2; ++o) {
-                if constexpr (kPhase == kGram) {
-                  v[o] = acc[u + o] * (kO / (kX * kX));
-                } else if constexpr (kPhase == kSquare) {  // b O + c (O^2 + (D_i + D_j) O)
-                  const float by = di + __shfl_sync(0xffffffffu, dh, (h & 1) * 16 + u + o);
-                  v[o] = __fmaf_rn(by, was[u + o], acc[u + o] * (c5 / kO));
-                } else {
-                  v[o] = __fmaf_rn(ei, was[u + o], acc[u + o] * (1.f / kO));
-                }
-              }
-              two_halves(v[0], v[1], nh + u / 2, nl + u / 2);
-            }
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-              *reinterpret_cast<uint4*>(at[p]) = *reinterpret_cast<const uint4*>(nh + p * 4);
-              if (kLow) *reinterpret_cast<uint4*>(at[p] + kHeldBytes) = *reinterpret_cast<const uint4*>(nl + p * 4);
-            }
-            const int on = (int)(row - (cols + c * 64 + h * 16));  // the column that is on the diagonal
-            if (kPhase != kUpdate && tr == tc && on >= 0 && on < 16) {
+            const int on = (int)(row - (cols + c * 64 + h));  // the column that is on the diagonal
+            if (kPhase != kUpdate && tr == tc && on >= 0 && on < kStep) {
               float mid = 0.f;
 #pragma unroll
-              for (int u = 0; u < 16; ++u) mid = u == on ? acc[u] : mid;
+              for (int u = 0; u < kStep; ++u) mid = u == on ? acc[u] : mid;
               if (kPhase == kGram) P.d[k * S.mp + row] = mid * (1.f / (kX * kX));
               else P.e[k * S.mp + row] = c3 * dr + c5 * __fmaf_rn(dr, dr, mid * (1.f / (kO * kO)));
-              char* place = on < 8 ? at[0] : at[1];
-              *reinterpret_cast<uint16_t*>(place + on % 8 * 2) = 0;
-              if (kLow) *reinterpret_cast<uint16_t*>(place + kHeldBytes + on % 8 * 2) = 0;
+            }
+#pragma unroll
+            for (int p = 0; p < kStep / 8; ++p) {
+              alignas(16) __half2 nh[4], nl[4];
+#pragma unroll
+              for (int u = 0; u < 8; u += 2) {
+                float v[2];
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                  const int j = p * 8 + u + o;
+                  if constexpr (kPhase == kGram) {
+                    v[o] = acc[j] * (kO / (kX * kX));
+                  } else if constexpr (kPhase == kSquare) {  // b O + c (O^2 + (D_i + D_j) O)
+                    v[o] = __fmaf_rn(di + __shfl_sync(0xffffffffu, dh, h % 32 + j), was[j], acc[j] * (c5 / kO));
+                  } else {
+                    v[o] = __fmaf_rn(ei, was[j], acc[j] * (1.f / kO));
+                  }
+                }
+                two_halves(v[0], v[1], nh + u / 2, nl + u / 2);
+              }
+              *reinterpret_cast<uint4*>(at[p]) = *reinterpret_cast<const uint4*>(nh);
+              if (kLow) *reinterpret_cast<uint4*>(at[p] + kHeldBytes) = *reinterpret_cast<const uint4*>(nl);
+            }
+            if (kPhase != kUpdate && tr == tc && on >= 0 && on < kStep) {  // (O and R have none)
+              char* place = b + piece_at((uint32_t)lane, (uint32_t)((h + on) / 8)) + on % 8 * 2;
+              *reinterpret_cast<uint16_t*>(place) = 0;
+              if (kLow) *reinterpret_cast<uint16_t*>(place + kHeldBytes) = 0;
             }
           }
-          if (c == CG - 1) done();
+          if (c == items - 1) done();
           fence_proxy_async();
           __syncwarp();
           if (lane == 0) {
-            const int64_t at = part_of(k, tr, tc, c);
+            const int64_t at = part + c * kBlock;
             bulk_store(to.hi + at, b, kHeldBytes);
             if (kLow) bulk_store(to.lo + at, b + kHeldBytes, kHeldBytes);
             bulk_commit();
           }
-          if (kPhase != kUpdate && P.triangle && tr != tc) {
+          if (kPhase != kUpdate && P.triangle[kPhase % kUpdate] && tr != tc) {
             // the same above the diagonal: this warp's 64 columns are rows there, two of them a lane, its rows
             // 32 columns, four pieces
             const int64_t first_row = cols + c * 64;
@@ -813,33 +837,33 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
           __syncwarp();
           if (lane == 0 && kPhase != kGram && Pl::kBuffers == 1) {
             bulk_read();
-            fetch(c + 1 < CG ? t : t + step, c + 1 < CG ? c + 1 : 0);
+            fetch_after(c);
           }
         }
       };
 
       for (int64_t unit = first; unit < parts.all && going; unit += step) {
-        const uint32_t acc_at = tmem + e * (64 * CG) + ((uint32_t)w << 21);  // this warp's part of the first accumulator
+        const uint32_t acc_at = tmem + e * (64 * Pl::kItems) + ((uint32_t)w << 21);  // this warp's part of the first accumulator
         int64_t t;
         int begin, end;
         parts.at(unit, &t, &begin, &end);
         if constexpr (kFine) {
-          float sum[64 * CG];
+          float sum[64 * Pl::kItems];
 #pragma unroll
-          for (int i = 0; i < 64 * CG; ++i) sum[i] = 0.f;
+          for (int i = 0; i < 64 * Pl::kItems; ++i) sum[i] = 0.f;
           for (int kb = begin; kb < end; kb += Pl::kChunk) {
             going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
             if (!going) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 4 * CG; i += 2) {
-              float one[16], two[16];
-              tmem_load16(acc_at + (it & 1) * kColumns + i * 16, one);
-              tmem_load16(acc_at + (it & 1) * kColumns + i * 16 + 16, two);
+            for (int i = 0; i < 64 * Pl::kItems; i += 2 * kStep) {
+              float one[kStep], two[kStep];
+              tmem_load(acc_at + (it & 1) * kColumns + i, one);
+              tmem_load(acc_at + (it & 1) * kColumns + i + kStep, two);
               tmem_loaded(one);
               tmem_loaded(two);
 #pragma unroll
-              for (int u = 0; u < 16; ++u) sum[i * 16 + u] += one[u], sum[i * 16 + 16 + u] += two[u];
+              for (int u = 0; u < kStep; ++u) sum[i + u] += one[u], sum[i + kStep + u] += two[u];
             }
             if (kb + Pl::kChunk < end) {
               asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -850,72 +874,74 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
           }
           // back into the last accumulator: what follows takes them from there in a loop
 #pragma unroll
-          for (int i = 0; i < 4 * CG; ++i) tmem_store16(acc_at + (it & 1) * kColumns + i * 16, sum + i * 16);
+          for (int i = 0; i < 64 * Pl::kItems; i += kStep) tmem_store(acc_at + (it & 1) * kColumns + i, sum + i);
           tmem_stored();
         } else {
           going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         }
         if (!going) break;
-        float next[16];
-        tmem_load16(acc_at + (it & 1) * kColumns, next);
-        auto sums = [&](int c, int h, float (&acc)[16]) {
+        float next[kStep];
+        tmem_load(acc_at + (it & 1) * kColumns, next);
+        auto sums = [&](int at, float (&acc)[kStep]) {
           tmem_loaded(next);
 #pragma unroll
-          for (int u = 0; u < 16; ++u) acc[u] = next[u];
-          if (c < CG - 1 || h < 3) tmem_load16(acc_at + (it & 1) * kColumns + c * 64 + h * 16 + 16, next);
+          for (int u = 0; u < kStep; ++u) acc[u] = next[u];
+          if (at + kStep < 64 * Pl::kItems) tmem_load(acc_at + (it & 1) * kColumns + at + kStep, next);
         };
         auto done = [&] {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) arrive_first<CG>(&bars.taken[it & 1]);
         };
-        if (kPhase == kGram && parts.splits > 1) {
-          float* share = share_of(t, (int)(unit % parts.splits));
+        if (kPhase == kGram && unit >= parts.whole) {
+          float* share = share_of(t, parts.split_of(unit));
 #pragma unroll 1
-          for (int i = 0; i < 4 * CG; ++i) {
-            float acc[16];
-            sums(i / 4, i % 4, acc);
+          for (int i = 0; i < 64 * Pl::kItems; i += kStep) {
+            float acc[kStep];
+            sums(i, acc);
 #pragma unroll
-            for (int u = 0; u < 16; ++u) share[(i * 16 + u) * 32] = acc[u];
+            for (int u = 0; u < kStep; ++u) share[(i + u) * 32] = acc[u];
           }
           done();  // (a barrier of the warp)
-          if (lane == 0)
-            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(P.shared + (t * CG + rank) * Pl::kWarps + warp - 2) : "memory");
+          if (lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(shared(t)) : "memory");
         } else {
-          finish(t, sums, done);
+          finish(t, unit + step < parts.whole ? unit + step : -1, 0, Pl::kItems, sums, done);
         }
         tmem_loaded(next);  // (nothing is on its way, but where a wait gave up)
         ++it;
       }
       if constexpr (kPhase == kGram) {
-        // Shares of tiles are added up, in their order, by the warps that have the same place in the tile: of
-        // eight, each share's block takes its part. (None waits before all its own shares are out.)
-        if (parts.splits > 1)
+        // Shares of tiles are added up, in their order, by the warps that have the same place in the tile:
+        // each share's block takes some items of them. (None waits before all its own shares are out.)
+        if (parts.all > parts.whole)
           for (int64_t unit = first; unit < parts.all && going; unit += step) {
-            const int64_t t = unit / parts.splits;
-            if ((warp - 2) % parts.splits != (int)(unit % parts.splits)) continue;
-            const uint32_t* count = P.shared + (t * CG + rank) * Pl::kWarps + warp - 2;
-            going = __all_sync(0xffffffffu, lane != 0 || wait_count(count, (uint32_t)parts.splits * (index / 3 + 1), dead));
-            if (!going) break;
-            auto sums = [&](int c, int h, float (&acc)[16]) {
+            if (unit < parts.whole) continue;
+            const int64_t t = parts.whole + (unit - parts.whole) / parts.splits;
+            const uint32_t to = (uint32_t)parts.splits * (index / 3 + 1);
+            going = __all_sync(0xffffffffu, lane != 0 || wait_count(shared(t), to, dead));
+            auto sums = [&](int at, float (&acc)[kStep]) {
 #pragma unroll
-              for (int u = 0; u < 16; ++u) acc[u] = 0.f;
+              for (int u = 0; u < kStep; ++u) acc[u] = 0.f;
+#pragma unroll 1
               for (int split = 0; split < parts.splits; split += 4) {
-                float of[4][16];
+                float of[4][kStep];
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                  const float* share = share_of(t, split + v) + (c * 64 + h * 16) * 32;
+                  const float* share = share_of(t, split + v) + at * 32;
 #pragma unroll
-                  for (int u = 0; u < 16; ++u) of[v][u] = split + v < parts.splits ? __ldcg(share + u * 32) : 0.f;
+                  for (int u = 0; u < kStep; ++u) of[v][u] = split + v < parts.splits ? __ldcg(share + u * 32) : 0.f;
                 }
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
 #pragma unroll
-                  for (int u = 0; u < 16; ++u) acc[u] += of[v][u];
+                  for (int u = 0; u < kStep; ++u) acc[u] += of[v][u];
               }
             };
-            finish(t, sums, [] {});
+            for (int c = 0; c < Pl::kItems && going; ++c) {
+              if (((warp - 2) * Pl::kItems + c) % parts.splits != parts.split_of(unit)) continue;
+              finish(t, -1, c, c + 1, sums, [] {});
+            }
           }
       }
       // what this block wrote is there for the next phase (which orders its copies after it)
@@ -958,8 +984,12 @@ cudaError_t launch_phases(const CUtensorMap& map, const ProductArgs& P, int devi
   }
   const bool together = P.end - P.begin > 1;
   if ((CG > 1 || together) && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
-  const int64_t rows = P.S.mp / (128 * CG), cols = P.S.np / (128 * CG);
-  const int64_t most = sms / CG, tiles = P.K * std::max(rows * cols, (P.triangle ? rows * (rows + 1) / 2 : rows * rows) * P.splits);
+  const int64_t rows = P.S.mp / (128 * CG), cols = P.S.np / (128 * CG), most = sms / CG;
+  int64_t tiles = P.K * rows * cols;
+  for (int i = 0; i < 2; ++i) {
+    const int64_t all = P.K * (P.triangle[i] ? rows * (rows + 1) / 2 : rows * rows);
+    tiles = std::max(tiles, i == 0 && P.splits > 1 ? P.whole + (all - P.whole) * P.splits : all);
+  }
   LaunchConfig l((tiles < most ? tiles : most) * CG, Pl::kThreads, CG, smem, s);
   if (together) {  // in the place of programmatic serialization
     l.at[0].id = cudaLaunchAttributeCooperative;
@@ -1010,16 +1040,40 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // taken in. By what the phases take, in cycles.
 struct Course {
   Shape S;
-  bool pairs, triangle;
-  int splits;
-  int64_t tiles() const {  // of a symmetric product
-    const int64_t R = S.mp / (pairs ? 256 : 128);
-    return triangle ? R * (R + 1) / 2 : R * R;
-  }
+  bool pairs;
+  struct Symmetric {  // A, B
+    bool triangle;
+    int64_t tiles;
+  } of[2];
+  int64_t whole;  // of A, those that are not shared,
+  int splits;     // and the shares of the others
 };
 constexpr int kSms = 152, kMostSplits = 16;
-int64_t phase_cycles(int64_t units, int slots, int64_t kblocks, int64_t per_kblock, int64_t finish) {
-  return (units + slots - 1) / slots * std::max(kblocks * per_kblock, finish) + finish;
+// What a tile takes: its products of 64 columns, and what becomes of its sums meanwhile (fine: afterwards,
+// since the same warps take the sums of the next tile out); and what the last tile leaves behind.
+struct Cost {
+  int64_t kblock, use, tail;
+  bool fine;
+  int64_t tile(int64_t kblocks) const { return fine ? kblocks * kblock + use : std::max(kblocks * kblock, use); }
+};
+int64_t phase_cycles(int64_t tiles, int slots, int64_t kblocks, const Cost& c) {
+  return (tiles + slots - 1) / slots * c.tile(kblocks) + c.tail;
+}
+// The same with the tiles of the last round in shares, the best number of them.
+int64_t shared_cycles(int64_t tiles, int slots, int64_t kblocks, const Cost& c, int cg, int* splits) {
+  int64_t least = phase_cycles(tiles, slots, kblocks, c);
+  *splits = 1;
+  const int64_t rest = tiles % slots, whole = tiles - rest;
+  for (int64_t s = 2; rest && s <= kMostSplits && s <= kblocks; ++s) {
+    const int64_t each = (kblocks + s - 1) / s;
+    if ((s - 1) * each >= kblocks) continue;  // a share of nothing
+    const int64_t rounds = (rest * s + slots - 1) / slots;
+    // written, and added up: of the 8 cg parts of a tile, some by each share's warps
+    const int64_t sum = 3000 + ((8 * cg + s - 1) / s + 7) / 8 * (1500 + 4000 * ((s + 3) / 4));
+    const int64_t t = phase_cycles(whole, slots, kblocks, c) + rounds * (each * c.kblock + sum);
+    if (t < least) least = t, *splits = (int)s;
+  }
+  return least;
 }
 Course course_of(int64_t K, int64_t m, int64_t n, bool fine) {
   if (m > n) std::swap(m, n);
@@ -1027,23 +1081,29 @@ Course course_of(int64_t K, int64_t m, int64_t n, bool fine) {
   int64_t least = INT64_MAX;
   for (int cg = 1; cg <= 2; ++cg) {
     const int unit = 128 * cg, slots = kSms / cg;
-    const int64_t per = cg == 1 ? (fine ? 1130 : 560) : (fine ? 1560 : 560), finish = cg == 1 ? 2500 : 4500;
+    const Cost cost = cg == 1 ? (fine ? Cost{1800, 3000, 5000, true} : Cost{900, 5000, 3500, false})
+                              : (fine ? Cost{2200, 10000, 10000, true} : Cost{640, 12000, 9000, false});
     const Shape S{m, n, up(m, unit), up(n, unit)};
-    const int64_t R = S.mp / unit, C = S.np / unit, kn = (n + 63) / 64, km = (m + 63) / 64;
-    const int64_t update = phase_cycles(K * R * C, slots, km, per, finish);
-    for (int triangle = 0; triangle < 2; ++triangle) {
-      const int64_t tiles = K * (triangle ? R * (R + 1) / 2 : R * R), end = finish + (triangle && R > 1 ? 4000 * cg : 0);
-      const int64_t square = phase_cycles(tiles, slots, km, per, end);
-      int splits = 1;
-      int64_t gram = phase_cycles(tiles, slots, kn, per, end);
-      for (int64_t s = 2; s <= kMostSplits && s <= kn; ++s) {
-        if ((s - 1) * ((kn + s - 1) / s) >= kn) continue;  // a share without columns
-        const int64_t sum = (tiles * s + slots - 1) / slots * (1500 + 4000 * cg * ((s + 3) / 4));  // written, and added up
-        const int64_t t = phase_cycles(tiles * s, slots, (kn + s - 1) / s, per, end) + sum;
-        if (t < gram) gram = t, splits = (int)s;
+    const int64_t R = S.mp / unit, C = S.np / unit;
+    Course c{S, cg == 2, {}, 0, 1};
+    int64_t all = phase_cycles(K * R * C, slots, (m + 63) / 64, cost);
+    for (int phase = 0; phase < 2; ++phase) {
+      int64_t cycles = INT64_MAX;
+      for (int triangle = 0; triangle < 2; ++triangle) {
+        const Course::Symmetric of{triangle == 1, K * (triangle ? R * (R + 1) / 2 : R * R)};
+        Cost two = cost;
+        if (triangle && R > 1) two.tail += 3000 * cg;  // written above the diagonal too
+        int splits = 1;
+        const int64_t t = phase ? phase_cycles(of.tiles, slots, (m + 63) / 64, two)
+                                : shared_cycles(of.tiles, slots, (n + 63) / 64, two, cg, &splits);
+        if (t >= cycles) continue;
+        cycles = t;
+        c.of[phase] = of;
+        if (phase == 0) c.whole = of.tiles - of.tiles % slots, c.splits = splits;
       }
-      if (gram + square + update < least) least = gram + square + update, best = Course{S, cg == 2, triangle == 1, splits};
+      all += cycles;
     }
+    if (all < least) least = all, best = c;
   }
   return best;
 }
@@ -1065,13 +1125,13 @@ int64_t work_of(bool fine, int64_t K, const Course& c, char* at, Work* w) {
   };
   const Shape& S = c.S;
   const int cg = c.pairs ? 2 : 1;
-  const int64_t tiles = c.splits > 1 ? K * c.tiles() : 0;
+  const int64_t shared = c.splits > 1 ? c.of[0].tiles - c.whole : 0;  // tiles in shares
   Work v;
   v.part = reinterpret_cast<double*>(take(8 * K * kMostSizeParts));
-  v.counters = 2 + tiles * cg * 8;
+  v.counters = 2 + shared * cg * 8;  // (at most 8 warps of a block read sums back)
   v.counts = reinterpret_cast<uint32_t*>(take(4 * v.counters));
   v.shared = v.counts + 2;
-  v.shares = reinterpret_cast<float*>(take(4 * tiles * c.splits * (128 * cg) * (128 * cg)));
+  v.shares = reinterpret_cast<float*>(take(4 * shared * c.splits * (128 * cg) * (128 * cg)));
   v.d = reinterpret_cast<float*>(take(4 * K * S.mp));
   v.e = reinterpret_cast<float*>(take(4 * K * S.mp));
   for (Halves2* h : {&v.x, &v.y, &v.o, &v.r}) {
@@ -1150,7 +1210,8 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
                    parts, w.x);
     if (e != cudaSuccess) return e;
     ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps,
-                  course.triangle, course.splits, w.shares, w.shared, w.counts + 1, w.counts, {}};
+                  {course.of[0].triangle, course.of[1].triangle}, course.whole, course.splits, w.shares, w.shared,
+                  w.counts + 1, w.counts, {}};
     std::copy(coefficients_host, coefficients_host + 3 * steps, P.coef);
     if (pairs) e = all_steps<2, fine>(map, P, device, sms, s);
     if (pairs && too_large_here(e)) {  // a context without room for clusters
