@@ -730,9 +730,6 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         [[maybe_unused]] const float dr = kPhase == kSquare ? D[row] : 0.f, di = c3 + c5 * dr;
         [[maybe_unused]] const float ei = kPhase == kUpdate ? c1 + P.e[k * S.mp + row] : 0.f;
         const int64_t cols = ((int64_t)tc * (Pl::kWarps / 4) + e) * (64 * Pl::kItems);  // the warp's first column
-        float dj[2 * Pl::kItems];
-#pragma unroll
-        for (int i = 0; i < 2 * Pl::kItems; ++i) dj[i] = kPhase == kSquare ? c5 * D[cols + i * 32 + lane] : 0.f;
         // (Loops that are not unrolled: each tile goes through this code once, and instructions have to be
         // fetched. 64 columns took 4,500 to 9,000 cycles unrolled.)
 #pragma unroll 1
@@ -749,24 +746,40 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
             ++q;
           }
           if (!going) return;
-#pragma unroll 1
-          for (int h = 0; h < 64; h += kStep) {  // so many columns, eight a piece
-            char* at[kStep / 8];
-            float was[kStep];
+          // this lane's halves of kStep columns, two pieces of each plane; read a step ahead where there are registers for it
+          uint4 halves[2 * kStep / 8];
+          auto read = [&](int h) {
 #pragma unroll
             for (int p = 0; p < kStep / 8; ++p) {
-              at[p] = b + piece_at((uint32_t)lane, (uint32_t)(h / 8 + p));
-              if (kPhase != kGram) Vec<__half>::get(*reinterpret_cast<const uint4*>(at[p]), was + p * 8);
-              if (kPhase != kGram && kLow) {
-                float low[8];
-                Vec<__half>::get(*reinterpret_cast<const uint4*>(at[p] + kHeldBytes), low);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) was[p * 8 + u] += low[u];
-              }
+              const char* at = b + piece_at((uint32_t)lane, (uint32_t)(h / 8 + p));
+              halves[2 * p] = *reinterpret_cast<const uint4*>(at);
+              if (kLow) halves[2 * p + 1] = *reinterpret_cast<const uint4*>(at + kHeldBytes);
             }
-            [[maybe_unused]] float dh = dj[0];
+          };
+          if (kPhase != kGram && !kFine) read(0);
+#pragma unroll 1
+          for (int h = 0; h < 64; h += kStep) {  // so many columns, eight a piece
+            float was[kStep];
+            if (kPhase != kGram) {
+              if (kFine) read(h);
 #pragma unroll
-            for (int i = 1; i < 2 * Pl::kItems; ++i) dh = i == c * 2 + h / 32 ? dj[i] : dh;
+              for (int p = 0; p < kStep / 8; ++p) {
+                Vec<__half>::get(halves[2 * p], was + p * 8);
+                if (kLow) {
+                  float low[8];
+                  Vec<__half>::get(halves[2 * p + 1], low);
+#pragma unroll
+                  for (int u = 0; u < 8; ++u) was[p * 8 + u] += low[u];
+                }
+              }
+              if (!kFine && h + kStep < 64) read(h + kStep);
+            }
+            // D of the columns, the same for all lanes
+            [[maybe_unused]] float dc[kStep];
+            if (kPhase == kSquare)
+#pragma unroll
+              for (int u = 0; u < kStep; u += 4)
+                Vec<float>::get(*reinterpret_cast<const uint4*>(D + cols + c * 64 + h + u), dc + u);
             float acc[kStep];
             sums(c * 64 + h, acc);
             // (acc: X X' 2^28 times, O^2 2^22 times, R X 2^25 times)
@@ -790,15 +803,16 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
                   if constexpr (kPhase == kGram) {
                     v[o] = acc[j] * (kO / (kX * kX));
                   } else if constexpr (kPhase == kSquare) {  // b O + c (O^2 + (D_i + D_j) O)
-                    v[o] = __fmaf_rn(di + __shfl_sync(0xffffffffu, dh, h % 32 + j), was[j], acc[j] * (c5 / kO));
+                    v[o] = __fmaf_rn(__fmaf_rn(c5, dc[j], di), was[j], acc[j] * (c5 / kO));
                   } else {
                     v[o] = __fmaf_rn(ei, was[j], acc[j] * (1.f / kO));
                   }
                 }
                 two_halves(v[0], v[1], nh + u / 2, nl + u / 2);
               }
-              *reinterpret_cast<uint4*>(at[p]) = *reinterpret_cast<const uint4*>(nh);
-              if (kLow) *reinterpret_cast<uint4*>(at[p] + kHeldBytes) = *reinterpret_cast<const uint4*>(nl);
+              char* at = b + piece_at((uint32_t)lane, (uint32_t)(h / 8 + p));
+              *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(nh);
+              if (kLow) *reinterpret_cast<uint4*>(at + kHeldBytes) = *reinterpret_cast<const uint4*>(nl);
             }
             if (kPhase != kUpdate && tr == tc && on >= 0 && on < kStep) {  // (O and R have none)
               char* place = b + piece_at((uint32_t)lane, (uint32_t)((h + on) / 8)) + on % 8 * 2;
