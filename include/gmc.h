@@ -584,8 +584,8 @@ int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_
  * a worker's gradient of a weight matrix is orthogonalised so before gmc_step takes it.
  *
  * Matrix k's row i is n contiguous elements at x_dev + k*ldk + i*ld (out_dev likewise, by its
- * own strides; ldk is ignored where K = 1, ld where m = 1), of type `dtype`. out_dev may be x_dev, or overlap it in
- * any way: x is read before out is written. coefficients_host: 3*steps floats, a, b, c of each step;
+ * own strides; ldk is ignored where K = 1, ld where m = 1), of type `dtype`. out_dev may be x_dev (with the same
+ * strides); other overlaps are the caller's mistake. coefficients_host: 3*steps floats, a, b, c of each step;
  * 1 <= steps <= 16. A matrix of zeros gives zeros; one that holds inf or NaN gives NaN. The
  * singular values have to stay below 4 on the way, else a matrix may become NaN.
  * |G| is summed in 64 bits, products in 32. Their factors are halves: one for bfloat16

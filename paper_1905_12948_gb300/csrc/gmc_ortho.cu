@@ -1048,6 +1048,329 @@ cudaError_t map_of(void* base, int64_t bytes, CUtensorMap* map) {
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
+// -- small matrices -----------------------------------------------------------------
+
+// X of up to 128 rows and 128 columns a block, in shared memory from the first step to the last: one launch
+// for everything. The blocks of a cluster have 128 columns each; of A = X X' each adds up the shares of all
+// for its own columns, and gives them to all. A^2 and B are each block's own. What bounds it is the chain of
+// products, of 0.2 us each, and of what is made of their sums.
+constexpr int kSmallSide = 128, kMostSmallParts = 8;
+struct SmallArgs {
+  int64_t m, n;  // of X
+  int steps, parts;
+  float scale;
+  float coef[3 * kMostSteps];
+};
+template <bool kFine>
+struct alignas(1024) SmallSmem {
+  __half xh[2][kBlock], xl[2][kBlock];  // X, blocks of 64 columns
+  __half oh[2][kBlock];                 // O, then R
+  __half ol[kFine ? 2 : 1][kFine ? kBlock : 8];
+  float share[kSmallSide * kSmallSide]; // of A's columns that are this block's, by the blocks they come from
+  float d[kSmallSide], e[kSmallSide];   // diagonals of A and B
+  double squares[kMostSmallParts], ws[8];
+  uint64_t done;                        // products
+  uint32_t tmem, dead;
+};
+__device__ __forceinline__ void store_at(uint32_t addr, uint32_t rank, const uint4& v) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(remote(addr, rank)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+               : "memory");
+}
+__device__ __forceinline__ void store_at(uint32_t addr, uint32_t rank, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(remote(addr, rank)), "f"(v) : "memory");
+}
+__device__ __forceinline__ void store_at(uint32_t addr, uint32_t rank, double v) {
+  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(remote(addr, rank)), "d"(v) : "memory");
+}
+
+template <typename T, bool kTurned>
+__global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old,
+                                                  const __grid_constant__ SmallArgs A) {
+  constexpr bool kFine = !std::is_same<T, __nv_bfloat16>::value;
+  extern __shared__ char raw[];
+  auto& sm = *reinterpret_cast<SmallSmem<kFine>*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int tid = (int)threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const uint32_t parts = (uint32_t)A.parts, rank = parts > 1 ? cluster_rank() : 0;
+  const int64_t k = blockIdx.x / parts, j0 = (int64_t)rank * kSmallSide;
+  if (parts > 1) cluster_arrive();  // (it has begun)
+  if (tid == 0) {
+    mbar_init(&sm.done, 1);
+    sm.dead = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0) tmem_alloc<1>(&sm.tmem, kSmallSide);
+  griddep_wait();
+
+  // this block's columns of G: eight pieces of eight columns a thread, neighbours along a row of G
+  g += k * sk;
+  float f[8][8];
+  double s = 0.;
+  const bool vectors = !kTurned && ((reinterpret_cast<uintptr_t>(g) | (uintptr_t)(ld * sizeof(T))) & 15) == 0;
+  auto piece_of = [&](int u, int* row, int* piece) {
+    *row = kTurned ? tid % 128 : tid / 16 + 16 * u;
+    *piece = kTurned ? tid / 128 + 2 * u : tid % 16;
+  };
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    int row, piece;
+    piece_of(u, &row, &piece);
+    const int64_t j = j0 + piece * 8;
+    const T* x = g + (kTurned ? j * ld + row : row * ld + j);
+    if (vectors && row < A.m && j + 8 <= A.n) {
+#pragma unroll
+      for (int v = 0; v < 8; v += Vec<T>::N) Vec<T>::get(*reinterpret_cast<const uint4*>(x + v), f[u] + v);
+    } else {
+#pragma unroll
+      for (int v = 0; v < 8; ++v) f[u][v] = row < A.m && j + v < A.n ? Vec<T>::one(x[v * (kTurned ? ld : 1)]) : 0.f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = f[u][i];
+    s += squares<8>(v);
+  }
+  s = warp_sum(s);
+  if (lane == 0) sm.ws[warp] = s;
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *(volatile uint32_t*)&sm.tmem;
+  s = 0.;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s += sm.ws[i];
+  if (parts > 1) {
+    cluster_wait();  // all have begun
+    if (tid < (int)parts) store_at(smem_addr(&sm.squares[rank]), (uint32_t)tid, s);
+    cluster_arrive();
+    cluster_wait();
+    s = 0.;
+    for (uint32_t i = 0; i < parts; ++i) s += sm.squares[i];
+  }
+  const Scaled by = scaled_by(s);
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    int row, piece;
+    piece_of(u, &row, &piece);
+    alignas(16) __half2 hi[4], lo[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      float x[2];
+#pragma unroll
+      for (int o = 0; o < 2; ++o)  // (what pads a matrix that is NaN stays 0)
+        x[o] = row < A.m && j0 + piece * 8 + 2 * v + o < A.n ? by(f[u][2 * v + o]) : 0.f;
+      two_halves(x[0], x[1], hi + v, lo + v);
+    }
+    const uint32_t in = piece_at((uint32_t)row, (uint32_t)(piece % 8));
+    *reinterpret_cast<uint4*>(reinterpret_cast<char*>(sm.xh[piece / 8]) + in) = *reinterpret_cast<uint4*>(hi);
+    *reinterpret_cast<uint4*>(reinterpret_cast<char*>(sm.xl[piece / 8]) + in) = *reinterpret_cast<uint4*>(lo);
+  }
+
+  // Sums of this thread: its row, 64 columns.
+  const int row = warp % 4 * 32 + lane, half = warp / 4;
+  const uint32_t acc_at = tmem + half * 64 + ((uint32_t)(warp % 4) << 21);
+  uint32_t products = 0;
+  // All threads: what they wrote is there for the products, which `issue` issues; they are done.
+  auto product = [&](auto&& issue) {
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    fence_proxy_async();
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (tid == 0) {
+      issue();
+      commit<1>(&sm.done);
+    }
+    wait_for(&sm.done, products & 1, &sm.dead);
+    ++products;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  };
+  const uint32_t xh = smem_addr(sm.xh), xl = smem_addr(sm.xl), oh = smem_addr(sm.oh), ol = smem_addr(sm.ol);
+  constexpr uint32_t what = 1u << 4 | (128 / 8) << 17 | (128 / 16) << 24;
+  constexpr uint32_t kBlockBytes = 2 * kBlock;
+  // L R' (or L R: the right factor's rows are the sum's index), the small terms first
+  auto issue = [&](uint32_t lh, uint32_t ll, uint32_t rh, uint32_t rl, bool rows) {
+    for (int t = kFine ? 0 : 2; t < 3; ++t) {
+      const uint32_t l = t == 1 ? ll : lh, r = t == 0 ? rl : rh;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {  // 16 of the sum
+        const uint64_t dl = factor(l + q / 4 * kBlockBytes, 0) + (q % 4 * 32 >> 4);
+        const uint64_t dr = rows ? factor(r, kBlockBytes) + (q * 2048 >> 4) : factor(r + q / 4 * kBlockBytes, 0) + (q % 4 * 32 >> 4);
+        mma<1>(tmem, dl, dr, rows ? what | 1u << 16 : what, q > 0 || t > (kFine ? 0 : 2));
+      }
+    }
+  };
+  // eight columns of a plane of this thread's row
+  auto place = [&](void* plane, int column) {
+    return reinterpret_cast<uint4*>(static_cast<char*>(plane) + column / 64 * kBlockBytes + piece_at((uint32_t)row, (uint32_t)(column % 64 / 8)));
+  };
+  auto both = [&](void* hi, void* lo, bool two, int column, float* v) {  // as numbers
+    Vec<__half>::get(*place(hi, column), v);
+    if (!two) return;
+    float low[8];
+    Vec<__half>::get(*place(lo, column), low);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] += low[u];
+  };
+  auto halves = [&](const float* v, uint4* hi, uint4* lo) {
+    alignas(16) __half2 h[4], l[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) two_halves(v[2 * u], v[2 * u + 1], h + u, l + u);
+    *hi = *reinterpret_cast<uint4*>(h);
+    *lo = *reinterpret_cast<uint4*>(l);
+  };
+
+#pragma unroll 1
+  for (int step = 0; step < A.steps; ++step) {
+    const float c1 = A.coef[3 * step], c3 = A.coef[3 * step + 1], c5 = A.coef[3 * step + 2];
+    product([&] { issue(xh, xl, xh, xl, false); });
+    if (parts == 1) {
+#pragma unroll 1
+      for (int h = 0; h < 64; h += kStep) {
+        float acc[kStep];
+        tmem_load(acc_at + h, acc);
+        tmem_loaded(acc);
+#pragma unroll
+        for (int p = 0; p < kStep; p += 8) {
+          const int column = half * 64 + h + p;
+          float v[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {
+            v[u] = acc[p + u] * (kO / (kX * kX));
+            if (column + u == row) sm.d[row] = acc[p + u] * (1.f / (kX * kX)), v[u] = 0.f;
+          }
+          uint4 hi, lo;
+          halves(v, &hi, &lo);
+          *place(sm.oh, column) = hi;
+          if (kFine) *place(sm.ol, column) = lo;
+        }
+      }
+    } else {
+      // this block's shares to the blocks that add them up, `wide` columns each
+      const int wide = kSmallSide / (int)parts;
+#pragma unroll 1
+      for (int h = 0; h < 64; h += kStep) {
+        float acc[kStep];
+        tmem_load(acc_at + h, acc);
+        tmem_loaded(acc);
+        const int column = half * 64 + h;
+        const uint32_t to = smem_addr(sm.share + ((int)rank * kSmallSide + row) * wide + column % wide);
+#pragma unroll
+        for (int u = 0; u < kStep; u += 4)
+          store_at(to + 4 * u, (uint32_t)(column / wide), make_uint4(__float_as_uint(acc[u]), __float_as_uint(acc[u + 1]),
+                                                                      __float_as_uint(acc[u + 2]), __float_as_uint(acc[u + 3])));
+      }
+      cluster_arrive();
+      cluster_wait();
+#pragma unroll 1
+      for (int i = tid; i < kSmallSide * wide / 8; i += 256) {
+        const int r = i % kSmallSide, c = i / kSmallSide * 8, column = (int)rank * wide + c;
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = 0.f;
+#pragma unroll 1
+        for (uint32_t p = 0; p < parts; ++p) {
+          const float* share = sm.share + ((int)p * kSmallSide + r) * wide + c;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) v[u] += share[u];
+        }
+        float mid = 0.f;
+        const int on = r - column;  // the column that is on the diagonal
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          if (u == on) mid = v[u] * (1.f / (kX * kX));
+          v[u] = u == on ? 0.f : v[u] * (kO / (kX * kX));
+        }
+        uint4 hi, lo;
+        halves(v, &hi, &lo);
+        const uint32_t at = (uint32_t)(column / 64) * kBlockBytes + piece_at((uint32_t)r, (uint32_t)(column % 64 / 8));
+        for (uint32_t p = 0; p < parts; ++p) {
+          store_at(oh + at, p, hi);
+          if (kFine) store_at(ol + at, p, lo);
+          if (on >= 0 && on < 8) store_at(smem_addr(sm.d + r), p, mid);
+        }
+      }
+      fence_proxy_async_all();
+      cluster_arrive();
+      cluster_wait();
+    }
+    product([&] { issue(oh, ol, oh, ol, false); });
+    const float dr = sm.d[row], di = c3 + c5 * dr;
+#pragma unroll 1
+    for (int h = 0; h < 64; h += kStep) {
+      float acc[kStep];
+      tmem_load(acc_at + h, acc);
+      tmem_loaded(acc);
+#pragma unroll
+      for (int p = 0; p < kStep; p += 8) {
+        const int column = half * 64 + h + p;
+        float v[8];
+        both(sm.oh, sm.ol, kFine, column, v);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          v[u] = __fmaf_rn(__fmaf_rn(c5, sm.d[column + u], di), v[u], acc[p + u] * (c5 / kO));
+          if (column + u == row) sm.e[row] = c3 * dr + c5 * __fmaf_rn(dr, dr, acc[p + u] * (1.f / (kO * kO))), v[u] = 0.f;
+        }
+        uint4 hi, lo;
+        halves(v, &hi, &lo);
+        *place(sm.oh, column) = hi;
+        if (kFine) *place(sm.ol, column) = lo;
+      }
+    }
+    product([&] { issue(oh, ol, xh, xl, true); });
+    const float ei = c1 + sm.e[row];
+    const bool last = step + 1 == A.steps;
+    const float by_out = *(volatile uint32_t*)&sm.dead ? __uint_as_float(kNan) : A.scale * (1.f / kX);
+#pragma unroll 1
+    for (int h = 0; h < 64; h += kStep) {
+      float acc[kStep];
+      tmem_load(acc_at + h, acc);
+      tmem_loaded(acc);
+#pragma unroll
+      for (int p = 0; p < kStep; p += 8) {
+        const int column = half * 64 + h + p;
+        float v[8];
+        both(sm.xh, sm.xl, true, column, v);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = __fmaf_rn(ei, v[u], acc[p + u] * (1.f / kO));
+        if (!last) {
+          uint4 hi, lo;
+          halves(v, &hi, &lo);
+          *place(sm.xh, column) = hi;
+          *place(sm.xl, column) = lo;
+        } else if (row < A.m) {
+          const int64_t j = j0 + column;
+          T* o = out + k * osk + (kTurned ? j * old + row : row * old + j);
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            if (j + u < A.n) o[u * (kTurned ? old : 1)] = Vec<T>::round(v[u] * by_out);
+        }
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 0) tmem_free<1>(tmem, kSmallSide);
+}
+
+template <typename T>
+cudaError_t launch_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old, bool turned, int64_t K,
+                         const SmallArgs& A, int device, cudaStream_t s) {
+  constexpr int smem = (int)sizeof(SmallSmem<!std::is_same<T, __nv_bfloat16>::value>) + 1024;
+  static_assert(smem <= 232448, "shared memory of a block");
+  auto* f = turned ? k_small<T, true> : k_small<T, false>;
+  static std::atomic<uint64_t> known[2];  // devices whose limit is raised
+  if (device >= 64 || !(known[turned].load(std::memory_order_relaxed) >> device & 1)) {
+    const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    if (device < 64) known[turned].fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
+  }
+  if (A.parts > 1 && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
+  LaunchConfig l(K * A.parts, 256, A.parts, smem, s);
+  return cudaLaunchKernelEx(&l.cfg, f, g, sk, ld, out, osk, old, A);
+}
+
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // How a call is carried out: tiles of one block or of a pair, and the shares that X's columns are
@@ -1217,6 +1540,14 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
     constexpr bool fine = !std::is_same<T, __nv_bfloat16>::value;
     const T* g = static_cast<const T*>(x_dev);
     T* o = static_cast<T*>(out_dev);
+    if (S.m <= kSmallSide && S.n <= kSmallSide * kMostSmallParts) {
+      SmallArgs A{S.m, S.n, steps, 1, scale, {}};
+      while (A.parts * kSmallSide < S.n) A.parts *= 2;
+      std::copy(coefficients_host, coefficients_host + 3 * steps, A.coef);
+      const cudaError_t e = launch_small<T>(g, ldk, ld, o, out_ldk, out_ld, turned, K, A, device, s);
+      if (!too_large_here(e)) return e;
+      cudaGetLastError();  // a context without room for clusters
+    }
     cudaError_t e = launch_pdl(k_size<T>, dim3((unsigned)parts, (unsigned)K), dim3(256), 0, s, g, ldk, ld, m, n, w.part, w.counts,
                                w.counters);
     if (e != cudaSuccess) return e;
