@@ -1083,6 +1083,8 @@ __device__ __forceinline__ void store_at(uint32_t addr, uint32_t rank, double v)
   asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(remote(addr, rank)), "d"(v) : "memory");
 }
 
+__device__ __forceinline__ int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
+
 template <typename T, bool kTurned>
 __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old,
                                                   const __grid_constant__ SmallArgs A) {
@@ -1167,9 +1169,11 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
     *reinterpret_cast<uint4*>(reinterpret_cast<char*>(sm.xl[piece / 8]) + in) = *reinterpret_cast<uint4*>(lo);
   }
 
-  // Sums of this thread: its row, 64 columns.
-  const int row = warp % 4 * 32 + lane, half = warp / 4;
-  const uint32_t acc_at = tmem + half * 64 + ((uint32_t)(warp % 4) << 21);
+  // Sums of this thread: its row, every other kStep columns. Of A and B, what lies beyond X's rows is neither
+  // computed nor looked at.
+  const int row = warp % 4 * 32 + lane, half = warp / 4 * kStep, side = (int)up16(A.m);
+  const bool in_rows = warp % 4 * 32 < side;  // (the same for a warp)
+  const uint32_t acc_at = tmem + ((uint32_t)(warp % 4) << 21);
   uint32_t products = 0;
   // All threads: what they wrote is there for the products, which `issue` issues; they are done.
   auto product = [&](auto&& issue) {
@@ -1186,17 +1190,16 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   };
   const uint32_t xh = smem_addr(sm.xh), xl = smem_addr(sm.xl), oh = smem_addr(sm.oh), ol = smem_addr(sm.ol);
-  constexpr uint32_t what = 1u << 4 | (128 / 8) << 17 | (128 / 16) << 24;
   constexpr uint32_t kBlockBytes = 2 * kBlock;
-  // L R' (or L R: the right factor's rows are the sum's index), the small terms first
-  auto issue = [&](uint32_t lh, uint32_t ll, uint32_t rh, uint32_t rl, bool rows) {
+  // `columns` columns of L R' (or L R: the right factor's rows are the sum's index) over `terms`, the small terms first
+  auto issue = [&](uint32_t lh, uint32_t ll, uint32_t rh, uint32_t rl, bool rows, int columns, int terms) {
+    const uint32_t what = 1u << 4 | (rows ? 1u << 16 : 0) | (uint32_t)(columns / 8) << 17 | (128 / 16) << 24;
     for (int t = kFine ? 0 : 2; t < 3; ++t) {
       const uint32_t l = t == 1 ? ll : lh, r = t == 0 ? rl : rh;
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {  // 16 of the sum
+      for (int q = 0; q < terms / 16; ++q) {
         const uint64_t dl = factor(l + q / 4 * kBlockBytes, 0) + (q % 4 * 32 >> 4);
         const uint64_t dr = rows ? factor(r, kBlockBytes) + (q * 2048 >> 4) : factor(r + q / 4 * kBlockBytes, 0) + (q % 4 * 32 >> 4);
-        mma<1>(tmem, dl, dr, rows ? what | 1u << 16 : what, q > 0 || t > (kFine ? 0 : 2));
+        mma<1>(tmem, dl, dr, what, q > 0 || t > (kFine ? 0 : 2));
       }
     }
   };
@@ -1223,16 +1226,16 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
 #pragma unroll 1
   for (int step = 0; step < A.steps; ++step) {
     const float c1 = A.coef[3 * step], c3 = A.coef[3 * step + 1], c5 = A.coef[3 * step + 2];
-    product([&] { issue(xh, xl, xh, xl, false); });
+    product([&] { issue(xh, xl, xh, xl, false, side, kSmallSide); });
     if (parts == 1) {
 #pragma unroll 1
-      for (int h = 0; h < 64; h += kStep) {
+      for (int at = half; at < side && in_rows; at += 2 * kStep) {
         float acc[kStep];
-        tmem_load(acc_at + h, acc);
+        tmem_load(acc_at + at, acc);
         tmem_loaded(acc);
 #pragma unroll
         for (int p = 0; p < kStep; p += 8) {
-          const int column = half * 64 + h + p;
+          const int column = at + p;
           float v[8];
 #pragma unroll
           for (int u = 0; u < 8; ++u) {
@@ -1247,32 +1250,37 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
       }
     } else {
       // this block's shares to the blocks that add them up, `wide` columns each
-      const int wide = kSmallSide / (int)parts;
+      const int wide = (side / 8 + (int)parts - 1) / (int)parts * 8;
 #pragma unroll 1
-      for (int h = 0; h < 64; h += kStep) {
+      for (int at = half; at < side && in_rows; at += 2 * kStep) {
         float acc[kStep];
-        tmem_load(acc_at + h, acc);
+        tmem_load(acc_at + at, acc);
         tmem_loaded(acc);
-        const int column = half * 64 + h;
-        const uint32_t to = smem_addr(sm.share + ((int)rank * kSmallSide + row) * wide + column % wide);
 #pragma unroll
-        for (int u = 0; u < kStep; u += 4)
-          store_at(to + 4 * u, (uint32_t)(column / wide), make_uint4(__float_as_uint(acc[u]), __float_as_uint(acc[u + 1]),
-                                                                      __float_as_uint(acc[u + 2]), __float_as_uint(acc[u + 3])));
+        for (int u = 0; u < kStep; u += 4) {
+          const int column = at + u;
+          const uint32_t to = smem_addr(sm.share + ((int)rank * side + row) * wide + column % wide);
+          if (row < side)
+            store_at(to, (uint32_t)(column / wide), make_uint4(__float_as_uint(acc[u]), __float_as_uint(acc[u + 1]),
+                                                               __float_as_uint(acc[u + 2]), __float_as_uint(acc[u + 3])));
+        }
       }
       cluster_arrive();
       cluster_wait();
+      // (pieces of eight columns of a row: all of a piece's shares, then its halves to all blocks)
 #pragma unroll 1
-      for (int i = tid; i < kSmallSide * wide / 8; i += 256) {
-        const int r = i % kSmallSide, c = i / kSmallSide * 8, column = (int)rank * wide + c;
+      for (int i = tid; i < side * wide / 8; i += 256) {
+        const int r = i % side, c = i / side * 8, column = (int)rank * wide + c;
+        if (column >= side) break;
         float v[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) v[u] = 0.f;
 #pragma unroll 1
         for (uint32_t p = 0; p < parts; ++p) {
-          const float* share = sm.share + ((int)p * kSmallSide + r) * wide + c;
-#pragma unroll
-          for (int u = 0; u < 8; ++u) v[u] += share[u];
+          const float4* share = reinterpret_cast<const float4*>(sm.share + ((int)p * side + r) * wide + c);
+          const float4 x = share[0], y = share[1];
+          v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+          v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
         }
         float mid = 0.f;
         const int on = r - column;  // the column that is on the diagonal
@@ -1290,20 +1298,20 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
           if (on >= 0 && on < 8) store_at(smem_addr(sm.d + r), p, mid);
         }
       }
-      fence_proxy_async_all();
+      asm volatile("fence.proxy.async.shared::cluster;" ::: "memory");
       cluster_arrive();
       cluster_wait();
     }
-    product([&] { issue(oh, ol, oh, ol, false); });
+    product([&] { issue(oh, ol, oh, ol, false, side, side); });
     const float dr = sm.d[row], di = c3 + c5 * dr;
 #pragma unroll 1
-    for (int h = 0; h < 64; h += kStep) {
+    for (int at = half; at < side && in_rows; at += 2 * kStep) {
       float acc[kStep];
-      tmem_load(acc_at + h, acc);
+      tmem_load(acc_at + at, acc);
       tmem_loaded(acc);
 #pragma unroll
       for (int p = 0; p < kStep; p += 8) {
-        const int column = half * 64 + h + p;
+        const int column = at + p;
         float v[8];
         both(sm.oh, sm.ol, kFine, column, v);
 #pragma unroll
@@ -1317,18 +1325,18 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
         if (kFine) *place(sm.ol, column) = lo;
       }
     }
-    product([&] { issue(oh, ol, xh, xl, true); });
+    product([&] { issue(oh, ol, xh, xl, true, kSmallSide, side); });
     const float ei = c1 + sm.e[row];
     const bool last = step + 1 == A.steps;
     const float by_out = *(volatile uint32_t*)&sm.dead ? __uint_as_float(kNan) : A.scale * (1.f / kX);
 #pragma unroll 1
-    for (int h = 0; h < 64; h += kStep) {
+    for (int at = half; at < kSmallSide && in_rows; at += 2 * kStep) {
       float acc[kStep];
-      tmem_load(acc_at + h, acc);
+      tmem_load(acc_at + at, acc);
       tmem_loaded(acc);
 #pragma unroll
       for (int p = 0; p < kStep; p += 8) {
-        const int column = half * 64 + h + p;
+        const int column = at + p;
         float v[8];
         both(sm.xh, sm.xl, true, column, v);
 #pragma unroll
