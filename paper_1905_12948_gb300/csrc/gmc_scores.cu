@@ -25,11 +25,13 @@ constexpr int kBatches = 16;  // of a sweep, before its candidates are looked fo
 // a log-probability is off by 2^-25 of itself, and no second word of c is wanted.
 inline Base score_base(float scale) { return Base{scale, (float)((double)scale * kLog2e), 0.f}; }
 
-// The threads that work on a row: a block, of which up to 8 share a row as a cluster, or a warp.
+// The threads that work on a row: a block of 256, of which up to 8 share a row as a cluster, a block of 128, or a
+// warp, of which eight are a block.
 template <int G>
 struct Team {
-  static_assert(G == 32 || G == kLossThreads, "a warp or a block");
-  static constexpr int kRows = kLossThreads / G;  // rows of a block
+  static_assert(G == 32 || G == 128 || G == kLossThreads, "a warp or a block");
+  static constexpr int kThreads = G == 32 ? kLossThreads : G;  // of a block
+  static constexpr int kRows = kThreads / G;                   // rows of a block
   __device__ static int tid() { return G == 32 ? (int)threadIdx.x % 32 : (int)threadIdx.x; }
   __device__ static int of_block() { return G == 32 ? (int)threadIdx.x / 32 : 0; }
   __device__ static void sync() {
@@ -536,9 +538,10 @@ __device__ __forceinline__ void write_scores(const ScoreArgs& A, const Moments& 
 }
 
 // Rows by blocks, by clusters of `parts` blocks where there are few, by warps where there are many
-// short ones. Bound by memory.
+// short ones. Bound by memory where rows are long (8,192 x 131,072 bf16: 305 us, 7.0 TB/s, with 8 alternatives 363), else by
+// the chain of reads, sums and candidates of each row (4,096 x 50,257 bf16: 72 us, 5.7 TB/s, with 8 alternatives 92).
 template <typename T, int G, bool kTop>
-__global__ void __launch_bounds__(kLossThreads, G == 32 && kTop ? 4 : 5) k_scores(Rows<T> R, ScoreArgs A, int parts) {
+__global__ void __launch_bounds__(Team<G>::kThreads, G == 128 ? 10 : G == 32 && kTop ? 4 : 5) k_scores(Rows<T> R, ScoreArgs A, int parts) {
   using Te = Team<G>;
   __shared__ Held<G> held[kTop ? Te::kRows : 1];
   __shared__ Moments cs[kMaxParts];
@@ -758,15 +761,31 @@ __global__ void __launch_bounds__(kLossThreads, G == 32 ? 4 : 5) k_scores_grad(R
     if (mine[o]) out[ys[tid + o * G]] = Vec<T>::round(at_y[o]);
 }
 
-constexpr int64_t kWarpScores = 32768, kWarpGrad = 18432;  // bytes of a row at most
-bool by_warps(int64_t n, int64_t row_bytes, int64_t most) { return n >= 600 && row_bytes <= most && row_bytes <= 12 * n; }
+// The team of a row. A row begins and ends with some microseconds of reads that wait for one another: a smaller
+// team streams longer in between, and more of them share an SM. The scores of bf16 rows, with 8
+// alternatives, in us, by blocks of 256, of 128 and by warps:
+//   rows   length     256    128  warps
+//    700    4,096    10.5    8.2    9.0
+//  2,000    2,000      -    14.9    9.4
+// 16,000    4,096      -    90.3   51.5
+//  4,000   12,000      -    35.9   29.9
+//  2,000   16,384    29.6   24.8
+//  4,096   50,257   102.5   92.3
+//  1,000   60,000    36.9   31.8
+// Gradients by warps as in gmc_loss.cu.
+constexpr int64_t kWarpScores = 32768, kWarpGrad = 18432, kHalfScores = 131072;  // bytes of a row at most
+bool by_warps(int64_t n, int64_t rows, int64_t row_bytes, int64_t most) {
+  return n >= rows && row_bytes <= most && row_bytes <= 12 * n;
+}
 
 template <typename T, bool kTop>
 cudaError_t launch_scores(const Rows<T>& R, const ScoreArgs& A, cudaStream_t s) {
   const int64_t bytes = R.V * (int64_t)sizeof(T);
-  if (by_warps(R.n, bytes, kWarpScores))
+  if (by_warps(R.n, 1400, bytes, kWarpScores))
     return launch(k_scores<T, 32, kTop>, (R.n + 7) / 8, kLossThreads, 1, s, R, A, 1);
-  return with_parts(parts_for(R.n, bytes), [&](int parts) {
+  const int most = parts_for(R.n, bytes);
+  if (most == 1 && bytes <= kHalfScores) return launch(k_scores<T, 128, kTop>, R.n, 128, 1, s, R, A, 1);
+  return with_parts(most, [&](int parts) {
     return launch(k_scores<T, kLossThreads, kTop>, R.n * parts, kLossThreads, parts, s, R, A, parts);
   });
 }
@@ -821,7 +840,7 @@ int gmc_token_scores_backward(const void* logits_dev, int32_t dtype, int64_t n, 
     const int64_t bytes = vocab * (int64_t)sizeof(T);
     const float4* st = reinterpret_cast<const float4*>(stats_dev);
     const cudaStream_t q = static_cast<cudaStream_t>(stream);
-    if (by_warps(n, bytes, kWarpGrad))
+    if (by_warps(n, 600, bytes, kWarpGrad))
       return launch(k_scores_grad<T, 32>, (n + 7) / 8, kLossThreads, 1, q, R, (int)given, st, dlogp_dev, dentropy_dev,
                     static_cast<T*>(dlogits_dev), dld, 1);
     int parts = parts_for(n, bytes);
