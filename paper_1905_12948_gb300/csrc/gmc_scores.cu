@@ -309,7 +309,9 @@ struct Mark {
   __device__ static uint32_t of(uint32_t t0, uint32_t t1) {
     return Vec<T>::top(__byte_perm(t0, t1, 0x5410), __byte_perm(t0, t1, 0x7632));
   }
-  __device__ static bool reaches(uint32_t w, uint32_t from);
+  __device__ static bool reaches(uint32_t w, uint32_t from) { return mask(w, from) != 0; }
+  __device__ static int count(uint32_t w, uint32_t from) { return __popc(mask(w, from) & 0x00010001u); }
+  __device__ static uint32_t mask(uint32_t w, uint32_t from);
   // upper halves of the orders of its logits, and back
   __device__ static uint32_t ordered(uint32_t w) {
     const uint32_t sign = (w >> 15 & 0x00010001u) * 0x7fffu;  // 0x7fff where negative
@@ -334,18 +336,19 @@ struct Mark {
   }
 };
 template <>
-__device__ __forceinline__ bool Mark<__nv_bfloat16>::reaches(uint32_t w, uint32_t from) {
-  return __hge2_mask(*reinterpret_cast<__nv_bfloat162*>(&w), *reinterpret_cast<__nv_bfloat162*>(&from)) != 0;
+__device__ __forceinline__ uint32_t Mark<__nv_bfloat16>::mask(uint32_t w, uint32_t from) {
+  return __hge2_mask(*reinterpret_cast<__nv_bfloat162*>(&w), *reinterpret_cast<__nv_bfloat162*>(&from));
 }
 template <>
-__device__ __forceinline__ bool Mark<__half>::reaches(uint32_t w, uint32_t from) {
-  return __hge2_mask(*reinterpret_cast<__half2*>(&w), *reinterpret_cast<__half2*>(&from)) != 0;
+__device__ __forceinline__ uint32_t Mark<__half>::mask(uint32_t w, uint32_t from) {
+  return __hge2_mask(*reinterpret_cast<__half2*>(&w), *reinterpret_cast<__half2*>(&from));
 }
 template <>
 struct Mark<float> {
   static constexpr uint32_t kNone = Vec<float>::kLow;
   __device__ static uint32_t of(uint32_t t0, uint32_t t1) { return Vec<float>::top(t0, t1); }
   __device__ static bool reaches(uint32_t w, uint32_t from) { return __uint_as_float(w) >= __uint_as_float(from); }
+  __device__ static int count(uint32_t w, uint32_t from) { return reaches(w, from); }
   __device__ static uint32_t ordered(uint32_t w) { return order_of(__uint_as_float(w)); }
   __device__ static uint32_t raw(uint32_t w) { return __float_as_uint(value_of(w)); }
   __device__ static int reach(uint32_t ordered, uint32_t half) { return ordered >> 16 >= half; }
@@ -386,6 +389,7 @@ __device__ __forceinline__ bool counts(const int64_t* y, int given) {
 template <typename T, int G, bool kTop>
 __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base& b, int part, int parts, int top, Held<G>* H) {
   constexpr int N = Wide<T>::N, U = kSweepVecs, M = Vec<T>::N;
+  [[maybe_unused]] constexpr int kFew = sizeof(T) / 2;  // batches of a warp that leave 64 marks behind
   const int tid = Team<G>::tid();
   const int head = wide_head(x, V);
   const int64_t nv = (V - head) / N;
@@ -436,6 +440,26 @@ __device__ __forceinline__ Moments score_sweep(const T* x, int64_t V, const Base
       if constexpr (G == 32) {
         if (top <= 8) {
           least = jth_largest(order_of(Vec<T>::top_of(best)), top);
+        } else if (batches <= kFew && top > 32) {
+          // (64 marks bound 64 alternatives badly: 16,000 rows of 1,000 bf16 230 us, so 90.) The largest upper
+          // half of an order that `top` of the elements reach.
+          uint4 v[2 * U * kFew];
+#pragma unroll
+          for (int u = 0; u < 2 * U * kFew; ++u) {
+            const int64_t vec = begin + u / (2 * U) * (U * G) + tid + u / 2 % U * G;
+            v[u] = make_uint4(Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow, Vec<T>::kLow);
+            if (vec < hi) v[u] = *reinterpret_cast<const uint4*>(q + vec * N + (u & 1) * M);
+          }
+          uint32_t half = 0;
+          for (uint32_t bit = 0x8000; bit; bit >>= 1) {
+            const uint32_t word = Mark<T>::word(value_of(Mark<T>::order(half | bit)));
+            int reach = 0;
+#pragma unroll
+            for (int u = 0; u < 2 * U * kFew; ++u)
+              reach += Mark<T>::count(v[u].x, word) + Mark<T>::count(v[u].y, word) + Mark<T>::count(v[u].z, word) + Mark<T>::count(v[u].w, word);
+            if (__reduce_add_sync(0xffffffffu, reach) >= top) half |= bit;
+          }
+          least = half ? Mark<T>::order(half) : 0;
         } else {
           // the largest upper half of an order that `top` of the vectors reach
           for (int i = 0; i < batches; ++i) H->most[i][tid] = Mark<T>::ordered(H->most[i][tid]);
