@@ -3,6 +3,7 @@ compressed by GMC (Alg. 1) each step.
 
     python examples/posttrain.py --loss policy
     python examples/posttrain.py --loss preference
+    python examples/posttrain.py --loss policy --entropy 0.01 --orthogonal
 
 The model: an embedding E of 64 prompt tokens, dropout, a head W of `vocab` tokens. Every
 worker has its own prompts and its own dropout masks, which follow from (seed, step, worker):
@@ -10,7 +11,9 @@ worker has its own prompts and its own dropout masks, which follow from (seed, s
     h = dropout(E[prompt])         dropout, the K workers in one call
     logits = h W^T                 a matrix product of torch
     loss, dlogits                  TokenLoss.policy or TokenLoss.preference
+    + dentropy                     with --entropy: token_scores and its gradient
     dW = dlogits^T h               and, through dropout_backward, dE
+    orthogonalize                  with --orthogonal: each worker's dE and dW, where they lie
     GMC.step(K x d gradients)      top-k of each worker's accumulator, one update
 
 policy: a token is sampled from the model itself for every prompt; tokens of a prompt's own
@@ -26,7 +29,8 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import torch
 
-from paper_1905_12948_gb300 import GMC, TokenLoss, dropout, dropout_backward, token_logp
+from paper_1905_12948_gb300 import (GMC, TokenLoss, dropout, dropout_backward, orthogonalize, token_logp, token_scores,
+                                    token_scores_backward)
 
 PROMPTS, CLASSES = 64, 8
 
@@ -41,6 +45,8 @@ def parse(argv=None):
     ap.add_argument("--rows", type=int, default=256, help="tokens a worker scores each step")
     ap.add_argument("--ratio", type=float, default=0.05, help="share of the gradient that a worker sends")
     ap.add_argument("--dropout", type=float, default=0.1)
+    ap.add_argument("--entropy", type=float, default=0.0, help="policy: weight of the mean entropy in the reward")
+    ap.add_argument("--orthogonal", action="store_true", help="orthogonalise the workers' gradients of both matrices")
     ap.add_argument("--seed", type=int, default=0)
     return ap.parse_args(argv)
 
@@ -64,7 +70,12 @@ def policy_worker(loss, logits, prompts, reference, a, gen):
     reward = (y % CLASSES == prompts % CLASSES).float()
     old = token_logp(logits, y)                     # the policy that sampled them: this one
     r = loss.policy(logits, y, old, reward - reward.mean(), ref_logp=token_logp(reference, y), kl=0.01)
-    return float(reward.mean()), r.dlogits
+    dlogits = r.dlogits
+    if a.entropy:                                   # a loss of -entropy * the rows' mean entropy
+        s = token_scores(logits, return_stats=True)
+        slope = torch.full_like(s.entropy, -a.entropy / len(y))
+        dlogits = dlogits + token_scores_backward(logits, None, s.stats, dentropy=slope)
+    return float(reward.mean()), dlogits
 
 
 def preference_worker(loss, logits, targets, offsets, reference):
@@ -77,7 +88,8 @@ def train(a):
     gen = torch.Generator(device="cuda").manual_seed(a.seed)
     d = (PROMPTS + a.vocab) * a.width
     w0 = torch.randn(d, device="cuda") * 0.1
-    eta = 20.0 if a.loss == "policy" else 5.0
+    # (an orthogonalised gradient has singular values of 0.7 to 1.2, whatever the loss)
+    eta = 0.5 if a.orthogonal else 20.0 if a.loss == "policy" else 5.0
     gmc = GMC(d, a.workers, beta=0.9, eta=eta, compressor="topk", ratio=a.ratio, seed=a.seed)
     gmc.set_params(w0)
     length = 8                                       # of an answer, in tokens
@@ -115,6 +127,10 @@ def train(a):
         dE = dropout_backward(dh, a.dropout, seed=a.seed, t=t)
         for k in range(a.workers):
             grads[k, : PROMPTS * a.width].view(PROMPTS, a.width).index_add_(0, prompts[k], dE[k])
+        if a.orthogonal:
+            for part, tokens in ((grads[:, : PROMPTS * a.width], PROMPTS), (grads[:, PROMPTS * a.width:], a.vocab)):
+                matrices = part.view(a.workers, tokens, a.width)
+                orthogonalize(matrices, out=matrices)
         gmc.step(grads)
         history.append(value)
         if t % 10 == 0 or t == a.steps - 1:
