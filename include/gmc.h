@@ -591,7 +591,8 @@ int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_
  * |G| is summed in 64 bits, products in 32. Their factors are halves: one for bfloat16
  * matrices, whose result is off by less than its own rounding, and the sum of two (22 bits) for float and half;
  * X itself is kept in 22 bits and the diagonals of A and B in 32.
- * The same call gives the same bits.
+ * The same call gives the same bits. Its blocks wait for one another, bounded (about two seconds without progress),
+ * after which out is NaN; where a context has no room for all of them at once, a launch does one product.
  * workspace_dev: gmc_orthogonalize_workspace(dtype, K, m, n) bytes, 256-byte aligned, whose
  * contents do not matter; it belongs to the call until the stream has passed it. K <= 65535, m, n <= 2^20, K*m*n <= 2^36
  * (the workspace call answers -1 otherwise). Takes no handle, runs on the current device,
@@ -601,6 +602,16 @@ int64_t gmc_orthogonalize_workspace(int32_t dtype, int64_t K, int64_t m, int64_t
 int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev, int64_t out_ldk, int64_t out_ld,
                       int32_t dtype, int64_t K, int64_t m, int64_t n, int32_t steps, const float* coefficients_host,
                       float scale, void* workspace_dev, int64_t workspace_bytes, void* stream);
+
+/* gmc_test_orthogonalize_course -- for tests to say which way a gmc_orthogonalize goes by its sizes: 0 in shared memory,
+ * else 1, + 2 by pairs of blocks, + 4 and + 8 with the triangle of A, of B alone, + 16 times the shares that
+ * tiles of A are summed in, + 4096 where some are summed whole; -1 for sizes that it refuses. */
+int gmc_test_orthogonalize_course(int32_t dtype, int64_t K, int64_t m, int64_t n);
+
+/* gmc_test_withhold_phase -- the next gmc_orthogonalize of the process (only that one): its first block does not do what
+ * others wait for, and every wait in it is bounded by wait_limit_ns (1 .. 2e9; 0 disarms the hook) instead of about two
+ * seconds. The waits give up, and out is NaN (of a matrix in shared memory: the first one of the call). GMC_EINVAL for a limit out of range. */
+int gmc_test_withhold_phase(uint64_t wait_limit_ns);
 
 /* gmc_strerror -- a static message for a status code. */
 const char* gmc_strerror(int status);

@@ -269,18 +269,23 @@ __device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity)
       : "memory");
   return ok != 0;
 }
+// What a block's waits have in common: whether one of its threads has given up, and after how long they do.
+struct Patience {
+  volatile uint32_t* dead;
+  uint64_t ns;
+};
 // As wait_bounded, ordered after arrivals from the other block of the cluster; gives up at once where
 // a thread of this block has given up. (The timer takes longer to read than most waits last: it is
 // looked at every 256th time.)
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile uint32_t* dead) {
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, const Patience& p) {
   uint64_t t0 = 0;
   for (uint32_t n = 1; !try_wait_cluster(bar, parity); ++n) {
     if (n % 256) continue;
-    if (*dead) return false;
+    if (*p.dead) return false;
     const uint64_t now = global_ns();
     if (t0 == 0) t0 = now;
-    if (now - t0 > kWaitLimitNs) {
-      *dead = 1;
+    if (now - t0 > p.ns) {
+      *p.dead = 1;
       return false;
     }
   }
@@ -288,18 +293,18 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatil
 }
 
 // Until a count that others raise has come to `to`.
-__device__ __forceinline__ bool wait_count(const uint32_t* p, uint32_t to, volatile uint32_t* dead) {
+__device__ __forceinline__ bool wait_count(const uint32_t* count, uint32_t to, const Patience& p) {
   uint64_t t0 = 0;
   for (uint32_t n = 1;; ++n) {
     uint32_t v;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(count) : "memory");
     if (v >= to) return true;
     if (n % 64) continue;
-    if (*dead) return false;
+    if (*p.dead) return false;
     const uint64_t now = global_ns();
     if (t0 == 0) t0 = now;
-    if (now - t0 > kWaitLimitNs) {
-      *dead = 1;
+    if (now - t0 > p.ns) {
+      *p.dead = 1;
       return false;
     }
   }
@@ -418,6 +423,8 @@ struct ProductArgs {
   float* shares;        // their sums,
   uint32_t* shared;     // and how many of them are there, by warps
   uint32_t* phases;     // counts the blocks that are done with each
+  uint64_t wait_ns;     // bound of every wait
+  bool hold;            // test hook: the first block does not say that it is done
   uint32_t* gave_up;
   float coef[3 * kMostSteps];
 };
@@ -549,13 +556,13 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
   }
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *(volatile uint32_t*)&bars.tmem;
-  volatile uint32_t* dead = &bars.dead;
+  const Patience patience{&bars.dead, P.wait_ns};
   griddep_wait();
 
   // Until every block is done with the phases before this one.
   auto wait_phase = [&](int index) {
     if (index == P.begin) return true;
-    const bool there = wait_count(P.phases, (uint32_t)(index - P.begin) * gridDim.x, dead);
+    const bool there = wait_count(P.phases, (uint32_t)(index - P.begin) * gridDim.x, patience);
     fence_proxy_async_all();
     return there;
   };
@@ -592,7 +599,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
           const int64_t ra = (int64_t)row * CG + rank, rb = (int64_t)col * CG + rank;
           for (int kb = begin; kb < end; ++kb, ++n) {
             const int s = (int)(n % Pl::kStages);
-            if (n >= Pl::kStages && !wait_for(&bars.empty[s], (n / Pl::kStages - 1) & 1, dead)) {
+            if (n >= Pl::kStages && !wait_for(&bars.empty[s], (n / Pl::kStages - 1) & 1, patience)) {
               going = false;
               break;
             }
@@ -638,12 +645,12 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
           parts.at(unit, &t, &kb, &last);
           while (kb < last && going) {
             const uint32_t acc = tmem + (it & 1) * kColumns;
-            going = it < 2 || wait_for(&bars.taken[it & 1], (it / 2 - 1) & 1, dead);
+            going = it < 2 || wait_for(&bars.taken[it & 1], (it / 2 - 1) & 1, patience);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const int begin = kb, end = last - kb > Pl::kChunk ? kb + Pl::kChunk : last;
             for (; kb < end && going; ++kb, ++n) {
               const int s = (int)(n % Pl::kStages);
-              going = wait_for(&bars.full[s], (n / Pl::kStages) & 1, dead);
+              going = wait_for(&bars.full[s], (n / Pl::kStages) & 1, patience);
               if (!going) break;
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               const uint32_t at = smem_addr(smem + s * Pl::kStageBytes);
@@ -742,7 +749,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
             __syncwarp();
           }
           if (kPhase != kGram) {
-            going = __all_sync(0xffffffffu, wait_for(in + q % Pl::kBuffers, (q / Pl::kBuffers) & 1, dead));
+            going = __all_sync(0xffffffffu, wait_for(in + q % Pl::kBuffers, (q / Pl::kBuffers) & 1, patience));
             ++q;
           }
           if (!going) return;
@@ -866,7 +873,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
 #pragma unroll
           for (int i = 0; i < 64 * Pl::kItems; ++i) sum[i] = 0.f;
           for (int kb = begin; kb < end; kb += Pl::kChunk) {
-            going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
+            going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, patience));
             if (!going) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -891,7 +898,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
           for (int i = 0; i < 64 * Pl::kItems; i += kStep) tmem_store(acc_at + (it & 1) * kColumns + i, sum + i);
           tmem_stored();
         } else {
-          going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, dead));
+          going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, patience));
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         }
         if (!going) break;
@@ -933,7 +940,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
             if (unit < parts.whole) continue;
             const int64_t t = parts.whole + (unit - parts.whole) / parts.splits;
             const uint32_t to = (uint32_t)parts.splits * (index / 3 + 1);
-            going = __all_sync(0xffffffffu, lane != 0 || wait_count(shared(t), to, dead));
+            going = __all_sync(0xffffffffu, lane != 0 || wait_count(shared(t), to, patience));
             auto sums = [&](int at, float (&acc)[kStep]) {
 #pragma unroll
               for (int u = 0; u < kStep; ++u) acc[u] = 0.f;
@@ -964,7 +971,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         fence_proxy_async_all();
       } else {
         asm volatile("bar.sync 1, %0;" ::"n"(32 * Pl::kWarps) : "memory");
-        if (warp == 2 && lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(P.phases) : "memory");
+        if (warp == 2 && lane == 0 && !(P.hold && blockIdx.x == 0)) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(P.phases) : "memory");
       }
     });
     if (lane == 0)
@@ -1059,6 +1066,8 @@ struct SmallArgs {
   int64_t m, n;  // of X
   int steps, parts;
   float scale;
+  uint64_t wait_ns;  // bound of every wait
+  bool hold;         // test hook: the first block does not issue its first product
   float coef[3 * kMostSteps];
 };
 template <bool kFine>
@@ -1181,11 +1190,11 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
     fence_proxy_async();
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (tid == 0) {
+    if (tid == 0 && !(A.hold && products == 0 && blockIdx.x == 0)) {
       issue();
       commit<1>(&sm.done);
     }
-    wait_for(&sm.done, products & 1, &sm.dead);
+    wait_for(&sm.done, products & 1, Patience{&sm.dead, A.wait_ns});
     ++products;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   };
@@ -1256,6 +1265,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
         float acc[kStep];
         tmem_load(acc_at + at, acc);
         tmem_loaded(acc);
+        if (*(volatile uint32_t*)&sm.dead) acc[0] = __uint_as_float(kNan);  // (which all of X gets)
 #pragma unroll
         for (int u = 0; u < kStep; u += 4) {
           const int column = at + u;
@@ -1362,6 +1372,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
   if (warp == 0) tmem_free<1>(tmem, kSmallSide);
 }
 
+bool in_shared_memory(const Shape& S) { return S.m <= kSmallSide && S.n <= kSmallSide * kMostSmallParts; }
 template <typename T>
 cudaError_t launch_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old, bool turned, int64_t K,
                          const SmallArgs& A, int device, cudaStream_t s) {
@@ -1489,6 +1500,9 @@ int64_t work_of(bool fine, int64_t K, const Course& c, char* at, Work* w) {
   return bytes;
 }
 
+// Test hook (gmc_test_withhold_phase): the next call's wait limit, 0 = off.
+std::atomic<uint64_t> g_hold_ns{0};
+
 bool sizes_ok(int32_t dtype, int64_t K, int64_t m, int64_t n) {
   if (dtype != GMC_F32 && dtype != GMC_BF16 && dtype != GMC_F16) return false;
   if (K < 0 || m < 0 || n < 0 || K > 65535 || m > (1 << 20) || n > (1 << 20)) return false;
@@ -1512,6 +1526,19 @@ int64_t gmc_orthogonalize_workspace(int32_t dtype, int64_t K, int64_t m, int64_t
   return bytes <= kMostWork ? bytes : -1;
 }
 
+int gmc_test_orthogonalize_course(int32_t dtype, int64_t K, int64_t m, int64_t n) {
+  if (!sizes_ok(dtype, K, m, n)) return -1;
+  const Course c = course_of(K, m, n, dtype != GMC_BF16);
+  if (in_shared_memory(c.S)) return 0;
+  return 1 | c.pairs << 1 | c.of[0].triangle << 2 | c.of[1].triangle << 3 | c.splits << 4 | (c.whole > 0) << 12;
+}
+
+int gmc_test_withhold_phase(uint64_t wait_limit_ns) {
+  if (wait_limit_ns > 2000000000ull) return GMC_EINVAL;
+  g_hold_ns.store(wait_limit_ns, std::memory_order_relaxed);
+  return GMC_OK;
+}
+
 int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev, int64_t out_ldk, int64_t out_ld,
                       int32_t dtype, int64_t K, int64_t m, int64_t n, int32_t steps, const float* coefficients_host,
                       float scale, void* workspace_dev, int64_t workspace_bytes, void* stream) {
@@ -1532,6 +1559,7 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool turned = m > n;
   bool pairs = course.pairs;
+  const uint64_t hold_ns = g_hold_ns.exchange(0, std::memory_order_relaxed);
   int device = 0, sms = 0;
   cudaError_t err = cudaGetDevice(&device);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
@@ -1548,8 +1576,8 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
     constexpr bool fine = !std::is_same<T, __nv_bfloat16>::value;
     const T* g = static_cast<const T*>(x_dev);
     T* o = static_cast<T*>(out_dev);
-    if (S.m <= kSmallSide && S.n <= kSmallSide * kMostSmallParts) {
-      SmallArgs A{S.m, S.n, steps, 1, scale, {}};
+    if (in_shared_memory(S)) {
+      SmallArgs A{S.m, S.n, steps, 1, scale, hold_ns ? hold_ns : kWaitLimitNs, hold_ns != 0, {}};
       while (A.parts * kSmallSide < S.n) A.parts *= 2;
       std::copy(coefficients_host, coefficients_host + 3 * steps, A.coef);
       const cudaError_t e = launch_small<T>(g, ldk, ld, o, out_ldk, out_ld, turned, K, A, device, s);
@@ -1564,7 +1592,7 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
     if (e != cudaSuccess) return e;
     ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps,
                   {course.of[0].triangle, course.of[1].triangle}, course.whole, course.splits, w.shares, w.shared,
-                  w.counts + 1, w.counts, {}};
+                  w.counts + 1, hold_ns ? hold_ns : kWaitLimitNs, hold_ns != 0, w.counts, {}};
     std::copy(coefficients_host, coefficients_host + 3 * steps, P.coef);
     if (pairs) e = all_steps<2, fine>(map, P, device, sms, s);
     if (pairs && too_large_here(e)) {  // a context without room for clusters
