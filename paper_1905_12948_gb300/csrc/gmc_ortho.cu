@@ -46,6 +46,10 @@ struct Shape {
 constexpr int kBlock = 128 * 64;  // halves of a block
 __device__ __forceinline__ uint32_t piece_at(uint32_t row, uint32_t piece) { return row * 128 + ((piece ^ (row & 7)) << 4); }
 
+// Whether factors are the sum of two halves: where the result keeps more bits than one has.
+template <typename T>
+constexpr bool kOfTwo = !std::is_same<T, __nv_bfloat16>::value;
+
 struct Halves2 {
   __half *hi, *lo;
 };
@@ -211,36 +215,13 @@ __global__ void __launch_bounds__(256) k_first(const T* g, int64_t sk, int64_t l
   }
   fence_proxy_async_all();
 }
-template <typename T, bool kTurned>
-__global__ void __launch_bounds__(256) k_last(T* out, int64_t sk, int64_t ld, Shape S, Halves2 X, float scale,
-                                              const uint32_t* gave_up) {
+// NaN for all of the result where a wait has given up.
+template <typename T>
+__global__ void __launch_bounds__(256) k_gave_up(T* out, int64_t sk, int64_t ld, int64_t m, int64_t n, const uint32_t* gave_up) {
   griddep_wait();
-  const int64_t k = blockIdx.y, xc = S.np / 64, rb = blockIdx.x / xc, cb = blockIdx.x % xc;
-  const int64_t from = k * S.x() + blockIdx.x * (int64_t)kBlock;
-  const float by = *gave_up ? __uint_as_float(kNan) : scale * (1.f / kX);
-  const bool vectors = !kTurned && ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(ld * sizeof(T)) | (uintptr_t)(sk * sizeof(T))) & 15) == 0;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    int row, piece;
-    piece_of<kTurned>(u, &row, &piece);
-    const int64_t i = rb * 128 + row, j0 = cb * 64 + piece * 8;
-    if (i >= S.m || j0 >= S.n) continue;
-    const uint32_t in = piece_at((uint32_t)row, (uint32_t)piece);
-    float hi[8], lo[8];
-    Vec<__half>::get(*reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(X.hi + from) + in), hi);
-    Vec<__half>::get(*reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(X.lo + from) + in), lo);
-#pragma unroll
-    for (int v = 0; v < 8; ++v) hi[v] = (hi[v] + lo[v]) * by;
-    T* x = out + k * sk + (kTurned ? j0 * ld + i : i * ld + j0);
-    if (vectors && j0 + 8 <= S.n) {
-#pragma unroll
-      for (int v = 0; v < 8; v += Vec<T>::N) *reinterpret_cast<uint4*>(x + v) = Vec<T>::put(hi + v);
-    } else {
-#pragma unroll
-      for (int v = 0; v < 8; ++v)
-        if (j0 + v < S.n) x[v * (kTurned ? ld : 1)] = Vec<T>::round(hi[v]);
-    }
-  }
+  if (!*gave_up) return;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < m * n; i += gridDim.x * 256ll)
+    out[blockIdx.y * sk + i / n * ld + i % n] = Vec<T>::round(__uint_as_float(kNan));
 }
 
 // -- products on the tensor cores ------------------------------------------------
@@ -417,6 +398,10 @@ struct ProductArgs {
   Halves2 x[2], o, r;   // X before and after each step, in turn; O, R
   float *d, *e;         // diagonals of A and B, mp each
   int begin, end;       // phases of this launch, three a step
+  int last;             // the phase that writes the result: element (i, j) of X at out + k * sk + i * si + j * sj, by
+  void* out;            // `scale`
+  int64_t sk, si, sj;
+  float scale;
   bool triangle[2];     // of A, of B: tiles on and below the diagonal
   int64_t whole;        // tiles of A that one block (or pair) sums alone,
   int splits;           // and in how many shares the others are summed
@@ -519,8 +504,10 @@ struct Parts {
 // is 256 x 256, 128 x 256 of it in each block's tensor memory; CG = 1: 128 x 128.
 // Warp 0 issues the copies, warp 1 the products; the others read the sums back (the tensor memory
 // holds two tiles) and put the new halves where the next product takes them from.
-template <int CG, bool kFine>
-__global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const __grid_constant__ CUtensorMap map, const __grid_constant__ ProductArgs P) {
+template <int CG, typename T>
+__global__ void __launch_bounds__(Plan<CG, kOfTwo<T>>::kThreads, 1) k_products(const __grid_constant__ CUtensorMap map,
+                                                                            const __grid_constant__ ProductArgs P) {
+  constexpr bool kFine = kOfTwo<T>;
   using Pl = Plan<CG, kFine>;
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -737,6 +724,7 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
         [[maybe_unused]] const float dr = kPhase == kSquare ? D[row] : 0.f, di = c3 + c5 * dr;
         [[maybe_unused]] const float ei = kPhase == kUpdate ? c1 + P.e[k * S.mp + row] : 0.f;
         const int64_t cols = ((int64_t)tc * (Pl::kWarps / 4) + e) * (64 * Pl::kItems);  // the warp's first column
+        [[maybe_unused]] const float by_out = P.scale * (1.f / kX);
         // (Loops that are not unrolled: each tile goes through this code once, and instructions have to be
         // fetched. 64 columns took 4,500 to 9,000 cycles unrolled.)
 #pragma unroll 1
@@ -815,7 +803,24 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
                     v[o] = __fmaf_rn(ei, was[j], acc[j] * (1.f / kO));
                   }
                 }
-                two_halves(v[0], v[1], nh + u / 2, nl + u / 2);
+                if (kPhase == kUpdate && index == P.last) {  // what they stand for, in the place of the halves
+                  const T r0 = Vec<T>::round(v[0] * by_out), r1 = Vec<T>::round(v[1] * by_out);
+                  if (P.sj != 1) {  // (neighbours are the lanes' rows)
+                    const int64_t col = cols + c * 64 + h + p * 8 + u;
+                    T* o = static_cast<T*>(P.out) + k * P.sk + row * P.si + col * P.sj;
+                    if (row < S.m && col < S.n) o[0] = r0;
+                    if (row < S.m && col + 1 < S.n) o[P.sj] = r1;
+                  } else if constexpr (sizeof(T) == 2) {
+                    memcpy(&nh[u / 2], &r0, 2);
+                    memcpy(reinterpret_cast<char*>(&nh[u / 2]) + 2, &r1, 2);
+                  } else {
+                    __half2* four = (u < 4 ? nh : nl) + u % 4;
+                    memcpy(four, &r0, 4);
+                    memcpy(four + 1, &r1, 4);
+                  }
+                } else {
+                  two_halves(v[0], v[1], nh + u / 2, nl + u / 2);
+                }
               }
               char* at = b + piece_at((uint32_t)lane, (uint32_t)(h / 8 + p));
               *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(nh);
@@ -828,6 +833,35 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
             }
           }
           if (c == items - 1) done();
+          if (kPhase == kUpdate && index == P.last) {
+            __syncwarp();
+            if (P.sj == 1) {
+              // the result's rows from where they lie, eight lanes a row's 64 columns
+              const int64_t row0 = ((int64_t)tr * CG + rank) * 128 + w * 32, col = cols + c * 64 + lane % 8 * 8;
+              T* o = static_cast<T*>(P.out) + k * P.sk + col;
+              const bool vectors = ((reinterpret_cast<uintptr_t>(P.out) | (uintptr_t)(P.sk * sizeof(T)) | (uintptr_t)(P.si * sizeof(T))) & 15) == 0;
+#pragma unroll 1
+              for (int r = lane / 8; r < 32 && row0 + r < S.m; r += 4) {
+                alignas(16) T e8[8];
+                const char* from_smem = b + piece_at((uint32_t)r, (uint32_t)(lane % 8));
+                memcpy(e8, from_smem, 16);
+                if (sizeof(T) == 4) memcpy(reinterpret_cast<char*>(e8) + 16 * (sizeof(T) / 4), from_smem + kHeldBytes, 16);
+                T* to_row = o + (row0 + r) * P.si;
+                if (vectors && col + 8 <= S.n) {
+#pragma unroll
+                  for (int u = 0; u < 8; u += Vec<T>::N) memcpy(__builtin_assume_aligned(to_row + u, 16), e8 + u, 16);
+                } else {
+#pragma unroll
+                  for (int u = 0; u < 8; ++u)
+                    if (col + u < S.n) to_row[u] = e8[u];
+                }
+              }
+            }
+            fence_proxy_async();  // (read and written before the next copy into it)
+            __syncwarp();
+            if (lane == 0 && Pl::kBuffers == 1) fetch_after(c);
+            continue;
+          }
           fence_proxy_async();
           __syncwarp();
           if (lane == 0) {
@@ -991,12 +1025,12 @@ __global__ void __launch_bounds__(Plan<CG, kFine>::kThreads, 1) k_products(const
 }
 
 // The phases [P.begin, P.end) in one launch: more than one need all blocks resident at once.
-template <int CG, bool kFine>
+template <int CG, typename T>
 cudaError_t launch_phases(const CUtensorMap& map, const ProductArgs& P, int device, int sms, cudaStream_t s) {
-  using Pl = Plan<CG, kFine>;
-  constexpr int smem = product_smem<CG, kFine>();
+  using Pl = Plan<CG, kOfTwo<T>>;
+  constexpr int smem = product_smem<CG, kOfTwo<T>>();
   static_assert(smem <= 232448, "shared memory of a block");
-  auto* f = k_products<CG, kFine>;
+  auto* f = k_products<CG, T>;
   static std::atomic<uint64_t> known{0};  // devices whose limit is raised
   if (device >= 64 || !(known.load(std::memory_order_relaxed) >> device & 1)) {
     const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -1019,16 +1053,16 @@ cudaError_t launch_phases(const CUtensorMap& map, const ProductArgs& P, int devi
   return cudaLaunchKernelEx(&l.cfg, f, map, P);
 }
 // All steps: in one launch, or, where the context has no room for all blocks, phase by phase.
-template <int CG, bool kFine>
+template <int CG, typename T>
 cudaError_t all_steps(const CUtensorMap& map, ProductArgs P, int device, int sms, cudaStream_t s) {
-  cudaError_t e = launch_phases<CG, kFine>(map, P, device, sms, s);
+  cudaError_t e = launch_phases<CG, T>(map, P, device, sms, s);
   if (!too_large_here(e)) return e;
   cudaGetLastError();  // this launch's
   const int end = P.end;
   P.splits = 1;  // (shares wait for each other)
   for (e = cudaSuccess; P.begin < end && e == cudaSuccess; ++P.begin) {
     P.end = P.begin + 1;
-    e = launch_phases<CG, kFine>(map, P, device, sms, s);
+    e = launch_phases<CG, T>(map, P, device, sms, s);
   }
   return e;
 }
@@ -1097,7 +1131,7 @@ __device__ __forceinline__ int64_t up16(int64_t v) { return (v + 15) / 16 * 16; 
 template <typename T, bool kTurned>
 __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old,
                                                   const __grid_constant__ SmallArgs A) {
-  constexpr bool kFine = !std::is_same<T, __nv_bfloat16>::value;
+  constexpr bool kFine = kOfTwo<T>;
   extern __shared__ char raw[];
   auto& sm = *reinterpret_cast<SmallSmem<kFine>*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const int tid = (int)threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -1376,7 +1410,7 @@ bool in_shared_memory(const Shape& S) { return S.m <= kSmallSide && S.n <= kSmal
 template <typename T>
 cudaError_t launch_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old, bool turned, int64_t K,
                          const SmallArgs& A, int device, cudaStream_t s) {
-  constexpr int smem = (int)sizeof(SmallSmem<!std::is_same<T, __nv_bfloat16>::value>) + 1024;
+  constexpr int smem = (int)sizeof(SmallSmem<kOfTwo<T>>) + 1024;
   static_assert(smem <= 232448, "shared memory of a block");
   auto* f = turned ? k_small<T, true> : k_small<T, false>;
   static std::atomic<uint64_t> known[2];  // devices whose limit is raised
@@ -1570,10 +1604,9 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
   // parts of |G|^2: as many blocks as are resident at once, of eight rows or pieces each
   const int64_t rows8 = (m * ((n + kSizePiece - 1) / kSizePiece) + 7) / 8, share = (sms * 8 + K - 1) / K;
   const int parts = (int)std::min({rows8, share, (int64_t)kMostSizeParts});
-  const dim3 blocks((unsigned)(S.x() / kBlock), (unsigned)K), some((unsigned)std::min(S.x() / kBlock, share), (unsigned)K);
+  const dim3 some((unsigned)std::min(S.x() / kBlock, share), (unsigned)K);
   err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
-    constexpr bool fine = !std::is_same<T, __nv_bfloat16>::value;
     const T* g = static_cast<const T*>(x_dev);
     T* o = static_cast<T*>(out_dev);
     if (in_shared_memory(S)) {
@@ -1591,19 +1624,20 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
                    parts, w.x);
     if (e != cudaSuccess) return e;
     ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps,
+                  3 * steps - 1, o, out_ldk, turned ? 1 : out_ld, turned ? out_ld : 1, scale,
                   {course.of[0].triangle, course.of[1].triangle}, course.whole, course.splits, w.shares, w.shared,
                   w.counts + 1, hold_ns ? hold_ns : kWaitLimitNs, hold_ns != 0, w.counts, {}};
     std::copy(coefficients_host, coefficients_host + 3 * steps, P.coef);
-    if (pairs) e = all_steps<2, fine>(map, P, device, sms, s);
+    if (pairs) e = all_steps<2, T>(map, P, device, sms, s);
     if (pairs && too_large_here(e)) {  // a context without room for clusters
       cudaGetLastError();
       pairs = false;
       P.splits = 1;
     }
-    if (!pairs) e = all_steps<1, fine>(map, P, device, sms, s);
+    if (!pairs) e = all_steps<1, T>(map, P, device, sms, s);
     if (e != cudaSuccess) return e;
-    return launch_pdl(turned ? k_last<T, true> : k_last<T, false>, blocks, dim3(256), 0, s, o, out_ldk, out_ld, S,
-                      steps % 2 ? w.y : w.x, scale, (const uint32_t*)w.counts);
+    return launch_pdl(k_gave_up<T>, dim3((unsigned)std::min<int64_t>(4, (m * n + 255) / 256), (unsigned)K), dim3(256), 0, s, o, out_ldk,
+                      out_ld, m, n, (const uint32_t*)w.counts);
   });
   return err == cudaSuccess ? GMC_OK : GMC_ECUDA;
 }
