@@ -1583,6 +1583,7 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
   if (K == 0 || m == 0 || n == 0) return GMC_OK;
   if (!strides_ok(x_dev, dtype, K, m, n, ldk, ld) || !strides_ok(out_dev, dtype, K, m, n, out_ldk, out_ld))
     return GMC_EINVAL;
+  if (out_dev == x_dev && ((m > 1 && out_ld != ld) || (K > 1 && out_ldk != ldk))) return GMC_EINVAL;  // in place: the same rows
   const bool of_two = dtype != GMC_BF16;
   const Course course = course_of(K, m, n, of_two);
   const Shape S = course.S;

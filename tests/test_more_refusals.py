@@ -57,7 +57,7 @@ def test_orthogonalize(lib, p):
     inf = (ctypes.c_float * 15)(*([float("inf")] * 15))
     for bad in (dict(x=None), dict(out=None), dict(x=p + 2), dict(out=p + 1), dict(ldk=19), dict(ld=4), dict(oldk=19), dict(old=4),
                 dict(dtype=5), dict(K=-1), dict(steps=0), dict(steps=17), dict(c=None), dict(c=inf), dict(scale=float("nan")),
-                dict(w=None), dict(w=p + 128), dict(bytes=need - 1)):
+                dict(w=None), dict(w=p + 128), dict(bytes=need - 1), dict(out=p, oldk=24), dict(out=p, oldk=24, old=6)):
         assert call(**bad) == 1, bad
     for nothing in (dict(K=0), dict(m=0), dict(n=0)):
         assert call(x=None, out=None, w=None, bytes=0, **nothing) == 0
