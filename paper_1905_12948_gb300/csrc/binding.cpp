@@ -451,7 +451,11 @@ PyObject* orthogonalize(Args a, Py_ssize_t na) {
     ~Release() { Py_DECREF(o); }
   } release{seq};
   const Py_ssize_t count = PySequence_Fast_GET_SIZE(seq);
-  const bool single = count == 3 && PyNumber_Check(PySequence_Fast_GET_ITEM(seq, 0));
+  bool single = false;  // three numbers (a row of an array is one too, by its methods, but has a length)
+  if (count == 3 && PyObject_Size(PySequence_Fast_GET_ITEM(seq, 0)) < 0) {
+    PyErr_Clear();
+    single = true;
+  }
   if (!single && count != steps) fail(PyExc_ValueError, "coefficients", "must be (a, b, c), or one such triple for each step");
   for (int64_t i = 0; i < steps; ++i) {
     PyObject* three = single ? (Py_INCREF(seq), seq)
