@@ -420,8 +420,9 @@ struct PhaseOf {
 
 constexpr int kFactorBytes = 16384;  // of a stage: 128 rows, or columns, by 64
 constexpr int kHeldBytes = 4096;     // a warp's part of a block of halves
-template <int CG, bool kFine>
+template <int CG, typename T>
 struct Plan {
+  static constexpr bool kFine = kOfTwo<T>;
   // Warps that read the sums back, 32 rows each; 64 columns at a time, with as many parts of a block (two
   // halves) on their way to it.
   static constexpr int kWarps = CG == 2 && !kFine ? 4 : 8;
@@ -432,9 +433,14 @@ struct Plan {
   static constexpr int kThreads = 64 + 32 * kWarps;
   static constexpr int kHeld = kWarps * kBuffers * 2 * kHeldBytes;
   // Sums in the tensor cores are cut off, not rounded: by a quarter of a last place an addition where
-  // all terms have one sign (4,608 columns of fp32 matrices: 2.8e-5 off the result, by three additions for
-  // 16 columns). They are added up in registers after 128.
-  static constexpr int kChunk = kFine ? 2 : 1 << 30;   // stages
+  // all terms have one sign, as on A's diagonal (4,608 columns of fp32 matrices: 2.8e-5 off the result, by three
+  // additions for 16 columns). They are added up in registers after so many stages. float: A after 128 columns, the
+  // others, whose terms have either sign, after 256 (8 x 512 x 4,608: 9e-7 off, 626 us; after 128 8e-7, 655; after 512
+  // 1.2e-6, 610, but 2.5e-6 for 1,024 x 1,024, where 32-bit arithmetic is 3e-6 off). half: A after 2,048 columns (its
+  // own rounding is 2e-4; 4 x 2,417 x 4,507 4,630 -> 4,230 us).
+  __host__ __device__ static constexpr int chunk(int phase) {
+    return std::is_same<T, float>::value ? (phase == kGram ? 2 : 4) : kFine && phase == kGram ? 32 : 1 << 30;
+  }
 };
 struct alignas(8) ProductBars {
   uint64_t full[5], empty[5];
@@ -442,9 +448,9 @@ struct alignas(8) ProductBars {
   uint64_t held[8][2];
   uint32_t tmem, dead;
 };
-template <int CG, bool kFine>
+template <int CG, typename T>
 constexpr int product_smem() {
-  using Pl = Plan<CG, kFine>;
+  using Pl = Plan<CG, T>;
   return Pl::kStages * Pl::kStageBytes + Pl::kHeld + 1024 + (int)sizeof(ProductBars);
 }
 
@@ -505,10 +511,10 @@ struct Parts {
 // Warp 0 issues the copies, warp 1 the products; the others read the sums back (the tensor memory
 // holds two tiles) and put the new halves where the next product takes them from.
 template <int CG, typename T>
-__global__ void __launch_bounds__(Plan<CG, kOfTwo<T>>::kThreads, 1) k_products(const __grid_constant__ CUtensorMap map,
+__global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __grid_constant__ CUtensorMap map,
                                                                             const __grid_constant__ ProductArgs P) {
   constexpr bool kFine = kOfTwo<T>;
-  using Pl = Plan<CG, kFine>;
+  using Pl = Plan<CG, T>;
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   char* held = smem + Pl::kStages * Pl::kStageBytes;
@@ -625,6 +631,7 @@ __global__ void __launch_bounds__(Plan<CG, kOfTwo<T>>::kThreads, 1) k_products(c
         const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, kPhase != kUpdate && P.triangle[kPhase % kUpdate]);
         const Parts parts(P, tiles, kPhase);
         // 32-bit sums of halves; the right factor's rows are the sum's index in kUpdate
+        constexpr int kChunk = Pl::chunk(kPhase);
         constexpr uint32_t what = 1u << 4 | (kPhase == kUpdate ? 1u << 16 : 0) | (CG * 128 / 8) << 17 | (CG * 128 / 16) << 24;
         for (int64_t unit = first; unit < parts.all && going; unit += step) {
           int64_t t;
@@ -634,7 +641,7 @@ __global__ void __launch_bounds__(Plan<CG, kOfTwo<T>>::kThreads, 1) k_products(c
             const uint32_t acc = tmem + (it & 1) * kColumns;
             going = it < 2 || wait_for(&bars.taken[it & 1], (it / 2 - 1) & 1, patience);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const int begin = kb, end = last - kb > Pl::kChunk ? kb + Pl::kChunk : last;
+            const int begin = kb, end = last - kb > kChunk ? kb + kChunk : last;
             for (; kb < end && going; ++kb, ++n) {
               const int s = (int)(n % Pl::kStages);
               going = wait_for(&bars.full[s], (n / Pl::kStages) & 1, patience);
@@ -902,11 +909,14 @@ __global__ void __launch_bounds__(Plan<CG, kOfTwo<T>>::kThreads, 1) k_products(c
         int64_t t;
         int begin, end;
         parts.at(unit, &t, &begin, &end);
-        if constexpr (kFine) {
+        constexpr int kChunk = Pl::chunk(kPhase);
+        bool added_up = false;
+        if constexpr (kFine && kChunk < 1 << 30) added_up = end - begin > kChunk;
+        if (added_up) {
           float sum[64 * Pl::kItems];
 #pragma unroll
           for (int i = 0; i < 64 * Pl::kItems; ++i) sum[i] = 0.f;
-          for (int kb = begin; kb < end; kb += Pl::kChunk) {
+          for (int kb = begin; kb < end; kb += kChunk) {
             going = __all_sync(0xffffffffu, wait_for(&bars.sums[it & 1], (it / 2) & 1, patience));
             if (!going) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -920,7 +930,7 @@ __global__ void __launch_bounds__(Plan<CG, kOfTwo<T>>::kThreads, 1) k_products(c
 #pragma unroll
               for (int u = 0; u < kStep; ++u) sum[i + u] += one[u], sum[i + kStep + u] += two[u];
             }
-            if (kb + Pl::kChunk < end) {
+            if (kb + kChunk < end) {
               asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
               __syncwarp();
               if (lane == 0) arrive_first<CG>(&bars.taken[it & 1]);
@@ -1027,8 +1037,8 @@ __global__ void __launch_bounds__(Plan<CG, kOfTwo<T>>::kThreads, 1) k_products(c
 // The phases [P.begin, P.end) in one launch: more than one need all blocks resident at once.
 template <int CG, typename T>
 cudaError_t launch_phases(const CUtensorMap& map, const ProductArgs& P, int device, int sms, cudaStream_t s) {
-  using Pl = Plan<CG, kOfTwo<T>>;
-  constexpr int smem = product_smem<CG, kOfTwo<T>>();
+  using Pl = Plan<CG, T>;
+  constexpr int smem = product_smem<CG, T>();
   static_assert(smem <= 232448, "shared memory of a block");
   auto* f = k_products<CG, T>;
   static std::atomic<uint64_t> known{0};  // devices whose limit is raised
