@@ -11,7 +11,8 @@
 //   - X is two halves, 22 bits, the second one what the first one left. The first steps multiply small
 //     singular values by `a` each, and a rounding of X to 11 bits with them: 3.4^5 of 2^-12
 //     would be left of it. Products take the first half (bfloat16 matrices: the result is off by 2 to 8e-4,
-//     its own rounding by 1.7e-3), or the terms hi hi + hi lo + lo hi (float and half: 1e-7 to 8e-6).
+//     its own rounding by 1.7e-3), or the terms hi hi + hi lo + lo hi (float: 0.6 to 1.5e-6, where 32-bit arithmetic
+//     is off by 2.3 to 5e-6).
 // X is kept 2^14 times, O and R 2^11 times what they are: the second halves then stay normal
 // numbers, and a singular value may come to 4.
 #include <algorithm>
@@ -111,10 +112,11 @@ __device__ __forceinline__ double squares(float* f) {
   return ldexp((double)sum_squares<N>(f), 2 * e);
 }
 // Sums of squares of parts of each matrix G (as it is given: m rows of n), in a fixed order: warps
-// take rows, or pieces of 4,096 elements of them.
+// take rows, or pieces of 4,096 elements of them. Bound by memory (2 x 4,096 x 25,088 bf16: 67 us, 6.1 TB/s; 8 x
+// 1,000 x 4,096, as many blocks as are resident: 15.7 us, twice as many 16.6).
 constexpr int kMostSizeParts = 256, kSizePiece = 4096;
 template <typename T>
-__global__ void __launch_bounds__(256) k_size(const T* g, int64_t sk, int64_t ld, int64_t m, int64_t n, double* part,
+__global__ void __launch_bounds__(256, 4) k_size(const T* g, int64_t sk, int64_t ld, int64_t m, int64_t n, double* part,
                                               uint32_t* counts, int64_t counters) {
   constexpr int N = Vec<T>::N;
   __shared__ double ws[8];
@@ -169,7 +171,9 @@ __device__ __forceinline__ void piece_of(int u, int* row, int* piece) {
   *row = kTurned ? t % 128 : t / 8 + 32 * u;
   *piece = kTurned ? t / 128 + 2 * u : t % 8;
 }
-// X = G / |G| as two halves, a block of them by a block.
+// X = G / |G| as two halves, a block of them by a block. Bound by memory, G (from the L2 cache where it fits) and four
+// bytes an element written: 8 x 1,000 x 4,096 bf16 43 us, 4.6 TB/s, 2 x 4,096 x 25,088 231 us, 5.3 TB/s. (Half a block
+// at a time with the next one's loads before: the same.) Turned, by loads of single elements: 72 us.
 template <typename T, bool kTurned>
 __global__ void __launch_bounds__(256) k_first(const T* g, int64_t sk, int64_t ld, Shape S, const double* part, int parts,
                                                Halves2 X) {
@@ -215,7 +219,7 @@ __global__ void __launch_bounds__(256) k_first(const T* g, int64_t sk, int64_t l
   }
   fence_proxy_async_all();
 }
-// NaN for all of the result where a wait has given up.
+// NaN for all of the result where a wait has given up. (The products write the result themselves. 1.8 us.)
 template <typename T>
 __global__ void __launch_bounds__(256) k_gave_up(T* out, int64_t sk, int64_t ld, int64_t m, int64_t n, const uint32_t* gave_up) {
   griddep_wait();
@@ -509,7 +513,12 @@ struct Parts {
 // in kUpdate) of the right one, 64 of the sum at a time; a pair of blocks (CG = 2) shares them, and its tile
 // is 256 x 256, 128 x 256 of it in each block's tensor memory; CG = 1: 128 x 128.
 // Warp 0 issues the copies, warp 1 the products; the others read the sums back (the tensor memory
-// holds two tiles) and put the new halves where the next product takes them from.
+// holds two tiles) and put the new halves where the next product takes them from, or the result into its place.
+// What bounds it: with deep sums the tensor cores under the power limit (2 x 4,096 x 25,088 bf16: 1.46 PFLOP/s; cuBLAS
+// 1.89 in a burst, 1.72 sustained); with short ones a block's port to the L2 cache, 53 to 60 bytes a cycle for the
+// factors and X, which is read and written whole (8 x 1,000 x 4,096: 16,500 cycles for a tile of 256 x 256, of which
+// the products take 8,200); with few tiles the barriers and the first copies after them (8 x 256 x 256: 6.5 us a
+// phase). Pairs of blocks, with tiles of 256 x 256, halve the factors' bytes; see course_of().
 template <int CG, typename T>
 __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __grid_constant__ CUtensorMap map,
                                                                             const __grid_constant__ ProductArgs P) {
@@ -1104,7 +1113,8 @@ cudaError_t map_of(void* base, int64_t bytes, CUtensorMap* map) {
 // X of up to 128 rows and 128 columns a block, in shared memory from the first step to the last: one launch
 // for everything. The blocks of a cluster have 128 columns each; of A = X X' each adds up the shares of all
 // for its own columns, and gives them to all. A^2 and B are each block's own. What bounds it is the chain of
-// products, of 0.2 us each, and of what is made of their sums.
+// products, of 0.2 us each, and of what is made of their sums: 16 x 16 bf16 19 us, by way of the workspace 31; 4 x
+// 1,000 x 64 fp32 52, so 108; 128 x 128 fp32 51.
 constexpr int kSmallSide = 128, kMostSmallParts = 8;
 struct SmallArgs {
   int64_t m, n;  // of X
@@ -1436,8 +1446,15 @@ cudaError_t launch_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk
 
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// How a call is carried out: tiles of one block or of a pair, and the shares that X's columns are
-// taken in. By what the phases take, in cycles.
+// How a call is carried out: tiles of one block or of a pair, triangles or whole squares of them, and the shares
+// that X's columns are taken in. By what the phases take, in cycles. Measured both ways, us (bf16, then float):
+//                          single tiles   pairs      whole squares  triangles   unshared  shared
+//    32 x    256 x  1,024   200   286    233   326    202   281     218   305
+//     1 x  1,024 x  1,024   156   262    215   341    156   256     184   275
+//     8 x    512 x  4,608   434   705    396   636    405   686     406   656    418   759  397   632
+//     8 x  1,000 x  4,096   934 1,751    716 1,596    734 1,835     735 1,621    735 1,796  715 1,596
+//     2 x  3,000 x  3,000 1,432 3,013    952 2,700  1,101 3,221     942 2,829    994 2,873  980 2,711
+//     7 x    136 x 13,517   427   554    444   579                                654 1,206  424   556
 struct Course {
   Shape S;
   bool pairs;
@@ -1613,9 +1630,9 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
   err = map_of(workspace_dev, need, &map);
   if (err != cudaSuccess) return GMC_ECUDA;
   // parts of |G|^2: as many blocks as are resident at once, of eight rows or pieces each
-  const int64_t rows8 = (m * ((n + kSizePiece - 1) / kSizePiece) + 7) / 8, share = (sms * 8 + K - 1) / K;
-  const int parts = (int)std::min({rows8, share, (int64_t)kMostSizeParts});
-  const dim3 some((unsigned)std::min(S.x() / kBlock, share), (unsigned)K);
+  const int64_t rows8 = (m * ((n + kSizePiece - 1) / kSizePiece) + 7) / 8;
+  const int parts = (int)std::min({rows8, (sms * 4 + K - 1) / K, (int64_t)kMostSizeParts});
+  const dim3 some((unsigned)std::min(S.x() / kBlock, (sms * 8 + K - 1) / K), (unsigned)K);
   err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
     const T* g = static_cast<const T*>(x_dev);
