@@ -60,7 +60,9 @@ __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.pr
 __device__ __forceinline__ void two_halves(float x, float y, __half2* hi, __half2* lo) {
   *hi = __floats2half2_rn(x, y);
   const float2 back = __half22float2(*hi);
-  *lo = __floats2half2_rn(x - back.x, y - back.y);
+  float a, b;
+  split(add_pair(pair_of(x, y), pair_of(-back.x, -back.y)), &a, &b);
+  *lo = __floats2half2_rn(a, b);
 }
 
 // What makes v of a matrix X: a power of two that puts the norm near 1 is taken out, in two steps (either
@@ -89,27 +91,29 @@ __device__ __forceinline__ Scaled scaled_by(double squares) {
 // The squares of N numbers added up: in 32 bits, with a power of two taken out where they would
 // not fit, so that the sum is the same at any magnitude.
 template <int N>
-__device__ __forceinline__ float sum_squares(const float* f) {
+__device__ __forceinline__ double squares(const float* f) {
   float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < N; ++i) s[i % 4] = __fmaf_rn(f[i], f[i], s[i % 4]);
-  return (s[0] + s[1]) + (s[2] + s[3]);
-}
-template <int N>
-__device__ __forceinline__ double squares(float* f) {
-  float s = sum_squares<N>(f);
-  if (s > 0x1p-90f && s < 0x1p100f) return (double)s;
+  float sum = (s[0] + s[1]) + (s[2] + s[3]);
+  if (sum > 0x1p-90f && sum < 0x1p100f) return (double)sum;
   float most = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(f[i]));
-  if (s != s || most == INFINITY) return (double)s;
+  if (sum != sum || most == INFINITY) return (double)sum;
   if (most == 0.f) return 0.;
   int e;
   frexpf(most, &e);
   const float p1 = power2(-(e / 2)), p2 = power2(-(e - e / 2));
 #pragma unroll
-  for (int i = 0; i < N; ++i) f[i] = f[i] * p1 * p2;
-  return ldexp((double)sum_squares<N>(f), 2 * e);
+  for (int i = 0; i < 4; ++i) s[i] = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float x = f[i] * p1 * p2;
+    s[i % 4] = __fmaf_rn(x, x, s[i % 4]);
+  }
+  sum = (s[0] + s[1]) + (s[2] + s[3]);
+  return ldexp((double)sum, 2 * e);
 }
 // Sums of squares of parts of each matrix G (as it is given: m rows of n), in a fixed order: warps
 // take rows, or pieces of 4,096 elements of them. Bound by memory (2 x 4,096 x 25,088 bf16: 67 us, 6.1 TB/s; 8 x
@@ -780,7 +784,10 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
                   float low[8];
                   Vec<__half>::get(halves[2 * p + 1], low);
 #pragma unroll
-                  for (int u = 0; u < 8; ++u) was[p * 8 + u] += low[u];
+                  for (int u = 0; u < 8; u += 2) {
+                    float* x = was + p * 8 + u;
+                    split(add_pair(pair_of(x[0], x[1]), pair_of(low[u], low[u + 1])), x, x + 1);
+                  }
                 }
               }
               if (!kFine && h + kStep < 64) read(h + kStep);
@@ -808,16 +815,15 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
 #pragma unroll
               for (int u = 0; u < 8; u += 2) {
                 float v[2];
-#pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                  const int j = p * 8 + u + o;
-                  if constexpr (kPhase == kGram) {
-                    v[o] = acc[j] * (kO / (kX * kX));
-                  } else if constexpr (kPhase == kSquare) {  // b O + c (O^2 + (D_i + D_j) O)
-                    v[o] = __fmaf_rn(__fmaf_rn(c5, dc[j], di), was[j], acc[j] * (c5 / kO));
-                  } else {
-                    v[o] = __fmaf_rn(ei, was[j], acc[j] * (1.f / kO));
-                  }
+                const int j = p * 8 + u;
+                const Pair sum = pair_of(acc[j], acc[j + 1]);
+                auto two = [](float x) { return pair_of(x, x); };
+                if constexpr (kPhase == kGram) {
+                  split(mul_pair(sum, two(kO / (kX * kX))), v, v + 1);
+                } else if constexpr (kPhase == kSquare) {  // b O + c (O^2 + (D_i + D_j) O)
+                  split(fma_pair(fma_pair(two(c5), pair_of(dc[j], dc[j + 1]), two(di)), pair_of(was[j], was[j + 1]), mul_pair(sum, two(c5 / kO))), v, v + 1);
+                } else {
+                  split(fma_pair(two(ei), pair_of(was[j], was[j + 1]), mul_pair(sum, two(1.f / kO))), v, v + 1);
                 }
                 if (kPhase == kUpdate && index == P.last) {  // what they stand for, in the place of the halves
                   const T r0 = Vec<T>::round(v[0] * by_out), r1 = Vec<T>::round(v[1] * by_out);
@@ -1129,9 +1135,10 @@ struct alignas(1024) SmallSmem {
   __half xh[2][kBlock], xl[2][kBlock];  // X, blocks of 64 columns
   __half oh[2][kBlock];                 // O, then R
   __half ol[kFine ? 2 : 1][kFine ? kBlock : 8];
-  float share[kSmallSide * kSmallSide]; // of A's columns that are this block's, by the blocks they come from
+  float share[kSmallSide * kSmallSide]; // of A's columns that are this block's, by the blocks they come from, by columns
   float d[kSmallSide], e[kSmallSide];   // diagonals of A and B
   double squares[kMostSmallParts], ws[8];
+  Scaled by;
   uint64_t done;                        // products
   uint32_t tmem, dead;
 };
@@ -1189,31 +1196,27 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
       for (int v = 0; v < 8; ++v) f[u][v] = row < A.m && j + v < A.n ? Vec<T>::one(x[v * (kTurned ? ld : 1)]) : 0.f;
     }
   }
-#pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = f[u][i];
-    s += squares<8>(v);
-  }
-  s = warp_sum(s);
+  s = warp_sum(squares<64>(&f[0][0]));
   if (lane == 0) sm.ws[warp] = s;
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *(volatile uint32_t*)&sm.tmem;
-  s = 0.;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s += sm.ws[i];
+  // (64-bit arithmetic is slow: by one warp)
+  if (warp == 0) s = warp_sum(lane < 8 ? sm.ws[lane] : 0.);
   if (parts > 1) {
     cluster_wait();  // all have begun
     if (tid < (int)parts) store_at(smem_addr(&sm.squares[rank]), (uint32_t)tid, s);
     cluster_arrive();
     cluster_wait();
-    s = 0.;
-    for (uint32_t i = 0; i < parts; ++i) s += sm.squares[i];
+    if (warp == 0) s = warp_sum(lane < (int)parts ? sm.squares[lane] : 0.);
   }
-  const Scaled by = scaled_by(s);
+  if (warp == 0) {
+    const Scaled by = scaled_by(s);
+    if (lane == 0) sm.by = by;
+  }
+  __syncthreads();
+  const Scaled by = sm.by;
 #pragma unroll
   for (int u = 0; u < 8; ++u) {
     int row, piece;
@@ -1236,6 +1239,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
   // computed nor looked at.
   const int row = warp % 4 * 32 + lane, half = warp / 4 * kStep, side = (int)up16(A.m);
   const bool in_rows = warp % 4 * 32 < side;  // (the same for a warp)
+  const int columns = A.n - j0 > kSmallSide ? kSmallSide : A.n > j0 ? (int)up16(A.n - j0) : 16;  // of X that are not padding
   const uint32_t acc_at = tmem + ((uint32_t)(warp % 4) << 21);
   uint32_t products = 0;
   // All threads: what they wrote is there for the products, which `issue` issues; they are done.
@@ -1289,7 +1293,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
 #pragma unroll 1
   for (int step = 0; step < A.steps; ++step) {
     const float c1 = A.coef[3 * step], c3 = A.coef[3 * step + 1], c5 = A.coef[3 * step + 2];
-    product([&] { issue(xh, xl, xh, xl, false, side, kSmallSide); });
+    product([&] { issue(xh, xl, xh, xl, false, side, columns); });
     if (parts == 1) {
 #pragma unroll 1
       for (int at = half; at < side && in_rows; at += 2 * kStep) {
@@ -1321,27 +1325,29 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
         tmem_loaded(acc);
         if (*(volatile uint32_t*)&sm.dead) acc[0] = __uint_as_float(kNan);  // (which all of X gets)
 #pragma unroll
-        for (int u = 0; u < kStep; u += 4) {
-          const int column = at + u;
-          const uint32_t to = smem_addr(sm.share + ((int)rank * side + row) * wide + column % wide);
+        for (int p = 0; p < kStep; p += 8) {
+          const int column = at + p;
+          const uint32_t to = remote(smem_addr(sm.share + ((int)rank * wide + column % wide) * side + row), (uint32_t)(column / wide));
           if (row < side)
-            store_at(to, (uint32_t)(column / wide), make_uint4(__float_as_uint(acc[u]), __float_as_uint(acc[u + 1]),
-                                                               __float_as_uint(acc[u + 2]), __float_as_uint(acc[u + 3])));
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+              asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + u * side * 4), "f"(acc[p + u]) : "memory");
         }
       }
       cluster_arrive();
       cluster_wait();
-      // (pieces of eight columns of a row: all of a piece's shares, then its halves to all blocks)
+      // (A is symmetric: its columns are rows. Pieces of eight columns of a row: all of a piece's shares, then its
+      // halves to all blocks, neighbours along a row)
 #pragma unroll 1
       for (int i = tid; i < side * wide / 8; i += 256) {
-        const int r = i % side, c = i / side * 8, column = (int)rank * wide + c;
-        if (column >= side) break;
+        const int c = i / (side / 8), column = i % (side / 8) * 8, r = (int)rank * wide + c;
+        if (r >= side) break;
         float v[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) v[u] = 0.f;
 #pragma unroll 1
         for (uint32_t p = 0; p < parts; ++p) {
-          const float4* share = reinterpret_cast<const float4*>(sm.share + ((int)p * side + r) * wide + c);
+          const float4* share = reinterpret_cast<const float4*>(sm.share + ((int)p * wide + c) * side + column);
           const float4 x = share[0], y = share[1];
           v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
           v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
@@ -1389,12 +1395,12 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
         if (kFine) *place(sm.ol, column) = lo;
       }
     }
-    product([&] { issue(oh, ol, xh, xl, true, kSmallSide, side); });
+    product([&] { issue(oh, ol, xh, xl, true, columns, side); });
     const float ei = c1 + sm.e[row];
     const bool last = step + 1 == A.steps;
     const float by_out = *(volatile uint32_t*)&sm.dead ? __uint_as_float(kNan) : A.scale * (1.f / kX);
 #pragma unroll 1
-    for (int at = half; at < kSmallSide && in_rows; at += 2 * kStep) {
+    for (int at = half; at < columns && in_rows; at += 2 * kStep) {
       float acc[kStep];
       tmem_load(acc_at + at, acc);
       tmem_loaded(acc);
@@ -1410,13 +1416,43 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
           halves(v, &hi, &lo);
           *place(sm.xh, column) = hi;
           *place(sm.xl, column) = lo;
-        } else if (row < A.m) {
+        } else if (kTurned) {  // (neighbours are the lanes' rows)
           const int64_t j = j0 + column;
-          T* o = out + k * osk + (kTurned ? j * old + row : row * old + j);
+          T* o = out + k * osk + j * old + row;
 #pragma unroll
           for (int u = 0; u < 8; ++u)
-            if (j + u < A.n) o[u * (kTurned ? old : 1)] = Vec<T>::round(v[u] * by_out);
+            if (row < A.m && j + u < A.n) o[u * old] = Vec<T>::round(v[u] * by_out);
+        } else {  // in the place of the halves
+          alignas(16) T e8[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) e8[u] = Vec<T>::round(v[u] * by_out);
+          memcpy(__builtin_assume_aligned(place(sm.xh, column), 16), e8, 16);
+          if (sizeof(T) == 4) memcpy(__builtin_assume_aligned(place(sm.xl, column), 16), reinterpret_cast<const char*>(e8) + sizeof(e8) - 16, 16);
         }
+      }
+    }
+  }
+  if (!kTurned) {
+    // the result's rows from where they lie, sixteen lanes a row
+    __syncthreads();
+    out += k * osk;
+    const bool rows16 = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(old * sizeof(T))) & 15) == 0;
+#pragma unroll 1
+    for (int r = tid / 16; r < A.m; r += 16) {
+      const int piece = tid % 16;
+      const int64_t j = j0 + piece * 8;
+      const uint32_t in = (uint32_t)(piece / 8) * kBlockBytes + piece_at((uint32_t)r, (uint32_t)(piece % 8));
+      alignas(16) T e8[8];
+      memcpy(e8, __builtin_assume_aligned(reinterpret_cast<const char*>(sm.xh) + in, 16), 16);
+      if (sizeof(T) == 4) memcpy(reinterpret_cast<char*>(e8) + sizeof(e8) - 16, __builtin_assume_aligned(reinterpret_cast<const char*>(sm.xl) + in, 16), 16);
+      T* o = out + r * old + j;
+      if (rows16 && j + 8 <= A.n) {
+#pragma unroll
+        for (int u = 0; u < 8; u += Vec<T>::N) memcpy(__builtin_assume_aligned(o + u, 16), e8 + u, 16);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (j + u < A.n) o[u] = e8[u];
       }
     }
   }
