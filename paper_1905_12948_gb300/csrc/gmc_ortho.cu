@@ -1119,9 +1119,10 @@ cudaError_t map_of(void* base, int64_t bytes, CUtensorMap* map) {
 // X of up to 128 rows and 128 columns a block, in shared memory from the first step to the last: one launch
 // for everything. The blocks of a cluster have 128 columns each; of A = X X' each adds up the shares of all
 // for its own columns, and gives them to all. A^2 and B are each block's own. What bounds it is the chain of
-// products, of 0.2 us each, and of what is made of their sums: 16 x 16 bf16 19 us, by way of the workspace 31; 4 x
-// 1,000 x 64 fp32 52, so 108; 128 x 128 fp32 51.
-constexpr int kSmallSide = 128, kMostSmallParts = 8;
+// products (0.3 us each, 1.1 of fp32) and of what is made of their sums by 16 warps (by 8: 128 x 128 bf16 26 us, so
+// 24); with clusters also the exchange of A, 64 KB into each block and 32 out of it (2 us). 16 x 16 bf16 12.5 us, by way of
+// the workspace 31; 128 x 128 fp32 41; 4 x 1,000 x 64 fp32 43, so 108; 8 x 128 x 1,024 bf16 49.
+constexpr int kSmallSide = 128, kMostSmallParts = 8, kSmallThreads = 512;
 struct SmallArgs {
   int64_t m, n;  // of X
   int steps, parts;
@@ -1137,7 +1138,7 @@ struct alignas(1024) SmallSmem {
   __half ol[kFine ? 2 : 1][kFine ? kBlock : 8];
   float share[kSmallSide * kSmallSide]; // of A's columns that are this block's, by the blocks they come from, by columns
   float d[kSmallSide], e[kSmallSide];   // diagonals of A and B
-  double squares[kMostSmallParts], ws[8];
+  double squares[kMostSmallParts], ws[kSmallThreads / 32];
   Scaled by;
   uint64_t done;                        // products
   uint32_t tmem, dead;
@@ -1156,7 +1157,7 @@ __device__ __forceinline__ void store_at(uint32_t addr, uint32_t rank, double v)
 __device__ __forceinline__ int64_t up16(int64_t v) { return (v + 15) / 16 * 16; }
 
 template <typename T, bool kTurned>
-__global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old,
+__global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old,
                                                   const __grid_constant__ SmallArgs A) {
   constexpr bool kFine = kOfTwo<T>;
   extern __shared__ char raw[];
@@ -1173,17 +1174,18 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
   if (warp == 0) tmem_alloc<1>(&sm.tmem, kSmallSide);
   griddep_wait();
 
-  // this block's columns of G: eight pieces of eight columns a thread, neighbours along a row of G
+  // this block's columns of G: some pieces of eight columns a thread, neighbours along a row of G
   g += k * sk;
-  float f[8][8];
+  constexpr int kPieces = kSmallSide * kSmallSide / 8 / kSmallThreads, kGroups = kSmallThreads / 128;
+  float f[kPieces][8];
   double s = 0.;
   const bool vectors = !kTurned && ((reinterpret_cast<uintptr_t>(g) | (uintptr_t)(ld * sizeof(T))) & 15) == 0;
   auto piece_of = [&](int u, int* row, int* piece) {
-    *row = kTurned ? tid % 128 : tid / 16 + 16 * u;
-    *piece = kTurned ? tid / 128 + 2 * u : tid % 16;
+    *row = kTurned ? tid % 128 : tid / 16 + kSmallThreads / 16 * u;
+    *piece = kTurned ? tid / 128 + kGroups * u : tid % 16;
   };
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
+  for (int u = 0; u < kPieces; ++u) {
     int row, piece;
     piece_of(u, &row, &piece);
     const int64_t j = j0 + piece * 8;
@@ -1196,14 +1198,14 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
       for (int v = 0; v < 8; ++v) f[u][v] = row < A.m && j + v < A.n ? Vec<T>::one(x[v * (kTurned ? ld : 1)]) : 0.f;
     }
   }
-  s = warp_sum(squares<64>(&f[0][0]));
+  s = warp_sum(squares<8 * kPieces>(&f[0][0]));
   if (lane == 0) sm.ws[warp] = s;
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *(volatile uint32_t*)&sm.tmem;
   // (64-bit arithmetic is slow: by one warp)
-  if (warp == 0) s = warp_sum(lane < 8 ? sm.ws[lane] : 0.);
+  if (warp == 0) s = warp_sum(lane < kSmallThreads / 32 ? sm.ws[lane] : 0.);
   if (parts > 1) {
     cluster_wait();  // all have begun
     if (tid < (int)parts) store_at(smem_addr(&sm.squares[rank]), (uint32_t)tid, s);
@@ -1218,7 +1220,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
   __syncthreads();
   const Scaled by = sm.by;
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
+  for (int u = 0; u < kPieces; ++u) {
     int row, piece;
     piece_of(u, &row, &piece);
     alignas(16) __half2 hi[4], lo[4];
@@ -1235,7 +1237,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
     *reinterpret_cast<uint4*>(reinterpret_cast<char*>(sm.xl[piece / 8]) + in) = *reinterpret_cast<uint4*>(lo);
   }
 
-  // Sums of this thread: its row, every other kStep columns. Of A and B, what lies beyond X's rows is neither
+  // Sums of this thread: its row, every fourth kStep columns. Of A and B, what lies beyond X's rows is neither
   // computed nor looked at.
   const int row = warp % 4 * 32 + lane, half = warp / 4 * kStep, side = (int)up16(A.m);
   const bool in_rows = warp % 4 * 32 < side;  // (the same for a warp)
@@ -1290,13 +1292,24 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
     *lo = *reinterpret_cast<uint4*>(l);
   };
 
+  // the sum on the diagonal, of eight columns that have it; O and R have none
+  auto taken_out = [&](const float* sums, int column) {
+    const int on = row - column;
+    reinterpret_cast<uint16_t*>(place(sm.oh, column))[on] = 0;
+    if (kFine) reinterpret_cast<uint16_t*>(place(sm.ol, column))[on] = 0;
+    float mid = 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) mid = u == on ? sums[u] : mid;
+    return mid;
+  };
+
 #pragma unroll 1
   for (int step = 0; step < A.steps; ++step) {
     const float c1 = A.coef[3 * step], c3 = A.coef[3 * step + 1], c5 = A.coef[3 * step + 2];
     product([&] { issue(xh, xl, xh, xl, false, side, columns); });
     if (parts == 1) {
 #pragma unroll 1
-      for (int at = half; at < side && in_rows; at += 2 * kStep) {
+      for (int at = half; at < side && in_rows; at += kGroups * kStep) {
         float acc[kStep];
         tmem_load(acc_at + at, acc);
         tmem_loaded(acc);
@@ -1305,21 +1318,19 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
           const int column = at + p;
           float v[8];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            v[u] = acc[p + u] * (kO / (kX * kX));
-            if (column + u == row) sm.d[row] = acc[p + u] * (1.f / (kX * kX)), v[u] = 0.f;
-          }
+          for (int u = 0; u < 8; ++u) v[u] = acc[p + u] * (kO / (kX * kX));
           uint4 hi, lo;
           halves(v, &hi, &lo);
           *place(sm.oh, column) = hi;
           if (kFine) *place(sm.ol, column) = lo;
+          if ((uint32_t)(row - column) < 8) sm.d[row] = taken_out(acc + p, column) * (1.f / (kX * kX));
         }
       }
     } else {
       // this block's shares to the blocks that add them up, `wide` columns each
       const int wide = (side / 8 + (int)parts - 1) / (int)parts * 8;
 #pragma unroll 1
-      for (int at = half; at < side && in_rows; at += 2 * kStep) {
+      for (int at = half; at < side && in_rows; at += kGroups * kStep) {
         float acc[kStep];
         tmem_load(acc_at + at, acc);
         tmem_loaded(acc);
@@ -1339,7 +1350,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
       // (A is symmetric: its columns are rows. Pieces of eight columns of a row: all of a piece's shares, then its
       // halves to all blocks, neighbours along a row)
 #pragma unroll 1
-      for (int i = tid; i < side * wide / 8; i += 256) {
+      for (int i = tid; i < side * wide / 8; i += kSmallThreads) {
         const int c = i / (side / 8), column = i % (side / 8) * 8, r = (int)rank * wide + c;
         if (r >= side) break;
         float v[8];
@@ -1375,24 +1386,24 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
     product([&] { issue(oh, ol, oh, ol, false, side, side); });
     const float dr = sm.d[row], di = c3 + c5 * dr;
 #pragma unroll 1
-    for (int at = half; at < side && in_rows; at += 2 * kStep) {
+    for (int at = half; at < side && in_rows; at += kGroups * kStep) {
       float acc[kStep];
       tmem_load(acc_at + at, acc);
       tmem_loaded(acc);
 #pragma unroll
       for (int p = 0; p < kStep; p += 8) {
         const int column = at + p;
-        float v[8];
+        float v[8], dc[8];
         both(sm.oh, sm.ol, kFine, column, v);
+        Vec<float>::get(*reinterpret_cast<const uint4*>(sm.d + column), dc);
+        Vec<float>::get(*reinterpret_cast<const uint4*>(sm.d + column + 4), dc + 4);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          v[u] = __fmaf_rn(__fmaf_rn(c5, sm.d[column + u], di), v[u], acc[p + u] * (c5 / kO));
-          if (column + u == row) sm.e[row] = c3 * dr + c5 * __fmaf_rn(dr, dr, acc[p + u] * (1.f / (kO * kO))), v[u] = 0.f;
-        }
+        for (int u = 0; u < 8; ++u) v[u] = __fmaf_rn(__fmaf_rn(c5, dc[u], di), v[u], acc[p + u] * (c5 / kO));
         uint4 hi, lo;
         halves(v, &hi, &lo);
         *place(sm.oh, column) = hi;
         if (kFine) *place(sm.ol, column) = lo;
+        if ((uint32_t)(row - column) < 8) sm.e[row] = c3 * dr + c5 * __fmaf_rn(dr, dr, taken_out(acc + p, column) * (1.f / (kO * kO)));
       }
     }
     product([&] { issue(oh, ol, xh, xl, true, columns, side); });
@@ -1400,7 +1411,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
     const bool last = step + 1 == A.steps;
     const float by_out = *(volatile uint32_t*)&sm.dead ? __uint_as_float(kNan) : A.scale * (1.f / kX);
 #pragma unroll 1
-    for (int at = half; at < columns && in_rows; at += 2 * kStep) {
+    for (int at = half; at < columns && in_rows; at += kGroups * kStep) {
       float acc[kStep];
       tmem_load(acc_at + at, acc);
       tmem_loaded(acc);
@@ -1438,7 +1449,7 @@ __global__ void __launch_bounds__(256, 1) k_small(const T* g, int64_t sk, int64_
     out += k * osk;
     const bool rows16 = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(old * sizeof(T))) & 15) == 0;
 #pragma unroll 1
-    for (int r = tid / 16; r < A.m; r += 16) {
+    for (int r = tid / 16; r < A.m; r += kSmallThreads / 16) {
       const int piece = tid % 16;
       const int64_t j = j0 + piece * 8;
       const uint32_t in = (uint32_t)(piece / 8) * kBlockBytes + piece_at((uint32_t)r, (uint32_t)(piece % 8));
@@ -1476,7 +1487,7 @@ cudaError_t launch_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk
     if (device < 64) known[turned].fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
   }
   if (A.parts > 1 && refuse_cooperative()) return cudaErrorCooperativeLaunchTooLarge;
-  LaunchConfig l(K * A.parts, 256, A.parts, smem, s);
+  LaunchConfig l(K * A.parts, kSmallThreads, A.parts, smem, s);
   return cudaLaunchKernelEx(&l.cfg, f, g, sk, ld, out, osk, old, A);
 }
 
