@@ -454,6 +454,7 @@ struct alignas(8) ProductBars {
   uint64_t full[5], empty[5];
   uint64_t sums[2], taken[2];  // accumulators: written, read back
   uint64_t held[8][2];
+  uint64_t phase;              // the phases before the next one are done
   uint32_t tmem, dead;
 };
 template <int CG, typename T>
@@ -550,6 +551,7 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
       mbar_init(&bars.taken[i], Pl::kWarps * CG);
     }
     for (int w = 0; w < Pl::kWarps; ++w) mbar_init(&bars.held[w][0], 1), mbar_init(&bars.held[w][1], 1);
+    mbar_init(&bars.phase, 1);
     bars.dead = 0;
     fence_mbar_init();
   }
@@ -565,10 +567,17 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
   const Patience patience{&bars.dead, P.wait_ns};
   griddep_wait();
 
-  // Until every block is done with the phases before this one.
-  auto wait_phase = [&](int index) {
+  // Until every block is done with the phases before this one. The thread that issues the copies looks at the count
+  // and tells the others of its block.
+  auto wait_phase = [&](int index, bool first_of_block) {
     if (index == P.begin) return true;
-    const bool there = wait_count(P.phases, (uint32_t)(index - P.begin) * gridDim.x, patience);
+    bool there;
+    if (first_of_block) {
+      there = wait_count(P.phases, (uint32_t)(index - P.begin) * gridDim.x, patience);
+      if (there) mbar_arrive(&bars.phase);
+    } else {
+      there = wait_for(&bars.phase, (index - P.begin - 1) & 1, patience);
+    }
     fence_proxy_async_all();
     return there;
   };
@@ -589,7 +598,7 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
         constexpr int kPhase = decltype(phase)::value;
         const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, kPhase != kUpdate && P.triangle[kPhase % kUpdate]);
         const Parts parts(P, tiles, kPhase);
-        going = going && wait_phase(index);
+        going = going && wait_phase(index, true);
         const Halves2 left = kPhase == kGram ? x : kPhase == kSquare ? P.o : P.r;
         const Halves2 right = kPhase == kSquare ? P.o : x;
         // rows of 64 halves from the workspace's beginning
@@ -695,7 +704,7 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
       const Tiles tiles(S, P.K, 128 * CG, kPhase != kUpdate, kPhase != kUpdate && P.triangle[kPhase % kUpdate]);
       const Parts parts(P, tiles, kPhase);
       const float c1 = P.coef[index / 3 * 3], c3 = P.coef[index / 3 * 3 + 1], c5 = P.coef[index / 3 * 3 + 2];
-      going = __all_sync(0xffffffffu, going && (lane != 0 || wait_phase(index)));
+      going = __all_sync(0xffffffffu, going && (lane != 0 || wait_phase(index, false)));
       constexpr bool kLow = kPhase == kUpdate || kFine;  // two halves are kept
       const Halves2 from = kPhase == kUpdate ? x : P.o;
       const Halves2 to = kPhase == kGram ? P.o : kPhase == kSquare ? P.r : P.x[(index / 3 + 1) & 1];
