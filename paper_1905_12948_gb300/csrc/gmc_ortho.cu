@@ -1505,12 +1505,12 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // How a call is carried out: tiles of one block or of a pair, triangles or whole squares of them, and the shares
 // that X's columns are taken in. By what the phases take, in cycles. Measured both ways, us (bf16, then float):
 //                          single tiles   pairs      whole squares  triangles   unshared  shared
-//    32 x    256 x  1,024   200   286    233   326    202   281     218   305
-//     1 x  1,024 x  1,024   156   262    215   341    156   256     184   275
-//     8 x    512 x  4,608   434   705    396   636    405   686     406   656    418   759  397   632
-//     8 x  1,000 x  4,096   934 1,751    716 1,596    734 1,835     735 1,621    735 1,796  715 1,596
-//     2 x  3,000 x  3,000 1,432 3,013    952 2,700  1,101 3,221     942 2,829    994 2,873  980 2,711
-//     7 x    136 x 13,517   427   554    444   579                                654 1,206  424   556
+//    32 x    256 x  1,024   183   265    228   319    184   262     196   290
+//     1 x  1,024 x  1,024   153   250    214   332    153   251     173   264    154   256  154   250
+//     8 x    512 x  4,608   416   695    394   634    404   679     406   655    415   744  395   634
+//     8 x  1,000 x  4,096   908 1,721    706 1,577    724 1,828     731 1,615    725 1,777  707 1,577
+//     2 x  3,000 x  3,000 1,436 3,005    938 2,685  1,090 3,202     951 2,757    971 2,887  971 2,693
+//     7 x    136 x 13,517   403   544    441   569                               655 1,198  405   543
 struct Course {
   Shape S;
   bool pairs;
