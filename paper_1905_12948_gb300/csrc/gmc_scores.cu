@@ -70,18 +70,6 @@ __device__ __forceinline__ void move(Moments* a, const Shift& to, const Base& b)
   a->s *= f;
 }
 template <typename T>
-__device__ __forceinline__ Moments merge(Moments a, Moments o, const Base& b) {
-  const float m = fmaxf(a.m, o.m);
-  const Shift h = shift_of(m, b);
-  move<T>(&a, h, b);
-  move<T>(&o, h, b);
-  Moments r;
-  r.m = m;
-  r.s = a.s + o.s;
-  r.t = a.t + o.t;
-  return r;
-}
-template <typename T>
 __device__ __forceinline__ uint32_t largest_word(const uint4& v) {
   return Vec<T>::top(Vec<T>::top(v.x, v.y), Vec<T>::top(v.z, v.w));
 }
@@ -269,6 +257,26 @@ __device__ __forceinline__ void cut(Held<G>* H, int top) {
   constexpr int N = Held<G>::N, per = N / G;  // keys of a thread
   Team<G>::sync();
   const int n = H->n < N ? H->n : N, tid = Team<G>::tid();
+  if (n <= G) {
+    // a key's place is counted by as many threads as there are for it, up to eight
+    int lanes = 1;
+    while (lanes < 8 && n * lanes * 2 <= G) lanes *= 2;
+    const int own = tid / lanes;
+    const uint64_t key = own < n ? H->key[own] : 0;
+    int place = 0;
+    if (own < n)
+#pragma unroll 4
+      for (int i = tid % lanes; i < n; i += lanes) place += H->key[i] > key;
+    for (int o = 1; o < lanes; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
+    Team<G>::sync();
+    if (own < n && place < top) {
+      H->key[place] = key;
+      if (place == top - 1) H->bound = key;
+    }
+    if (tid == 0) H->n = n < top ? n : top;
+    Team<G>::sync();
+    return;
+  }
   uint64_t mine[per];
   int rank[per];
 #pragma unroll
@@ -617,24 +625,21 @@ __global__ void __launch_bounds__(Team<G>::kThreads, G == 128 ? 10 : G == 32 && 
     cluster_arrive();
     cluster_wait();
     if (part != 0) return;
-    a = cs[0];
-    for (int i = 1; i < parts; ++i) a = merge<T>(a, cs[i], R.b);
+    a = warp_merge<T>((int)threadIdx.x % 32 < parts ? cs[threadIdx.x % 32] : Moments(), R.b);
     if (kTop) {
       // each key's place: its own in its list, and how many of the others' are above it
       for (int i = tid; i < parts * A.top; i += G) {
         const int list = i / A.top, own = i % A.top;
         const uint64_t key = ck[list][own];
-        int rank = own;
-        for (int l = 0; l < parts; ++l) {
-          if (l == list) continue;
-          int from = 0, to = A.top;  // so many are above
-          while (from < to) {
-            const int mid = (from + to) / 2;
-            if (ck[l][mid] > key) from = mid + 1;
-            else to = mid;
+        int above[kMaxParts] = {}, rank = 0;  // the lists are in order: so many of each, by halving, all at once
+        for (int bit = kMostTop; bit; bit >>= 1)
+#pragma unroll
+          for (int l = 0; l < kMaxParts; ++l) {
+            const int to = above[l] + bit;
+            if (l < parts && to <= A.top && ck[l][to - 1] > key) above[l] = to;
           }
-          rank += from;
-        }
+#pragma unroll
+        for (int l = 0; l < kMaxParts; ++l) rank += above[l];
         if (key && rank < A.top) H->key[rank] = key;
       }
       __syncthreads();
