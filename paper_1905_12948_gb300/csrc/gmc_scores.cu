@@ -257,8 +257,9 @@ __device__ __forceinline__ void cut(Held<G>* H, int top) {
   constexpr int N = Held<G>::N, per = N / G;  // keys of a thread
   Team<G>::sync();
   const int n = H->n < N ? H->n : N, tid = Team<G>::tid();
-  if (n <= G) {
-    // a key's place is counted by as many threads as there are for it, up to eight
+  if (G == 32 && n <= G) {
+    // a key's place is counted by as many lanes as there are for it (16,000 x 1,000 fp32, 20 best: 53 -> 50 us; in blocks it costs
+    // their sweeps registers, 8,192 x 131,072 bf16, 5 best: 363 -> 385)
     int lanes = 1;
     while (lanes < 8 && n * lanes * 2 <= G) lanes *= 2;
     const int own = tid / lanes;
