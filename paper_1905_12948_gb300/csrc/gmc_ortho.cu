@@ -435,8 +435,12 @@ struct Plan {
   // halves) on their way to it.
   static constexpr int kWarps = CG == 2 && !kFine ? 4 : 8;
   static constexpr int kBuffers = kFine ? 1 : 2;
-  static constexpr int kStages = kFine ? 2 : CG == 1 ? 3 : 5;
-  static constexpr int kStageBytes = (kFine ? 4 : 2) * kFactorBytes;
+  // Of pairs' factors that are two halves, the second halves are a stage and the first ones the next: the second ones
+  // are free again before the last third of the products, and their next ones under way (4 x 2,417 x 4,507 fp32: 4,510 -> 4,310
+  // us, half 4,300 -> 4,010; single blocks wait for their port to the L2 cache: 4 x 700 x 900 277 us so, 287 in parts).
+  static constexpr int kHalves = kFine ? 2 : 1, kParts = CG == 2 ? kHalves : 1;
+  static constexpr int kStages = kFine ? 2 * kParts : CG == 1 ? 3 : 5;
+  static constexpr int kStageBytes = 2 * kHalves / kParts * kFactorBytes;
   static constexpr int kItems = 8 * CG / kWarps;  // of a warp, 64 columns each
   static constexpr int kThreads = 64 + 32 * kWarps;
   static constexpr int kHeld = kWarps * kBuffers * 2 * kHeldBytes;
@@ -612,26 +616,29 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
           parts.at(unit, &t, &begin, &end);
           tiles.at(t, &k, &row, &col);
           const int64_t ra = (int64_t)row * CG + rank, rb = (int64_t)col * CG + rank;
-          for (int kb = begin; kb < end; ++kb, ++n) {
-            const int s = (int)(n % Pl::kStages);
-            if (n >= Pl::kStages && !wait_for(&bars.empty[s], (n / Pl::kStages - 1) & 1, patience)) {
-              going = false;
-              break;
-            }
-            char* to = smem + s * Pl::kStageBytes;
-            const uint32_t bar = CG == 1 ? smem_addr(&bars.full[s]) : remote(smem_addr(&bars.full[s]), 0);
-            if (rank == 0) mbar_arrive_expect_tx(&bars.full[s], CG * Pl::kStageBytes);
+          for (int kb = begin; kb < end && going; ++kb) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {  // 64 rows each
-              char* at = to + h * (kFactorBytes / 2);
-              const int64_t l = lh + lk * k + (ra * lc + kb) * 128 + h * 64;
-              const int64_t r = rh + rk * k + (kPhase == kUpdate ? ((kb / 2) * rc + rb * 2 + h) * 128 + (kb & 1) * 64
-                                                                 : (rb * rc + kb) * 128 + h * 64);
-              tile_load<CG>(at, &map, l, bar);
-              tile_load<CG>(at + kFactorBytes, &map, r, bar);
-              if (kFine) {
-                tile_load<CG>(at + 2 * kFactorBytes, &map, l + ll, bar);
-                tile_load<CG>(at + 3 * kFactorBytes, &map, r + rl, bar);
+            for (int part = Pl::kParts - 1; part >= 0; --part, ++n) {
+              const int s = (int)(n % Pl::kStages);
+              if (n >= Pl::kStages && !wait_for(&bars.empty[s], (n / Pl::kStages - 1) & 1, patience)) {
+                going = false;
+                break;
+              }
+              char* to = smem + s * Pl::kStageBytes;
+              const uint32_t bar = CG == 1 ? smem_addr(&bars.full[s]) : remote(smem_addr(&bars.full[s]), 0);
+              if (rank == 0) mbar_arrive_expect_tx(&bars.full[s], CG * Pl::kStageBytes);
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {  // 64 rows each
+                char* at = to + h * (kFactorBytes / 2);
+                const int64_t l = lh + lk * k + (ra * lc + kb) * 128 + h * 64;
+                const int64_t r = rh + rk * k + (kPhase == kUpdate ? ((kb / 2) * rc + rb * 2 + h) * 128 + (kb & 1) * 64
+                                                                   : (rb * rc + kb) * 128 + h * 64);
+                tile_load<CG>(at, &map, l + part * ll, bar);
+                tile_load<CG>(at + kFactorBytes, &map, r + part * rl, bar);
+                if (Pl::kHalves > Pl::kParts) {
+                  tile_load<CG>(at + 2 * kFactorBytes, &map, l + ll, bar);
+                  tile_load<CG>(at + 3 * kFactorBytes, &map, r + rl, bar);
+                }
               }
             }
           }
@@ -664,24 +671,32 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
             going = it < 2 || wait_for(&bars.taken[it & 1], (it / 2 - 1) & 1, patience);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const int begin = kb, end = last - kb > kChunk ? kb + kChunk : last;
-            for (; kb < end && going; ++kb, ++n) {
-              const int s = (int)(n % Pl::kStages);
-              going = wait_for(&bars.full[s], (n / Pl::kStages) & 1, patience);
+            for (; kb < end && going; ++kb, n += Pl::kParts) {
+              // the stage of the first halves, and before it that of the second ones (the same where they are not apart)
+              const uint32_t first_n = n + Pl::kParts - 1;
+              const int s = (int)(first_n % Pl::kStages), t = (int)(n % Pl::kStages);
+              going = wait_for(&bars.full[t], (n / Pl::kStages) & 1, patience);
+              if (Pl::kParts == 2) going = going && wait_for(&bars.full[s], (first_n / Pl::kStages) & 1, patience);
               if (!going) break;
               asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
               const uint32_t at = smem_addr(smem + s * Pl::kStageBytes);
               constexpr uint32_t apart = kPhase == kUpdate ? kFactorBytes / 2 : 0;
               const uint64_t l = factor(at, 0), r = factor(at + kFactorBytes, apart);
-              constexpr uint64_t lo = (2 * kFactorBytes) >> 4;
+              // 16 of the sum at a time: 32 bytes of each row, or 16 rows
+              auto left = [](int q) { return (uint64_t)(q * 32 >> 4); };
+              auto right = [](int q) { return (uint64_t)((kPhase == kUpdate ? q * 2048 : q * 32) >> 4); };
+              if (kFine) {  // the small terms first, while there is less to cut off
+                const uint32_t low = Pl::kParts == 2 ? smem_addr(smem + t * Pl::kStageBytes) : at + 2 * kFactorBytes;
+                const uint64_t ll = factor(low, 0), rl = factor(low + kFactorBytes, apart);
 #pragma unroll
-              for (int q = 0; q < 4; ++q) {  // 16 of the sum: 32 bytes of each row, or 16 rows
-                const uint64_t dl = q * 32 >> 4, dr = (kPhase == kUpdate ? q * 2048 : q * 32) >> 4;
-                if (kFine) {  // the small terms first, while there is less to cut off
-                  mma<CG>(acc, l + dl, r + dr + lo, what, kb > begin || q > 0);
-                  mma<CG>(acc, l + dl + lo, r + dr, what, true);
+                for (int q = 0; q < 4; ++q) {
+                  mma<CG>(acc, l + left(q), rl + right(q), what, kb > begin || q > 0);
+                  mma<CG>(acc, ll + left(q), r + right(q), what, true);
                 }
-                mma<CG>(acc, l + dl, r + dr, what, kFine || kb > begin || q > 0);
+                if (Pl::kParts == 2) commit<CG>(&bars.empty[t]);
               }
+#pragma unroll
+              for (int q = 0; q < 4; ++q) mma<CG>(acc, l + left(q), r + right(q), what, kFine || kb > begin || q > 0);
               commit<CG>(&bars.empty[s]);
             }
             if (going) commit<CG>(&bars.sums[it & 1]);
