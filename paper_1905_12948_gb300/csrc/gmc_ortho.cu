@@ -1520,12 +1520,12 @@ int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // How a call is carried out: tiles of one block or of a pair, triangles or whole squares of them, and the shares
 // that X's columns are taken in. By what the phases take, in cycles. Measured both ways, us (bf16, then float):
 //                          single tiles   pairs      whole squares  triangles   unshared  shared
-//    32 x    256 x  1,024   183   265    228   319    184   262     196   290
-//     1 x  1,024 x  1,024   153   250    214   332    153   251     173   264    154   256  154   250
-//     8 x    512 x  4,608   416   695    394   634    404   679     406   655    415   744  395   634
-//     8 x  1,000 x  4,096   908 1,721    706 1,577    724 1,828     731 1,615    725 1,777  707 1,577
-//     2 x  3,000 x  3,000 1,436 3,005    938 2,685  1,090 3,202     951 2,757    971 2,887  971 2,693
-//     7 x    136 x 13,517   403   544    441   569                               655 1,198  405   543
+//    32 x    256 x  1,024   182   262    229   319    182   260     196   289
+//     1 x  1,024 x  1,024   153   249    213   327    154   248     172   264    153   252  152   246
+//     8 x    512 x  4,608   417   690    397   625    404   664     411   644    416   734  397   622
+//     8 x  1,000 x  4,096   906 1,693    709 1,540    722 1,774     727 1,594    725 1,729  707 1,545
+//     2 x  3,000 x  3,000 1,413 2,985    951 2,563  1,086 3,058     940 2,685    963 2,768  975 2,575
+//     7 x    136 x 13,517   404   545    442   572                               655 1,187  405   541
 struct Course {
   Shape S;
   bool pairs;
