@@ -38,9 +38,15 @@ struct Team {
     if constexpr (G == 32) __syncwarp();
     else __syncthreads();
   }
+  // Also a barrier: what the team's threads wrote to shared memory before it is seen after it. (A warp's vote
+  // alone orders no memory.)
   __device__ static bool any(bool p) {
-    if constexpr (G == 32) return __any_sync(0xffffffffu, p);
-    else return __syncthreads_or(p);
+    if constexpr (G == 32) {
+      __syncwarp();
+      return __any_sync(0xffffffffu, p);
+    } else {
+      return __syncthreads_or(p);
+    }
   }
 };
 
