@@ -720,6 +720,7 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
       const Parts parts(P, tiles, kPhase);
       const float c1 = P.coef[index / 3 * 3], c3 = P.coef[index / 3 * 3 + 1], c5 = P.coef[index / 3 * 3 + 2];
       going = __all_sync(0xffffffffu, going && (lane != 0 || wait_phase(index, false)));
+      __syncwarp();  // (a vote orders no memory: the diagonals that all lanes read are those that lane 0 waited for)
       constexpr bool kLow = kPhase == kUpdate || kFine;  // two halves are kept
       const Halves2 from = kPhase == kUpdate ? x : P.o;
       const Halves2 to = kPhase == kGram ? P.o : kPhase == kSquare ? P.r : P.x[(index / 3 + 1) & 1];
@@ -1024,6 +1025,7 @@ __global__ void __launch_bounds__(Plan<CG, T>::kThreads, 1) k_products(const __g
             const int64_t t = parts.whole + (unit - parts.whole) / parts.splits;
             const uint32_t to = (uint32_t)parts.splits * (index / 3 + 1);
             going = __all_sync(0xffffffffu, lane != 0 || wait_count(shared(t), to, patience));
+            __syncwarp();  // (as above: the shares)
             auto sums = [&](int at, float (&acc)[kStep]) {
 #pragma unroll
               for (int u = 0; u < kStep; ++u) acc[u] = 0.f;
