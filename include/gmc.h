@@ -492,7 +492,8 @@ int gmc_token_scores(const void* logits_dev, int32_t dtype, int64_t n, int64_t v
  * given as there or others (those of the top alternatives, say), as long as the same rows
  * count. A token that is given twice gets both slopes. dlogp_dev: n x given floats,
  * dentropy_dev: n floats; NULL for zeros. A row whose slopes are all 0 is written as zeros and not
- * read; one with a target >= vocab is NaN. dlogits_dev may be logits_dev itself. */
+ * read; one with a target >= vocab is NaN, and so is one whose stats are NaN, also where its targets are the -1 that
+ * such a row has for alternatives (as long as it has a slope). dlogits_dev may be logits_dev itself. */
 int gmc_token_scores_backward(const void* logits_dev, int32_t dtype, int64_t n, int64_t vocab, int64_t ld, float scale,
                               const int64_t* targets_dev, int32_t given, const float* stats_dev, const float* dlogp_dev,
                               const float* dentropy_dev, void* dlogits_dev, int64_t dld, void* stream);

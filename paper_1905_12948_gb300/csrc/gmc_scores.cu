@@ -734,7 +734,14 @@ __global__ void __launch_bounds__(kLossThreads, G == 32 ? 4 : 5) k_scores_grad(R
     any |= gy != 0.f;
   }
   wrong = Te::any(wrong);
-  if (!Te::any(some)) h = 0.f;  // the row does not count
+  if (!Te::any(some)) {
+    if (st.y != st.y) {  // it counted, and its alternatives (-1: NaN has none) are the tokens: all of its slopes are looked at
+      bool slope = h != 0.f;
+      for (int j = tid; g && j < given; j += G) slope |= g[row * given + j] != 0.f;
+      wrong |= Te::any(slope);
+    }
+    h = 0.f;  // the row does not count
+  }
   any = Te::any(any) || h != 0.f;
   const bool skip = !wrong && (!any || st.y == INFINITY);
   float sum = 0.f;

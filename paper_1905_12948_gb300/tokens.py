@@ -113,7 +113,8 @@ def token_scores_backward(logits, targets, stats, dlogp=None, dentropy=None, *, 
                           stream=None):
     """Gradient of sum(dlogp * logp) + sum(dentropy * entropy) in the logits
     (gmc_token_scores_backward), of the logits' dtype; ``out`` may be the logits themselves. The
-    slopes of top alternatives are given as those of tokens: ``targets=scores.top_index``."""
+    slopes of top alternatives are given as those of tokens: ``targets=scores.top_index`` (a row that is
+    not finite, whose alternatives are -1, stays NaN)."""
     if stream is not None:
         with _on(stream, logits, "logits", targets, stats, dlogp, dentropy, out):
             return token_scores_backward(logits, targets, stats, dlogp, dentropy, scale=scale, out=out)

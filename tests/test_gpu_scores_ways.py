@@ -2,7 +2,7 @@
 rows against plain statements in 64 bits."""
 import pytest
 
-from test_gpu_scores import check_backward, given, make
+from test_gpu_scores import check_backward, check_forward, given, make
 
 pytestmark = pytest.mark.gpu
 
@@ -13,3 +13,35 @@ def test_gradient_by_warps_with_many_given_tokens(kind, n, V, k):
     """Every lane sums all of a row's slopes, and looks for its own token among all of them: what other lanes have put
     into shared memory. Tokens come twice in most of the rows, a fifth of which do not count."""
     check_backward(make(n, V, kind, seed=n), given(n, V, k, masked=0.2), kind)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n,V", [(6, 50), (6, 40_000), (700, 300)])
+def test_alternatives_of_a_row_that_is_not_a_number(kind, n, V):
+    """NaN and +inf make a row's alternatives -1: the gradient through them is NaN where the row has slopes, as with any
+    other tokens, and not that of a row that does not count."""
+    import torch
+    from paper_1905_12948_gb300 import token_scores, token_scores_backward
+    x = make(n, V, kind)
+    x[1, V // 2] = torch.nan
+    x[3, 7] = torch.inf
+    bad = torch.tensor([1, 3], device="cuda")
+    fine = torch.tensor([r for r in range(n) if r not in (1, 3)], device="cuda")
+    r = token_scores(x, top=4, return_stats=True)
+    assert (r.top_index[bad] == -1).all() and (r.top_index[fine] >= 0).all()
+    ones = torch.ones(n, 4, device="cuda")
+    h = torch.ones(n, device="cuda")
+    for slopes in ((ones, None), (None, h), (ones, h)):
+        d = token_scores_backward(x, r.top_index, r.stats, *slopes)
+        assert d[bad].isnan().all() and d[fine].isfinite().all()
+    ones[1], h[1] = 0, 0                         # without slopes it is not read
+    d = token_scores_backward(x, r.top_index, r.stats, ones, h)
+    assert (d[1] == 0).all() and d[3].isnan().all()
+    # rows that did not count are told apart: zeros, whatever their logits and slopes
+    y = given(n, V, 4)
+    y[1] = -1
+    r = token_scores(x, y, top=4, return_stats=True)
+    slope = torch.full((n, 4), torch.nan, device="cuda")
+    slope[2:] = 1
+    d = token_scores_backward(x, r.top_index, r.stats, slope, h)
+    assert (d[1] == 0).all() and d[3].isnan().all()
