@@ -126,10 +126,11 @@ struct Running {
     t = pair_of(a.t, 0.f);
     clamp = true;
     if constexpr (sizeof(T) == 2) {
-      // its exponent is -200, give or take a rounding to the type: at most 9 where the shift is below 2^12
+      // its exponent is -200, give or take a rounding to the type: at most 9 where the shift is below 2^12, but
+      // anything for a half that is not a normal number (scales from 2^21 on), which may be 0
       const float f = (h.hc - 200.f) / b.c;
-      clamp = h.far || fabsf(h.hc) > 4096.f || !(f > -60000.f);
       const T lowest = Vec<T>::round(f);
+      clamp = h.far || fabsf(h.hc) > 4096.f || !(f > -60000.f) || !(Vec<T>::one(lowest) * b.c - h.hc < -150.f);
       const uint32_t half = *reinterpret_cast<const uint16_t*>(&lowest);
       floor = clamp ? Vec<T>::kLow : half << 16 | half;
     }

@@ -45,3 +45,18 @@ def test_alternatives_of_a_row_that_is_not_a_number(kind, n, V):
     slope[2:] = 1
     d = token_scores_backward(x, r.top_index, r.stats, slope, h)
     assert (d[1] == 0).all() and d[3].isnan().all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("e", [-64, -40, 20, 30, 33, 34, 48, 64])
+@pytest.mark.parametrize("n,V", [(3, 50), (3, 9_000), (1_500, 600)])
+def test_any_scale(kind, e, n, V):
+    """Scales up to the largest, of rows whose largest logit is 0 (that of a normalised row), or far from it: a logit that lies far
+    below the largest adds nothing, however small a number of the type that is."""
+    import torch
+    x = make(n, V, kind, seed=V)
+    x -= x.amax(1, keepdim=True)
+    x[1] *= 2.0 ** -10          # (half: down to its subnormal numbers)
+    x[2] += 5
+    check_forward(x, None, 3, 2.0 ** e)
+    check_forward(x, given(n, V, 2), 0, 2.0 ** e)
