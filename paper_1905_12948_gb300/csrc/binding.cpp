@@ -156,15 +156,13 @@ void written(const Tensor& t) {
   if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 
-// `sizes` elements of a 1-D tensor from `at` on, as a tensor of its own (of another type: `at` counts that).
-Tensor part(const Tensor& whole, at::IntArrayRef sizes, int64_t at, caffe2::TypeMeta type) {
-  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), type);
+// `sizes` elements of a 1-D tensor from `at` on, as a tensor of its own.
+Tensor part(const Tensor& whole, at::IntArrayRef sizes, int64_t at) {
+  Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
   t.unsafeGetTensorImpl()->set_storage_offset(at);
   t.unsafeGetTensorImpl()->set_sizes_contiguous(sizes);
   return t;
 }
-
-Tensor part(const Tensor& whole, at::IntArrayRef sizes, int64_t at) { return part(whole, sizes, at, whole.dtype()); }
 
 void* stream_of(const Tensor& t) { return c10::cuda::getCurrentCUDAStream(t.device().index()).stream(); }
 
@@ -378,16 +376,15 @@ PyObject* token_scores(Args a, Py_ssize_t na) {
   const float scale = (float)number(a[3]);
   const bool with_stats = truth(a[4]);
   const c10::cuda::OptionalCUDAGuard guard(x.device());
-  // one allocation for all: 8-byte words, the numbers of 16 bytes a row first
-  const int64_t index_at = with_stats ? 2 * r.n : 0, floats_at = 2 * (index_at + r.n * top);
-  const int64_t best_at = floats_at, logp_at = best_at + r.n * top, entropy_at = logp_at + r.n * g.given;
-  const Tensor all = at::empty({(entropy_at + r.n + 1) / 2}, x.options().dtype(at::kLong));
-  const caffe2::TypeMeta f32 = caffe2::TypeMeta::Make<float>();
+  // one allocation for all floats, the numbers of 16 bytes a row first; the indices in one of their own: torch.save
+  // takes no storage that holds two types
+  const int64_t best_at = with_stats ? 4 * r.n : 0, logp_at = best_at + r.n * top, entropy_at = logp_at + r.n * g.given;
+  const Tensor all = at::empty({entropy_at + r.n}, x.options().dtype(at::kFloat));
   Tensor logp, best, index, stats;
-  const Tensor entropy = part(all, {r.n}, entropy_at, f32);
-  if (g.given) logp = part(all, g.shape, logp_at, f32);
-  if (top) best = part(all, {r.n, top}, best_at, f32), index = part(all, {r.n, top}, index_at);
-  if (with_stats) stats = part(all, {r.n, 4}, 0, f32);
+  const Tensor entropy = part(all, {r.n}, entropy_at);
+  if (g.given) logp = part(all, g.shape, logp_at);
+  if (top) best = part(all, {r.n, top}, best_at), index = at::empty({r.n, top}, x.options().dtype(at::kLong));
+  if (with_stats) stats = part(all, {r.n, 4}, 0);
   check(g_abi.token_scores(x.data_ptr(), k, r.n, r.v, r.ld, scale, g.y, g.given, (int32_t)top,
                            g.given ? logp.data_ptr<float>() : nullptr, entropy.data_ptr<float>(),
                            top ? best.data_ptr<float>() : nullptr, top ? index.data_ptr<int64_t>() : nullptr,

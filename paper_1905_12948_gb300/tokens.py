@@ -88,8 +88,8 @@ def token_logp_backward(logits, targets, stats, dlogp, *, scale: float = 1.0, ou
 
 
 class TokenScores(NamedTuple):
-    """None in the place of what was not asked for. All share one allocation: clone what is kept
-    beyond the others."""
+    """None in the place of what was not asked for. The float32 ones share one allocation: clone
+    what is kept beyond the others, or saved without them (torch.save writes all of an allocation)."""
     logp: object         # float32 of the targets' shape, 0 where a token is not scored
     entropy: object      # (n,) float32
     top_logp: object     # (n, top) float32, larger ones first

@@ -60,3 +60,19 @@ def test_any_scale(kind, e, n, V):
     x[2] += 5
     check_forward(x, None, 3, 2.0 ** e)
     check_forward(x, given(n, V, 2), 0, 2.0 ** e)
+
+
+def test_results_are_saved_and_read():
+    """A teacher's best tokens are kept in files: together, alone, and whole."""
+    import io
+
+    import torch
+    from paper_1905_12948_gb300 import token_scores
+    r = token_scores(make(5, 300, "bf16"), given(5, 300, 2), top=8, return_stats=True)
+    for some in (tuple(r), (r.top_logp, r.top_index), r.top_index, r.logp):
+        f = io.BytesIO()
+        torch.save(some, f)
+        f.seek(0)
+        back = torch.load(f)
+        pairs = [(some, back)] if torch.is_tensor(some) else zip(some, back)
+        assert all(torch.equal(a, b) and a.dtype == b.dtype for a, b in pairs)
