@@ -593,9 +593,10 @@ int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_
  * matrices, whose result is off by less than its own rounding, and the sum of two (22 bits) for float and half;
  * X itself is kept in 22 bits and the diagonals of A and B in 32.
  * The same call gives the same bits. Its blocks wait for one another, bounded (about two seconds without progress),
- * after which out is NaN; where a context has no room for all of them at once, a launch does one product.
+ * after which out is NaN (of the matrices that are worked on together); where a context has no room for all of them at once, a launch does one product.
  * workspace_dev: gmc_orthogonalize_workspace(dtype, K, m, n) bytes, 256-byte aligned, whose
- * contents do not matter; it belongs to the call until the stream has passed it. K <= 65535, m, n <= 2^20, K*m*n <= 2^36
+ * contents do not matter; it belongs to the call until the stream has passed it: a token size for sides of up to 128, at most
+ * 64 MB for a shorter side of up to 128 and a longer one of up to 1024, else at most 4 GB or that of one matrix. K <= 65535, m, n <= 2^20, K*m*n <= 2^36
  * (the workspace call answers -1 otherwise). Takes no handle, runs on the current device,
  * stream-ordered. GMC_EINVAL for a bad argument, GMC_ECUDA if a launch fails.
  */

@@ -1499,7 +1499,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
   if (warp == 0) tmem_free<1>(tmem, kSmallSide);
 }
 
-bool in_shared_memory(const Shape& S) { return S.m <= kSmallSide && S.n <= kSmallSide * kMostSmallParts; }
+bool in_shared_memory(int64_t m, int64_t n) {
+  return std::min(m, n) <= kSmallSide && std::max(m, n) <= kSmallSide * kMostSmallParts;
+}
 template <typename T>
 cudaError_t launch_small(const T* g, int64_t sk, int64_t ld, T* out, int64_t osk, int64_t old, bool turned, int64_t K,
                          const SmallArgs& A, int device, cudaStream_t s) {
@@ -1634,6 +1636,30 @@ int64_t work_of(bool fine, int64_t K, const Course& c, char* at, Work* w) {
   return bytes;
 }
 
+// The matrices of a call that are worked on together, and the workspace of so many. Its sides are padded to 128 or 256, so that
+// many thin matrices would take far more than their own size: K goes in slices of at most kSliceBytes (or one
+// matrix), some thousand matrices of 129 x 131 or milliseconds of work. Matrices that stay in shared memory want a workspace
+// where a context has no room for their clusters alone: slices of kSmallSliceBytes; those of one block none (its token size).
+constexpr int64_t kSliceBytes = int64_t(4) << 30, kSmallSliceBytes = int64_t(64) << 20, kNoWorkspace = 256;
+struct Slices {
+  int64_t each;
+  Course course;  // of `each` matrices
+  int64_t bytes;
+};
+Slices slices_of(bool fine, int64_t K, int64_t m, int64_t n) {
+  if (std::max(m, n) <= kSmallSide) return {K, Course{}, kNoWorkspace};
+  const int64_t most = in_shared_memory(m, n) ? kSmallSliceBytes : kSliceBytes;
+  for (int64_t parts = 1;; parts *= 2) {
+    Slices s;
+    s.each = (K + parts - 1) / parts;
+    s.course = course_of(s.each, m, n, fine);
+    s.bytes = work_of(fine, s.each, s.course, nullptr, nullptr);
+    const int64_t last = s.each ? K % s.each : 0;
+    if (last) s.bytes = std::max(s.bytes, work_of(fine, last, course_of(last, m, n, fine), nullptr, nullptr));
+    if (s.bytes <= most || s.each <= 1) return s;
+  }
+}
+
 // Test hook (gmc_test_withhold_phase): the next call's wait limit, 0 = off.
 std::atomic<uint64_t> g_hold_ns{0};
 
@@ -1649,21 +1675,57 @@ bool strides_ok(const void* p, int32_t dtype, int64_t K, int64_t m, int64_t n, i
   return K <= 1 || (sk >= (m - 1) * (m > 1 ? ld : 0) + n && sk <= (int64_t(1) << 40));
 }
 
+// K matrices by way of the workspace.
+template <typename T>
+cudaError_t orthogonalize_slice(const T* g, int64_t sk, int64_t ld, T* o, int64_t osk, int64_t old, int64_t K, int64_t m, int64_t n, int steps,
+                                const float* coefficients, float scale, const Course& course, void* workspace,
+                                const CUtensorMap& map, uint64_t wait_ns, bool hold, int device, int sms, cudaStream_t s) {
+  const Shape S = course.S;
+  const bool turned = m > n;
+  Work w;
+  work_of(kOfTwo<T>, K, course, static_cast<char*>(workspace), &w);
+  // parts of |G|^2: as many blocks as are resident at once, of eight rows or pieces each
+  const int64_t rows8 = (m * ((n + kSizePiece - 1) / kSizePiece) + 7) / 8;
+  const int parts = (int)std::min({rows8, (sms * 4 + K - 1) / K, (int64_t)kMostSizeParts});
+  const dim3 some((unsigned)std::min(S.x() / kBlock, (sms * 8 + K - 1) / K), (unsigned)K);
+  cudaError_t e = launch_pdl(k_size<T>, dim3((unsigned)parts, (unsigned)K), dim3(256), 0, s, g, sk, ld, m, n, w.part, w.counts,
+                             w.counters);
+  if (e != cudaSuccess) return e;
+  e = launch_pdl(turned ? k_first<T, true> : k_first<T, false>, some, dim3(256), 0, s, g, sk, ld, S, (const double*)w.part,
+                 parts, w.x);
+  if (e != cudaSuccess) return e;
+  ProductArgs P{S, K, static_cast<const __half*>(workspace), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps,
+                3 * steps - 1, o, osk, turned ? 1 : old, turned ? old : 1, scale,
+                {course.of[0].triangle, course.of[1].triangle}, course.whole, course.splits, w.shares, w.shared,
+                w.counts + 1, wait_ns, hold, w.counts, {}};
+  std::copy(coefficients, coefficients + 3 * steps, P.coef);
+  bool pairs = course.pairs;
+  if (pairs) e = all_steps<2, T>(map, P, device, sms, s);
+  if (pairs && too_large_here(e)) {  // a context without room for clusters
+    cudaGetLastError();
+    pairs = false;
+    P.splits = 1;
+  }
+  if (!pairs) e = all_steps<1, T>(map, P, device, sms, s);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(k_gave_up<T>, dim3((unsigned)std::min<int64_t>(4, (m * n + 255) / 256), (unsigned)K), dim3(256), 0, s, o, osk,
+                    old, m, n, (const uint32_t*)w.counts);
+}
+
 }  // namespace
 
 extern "C" {
 
 int64_t gmc_orthogonalize_workspace(int32_t dtype, int64_t K, int64_t m, int64_t n) {
   if (!sizes_ok(dtype, K, m, n)) return -1;
-  const bool fine = dtype != GMC_BF16;
-  const int64_t bytes = work_of(fine, K, course_of(K, m, n, fine), nullptr, nullptr);
+  const int64_t bytes = slices_of(dtype != GMC_BF16, K, m, n).bytes;
   return bytes <= kMostWork ? bytes : -1;
 }
 
 int gmc_test_orthogonalize_course(int32_t dtype, int64_t K, int64_t m, int64_t n) {
   if (!sizes_ok(dtype, K, m, n)) return -1;
-  const Course c = course_of(K, m, n, dtype != GMC_BF16);
-  if (in_shared_memory(c.S)) return 0;
+  if (in_shared_memory(m, n)) return 0;
+  const Course c = slices_of(dtype != GMC_BF16, K, m, n).course;
   return 1 | c.pairs << 1 | c.of[0].triangle << 2 | c.of[1].triangle << 3 | c.splits << 4 | (c.whole > 0) << 12;
 }
 
@@ -1684,61 +1746,37 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
   if (!strides_ok(x_dev, dtype, K, m, n, ldk, ld) || !strides_ok(out_dev, dtype, K, m, n, out_ldk, out_ld))
     return GMC_EINVAL;
   if (out_dev == x_dev && ((m > 1 && out_ld != ld) || (K > 1 && out_ldk != ldk))) return GMC_EINVAL;  // in place: the same rows
-  const bool of_two = dtype != GMC_BF16;
-  const Course course = course_of(K, m, n, of_two);
-  const Shape S = course.S;
-  Work w;
-  const int64_t need = work_of(of_two, K, course, static_cast<char*>(workspace_dev), &w);
-  if (!workspace_dev || reinterpret_cast<uintptr_t>(workspace_dev) % 256 || need > kMostWork || workspace_bytes < need)
+  const bool of_two = dtype != GMC_BF16, turned = m > n, small = in_shared_memory(m, n);
+  const Slices slices = slices_of(of_two, K, m, n);
+  if (!workspace_dev || reinterpret_cast<uintptr_t>(workspace_dev) % 256 || slices.bytes > kMostWork || workspace_bytes < slices.bytes)
     return GMC_EINVAL;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool turned = m > n;
-  bool pairs = course.pairs;
-  const uint64_t hold_ns = g_hold_ns.exchange(0, std::memory_order_relaxed);
+  const uint64_t hold_ns = g_hold_ns.exchange(0, std::memory_order_relaxed), wait_ns = hold_ns ? hold_ns : kWaitLimitNs;
   int device = 0, sms = 0;
   cudaError_t err = cudaGetDevice(&device);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (err != cudaSuccess) return GMC_ECUDA;
-  CUtensorMap map;
-  err = map_of(workspace_dev, need, &map);
-  if (err != cudaSuccess) return GMC_ECUDA;
-  // parts of |G|^2: as many blocks as are resident at once, of eight rows or pieces each
-  const int64_t rows8 = (m * ((n + kSizePiece - 1) / kSizePiece) + 7) / 8;
-  const int parts = (int)std::min({rows8, (sms * 4 + K - 1) / K, (int64_t)kMostSizeParts});
-  const dim3 some((unsigned)std::min(S.x() / kBlock, (sms * 8 + K - 1) / K), (unsigned)K);
   err = by_type(dtype, [&](auto t) {
     using T = decltype(t);
     const T* g = static_cast<const T*>(x_dev);
     T* o = static_cast<T*>(out_dev);
-    if (in_shared_memory(S)) {
-      SmallArgs A{S.m, S.n, steps, 1, scale, hold_ns ? hold_ns : kWaitLimitNs, hold_ns != 0, {}};
-      while (A.parts * kSmallSide < S.n) A.parts *= 2;
+    if (small) {
+      SmallArgs A{std::min(m, n), std::max(m, n), steps, 1, scale, wait_ns, hold_ns != 0, {}};
+      while (A.parts * kSmallSide < A.n) A.parts *= 2;
       std::copy(coefficients_host, coefficients_host + 3 * steps, A.coef);
       const cudaError_t e = launch_small<T>(g, ldk, ld, o, out_ldk, out_ld, turned, K, A, device, s);
-      if (!too_large_here(e)) return e;
+      if (A.parts == 1 || !too_large_here(e)) return e;
       cudaGetLastError();  // a context without room for clusters
     }
-    cudaError_t e = launch_pdl(k_size<T>, dim3((unsigned)parts, (unsigned)K), dim3(256), 0, s, g, ldk, ld, m, n, w.part, w.counts,
-                               w.counters);
-    if (e != cudaSuccess) return e;
-    e = launch_pdl(turned ? k_first<T, true> : k_first<T, false>, some, dim3(256), 0, s, g, ldk, ld, S, (const double*)w.part,
-                   parts, w.x);
-    if (e != cudaSuccess) return e;
-    ProductArgs P{S, K, static_cast<const __half*>(workspace_dev), {w.x, w.y}, w.o, w.r, w.d, w.e, 0, 3 * steps,
-                  3 * steps - 1, o, out_ldk, turned ? 1 : out_ld, turned ? out_ld : 1, scale,
-                  {course.of[0].triangle, course.of[1].triangle}, course.whole, course.splits, w.shares, w.shared,
-                  w.counts + 1, hold_ns ? hold_ns : kWaitLimitNs, hold_ns != 0, w.counts, {}};
-    std::copy(coefficients_host, coefficients_host + 3 * steps, P.coef);
-    if (pairs) e = all_steps<2, T>(map, P, device, sms, s);
-    if (pairs && too_large_here(e)) {  // a context without room for clusters
-      cudaGetLastError();
-      pairs = false;
-      P.splits = 1;
+    CUtensorMap map;
+    cudaError_t e = map_of(workspace_dev, slices.bytes, &map);
+    for (int64_t k = 0; k < K && e == cudaSuccess; k += slices.each) {
+      const int64_t some = std::min(slices.each, K - k);  // (the last slice may be smaller)
+      const Course course = some == slices.each ? slices.course : course_of(some, m, n, of_two);
+      e = orthogonalize_slice<T>(g + k * ldk, ldk, ld, o + k * out_ldk, out_ldk, out_ld, some, m, n, steps, coefficients_host, scale,
+                                 course, workspace_dev, map, wait_ns, hold_ns != 0, device, sms, s);
     }
-    if (!pairs) e = all_steps<1, T>(map, P, device, sms, s);
-    if (e != cudaSuccess) return e;
-    return launch_pdl(k_gave_up<T>, dim3((unsigned)std::min<int64_t>(4, (m * n + 255) / 256), (unsigned)K), dim3(256), 0, s, o, out_ldk,
-                      out_ld, m, n, (const uint32_t*)w.counts);
+    return e;
   });
   return err == cudaSuccess ? GMC_OK : GMC_ECUDA;
 }

@@ -19,3 +19,47 @@ def test_other_matrices_in_turn(kind, K, m, n):
     for _ in range(5):
         got = [orthogonalize(g) for g in some]
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def errors_of_all(g, out, kind):
+    """As test_gpu_orthogonalize_limits: errors of single small matrices are small by chance as well, so those of all are compared,
+    and each with the largest."""
+    import torch
+
+    import scores_ref as ref
+    want = ref.products(g)
+    off, size = (out.double() - want).flatten(1).norm(dim=1), want.flatten(1).norm(dim=1)
+    plain = (ref.in_float32(g) - want).flatten(1).norm(dim=1) + (ref.rounded(g, fine=kind != "bf16") - want).flatten(1).norm(dim=1)
+    last = torch.finfo(out.dtype).eps / 2 * size
+    assert off.norm() <= 2 * plain.norm() + last.norm()
+    assert (off <= 2 * (plain / size).max() * size + last).all()
+
+
+@pytest.mark.parametrize("kind,K,m,n", [("bf16", 9_001, 129, 131), ("f32", 5_003, 131, 129)])
+def test_matrices_in_slices(kind, K, m, n):
+    """More than one workspace holds: slices, the last of them smaller; in place."""
+    import torch
+    from paper_1905_12948_gb300 import load, orthogonalize
+    code = {"f32": 0, "bf16": 1}[kind]
+    need = load().gmc_orthogonalize_workspace
+    assert need(code, K, m, n) < 0.75 * K / 1000 * need(code, 1000, m, n)
+    g = make(K, m, n, kind)
+    out = orthogonalize(g.clone())
+    same = g.clone()
+    assert torch.equal(orthogonalize(same, out=same), out)
+    for at in range(0, K, 1_000):
+        errors_of_all(g[at: at + 1_000], out[at: at + 1_000], kind)
+
+
+@pytest.mark.parametrize("refused", [1, 2, 7])
+@pytest.mark.parametrize("kind,K,m,n", [("f32", 300, 100, 700), ("bf16", 1_001, 130, 40)])
+def test_small_matrices_in_a_context_without_room_for_clusters(kind, K, m, n, refused):
+    """Slices of some tens, by way of the workspace."""
+    from paper_1905_12948_gb300 import load, orthogonalize
+    g = make(K, m, n, kind)
+    load().gmc_test_refuse_cooperative(refused)
+    try:
+        out = orthogonalize(g)
+    finally:
+        load().gmc_test_refuse_cooperative(0)
+    errors_of_all(g, out, kind)
