@@ -589,15 +589,16 @@ int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_
  * strides); other overlaps are the caller's mistake. coefficients_host: 3*steps floats, a, b, c of each step;
  * 1 <= steps <= 16. A matrix of zeros gives zeros; one that holds inf or NaN gives NaN. The
  * singular values have to stay below 4 on the way, else a matrix may become NaN.
- * |G| is summed in 64 bits, products in 32. Their factors are halves: one for bfloat16
+ * |G| is summed in 64 bits, of sums of up to 32 squares in 32 bits; products are summed in 32. Their factors are halves: one for bfloat16
  * matrices, whose result is off by less than its own rounding, and the sum of two (22 bits) for float and half;
  * X itself is kept in 22 bits and the diagonals of A and B in 32.
  * The same call gives the same bits. Its blocks wait for one another, bounded (about two seconds without progress),
  * after which out is NaN (of the matrices that are worked on together); where a context has no room for all of them at once, a launch does one product.
  * workspace_dev: gmc_orthogonalize_workspace(dtype, K, m, n) bytes, 256-byte aligned, whose
  * contents do not matter; it belongs to the call until the stream has passed it: a token size for sides of up to 128, at most
- * 64 MB for a shorter side of up to 128 and a longer one of up to 1024, else at most 4 GB or that of one matrix. K <= 65535, m, n <= 2^20, K*m*n <= 2^36
- * (the workspace call answers -1 otherwise). Takes no handle, runs on the current device,
+ * 64 MB for a shorter side of up to 128 and a longer one of up to 1024, else at most 4 GB or that of one matrix. K <= 65535, m, n <= 2^20, K*m*n <= 2^36,
+ * and one matrix's workspace at most 2^38 bytes (the workspace call answers -1 otherwise): 8 bytes an element of m x n, and 4
+ * (bfloat16) or 8 an element of the shorter side's square, sides padded to 128 or 256. Takes no handle, runs on the current device,
  * stream-ordered. GMC_EINVAL for a bad argument, GMC_ECUDA if a launch fails.
  */
 int64_t gmc_orthogonalize_workspace(int32_t dtype, int64_t K, int64_t m, int64_t n);
