@@ -616,6 +616,10 @@ int gmc_test_orthogonalize_course(int32_t dtype, int64_t K, int64_t m, int64_t n
  * seconds. The waits give up, and out is NaN (of a matrix in shared memory: the first one of the call). GMC_EINVAL for a limit out of range. */
 int gmc_test_withhold_phase(uint64_t wait_limit_ns);
 
+/* gmc_test_withhold_product -- the same for matrices in shared memory, of product `product` (three a step, from 0) of
+ * block `block` (a block has 128 columns of a matrix, or rows of a tall one). The matrix that it works on is NaN, all of it. */
+int gmc_test_withhold_product(uint64_t wait_limit_ns, int32_t block, int32_t product);
+
 /* gmc_strerror -- a static message for a status code. */
 const char* gmc_strerror(int status);
 

@@ -1154,7 +1154,7 @@ struct SmallArgs {
   int steps, parts;
   float scale;
   uint64_t wait_ns;  // bound of every wait
-  bool hold;         // test hook: the first block does not issue its first product
+  int hold_block, hold_product;  // test hook: the product that this block does not issue; -1: none
   float coef[3 * kMostSteps];
 };
 template <bool kFine>
@@ -1166,9 +1166,12 @@ struct alignas(1024) SmallSmem {
   float d[kSmallSide], e[kSmallSide];   // diagonals of A and B
   double squares[kMostSmallParts], ws[kSmallThreads / 32];
   Scaled by;
-  uint64_t done;                        // products
+  uint64_t done, ended;                 // products; all of them, where a wait gave up
   uint32_t tmem, dead;
 };
+__device__ __forceinline__ void store_at(uint32_t addr, uint32_t rank, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote(addr, rank)), "r"(v) : "memory");
+}
 __device__ __forceinline__ void store_at(uint32_t addr, uint32_t rank, const uint4& v) {
   asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(remote(addr, rank)), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
                : "memory");
@@ -1194,6 +1197,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
   if (parts > 1) cluster_arrive();  // (it has begun)
   if (tid == 0) {
     mbar_init(&sm.done, 1);
+    mbar_init(&sm.ended, 1);
     sm.dead = 0;
     fence_mbar_init();
   }
@@ -1270,17 +1274,18 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
   const int columns = A.n - j0 > kSmallSide ? kSmallSide : A.n > j0 ? (int)up16(A.n - j0) : 16;  // of X that are not padding
   const uint32_t acc_at = tmem + ((uint32_t)(warp % 4) << 21);
   uint32_t products = 0;
+  bool waited = true;  // no wait gave up
   // All threads: what they wrote is there for the products, which `issue` issues; they are done.
   auto product = [&](auto&& issue) {
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     fence_proxy_async();
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if (tid == 0 && !(A.hold && products == 0 && blockIdx.x == 0)) {
+    if (tid == 0 && !((int)products == A.hold_product && (int)blockIdx.x == A.hold_block)) {
       issue();
       commit<1>(&sm.done);
     }
-    wait_for(&sm.done, products & 1, Patience{&sm.dead, A.wait_ns});
+    waited = wait_for(&sm.done, products & 1, Patience{&sm.dead, A.wait_ns}) && waited;
     ++products;
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   };
@@ -1317,6 +1322,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
     *hi = *reinterpret_cast<uint4*>(h);
     *lo = *reinterpret_cast<uint4*>(l);
   };
+
+  // After the last product, and in a cluster's blocks an arrival: whether a wait gave up is known in all of them.
+  auto all_told = [&] {
+    if (parts > 1) cluster_wait();
+    __syncthreads();
+  };
+  auto gave_up = [&] { return *(volatile uint32_t*)&sm.dead != 0; };
 
   // the sum on the diagonal, of eight columns that have it; O and R have none
   auto taken_out = [&](const float* sums, int column) {
@@ -1360,7 +1372,6 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
         float acc[kStep];
         tmem_load(acc_at + at, acc);
         tmem_loaded(acc);
-        if (*(volatile uint32_t*)&sm.dead) acc[0] = __uint_as_float(kNan);  // (which all of X gets)
 #pragma unroll
         for (int p = 0; p < kStep; p += 8) {
           const int column = at + p;
@@ -1435,7 +1446,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
     product([&] { issue(oh, ol, xh, xl, true, columns, side); });
     const float ei = c1 + sm.e[row];
     const bool last = step + 1 == A.steps;
-    const float by_out = *(volatile uint32_t*)&sm.dead ? __uint_as_float(kNan) : A.scale * (1.f / kX);
+    if (last) {  // a wait that gave up is one of the whole matrix
+      if (parts > 1) {
+        for (uint32_t p = 0; p < parts && !waited; ++p) store_at(smem_addr(&sm.dead), p, 1u);
+        cluster_arrive();
+      }
+      if (kTurned) all_told();
+    }
+    const float by_out = kTurned && last && gave_up() ? __uint_as_float(kNan) : A.scale * (1.f / kX);
 #pragma unroll 1
     for (int at = half; at < columns && in_rows; at += kGroups * kStep) {
       float acc[kStep];
@@ -1471,7 +1489,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
   }
   if (!kTurned) {
     // the result's rows from where they lie, sixteen lanes a row
-    __syncthreads();
+    all_told();
+    const bool nothing = gave_up();
     out += k * osk;
     const bool rows16 = ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)(old * sizeof(T))) & 15) == 0;
 #pragma unroll 1
@@ -1482,6 +1501,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
       alignas(16) T e8[8];
       memcpy(e8, __builtin_assume_aligned(reinterpret_cast<const char*>(sm.xh) + in, 16), 16);
       if (sizeof(T) == 4) memcpy(reinterpret_cast<char*>(e8) + sizeof(e8) - 16, __builtin_assume_aligned(reinterpret_cast<const char*>(sm.xl) + in, 16), 16);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (nothing) e8[u] = Vec<T>::round(__uint_as_float(kNan));
       T* o = out + r * old + j;
       if (rows16 && j + 8 <= A.n) {
 #pragma unroll
@@ -1492,6 +1514,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_small(const T* g, int64_t 
           if (j + u < A.n) o[u] = e8[u];
       }
     }
+  }
+  if (tid == 0 && gave_up()) {  // products that are late end before their memory is given back
+    commit<1>(&sm.ended);
+    wait_bounded(&sm.ended, 0, kWaitLimitNs);
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -1660,8 +1686,9 @@ Slices slices_of(bool fine, int64_t K, int64_t m, int64_t n) {
   }
 }
 
-// Test hook (gmc_test_withhold_phase): the next call's wait limit, 0 = off.
+// Test hooks (gmc_test_withhold_phase, gmc_test_withhold_product): the next call's wait limit, 0 = off, and what is withheld.
 std::atomic<uint64_t> g_hold_ns{0};
+std::atomic<int> g_hold_block{0}, g_hold_product{0};
 
 bool sizes_ok(int32_t dtype, int64_t K, int64_t m, int64_t n) {
   if (dtype != GMC_F32 && dtype != GMC_BF16 && dtype != GMC_F16) return false;
@@ -1730,7 +1757,13 @@ int gmc_test_orthogonalize_course(int32_t dtype, int64_t K, int64_t m, int64_t n
 }
 
 int gmc_test_withhold_phase(uint64_t wait_limit_ns) {
-  if (wait_limit_ns > 2000000000ull) return GMC_EINVAL;
+  return gmc_test_withhold_product(wait_limit_ns, 0, 0);
+}
+
+int gmc_test_withhold_product(uint64_t wait_limit_ns, int32_t block, int32_t product) {
+  if (wait_limit_ns > 2000000000ull || block < 0 || product < 0) return GMC_EINVAL;
+  g_hold_block.store(block, std::memory_order_relaxed);
+  g_hold_product.store(product, std::memory_order_relaxed);
   g_hold_ns.store(wait_limit_ns, std::memory_order_relaxed);
   return GMC_OK;
 }
@@ -1761,7 +1794,8 @@ int gmc_orthogonalize(const void* x_dev, int64_t ldk, int64_t ld, void* out_dev,
     const T* g = static_cast<const T*>(x_dev);
     T* o = static_cast<T*>(out_dev);
     if (small) {
-      SmallArgs A{std::min(m, n), std::max(m, n), steps, 1, scale, wait_ns, hold_ns != 0, {}};
+      SmallArgs A{std::min(m, n), std::max(m, n), steps, 1, scale, wait_ns, hold_ns ? g_hold_block.load() : -1,
+                  hold_ns ? g_hold_product.load() : -1, {}};
       while (A.parts * kSmallSide < A.n) A.parts *= 2;
       std::copy(coefficients_host, coefficients_host + 3 * steps, A.coef);
       const cudaError_t e = launch_small<T>(g, ldk, ld, o, out_ldk, out_ld, turned, K, A, device, s);

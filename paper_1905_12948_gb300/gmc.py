@@ -88,6 +88,7 @@ _SIGNATURES = {
                                          _f32, _c_p, _i64, _c_p]),
     "gmc_test_orthogonalize_course": (ctypes.c_int, [_i32, _i64, _i64, _i64]),
     "gmc_test_withhold_phase": (ctypes.c_int, [_u64]),
+    "gmc_test_withhold_product": (ctypes.c_int, [_u64, _i32, _i32]),
     "gmc_test_fail_alloc": (_i64, [_i64]),
     "gmc_test_withhold_copy": (ctypes.c_int, [_c_p, _i64, _i32, _u64]),
     "gmc_test_pass": (ctypes.c_int, [_c_p]),

@@ -63,3 +63,37 @@ def test_small_matrices_in_a_context_without_room_for_clusters(kind, K, m, n, re
     finally:
         load().gmc_test_refuse_cooperative(0)
     errors_of_all(g, out, kind)
+
+
+@pytest.mark.parametrize("product", [0, 1, 2, 3, 7, 12, 13, 14])
+@pytest.mark.parametrize("block,matrix", [(0, 0), (3, 0), (6, 1), (7, 1)])
+@pytest.mark.parametrize("kind,m,n", [("bf16", 100, 500), ("bf16", 500, 100), ("f32", 30, 400)])
+def test_a_wait_that_runs_out_in_a_cluster(kind, m, n, block, matrix, product):
+    """Four blocks a matrix: one of them gives up, and all of the matrix is NaN, whichever product of whichever step it
+    was; the other matrices are what they are."""
+    import torch
+    from paper_1905_12948_gb300 import load, orthogonalize
+    lib = load()
+    g = make(3, m, n, kind)
+    want = orthogonalize(g)
+    assert lib.gmc_test_withhold_product(5_000_000, block, product) == 0
+    out = orthogonalize(g)
+    torch.cuda.synchronize()
+    assert out[matrix].isnan().all()
+    others = [k for k in range(3) if k != matrix]
+    assert torch.equal(out[others], want[others])
+    assert torch.equal(orthogonalize(g), want)      # the next call is not affected
+
+
+def test_one_block_whose_last_product_is_withheld():
+    import torch
+    from paper_1905_12948_gb300 import load, orthogonalize
+    lib = load()
+    for m, n in ((100, 90), (90, 100)):
+        g = make(2, m, n, "f32")
+        want = orthogonalize(g)
+        assert lib.gmc_test_withhold_product(5_000_000, 1, 14) == 0
+        out = orthogonalize(g)
+        assert out[1].isnan().all() and torch.equal(out[0], want[0]) and torch.equal(orthogonalize(g), want)
+    for bad in ((2_000_000_001, 0, 0), (1, -1, 0), (1, 0, -1)):
+        assert lib.gmc_test_withhold_product(*bad) == 1
