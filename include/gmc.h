@@ -585,7 +585,8 @@ int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_
  * a worker's gradient of a weight matrix is orthogonalised so before gmc_step takes it.
  *
  * Matrix k's row i is n contiguous elements at x_dev + k*ldk + i*ld (out_dev likewise, by its
- * own strides; ldk is ignored where K = 1, ld where m = 1), of type `dtype`. out_dev may be x_dev (with the same
+ * own strides; ldk is ignored where K = 1, ld where m = 1), of type `dtype`: one matrix after
+ * the other, or a row of each in turn (else rows might overlap, which is refused). out_dev may be x_dev (with the same
  * strides); other overlaps are the caller's mistake. coefficients_host: 3*steps floats, a, b, c of each step;
  * 1 <= steps <= 16. A matrix of zeros gives zeros; one that holds inf or NaN gives NaN. The
  * singular values have to stay below 4 on the way, else a matrix may become NaN.

@@ -428,7 +428,9 @@ Matrices matrices(const Tensor& t, const char* name) {
   if (s.n > 1 && t.stride(d - 1) != 1) fail(PyExc_TypeError, name, "must have contiguous rows");
   if (s.m <= 1) s.ld = s.n;
   if (s.K <= 1) s.ldk = s.m * s.ld;
-  if (s.ld < s.n || s.ldk < (s.m - 1) * s.ld + s.n) fail(PyExc_TypeError, name, "must have rows that do not overlap");
+  const bool apart = s.ld >= s.n && s.ldk >= (s.m - 1) * s.ld + s.n;  // a matrix after the other
+  const bool in_turn = s.m > 1 && s.ldk >= s.n && s.ld >= (s.K - 1) * s.ldk + s.n;  // a row of each
+  if (!apart && !in_turn) fail(PyExc_TypeError, name, "must have rows that do not overlap");
   return s;
 }
 

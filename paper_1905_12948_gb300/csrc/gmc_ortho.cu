@@ -1699,7 +1699,10 @@ bool strides_ok(const void* p, int32_t dtype, int64_t K, int64_t m, int64_t n, i
   const uintptr_t size = dtype == GMC_F32 ? 4 : 2;
   if (!p || reinterpret_cast<uintptr_t>(p) % size) return false;
   if (m > 1 && (ld < n || ld > (int64_t(1) << 40))) return false;
-  return K <= 1 || (sk >= (m - 1) * (m > 1 ? ld : 0) + n && sk <= (int64_t(1) << 40));
+  if (K <= 1) return true;
+  if (sk < n || sk > (int64_t(1) << 40)) return false;
+  // a matrix after the other, or a row of each in turn
+  return m <= 1 || sk >= (m - 1) * ld + n || ld >= (K - 1) * sk + n;
 }
 
 // K matrices by way of the workspace.

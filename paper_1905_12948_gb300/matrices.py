@@ -19,7 +19,8 @@ def orthogonalize(x, *, steps: int = 5, coefficients=QUINTIC, scale: float = 1.0
     """``scale`` * the orthogonalised matrices of x, by ``steps`` Newton-Schulz products
     X <- a X + (b A + c A^2) X, A = X X', from X = x / |x| (gmc_orthogonalize). x: (K, m, n), a
     matrix of each worker, or (m, n), of float32, bfloat16 or float16; a matrix's rows are
-    contiguous, the workers' and the rows' strides are free: the part of a K x d gradient that is a
+    contiguous, the workers' and the rows' strides are free, one matrix after the other or a row of each in
+    turn: the part of a K x d gradient that is a
     matrix, ``grads[:, at: at + m * n].view(K, m, n)``, is taken as it lies.
     ``coefficients``: (a, b, c), or one such triple for each step. ``out`` may be x."""
     if stream is not None:

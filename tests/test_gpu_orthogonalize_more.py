@@ -97,3 +97,43 @@ def test_one_block_whose_last_product_is_withheld():
         assert out[1].isnan().all() and torch.equal(out[0], want[0]) and torch.equal(orthogonalize(g), want)
     for bad in ((2_000_000_001, 0, 0), (1, -1, 0), (1, 0, -1)):
         assert lib.gmc_test_withhold_product(*bad) == 1
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("K,m,n", [(3, 40, 50), (2, 500, 100), (3, 300, 260), (4, 1, 77), (2, 130, 1_100)])
+def test_workers_rows_in_turn(kind, K, m, n):
+    """The workers' rows lie between one another's (m, K, n), apart or not; into such a tensor, and in place. (Where a row begins
+    at another offset from a 16-byte boundary, other 16 or 32 squares are added up in 32 bits before the 64 of the norm: a sum
+    may be rounded otherwise, the results are held to the formula's bound.)"""
+    import torch
+    from paper_1905_12948_gb300 import orthogonalize
+    g = make(K, m, n, kind)
+    want = orthogonalize(g)
+    for pad in (0, 3, 8):
+        buf = torch.full((m, K, n + pad), 7.0, dtype=g.dtype, device="cuda")
+        x = buf[:, :, :n].transpose(0, 1)
+        x.copy_(g)
+        assert x.stride(0) == n + pad
+        got = orthogonalize(x)
+        check(g, got, kind)
+        out = torch.full((m, K, n + pad), 7.0, dtype=g.dtype, device="cuda")
+        view = out[:, :, :n].transpose(0, 1)
+        assert orthogonalize(g, out=view).data_ptr() == view.data_ptr() and torch.equal(view, want)
+        assert torch.equal(orthogonalize(x, out=x), got) and (buf[:, :, n:] == 7).all() and (out[:, :, n:] == 7).all()
+    check(g, want, kind)
+
+
+def test_rows_that_overlap_are_refused():
+    import torch
+    from paper_1905_12948_gb300 import orthogonalize
+    buf = torch.randn(10_000, device="cuda")
+    before = buf.clone()
+    for shape, strides in (((3, 4, 10), (9, 30, 1)), ((3, 4, 10), (10, 29, 1)), ((3, 4, 10), (39, 10, 1)), ((3, 4, 10), (40, 9, 1)),
+                           ((3, 4, 10), (0, 10, 1)), ((3, 4, 10), (20, 20, 1)), ((3, 1, 10), (9, 10, 1)), ((3, 4, 10), (10, 0, 1))):
+        x = buf.as_strided(shape, strides)
+        with pytest.raises(TypeError, match="rows that do not overlap"):
+            orthogonalize(x)
+        with pytest.raises(TypeError, match="rows that do not overlap"):
+            orthogonalize(torch.randn(shape, device="cuda"), out=x)
+    torch.cuda.synchronize()
+    assert torch.equal(buf, before)
