@@ -589,7 +589,7 @@ int gmc_dropout(const void* x_dev, int64_t ldx, const void* residual_dev, int64_
  * the other, or a row of each in turn (else rows might overlap, which is refused). out_dev may be x_dev (with the same
  * strides); other overlaps are the caller's mistake. coefficients_host: 3*steps floats, a, b, c of each step;
  * 1 <= steps <= 16. A matrix of zeros gives zeros; one that holds inf or NaN gives NaN. The
- * singular values have to stay below 4 on the way, else a matrix may become NaN.
+ * singular values of X have to stay below 4 on the way, and those of b A + c A^2 below 32, else a matrix may become NaN.
  * |G| is summed in 64 bits, of sums of up to 32 squares in 32 bits; products are summed in 32. Their factors are halves: one for bfloat16
  * matrices, whose result is off by less than its own rounding, and the sum of two (22 bits) for float and half;
  * X itself is kept in 22 bits and the diagonals of A and B in 32.

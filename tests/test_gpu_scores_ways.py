@@ -165,3 +165,15 @@ def test_results_are_saved_and_read():
         back = torch.load(f)
         pairs = [(some, back)] if torch.is_tensor(some) else zip(some, back)
         assert all(torch.equal(a, b) and a.dtype == b.dtype for a, b in pairs)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("e", [-64, -40, 20, 34, 64])
+@pytest.mark.parametrize("n,V", [(4, 50), (4, 9_000), (700, 300)])
+def test_gradient_at_any_scale(kind, e, n, V):
+    """Slopes small enough for a large scale's gradient to fit the type."""
+    x = make(n, V, kind, seed=V)
+    x -= x.amax(1, keepdim=True)
+    x[1] *= 2.0 ** -10
+    x[2] += 5
+    check_backward(x, given(n, V, 3), kind, 2.0 ** e, unit=2.0 ** -max(e, 0))
