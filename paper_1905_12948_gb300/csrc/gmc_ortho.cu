@@ -14,7 +14,7 @@
 //     its own rounding by 1.7e-3), or the terms hi hi + hi lo + lo hi (float: 0.6 to 1.5e-6, where 32-bit arithmetic
 //     is off by 2.3 to 5e-6).
 // X is kept 2^14 times, O and R 2^11 times what they are: the second halves then stay normal
-// numbers, and a singular value may come to 4.
+// numbers, and a singular value of X may come to 4, one of A or B (less their diagonals) to 32.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -523,7 +523,7 @@ struct Parts {
 // is 256 x 256, 128 x 256 of it in each block's tensor memory; CG = 1: 128 x 128.
 // Warp 0 issues the copies, warp 1 the products; the others read the sums back (the tensor memory
 // holds two tiles) and put the new halves where the next product takes them from, or the result into its place.
-// What bounds it: with deep sums the tensor cores under the power limit (2 x 4,096 x 25,088 bf16: 1.46 PFLOP/s; cuBLAS
+// What bounds it: with deep sums the tensor cores under the power limit (2 x 4,096 x 25,088 bf16: 1.36 to 1.48 PFLOP/s, by card; cuBLAS
 // 1.89 in a burst, 1.72 sustained); with short ones a block's port to the L2 cache, 53 to 60 bytes a cycle for the
 // factors and X, which is read and written whole (8 x 1,000 x 4,096: 16,500 cycles for a tile of 256 x 256, of which
 // the products take 8,200); with few tiles the barriers and the first copies after them (8 x 256 x 256: 6.5 us a
@@ -1146,8 +1146,8 @@ cudaError_t map_of(void* base, int64_t bytes, CUtensorMap* map) {
 // for everything. The blocks of a cluster have 128 columns each; of A = X X' each adds up the shares of all
 // for its own columns, and gives them to all. A^2 and B are each block's own. What bounds it is the chain of
 // products (0.3 us each, 1.1 of fp32) and of what is made of their sums by 16 warps (by 8: 128 x 128 bf16 26 us, so
-// 24); with clusters also the exchange of A, 64 KB into each block and 32 out of it (2 us). 16 x 16 bf16 12.5 us, by way of
-// the workspace 31; 128 x 128 fp32 41; 4 x 1,000 x 64 fp32 43, so 108; 8 x 128 x 1,024 bf16 49.
+// 24); with clusters also the exchange of A, 64 KB into each block and 32 out of it (2 us). 16 x 16 bf16 12.8 us, by way of
+// the workspace 31; 128 x 128 fp32 41; 4 x 1,000 x 64 fp32 43, so 108; 8 x 128 x 1,024 bf16 48.
 constexpr int kSmallSide = 128, kMostSmallParts = 8, kSmallThreads = 512;
 struct SmallArgs {
   int64_t m, n;  // of X
