@@ -1664,7 +1664,7 @@ int64_t work_of(bool fine, int64_t K, const Course& c, char* at, Work* w) {
 
 // The matrices of a call that are worked on together, and the workspace of so many. Its sides are padded to 128 or 256, so that
 // many thin matrices would take far more than their own size: K goes in slices of at most kSliceBytes (or one
-// matrix), some thousand matrices of 129 x 131 or milliseconds of work. Matrices that stay in shared memory want a workspace
+// matrix): 5,000 of 129 x 131 bf16 6.0 ms, 65,535 in slices 79. Matrices that stay in shared memory want a workspace
 // where a context has no room for their clusters alone: slices of kSmallSliceBytes; those of one block none (its token size).
 constexpr int64_t kSliceBytes = int64_t(4) << 30, kSmallSliceBytes = int64_t(64) << 20, kNoWorkspace = 256;
 struct Slices {
